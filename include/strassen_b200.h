@@ -398,6 +398,79 @@ int strassen_probe_fp64(int kind, int64_t iters, void *stream, double *tflops_ou
 #define STRASSEN_STATIC_MAX_N 512
 int strassen_dgemm_static(int64_t n, const double *A, const double *B, double *C, void *stream);
 
+/*
+ * Feed-forward operators of a served model: rows of activations in 8 bits, weights in 4.  (The paper has no counterpart: these
+ * are products of a THIN block with a matrix, where the recursion above has nothing to save and the bytes of the matrix decide.)
+ * Together they are one feed-forward block:
+ *     sum, q, s = strassen_rms_norm_quant(x, residual)   gu = strassen_w4_matmul(gate and up weights, q, s)
+ *     q', s' = strassen_silu_mul_quant(gu)               y  = strassen_w4_matmul(down weights, q', s')
+ * All are asynchronous on `stream` (a cudaStream_t as void*), allocate nothing, keep nothing of a call for the next one, and
+ * give the same bits for the same inputs.  Matrices are row-major with a leading dimension (elements between rows, at least the
+ * row's length, not read for a single row); pointers are device pointers aligned to their elements.  16-byte aligned pointers and
+ * strides select the wide accesses.  m = 0 rows is allowed and does nothing.
+ *
+ * 8-bit rows: v is held as q = e4m3(v / s), rounded to nearest even, with one scale per row, s = max(max|v| / 448, 2^-64): a row of zeros
+ * is zeros with s = 2^-64.  A row that holds NaN gives NaN for its scale and throughout its q; so does an infinity in a norm's row.
+ */
+typedef enum strassen_type {
+    STRASSEN_BF16 = 0,
+    STRASSEN_F16 = 1,
+    STRASSEN_F32 = 2,
+    STRASSEN_E4M3 = 3            /* 8 bits: 4 of exponent, 3 of mantissa, no infinities, largest 448   */
+} strassen_type;
+
+/*
+ * strassen_rms_norm_quant -- root-mean-square norm with the residual's addition and an 8-bit output.
+ *   h = x + residual;  v_k = h_k weight_k / sqrt(mean(h^2) + eps);  q, scale: v in 8 bits.
+ *   m, k       rows and their length (>= 1)
+ *   type       of x, residual, weight and sum: STRASSEN_BF16, STRASSEN_F16 or STRASSEN_F32
+ *   residual, sum  both or neither (NULL).  sum receives h rounded once to `type` (the norm itself is of the unrounded sum, held in
+ *              32 bits); it may be exactly x or exactly residual, and must not overlap them in any other way (STRASSEN_ALIAS)
+ *   weight     k elements
+ *   q, scale   m x k e4m3 (leading dimension ldq), m floats; overlap nothing else
+ */
+int strassen_rms_norm_quant(int64_t m, int64_t k, int type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                            const void *weight, float eps, void *sum, int64_t lds, void *q, int64_t ldq, float *scale,
+                            void *stream);
+
+/*
+ * strassen_silu_mul_quant -- gated activation with an 8-bit output:  v = gate / (1 + exp(-gate)) * up.
+ * gate and up may be the two halves of one product's rows.  Types and outputs as above.
+ */
+int strassen_silu_mul_quant(int64_t m, int64_t k, int type, const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q,
+                            int64_t ldq, float *scale, void *stream);
+
+/*
+ * A matrix W (n x k) held in 4 bits with one scale, and if wanted one zero point, for every `group` consecutive
+ * positions of a row:  W[r][i] = S[r][i / group] * (Q[r][i] - Z[r][i / group]),  Q = 0..15,  Z = 8 where there are none.
+ *
+ * strassen_w4_create plans its layout on the host (n, k >= 1, any; group 32, 64 or 128; the last group of a row may be cut short;
+ * scale_type STRASSEN_BF16 or STRASSEN_F16); NULL on failure.  strassen_w4_bytes is the device memory that it needs.
+ * strassen_w4_pack lays it out on `stream`, once, into the caller's memory `packed` (256-byte aligned), which the matrix refers to
+ * from then on and never frees:
+ *   q       n rows of ceil(k / 2) bytes, position 2 i in the low half of byte i; the spare half of an odd row is not used
+ *   scales  n rows of ceil(k / group) of scale_type
+ *   zeros   n rows of ceil(k / group) bytes (their low four bits count), or NULL, as has_zeros says
+ * The inputs may be freed once the stream has passed that point.  Products on another stream have to be ordered behind it.
+ */
+typedef struct strassen_w4 strassen_w4; /* opaque host object */
+strassen_w4 *strassen_w4_create(int64_t n, int64_t k, int group, int scale_type, int has_zeros);
+size_t strassen_w4_bytes(const strassen_w4 *w);
+int strassen_w4_pack(strassen_w4 *w, const uint8_t *q, int64_t ldq, const void *scales, int64_t lds, const uint8_t *zeros, int64_t ldz,
+                     void *packed, void *stream);
+void strassen_w4_destroy(strassen_w4 *w);
+
+/*
+ * strassen_w4_matmul -- out (m x n) = diag(x_scale) x W^T for m rows of activations x (m x k).
+ *   type      of x: STRASSEN_BF16, STRASSEN_F16 or STRASSEN_E4M3
+ *   x_scale   m floats (the scales of 8-bit rows), or NULL for ones
+ *   out_type  STRASSEN_BF16 or STRASSEN_F16; out overlaps no input (STRASSEN_ALIAS)
+ * Sums are held in 32 bits and rounded once.  NaN and infinities in a row of x reach that row's outputs only.  Any number of calls
+ * may use one matrix at a time, on any streams.
+ */
+int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx, const float *x_scale, int out_type,
+                       void *out, int64_t ldo, void *stream);
+
 /* Text describing the last failure on the calling thread ("" if none).  Thread-local. */
 const char *strassen_last_error(void);
 

@@ -10,7 +10,19 @@ from __future__ import annotations
 from . import binding
 from .binding import StrassenError  # noqa: F401
 
-__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError"]
+__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError", "W4Matrix", "FeedForward", "rms_norm_quant", "silu_mul_quant",
+           "quant_rows"]
+_FEED_FORWARD = ("W4Matrix", "FeedForward", "rms_norm_quant", "silu_mul_quant", "quant_rows")
+
+
+def __getattr__(name):
+    """The feed-forward operators, imported (with torch) on first use."""
+    if name in _FEED_FORWARD:
+        from . import feed_forward
+        for n in _FEED_FORWARD:
+            globals()[n] = getattr(feed_forward, n)
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))
 
 
 class Plan:

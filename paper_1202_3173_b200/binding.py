@@ -24,6 +24,7 @@ STRASSEN_FLAG_NO_FUSED_STEP = 128
 STRASSEN_FLAG_NO_DFS_FOLD = 256
 STATUS_NAMES = {0: "OK", -1: "INVALID_ARG", -2: "BAD_SCHEDULE", -3: "WORKSPACE_TOO_SMALL", -4: "ALIAS",
                 -5: "MISALIGNED", -6: "CUDA_ERROR", -7: "OUT_OF_MEMORY"}
+STRASSEN_BF16, STRASSEN_F16, STRASSEN_F32, STRASSEN_E4M3 = range(4)
 K_FORM, K_GEMM, K_RECOMBINE, K_FORM_ONE, K_ACCUMULATE, K_PEEL, K_SCALE, K_FUSED_STEP, K_LINCOMB, K_COUNT = range(10)
 KERNEL_KINDS = ("form", "gemm", "recombine", "form_one", "accumulate", "peel", "scale", "fused_step", "lincomb")
 
@@ -87,6 +88,13 @@ SYMBOLS = [
     ("strassen_bfs_form_shares", _int, [_i64, _i64, _vp, _i64, _vp, _i64, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _i64, _vp]),
     ("strassen_bfs_combine_shares", _int, [_i64, _i64, ctypes.POINTER(_vp), _i64, _vp, _i64, _vp]),
     ("strassen_dgemm_static", _int, [_i64, _vp, _vp, _vp, _vp]),
+    ("strassen_rms_norm_quant", _int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, ctypes.c_float, _vp, _i64, _vp, _i64, _vp, _vp]),
+    ("strassen_silu_mul_quant", _int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    ("strassen_w4_create", _vp, [_i64, _i64, _int, _int, _int]),
+    ("strassen_w4_bytes", _sz, [_vp]),
+    ("strassen_w4_pack", _int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    ("strassen_w4_destroy", None, [_vp]),
+    ("strassen_w4_matmul", _int, [_vp, _i64, _int, _vp, _i64, _vp, _int, _vp, _i64, _vp]),
     ("strassen_last_error", _cp, []),
 ]
 STRASSEN_STATIC_MAX_N = 512
@@ -291,3 +299,38 @@ def strassen_probe_fp64(kind: int, iters: int, stream: int = 0) -> float:
     out = ctypes.c_double()
     _check(lib().strassen_probe_fp64(kind, iters, stream, ctypes.byref(out)))
     return out.value
+
+
+def strassen_rms_norm_quant(m: int, k: int, type: int, x: int, ldx: int, residual: int, ldr: int, weight: int, eps: float, sum: int,
+                            lds: int, q: int, ldq: int, scale: int, stream: int = 0) -> None:
+    """x, residual, weight, sum, q, scale: device addresses; residual and sum are 0 where there is no residual."""
+    _check(lib().strassen_rms_norm_quant(m, k, type, x, ldx, residual, ldr, weight, eps, sum, lds, q, ldq, scale, stream))
+
+
+def strassen_silu_mul_quant(m: int, k: int, type: int, gate: int, ldg: int, up: int, ldu: int, q: int, ldq: int, scale: int,
+                            stream: int = 0) -> None:
+    _check(lib().strassen_silu_mul_quant(m, k, type, gate, ldg, up, ldu, q, ldq, scale, stream))
+
+
+def strassen_w4_create(n: int, k: int, group: int, scale_type: int, has_zeros: bool) -> int:
+    h = lib().strassen_w4_create(n, k, group, scale_type, int(has_zeros))
+    if not h:
+        raise StrassenError(-1, strassen_last_error())
+    return h
+
+
+def strassen_w4_bytes(matrix: int) -> int:
+    return lib().strassen_w4_bytes(matrix)
+
+
+def strassen_w4_pack(matrix: int, q: int, ldq: int, scales: int, lds: int, zeros: int, ldz: int, packed: int, stream: int = 0) -> None:
+    _check(lib().strassen_w4_pack(matrix, q, ldq, scales, lds, zeros, ldz, packed, stream))
+
+
+def strassen_w4_destroy(matrix: int) -> None:
+    lib().strassen_w4_destroy(matrix)
+
+
+def strassen_w4_matmul(matrix: int, m: int, type: int, x: int, ldx: int, x_scale: int, out_type: int, out: int, ldo: int,
+                       stream: int = 0) -> None:
+    _check(lib().strassen_w4_matmul(matrix, m, type, x, ldx, x_scale, out_type, out, ldo, stream))

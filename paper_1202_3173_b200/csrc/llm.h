@@ -1,0 +1,78 @@
+// Feed-forward operators: what the host entry points (llm_api.cu) and the kernels share.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace strassen {
+
+constexpr float kE4M3Max = 448.f;                    // largest finite e4m3
+constexpr float kMinRowScale = 5.421010862427522e-20f;   // 2^-64: scale of a row of zeros; its reciprocal is finite
+
+// ---- passes over rows (rows8.cu) ----------------------------------------------------------------------------------
+struct RowArgs {
+    int64_t m, k;
+    int type;                    // STRASSEN_BF16 / F16 / F32
+    const void *a, *b;           // norm: x and the residual (or NULL); gate: gate and up
+    int64_t lda, ldb;            // elements between rows
+    const void *weight;          // norm only
+    float eps;
+    void *sum;                   // norm with a residual: x + residual
+    int64_t lds;
+    uint8_t *q;                  // e4m3
+    int64_t ldq;
+    float *scale;
+};
+cudaError_t launch_rms_norm_quant(const RowArgs &a, cudaStream_t stream);
+cudaError_t launch_silu_mul_quant(const RowArgs &a, cudaStream_t stream);
+
+// ---- 4-bit weights (w4_pack.cu, w4_thin.cu, w4_tiles.cu) -----------------------------------------------------------
+// Laid-out weights: tiles of 128 rows x 128 inner positions, one after another along the inner dimension, then along the
+// rows.  A tile is four chunks c = 0..3 of 128 rows x 16 bytes; the four 32-bit words of a row's 16 bytes hold
+// k = 32 w + 8 c + (0..7), w = 0..3, in the nibble order 0, 2, 4, 6, 1, 3, 5, 7 from the lowest nibble up, so that (word & 0x000f000f)
+// is the pair k = 0, 1, ((word >> 4) & 0x000f000f) the pair 2, 3, and so on.  A 16 x 128 piece is then the operand of
+// eight m16n8k16 products with one 16-byte load per lane and row, 32 rows x 128 are the rows of 32 lanes of tensor memory.
+constexpr int kW4Rows = 128, kW4Depth = 128, kW4TileBytes = kW4Rows * kW4Depth / 2;
+
+struct W4Layout {
+    int64_t n, k;
+    int group;                   // 32, 64 or 128
+    int scale_type;              // STRASSEN_BF16 / F16
+    int has_zeros;
+    int64_t row_tiles, depth_tiles;
+    // byte offsets of the sections of the packed memory
+    size_t scale_off, zero_off, exponent_off, bytes;
+
+    // position of row r (0..127) of a tile in the scale and zero sections: rows g and g + 8 of a 16-row piece are neighbours
+    __host__ __device__ static int row_place(int r) { return (r & ~15) | ((r & 7) << 1) | ((r >> 3) & 1); }
+};
+
+struct W4Args {
+    W4Layout lay;
+    const uint8_t *packed;
+    int64_t m;
+    int type;                    // STRASSEN_BF16 / F16 / E4M3
+    const void *x;
+    int64_t ldx;
+    const float *x_scale;
+    int out_type;                // STRASSEN_BF16 / F16
+    void *out;
+    int64_t ldo;
+    void *workspace;
+};
+
+struct W4PackArgs {
+    W4Layout lay;
+    const uint8_t *q;
+    int64_t ldq;
+    const void *scales;
+    int64_t lds;
+    const uint8_t *zeros;
+    int64_t ldz;
+    uint8_t *packed;
+};
+cudaError_t launch_w4_pack(const W4PackArgs &a, cudaStream_t stream);
+cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream);
+
+}  // namespace strassen

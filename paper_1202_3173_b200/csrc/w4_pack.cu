@@ -1,0 +1,87 @@
+// Laying out 4-bit weights, once for a matrix: from rows of packed nibbles to the tiles that the products read (llm.h).
+//
+// Positions past the inner size hold the row's zero point (their value is 0), rows past the matrix the nibble 8 with a scale of 0.
+// The exponent section holds, for each row, the power of two 2^e with 1 <= max_g |S_g| 2^-e < 2: the tiled product holds
+// its weights in 16 bits as S 2^-e (Q - Z), so that small scales do not fall into the subnormal range of f16, and multiplies its
+// 32-bit sums by 2^e, both exactly.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "llm.h"
+#include "strassen_b200.h"
+
+namespace strassen {
+
+namespace {
+
+__device__ __forceinline__ float scale_value(uint16_t bits, int type)
+{
+    return type == STRASSEN_BF16 ? __uint_as_float(uint32_t(bits) << 16) : __half2float(__ushort_as_half(bits));
+}
+
+// One thread per row and chunk of a tile: 32 nibbles, 16 bytes out.
+__global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
+{
+    const int64_t tile = blockIdx.x;
+    const int64_t nt = tile / p.lay.depth_tiles, kb = tile % p.lay.depth_tiles;
+    const int c = threadIdx.x >> 7, r = threadIdx.x & 127;
+    const int64_t row = nt * kW4Rows + r;
+    const uint8_t *src = p.q + row * p.ldq;
+    uint32_t out[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int64_t k0 = kb * kW4Depth + 32 * w + 8 * c;
+        uint32_t pad = 8;
+        if (p.lay.has_zeros && row < p.lay.n && k0 < p.lay.k) pad = p.zeros[row * p.ldz + k0 / p.lay.group] & 15;
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t k = k0 + i;
+            uint32_t v = pad;
+            if (row < p.lay.n && k < p.lay.k) v = (src[k >> 1] >> (4 * (i & 1))) & 15;
+            word |= v << (4 * (i >> 1) + 16 * (i & 1));
+        }
+        out[w] = word;
+    }
+    uint4 *dst = reinterpret_cast<uint4 *>(p.packed + tile * kW4TileBytes);
+    dst[c * kW4Rows + r] = make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// One warp per row: its scales and zero points to their places, and its exponent.
+__global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
+{
+    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int64_t nt = row / kW4Rows;
+    const int place = W4Layout::row_place(int(row % kW4Rows));
+    const int64_t groups = (p.lay.k + p.lay.group - 1) / p.lay.group, places = p.lay.depth_tiles * (kW4Depth / p.lay.group);
+    uint16_t *scales = reinterpret_cast<uint16_t *>(p.packed + p.lay.scale_off) + nt * places * kW4Rows + place;
+    uint8_t *zeros = p.packed + p.lay.zero_off + nt * places * kW4Rows + place;
+    float mx = 0.f;
+    for (int64_t g = lane; g < places; g += 32) {
+        const bool on = row < p.lay.n && g < groups;
+        const uint16_t s = on ? static_cast<const uint16_t *>(p.scales)[row * p.lds + g] : uint16_t(0);
+        scales[g * kW4Rows] = s;
+        if (p.lay.has_zeros) zeros[g * kW4Rows] = on ? uint8_t(p.zeros[row * p.ldz + g] & 15) : uint8_t(8);
+        const float v = fabsf(scale_value(s, p.lay.scale_type));
+        if (isfinite(v)) mx = fmaxf(mx, v);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
+    if (lane == 0) {
+        int e = mx > 0.f ? ilogbf(mx) : 0;
+        e = e < -126 ? -126 : e;
+        reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[row] = ldexpf(1.f, e);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_w4_pack(const W4PackArgs &p, cudaStream_t stream)
+{
+    pack_weights_kernel<<<unsigned(p.lay.row_tiles * p.lay.depth_tiles), 512, 0, stream>>>(p);
+    pack_scales_kernel<<<unsigned(p.lay.row_tiles * kW4Rows / 4), 128, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace strassen

@@ -1,0 +1,423 @@
+"""The feed-forward operators against their formulas in 64 bits: norm and gate with 8-bit rows, products with 4-bit weights.
+
+Tolerances.  u is the unit roundoff of a format: 2^-4 for e4m3 (smallest step of its subnormals 2^-9), 2^-8 for bf16, 2^-11 for f16.
+  8-bit rows   |q s - v| <= 2^-4 |v| + 2^-10 s + 1e-5 max|v|   (one rounding of v / s; the last term: sums and quotients in 32 bits)
+               |s - s64| <= 1e-5 s64, sum equal to the sum in 32 bits rounded once
+  products     |y - y64| <= u |y64| + (K 2^-23 + w) sum_k |x_k| |S| (|Q - Z| + Z) xs
+               u for the result's rounding, K 2^-23 for sums in 32 bits; w = 0 up to 16 rows, where no weight is rounded, and beyond
+               that the unit roundoff of the 16-bit weights (bf16 for bf16 rows, f16 for f16 and e4m3 rows)
+               and in the 2-norm over the result: at most 2 u + 2 w + K 2^-23 (roundings of independent signs do not add up)
+"""
+import pytest
+import torch
+
+from paper_1202_3173_b200 import StrassenError, binding
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32, E4M3 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn
+U = {BF16: 2.0 ** -8, F16: 2.0 ** -11}
+EPS = 1e-6
+
+
+def sw():
+    import paper_1202_3173_b200 as m
+    return m
+
+
+def gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def strided(t, pad, shift=0, fill=float("nan")):
+    """The values of t as rows of a wider buffer that starts ``shift`` elements in; what lies between is ``fill``."""
+    m, k = t.shape
+    buf = torch.full((m * (k + pad) + shift + pad,), fill, device=t.device).to(t.dtype)
+    v = buf[shift:shift + m * (k + pad)].view(m, k + pad)[:, :k]
+    v.copy_(t)
+    return v
+
+
+# ---- rows to 8 bits ----------------------------------------------------------------------------------------------
+
+def check_rows(q, s, v):
+    s64 = (v.abs().amax(1) / 448).clamp_min(2.0 ** -64)
+    assert ((s.double() - s64).abs() <= 1e-5 * s64).all()
+    got = q.double() * s.double()[:, None]
+    lim = 2.0 ** -4 * v.abs() + 2.0 ** -10 * s64[:, None] + 1e-5 * v.abs().amax(1, keepdim=True)
+    assert torch.isfinite(got).all() and ((got - v).abs() <= lim).all(), float(((got - v).abs() - lim).max())
+    # the row's largest value takes the largest e4m3 number
+    big = v.abs().amax(1) > 448 * 2.0 ** -64
+    assert (q.float().abs().amax(1)[big] == 448).all()
+
+
+def norm64(x, w, r=None):
+    h = x.double() if r is None else x.double() + r.double()
+    return h / torch.sqrt((h * h).mean(1, keepdim=True) + EPS) * w.double()
+
+
+NORM_SHAPES = [(1, 1), (3, 7), (1, 8), (5, 64), (2, 1000), (7, 1023), (4, 4096), (3, 8200), (2, 12345), (1, 16384), (300, 512), (2, 40000), (2, 40001)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("m,k", NORM_SHAPES)
+def test_norm(m, k, dtype):
+    g = gen(m * 131 + k)
+    x, r = (torch.randn(m, k, device="cuda", generator=g).to(dtype) * 3 for _ in range(2))
+    w = (1 + 0.3 * torch.randn(k, device="cuda", generator=g)).to(dtype)
+    q, s = sw().rms_norm_quant(x, w, EPS)
+    check_rows(q, s, norm64(x, w))
+    q, s, h = sw().rms_norm_quant(x, w, EPS, residual=r)
+    check_rows(q, s, norm64(x, w, r))
+    assert torch.equal(h, (x.float() + r.float()).to(dtype))
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 0), (8, 8), (1, 0), (3, 1), (16, 5)])
+@pytest.mark.parametrize("k", [7, 256, 2049, 40001])
+def test_norm_strides_and_alignment(k, pad, shift):
+    g = gen(k + pad)
+    x, r = (strided(torch.randn(5, k, device="cuda", generator=g).to(F16), pad, shift) for _ in range(2))
+    w = torch.rand(k + shift, device="cuda", generator=g).to(F16)[shift:]
+    buf = torch.zeros(5, k + pad + shift, device="cuda").to(E4M3)
+    q, s, h = buf[:, shift:shift + k], torch.empty(5, device="cuda"), strided(torch.zeros(5, k, device="cuda").to(F16), pad, shift)
+    got = sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, h))
+    assert got[0] is q and got[2] is h
+    check_rows(q, s, norm64(x, w, r))
+    assert torch.equal(h, (x.float() + r.float()).to(F16))
+    # nothing was written beside the rows
+    assert (buf[:, :shift].float() == 0).all() and (buf[:, shift + k:].float() == 0).all()
+    wide = h.as_strided((4, pad), (k + pad, 1), h.storage_offset() + k)
+    assert torch.isnan(wide.float()).all()
+
+
+@pytest.mark.parametrize("k", [300, 4096, 70001])
+def test_norm_sum_in_place(k):
+    g = gen(k)
+    for which in ("x", "residual"):
+        x, r = (torch.randn(6, k, device="cuda", generator=g).to(BF16) for _ in range(2))
+        want, v = (x.float() + r.float()).to(BF16), norm64(x, torch.ones(k, device="cuda"), r)
+        q, s = sw().quant_rows(6, k)
+        sw().rms_norm_quant(x, torch.ones(k, device="cuda", dtype=BF16), EPS, residual=r, out=(q, s, x if which == "x" else r))
+        assert torch.equal(x if which == "x" else r, want)
+        check_rows(q, s, v)
+
+
+def test_norm_rows_of_zeros_nan_and_infinity():
+    for k in (96, 40000):
+        x = torch.randn(6, k, device="cuda")
+        x[1] = 0
+        x[2, 5] = float("nan")
+        x[3, 7] = float("inf")
+        x[4] = 1e-30                                  # far below eps: the smallest scale
+        q, s = sw().rms_norm_quant(x, torch.ones(k, device="cuda"), EPS)
+        assert s[1] == 2.0 ** -64 and (q[1].float() == 0).all()
+        assert torch.isnan(s[2:4]).all() and torch.isnan(q[2:4].float()).all()
+        check_rows(q[[0, 1, 4, 5]], s[[0, 1, 4, 5]], norm64(x[[0, 1, 4, 5]], torch.ones(k, device="cuda")))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("m,f", [(1, 1), (3, 7), (2, 64), (4, 1000), (33, 2047), (1, 16384), (5, 11008), (2, 33000), (2, 40001)])
+def test_gate(m, f, dtype):
+    g = gen(m + f)
+    gu = torch.randn(m, 2 * f, device="cuda", generator=g).to(dtype) * 4
+    q, s = sw().silu_mul_quant(gu[:, :f], gu[:, f:])
+    a, b = gu.double().split(f, 1)
+    check_rows(q, s, a * torch.special.expit(a) * b)
+
+
+def test_gate_extremes():
+    g = torch.tensor([[-100.0, -1e4, 0.0, 50.0], [0.0, 0.0, 0.0, 0.0], [float("nan"), 1.0, 1.0, 1.0], [1.0, 2.0, 3.0, 4.0]], device="cuda")
+    u = torch.tensor([[3.0, 5.0, 7.0, -2.0], [1.0, 2.0, 3.0, 4.0], [1.0, 1.0, 1.0, 1.0], [0.0, 0.0, 0.0, 0.0]], device="cuda")
+    q, s = sw().silu_mul_quant(g, u)
+    check_rows(q[[0, 1, 3]], s[[0, 1, 3]], (g.double() * torch.special.expit(g.double()) * u.double())[[0, 1, 3]])
+    assert (s[[1, 3]] == 2.0 ** -64).all() and torch.isnan(s[2]) and torch.isnan(q[2].float()).all()
+
+
+def test_row_operators_take_no_rows():
+    x = torch.empty(0, 64, device="cuda", dtype=BF16)
+    q, s, h = sw().rms_norm_quant(x, torch.ones(64, device="cuda", dtype=BF16), EPS, residual=x)
+    assert q.shape == (0, 64) and s.shape == (0,) and h.shape == (0, 64)
+    assert sw().silu_mul_quant(x, x)[0].shape == (0, 64)
+
+
+# ---- products with 4-bit weights -----------------------------------------------------------------------------------
+
+def weights(n, k, group, zeros, dtype, seed, spread=1.0):
+    g = gen(seed)
+    groups = -(-k // group)
+    q = torch.randint(0, 256, (n, (k + 1) // 2), device="cuda", generator=g, dtype=torch.uint8)
+    s = (0.01 * torch.randn(n, groups, device="cuda", generator=g) * spread ** torch.rand(n, groups, device="cuda", generator=g)).to(dtype)
+    z = torch.randint(0, 16, (n, groups), device="cuda", generator=g, dtype=torch.uint8) if zeros else None
+    return q, s, z
+
+
+def dense64(q, s, z, k, group):
+    """(W, |S| (|Q - Z| + Z)) in 64 bits."""
+    n = q.shape[0]
+    nib = torch.empty(n, 2 * q.shape[1], device="cuda", dtype=torch.float64)
+    nib[:, 0::2] = (q & 15).double()
+    nib[:, 1::2] = (q >> 4).double()
+    at = torch.arange(k, device="cuda") // group
+    zz = z.double()[:, at] if z is not None else torch.full((n, k), 8.0, device="cuda", dtype=torch.float64)
+    d = nib[:, :k] - zz
+    return s.double()[:, at] * d, s.double()[:, at].abs() * (d.abs() + zz)
+
+
+def rows(m, k, dtype, seed):
+    g = gen(seed)
+    x = torch.randn(m, k, device="cuda", generator=g)
+    if dtype != E4M3:
+        return x.to(dtype), None
+    xs = x.abs().amax(1) / 448
+    return (x / xs[:, None]).clamp(-448, 448).to(E4M3), xs
+
+
+def check_product(y, x, xs, W, A, out_dtype):
+    m, k = x.shape
+    xd = x.double() if xs is None else x.double() * xs.double()[:, None]
+    want, size = xd @ W.t(), xd.abs() @ A.t()
+    w = 0.0 if m <= 16 else U[BF16] if x.dtype == BF16 else U[F16]
+    assert y.dtype == out_dtype and torch.isfinite(y).all()
+    err = (y.double() - want).abs()
+    lim = U[out_dtype] * want.abs() + (k * 2.0 ** -23 + w) * size + (6e-8 if out_dtype == F16 else 0)      # f16 results below its normal range
+    assert (err <= lim).all(), float((err - lim).max())
+    assert err.norm() <= (2 * U[out_dtype] + 2 * w + k * 2.0 ** -23) * want.norm() + 6e-8 * err.numel() ** 0.5, float(err.norm() / want.norm())
+
+
+W4_SHAPES = [(1, 1, 1), (1, 128, 128), (2, 16, 130), (1, 4096, 4096), (3, 100, 1000), (5, 129, 257), (8, 512, 2048), (9, 33, 640), (16, 300, 4097),
+             (17, 256, 512), (31, 130, 300), (64, 1000, 1024), (100, 257, 4099), (129, 128, 384), (257, 640, 1111), (1, 40, 16384), (2, 5000, 96)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, False), (32, True), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("m,n,k", W4_SHAPES)
+def test_w4_product(m, n, k, group, zeros):
+    for dtype, out_dtype, sdtype in ((BF16, BF16, BF16), (F16, F16, F16), (E4M3, BF16, BF16), (E4M3, F16, F16), (BF16, F16, F16)):
+        q, s, z = weights(n, k, group, zeros, sdtype, n + k)
+        W, A = dense64(q, s, z, k, group)
+        x, xs = rows(m, k, dtype, m + k)
+        matrix = sw().W4Matrix(q, s, z, k=k, group=group)
+        check_product(matrix(x, xs, dtype=out_dtype), x, xs, W, A, out_dtype)
+
+
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (2, 0), (3, 1), (8, 0), (8, 8), (16, 16), (7, 3)])
+@pytest.mark.parametrize("m", [1, 6, 20, 150])
+def test_w4_strides_and_alignment(m, pad, shift):
+    n, k, group = 200, 777, 64
+    for dtype in (BF16, E4M3):
+        q, s, z = weights(n, k, group, True, BF16, 5)
+        W, A = dense64(q, s, z, k, group)
+        x, xs = rows(m, k, dtype, 9)
+        x = strided(x, pad, shift)                    # NaN beside the rows: none of it may reach a sum
+        qs, ss, zs = strided(q, pad, shift, 0), strided(s, pad, shift), strided(z, pad, shift, 0)
+        out = strided(torch.zeros(m, n, device="cuda").to(BF16), pad, shift, 7.0)
+        matrix = sw().W4Matrix(qs, ss, zs, k=k, group=group)
+        assert matrix(x, xs, out=out) is out
+        check_product(out, x, xs, W, A, BF16)
+        if m > 1 and pad:
+            assert (out.as_strided((m - 1, pad), (n + pad, 1), out.storage_offset() + n) == 7).all()
+
+
+@pytest.mark.parametrize("m", [3, 40])
+def test_w4_scales_over_a_wide_range(m):
+    """Scales from 1e-6 to 1e-2 within a row, and rows of very small and very large scales."""
+    n, k, group = 130, 1024, 32
+    for dtype in (BF16, E4M3):
+        q, s, z = weights(n, k, group, True, BF16, 3, spread=1e-4)
+        s[1] = (s[1].float() * 1e-25).to(BF16)
+        s[2] = (s[2].float() * 1e25).to(BF16)
+        s[3] = 0
+        W, A = dense64(q, s, z, k, group)
+        x, xs = rows(m, k, dtype, 4)
+        y = sw().W4Matrix(q, s, z, group=group)(x, xs)
+        assert (y[:, 3] == 0).all()
+        for part in ([0] + list(range(4, n)), [1], [2]):
+            check_product(y[:, part], x, xs, W[part], A[part], BF16)
+
+
+@pytest.mark.parametrize("m", [1, 8, 33, 200])
+def test_w4_special_values_stay_in_their_row(m):
+    n, k = 150, 500
+    q, s, z = weights(n, k, 128, False, BF16, 3)
+    W, A = dense64(q, s, z, k, 128)
+    matrix = sw().W4Matrix(q, s, None, k=k)
+    x, _ = rows(m + 2, k, BF16, 4)
+    x[0, 3], x[m + 1, k - 1] = float("nan"), float("inf")
+    y = matrix(x)
+    assert torch.isnan(y[0]).all() and not torch.isfinite(y[m + 1]).any()
+    w = U[BF16] if m + 2 > 16 else 0.0
+    want, size = x[1:m + 1].double() @ W.t(), x[1:m + 1].double().abs() @ A.t()
+    assert ((y[1:m + 1].double() - want).abs() <= U[BF16] * want.abs() + (k * 2.0 ** -23 + w) * size).all()
+    # rows of zeros give zeros
+    assert (matrix(torch.zeros(m, k, device="cuda", dtype=BF16)) == 0).all()
+
+
+@pytest.mark.parametrize("m", [1, 7, 64, 300])
+def test_w4_gives_the_same_bits_every_time_and_for_a_row_alone_in_its_launch_shape(m):
+    q, s, z = weights(900, 2100, 64, True, BF16, 8)
+    matrix = sw().W4Matrix(q, s, z, k=2100, group=64)
+    x, _ = rows(m, 2100, BF16, 1)
+    y = matrix(x)
+    for _ in range(5):
+        assert torch.equal(matrix(x), y)
+
+
+def test_w4_offsets_past_32_bits():
+    """Rows of x and of the result more than 2^31 elements apart."""
+    n, k, far = 192, 256, 2 ** 31 + 64
+    q, s, z = weights(n, k, 128, False, BF16, 2)
+    W, A = dense64(q, s, z, k, 128)
+    matrix = sw().W4Matrix(q, s, z, k=k)
+    xbuf = torch.zeros(2 * far + 512, dtype=torch.uint8, device="cuda").view(E4M3)
+    obuf = torch.zeros(far + 512, dtype=BF16, device="cuda")
+    x, xs = rows(2, k, E4M3, 3)
+    xv = xbuf.as_strided((2, k), (far, 1))
+    xv.view(torch.uint8).copy_(x.view(torch.uint8))
+    out = obuf.as_strided((2, n), (far, 1))
+    matrix(xv, xs, out=out)
+    check_product(out.contiguous(), x, xs, W, A, BF16)
+    # ... and of the row operators
+    q8, s8 = sw().rms_norm_quant(out, torch.ones(n, device="cuda", dtype=BF16), EPS)
+    check_rows(q8, s8, norm64(out.contiguous(), torch.ones(n, device="cuda")))
+
+
+def test_w4_no_rows():
+    q, s, z = weights(10, 64, 32, False, F16, 2)
+    assert sw().W4Matrix(q, s, group=32)(torch.empty(0, 64, device="cuda", dtype=F16)).shape == (0, 10)
+
+
+# ---- together ------------------------------------------------------------------------------------------------------
+
+def block(width, inner, group, seed):
+    from paper_1202_3173_b200.feed_forward import FeedForward, W4Matrix
+    made, dense = [], []
+    for n, k in ((2 * inner, width), (width, inner)):
+        q, s, z = weights(n, k, group, True, BF16, seed + n)
+        made.append(W4Matrix(q, s, z, k=k, group=group))
+        dense.append(dense64(q, s, z, k, group)[0])
+    norm = (1 + 0.1 * torch.randn(width, device="cuda", generator=gen(seed))).to(BF16)
+    return FeedForward(norm, *made), norm, dense
+
+
+@pytest.mark.parametrize("m", [1, 5, 40])
+@pytest.mark.parametrize("width,inner,group", [(256, 512, 128), (133, 301, 32)])
+def test_feed_forward_block(m, width, inner, group):
+    ff, norm, (w1, w2) = block(width, inner, group, 3)
+    g = gen(m)
+    x, r = (torch.randn(m, width, device="cuda", generator=g).to(BF16) for _ in range(2))
+    y, h = ff(x, r)
+    assert torch.equal(h, (x.float() + r.float()).to(BF16))
+    n = norm64(x, norm, r)
+    a, b = (n @ w1.t()).split(inner, 1)
+    want = (a * torch.special.expit(a) * b) @ w2.t()
+    # two roundings to e4m3 of relative size 2^-4 / sqrt(3) at most each (root mean square), the first entering both factors of the gate
+    assert (y.double() - want).norm() <= 2.0 ** -4 * 3 * want.norm()
+
+
+def test_feed_forward_on_another_stream_and_in_a_graph():
+    ff, _, _ = block(256, 512, 128, 3)
+    x, r = (torch.randn(4, 256, device="cuda", generator=gen(1)).to(BF16) for _ in range(2))
+    want, _ = ff(x, r)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            got, _ = ff(x, r)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held, _ = ff(x, r)
+    other = torch.randn(4, 256, device="cuda", generator=gen(2)).to(BF16)
+    eager, _ = ff(other, r)
+    x.copy_(other)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(held, eager)
+
+
+def test_operators_keep_stream_order():
+    """Inputs rewritten and outputs consumed between calls of one stream, nothing waited for."""
+    ff, _, _ = block(512, 1024, 128, 3)
+    xs = [torch.randn(4, 512, device="cuda", generator=gen(i)).to(BF16) for i in range(6)]
+    r = torch.zeros_like(xs[0])
+    want = [ff(x, r)[0].clone() for x in xs]
+    torch.cuda.synchronize()
+    held, got = torch.empty_like(xs[0]), []
+    for _ in range(10):
+        for i, x in enumerate(xs):
+            held.copy_(x)
+            y, _ = ff(held, r)
+            got.append((i, y))
+    torch.cuda.synchronize()
+    for i, y in got:
+        assert torch.equal(y, want[i])
+
+
+# ---- refusals -------------------------------------------------------------------------------------------------------
+
+def test_refusals_of_shapes_types_and_devices():
+    m = sw()
+    x = torch.randn(4, 64, device="cuda").to(BF16)
+    w = torch.ones(64, device="cuda", dtype=BF16)
+    q, s = m.quant_rows(4, 64)
+    bad = [lambda: m.rms_norm_quant(x.cpu(), w), lambda: m.rms_norm_quant(x, w.cpu()), lambda: m.rms_norm_quant(x, w[:63]),
+           lambda: m.rms_norm_quant(x, w.float()), lambda: m.rms_norm_quant(x.double(), w.double()), lambda: m.rms_norm_quant(x[0], w),
+           lambda: m.rms_norm_quant(x.t(), w[:4]), lambda: m.rms_norm_quant(x, w, residual=x[:3]), lambda: m.rms_norm_quant(x, w, residual=x.half()),
+           lambda: m.rms_norm_quant(x, w, out=(q, s[:3])), lambda: m.rms_norm_quant(x, w, out=(q[:, :63], s)), lambda: m.rms_norm_quant(x, w, out=(q, s, x)),
+           lambda: m.silu_mul_quant(x, x[:, :63]), lambda: m.silu_mul_quant(x, x.float()), lambda: m.silu_mul_quant(x, x, out=(q.float(), s))]
+    qq, ss, zz = weights(32, 64, 32, True, BF16, 1)
+    W = m.W4Matrix(qq, ss, zz, group=32)
+    bad += [lambda: m.W4Matrix(qq.int(), ss, zz, group=32), lambda: m.W4Matrix(qq.cpu(), ss, zz, group=32), lambda: m.W4Matrix(qq, ss.float(), zz, group=32),
+            lambda: m.W4Matrix(qq, ss[:, :1], zz, group=32), lambda: m.W4Matrix(qq, ss, zz[:31], group=32), lambda: m.W4Matrix(qq, ss, zz, k=70, group=32),
+            lambda: W(x[:, :63]), lambda: W(x.float()), lambda: W(x.cpu()), lambda: W(x, s[:3]), lambda: W(x, s.double()),
+            lambda: W(x, out=torch.empty(4, 31, device="cuda", dtype=BF16)), lambda: W(x, out=torch.empty(4, 32, device="cuda")),
+            lambda: W(x, out=torch.empty(4, 32, device="cuda", dtype=BF16), dtype=F16), lambda: m.FeedForward(w, W, W)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("refusal %d" % i)
+    W.close()
+    with pytest.raises(ValueError):
+        W(x)
+
+
+def test_refusals_at_the_c_boundary():
+    x = torch.randn(4, 64, device="cuda").to(BF16)
+    w = torch.ones(64, device="cuda", dtype=BF16)
+    q, s = sw().quant_rows(4, 64)
+    p = lambda t: t.data_ptr()  # noqa: E731
+    b = binding
+    norm = lambda **k: b.strassen_rms_norm_quant(**{**dict(m=4, k=64, type=0, x=p(x), ldx=64, residual=0, ldr=0, weight=p(w), eps=1e-6, sum=0, lds=0,  # noqa: E731
+                                                           q=p(q), ldq=64, scale=p(s)), **k})
+    for status, change in ((-1, dict(m=-1)), (-1, dict(k=0)), (-1, dict(type=3)), (-1, dict(type=9)), (-1, dict(x=0)), (-1, dict(weight=0)), (-1, dict(q=0)),
+                           (-1, dict(scale=0)), (-1, dict(ldx=63)), (-1, dict(ldq=63)), (-1, dict(eps=-1.0)), (-1, dict(eps=float("nan"))),
+                           (-1, dict(residual=p(x), ldr=64)), (-1, dict(sum=p(x), lds=64)), (-5, dict(x=p(x) + 1)), (-5, dict(scale=p(s) + 2)), (-5, dict(weight=p(w) + 1)),
+                           (-4, dict(q=p(x))), (-4, dict(scale=p(x))), (-4, dict(q=p(w))), (-4, dict(residual=p(x), ldr=64, sum=p(x) + 128, lds=64))):
+        with pytest.raises(StrassenError) as e:
+            norm(**change)
+        assert e.value.status == status, (change, str(e.value))
+    norm(m=0, x=0, q=0)
+    qq, ss, zz = weights(32, 64, 32, True, BF16, 1)
+    h = b.strassen_w4_create(32, 64, 32, 0, True)
+    out = torch.empty(4, 32, device="cuda", dtype=BF16)
+    mem = torch.empty(b.strassen_w4_bytes(h), dtype=torch.uint8, device="cuda")
+    mul = lambda **k: b.strassen_w4_matmul(**{**dict(matrix=h, m=4, type=0, x=p(x), ldx=64, x_scale=0, out_type=0, out=p(out), ldo=32), **k})  # noqa: E731
+    with pytest.raises(StrassenError):
+        mul()                                            # not laid out yet
+    pack = lambda **k: b.strassen_w4_pack(**{**dict(matrix=h, q=p(qq), ldq=32, scales=p(ss), lds=2, zeros=p(zz), ldz=2, packed=p(mem)), **k})  # noqa: E731
+    for status, change in ((-1, dict(q=0)), (-1, dict(scales=0)), (-1, dict(zeros=0)), (-1, dict(packed=0)), (-1, dict(ldq=31)), (-1, dict(lds=1)), (-1, dict(ldz=1)),
+                           (-5, dict(packed=p(mem) + 16)), (-5, dict(scales=p(ss) + 1)), (-1, dict(matrix=0))):
+        with pytest.raises(StrassenError) as e:
+            pack(**change)
+        assert e.value.status == status, (change, str(e.value))
+    pack()
+    for status, change in ((-1, dict(matrix=0)), (-1, dict(m=-1)), (-1, dict(type=2)), (-1, dict(out_type=2)), (-1, dict(out_type=3)), (-1, dict(x=0)), (-1, dict(out=0)),
+                           (-1, dict(ldx=63)), (-1, dict(ldo=31)), (-5, dict(x=p(x) + 1)), (-5, dict(out=p(out) + 1)), (-5, dict(x_scale=p(s) + 1)),
+                           (-4, dict(out=p(x))), (-4, dict(out=p(mem)))):
+        with pytest.raises(StrassenError) as e:
+            mul(**change)
+        assert e.value.status == status, (change, str(e.value))
+    mul()
+    mul(m=0, x=0)
+    torch.cuda.synchronize()
+    b.strassen_w4_destroy(h)
