@@ -471,6 +471,14 @@ void strassen_w4_destroy(strassen_w4 *w);
 int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx, const float *x_scale, int out_type,
                        void *out, int64_t ldo, void *stream);
 
+/*
+ * strassen_device_status -- wait for the current device and say whether a kernel of strassen_w4_matmul has given up since
+ * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
+ * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else
+ * STRASSEN_CUDA_ERROR, and the flag is cleared.
+ */
+int strassen_device_status(void);
+
 /* Text describing the last failure on the calling thread ("" if none).  Thread-local. */
 const char *strassen_last_error(void);
 

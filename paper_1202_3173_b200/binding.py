@@ -95,6 +95,7 @@ SYMBOLS = [
     ("strassen_w4_pack", _int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     ("strassen_w4_destroy", None, [_vp]),
     ("strassen_w4_matmul", _int, [_vp, _i64, _int, _vp, _i64, _vp, _int, _vp, _i64, _vp]),
+    ("strassen_device_status", _int, []),
     ("strassen_last_error", _cp, []),
 ]
 STRASSEN_STATIC_MAX_N = 512
@@ -334,3 +335,7 @@ def strassen_w4_destroy(matrix: int) -> None:
 def strassen_w4_matmul(matrix: int, m: int, type: int, x: int, ldx: int, x_scale: int, out_type: int, out: int, ldo: int,
                        stream: int = 0) -> None:
     _check(lib().strassen_w4_matmul(matrix, m, type, x, ldx, x_scale, out_type, out, ldo, stream))
+
+
+def strassen_device_status() -> None:
+    _check(lib().strassen_device_status())

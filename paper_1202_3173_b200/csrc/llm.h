@@ -73,6 +73,10 @@ struct W4PackArgs {
     uint8_t *packed;
 };
 cudaError_t launch_w4_pack(const W4PackArgs &a, cudaStream_t stream);
+// Most rows of x that the kernel for few rows (w4_thin.cu) takes; beyond that the tiles of w4_tiles.cu.
+constexpr int64_t kThinRows = 16;
+cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream);
+cudaError_t read_gave_up(int *flag);        // reads and clears the flag of w4_tiles.cu
 cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream);
 
 }  // namespace strassen

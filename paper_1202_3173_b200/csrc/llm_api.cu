@@ -234,6 +234,20 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
     const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, nullptr};
-    const cudaError_t e = launch_w4_thin(a, sms, static_cast<cudaStream_t>(stream));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = m <= kThinRows ? launch_w4_thin(a, sms, st) : launch_w4_tiles(a, sms, st);
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
+}
+
+extern "C" int strassen_device_status(void)
+{
+    set_last_error("");
+    int sms = 0, rc = current_device(&sms);
+    if (rc != STRASSEN_OK) return rc;
+    cudaError_t e = cudaDeviceSynchronize();
+    int flag = 0;
+    if (e == cudaSuccess) e = read_gave_up(&flag);
+    if (e != cudaSuccess) return cuda_fail(e, "reading the device's status");
+    if (flag) return fail(STRASSEN_CUDA_ERROR, "a product gave up waiting for its own copies or tensor instructions; its results are not valid");
+    return STRASSEN_OK;
 }

@@ -421,3 +421,9 @@ def test_refusals_at_the_c_boundary():
     mul(m=0, x=0)
     torch.cuda.synchronize()
     b.strassen_w4_destroy(h)
+
+
+def test_device_status_is_clean():
+    q, s, z = weights(256, 1024, 128, False, BF16, 2)
+    sw().W4Matrix(q, s)(rows(64, 1024, BF16, 1)[0])
+    binding.strassen_device_status()
