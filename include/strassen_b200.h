@@ -465,11 +465,20 @@ void strassen_w4_destroy(strassen_w4 *w);
  *   type      of x: STRASSEN_BF16, STRASSEN_F16 or STRASSEN_E4M3
  *   x_scale   m floats (the scales of 8-bit rows), or NULL for ones
  *   out_type  STRASSEN_BF16 or STRASSEN_F16; out overlaps no input (STRASSEN_ALIAS)
- * Sums are held in 32 bits and rounded once.  NaN and infinities in a row of x reach that row's outputs only.  Any number of calls
+ *   workspace as strassen_w4_workspace_bytes says, NULL if that is 0 (STRASSEN_WORKSPACE_TOO_SMALL)
+ * Sums are held in 32 bits and rounded once.  For more than STRASSEN_W4_THIN_ROWS rows the weights are rounded to 16 bits on their way to the
+ * tensor cores: to bf16 beside bf16 rows, to f16 beside f16 and e4m3 rows.  NaN and infinities in a row of x reach that row's outputs only.  Any number of calls
  * may use one matrix at a time, on any streams.
  */
 int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx, const float *x_scale, int out_type,
-                       void *out, int64_t ldo, void *stream);
+                       void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+#define STRASSEN_W4_THIN_ROWS 16
+
+/* Bytes of workspace (256-byte aligned device memory, free again once the call's kernels are done) that strassen_w4_matmul
+ * needs for these rows: none for up to STRASSEN_W4_THIN_ROWS rows, nor for bf16 and f16 rows that start at multiples of 16 bytes; otherwise the rows in
+ * 16 bits (e4m3 rows, other alignments). */
+size_t strassen_w4_workspace_bytes(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx);
 
 /*
  * strassen_device_status -- wait for the current device and say whether a kernel of strassen_w4_matmul has given up since

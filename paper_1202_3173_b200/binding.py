@@ -94,11 +94,13 @@ SYMBOLS = [
     ("strassen_w4_bytes", _sz, [_vp]),
     ("strassen_w4_pack", _int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     ("strassen_w4_destroy", None, [_vp]),
-    ("strassen_w4_matmul", _int, [_vp, _i64, _int, _vp, _i64, _vp, _int, _vp, _i64, _vp]),
+    ("strassen_w4_matmul", _int, [_vp, _i64, _int, _vp, _i64, _vp, _int, _vp, _i64, _vp, _sz, _vp]),
+    ("strassen_w4_workspace_bytes", _sz, [_vp, _i64, _int, _vp, _i64]),
     ("strassen_device_status", _int, []),
     ("strassen_last_error", _cp, []),
 ]
 STRASSEN_STATIC_MAX_N = 512
+STRASSEN_W4_THIN_ROWS = 16
 
 _lib = None
 
@@ -333,8 +335,12 @@ def strassen_w4_destroy(matrix: int) -> None:
 
 
 def strassen_w4_matmul(matrix: int, m: int, type: int, x: int, ldx: int, x_scale: int, out_type: int, out: int, ldo: int,
-                       stream: int = 0) -> None:
-    _check(lib().strassen_w4_matmul(matrix, m, type, x, ldx, x_scale, out_type, out, ldo, stream))
+                       workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().strassen_w4_matmul(matrix, m, type, x, ldx, x_scale, out_type, out, ldo, workspace, workspace_bytes, stream))
+
+
+def strassen_w4_workspace_bytes(matrix: int, m: int, type: int, x: int, ldx: int) -> int:
+    return lib().strassen_w4_workspace_bytes(matrix, m, type, x, ldx)
 
 
 def strassen_device_status() -> None:

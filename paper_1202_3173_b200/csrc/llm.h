@@ -5,6 +5,8 @@
 
 #include <cstdint>
 
+#include "strassen_b200.h"
+
 namespace strassen {
 
 constexpr float kE4M3Max = 448.f;                    // largest finite e4m3
@@ -74,7 +76,12 @@ struct W4PackArgs {
 };
 cudaError_t launch_w4_pack(const W4PackArgs &a, cudaStream_t stream);
 // Most rows of x that the kernel for few rows (w4_thin.cu) takes; beyond that the tiles of w4_tiles.cu.
-constexpr int64_t kThinRows = 16;
+constexpr int64_t kThinRows = STRASSEN_W4_THIN_ROWS;
+// A run of rows of x that one matrix multiplies: rows first .. first + count - 1 of the rows in order.
+struct W4Tile {
+    int expert, first, count, unused;
+};
+int64_t w4_tiles_workspace(const W4Args &a);        // bytes; 0: none is needed
 cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream);
 cudaError_t read_gave_up(int *flag);        // reads and clears the flag of w4_tiles.cu
 cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream);

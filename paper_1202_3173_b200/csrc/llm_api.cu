@@ -210,8 +210,20 @@ extern "C" int strassen_w4_pack(strassen_w4 *w, const uint8_t *q, int64_t ldq, c
     return STRASSEN_OK;
 }
 
+extern "C" size_t strassen_w4_workspace_bytes(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx)
+{
+    if (!w || m <= kThinRows || m > kMaxExtent) return 0;
+    W4Args a = {};
+    a.lay = w->lay;
+    a.m = m;
+    a.type = type;
+    a.x = x;
+    a.ldx = ldx;
+    return size_t(w4_tiles_workspace(a));
+}
+
 extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx, const float *x_scale, int out_type,
-                                  void *out, int64_t ldo, void *stream)
+                                  void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
 {
     set_last_error("");
     if (!w) return fail(STRASSEN_INVALID_ARG, "the matrix must be non-NULL");
@@ -233,7 +245,16 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
         return fail(STRASSEN_ALIAS, "out overlaps an input");
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
-    const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, nullptr};
+    const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, workspace};
+    const int64_t need = m > kThinRows ? w4_tiles_workspace(a) : 0;
+    if (need > 0) {
+        if (!workspace || workspace_bytes < size_t(need))
+            return fail(STRASSEN_WORKSPACE_TOO_SMALL, "these rows need a workspace of " + std::to_string(need) + " bytes (strassen_w4_workspace_bytes)");
+        if (misaligned(workspace, 256)) return fail(STRASSEN_MISALIGNED, "workspace must be 256-byte aligned");
+        const Range ws = {reinterpret_cast<uintptr_t>(workspace), reinterpret_cast<uintptr_t>(workspace) + uintptr_t(need)};
+        if (overlap(ws, o) || overlap(ws, rows_of(x, m, l.k, ldx, t)) || overlap(ws, rows_of(x_scale, x_scale ? 1 : 0, m, m, 4)))
+            return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
+    }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = m <= kThinRows ? launch_w4_thin(a, sms, st) : launch_w4_tiles(a, sms, st);
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");

@@ -1,28 +1,37 @@
 // Products of many rows with a matrix of 4-bit weights on the fifth-generation tensor cores.
 //
-// The weights are the 128-row operand of tcgen05.mma, so few rows of x make a narrow product and not a padded one:
-//     D (128 rows of weights x up to 128 rows of x, 32 bits, tensor memory) += A (tensor memory) . B (shared memory)
-// A CTA of 18 warps owns HALVES x 128 rows of weights and up to 128 rows of x:
-//   * warp 17 streams the laid-out weights and their scales into a ring of shared memory (bulk copies);
-//   * warps 0-7 turn them into 16-bit floats in registers, a thread one row of the tile, and store them to tensor memory as the
-//     A operand: the weights never go back to shared memory, whose bandwidth the B operand needs;
-//   * warps 8-15 bring the rows of x into the 128-byte swizzled form of the B operand, from any alignment, as 16-bit or e4m3 values, zeros past
-//     the inner size and past the last row;
-//   * one thread of warp 16 issues the products, 8 x HALVES for each 128 of the inner dimension;
-//   * warps 0-7 read D back, multiply by the row's power of two and x's scale in 32 bits, and write through shared memory.
+// The weights are the rows of the product, so few rows of x make a narrow product and not a padded one:
+//     D (256 rows of weights x up to 256 rows of x, 32 bits, tensor memory) += A (tensor memory) . B (shared memory)
+// A pair of CTAs (tcgen05 cta_group::2) owns such a tile: each holds 128 rows of weights, and HALF of the rows of x, which both
+// tensor cores read: with 128 x 256 tiles of single CTAs the rows of x alone would cross L2 -> SM at 64 bytes a clock and SM.
+// A CTA of 18 warps:
+//   * warp 16 streams the laid-out weights with their scales (bulk copies) and its half of the rows of x (tensor-map copies, which swizzle
+//     and fill with zeros past the inner size and the last row) into a ring of shared memory;
+//   * warps 0-15 turn weights into 16-bit floats in registers, a thread one row of a 128 x 128 tile, and store them to tensor memory as
+//     the A operand: they never go back to shared memory, whose bandwidth the B operand needs.  Four groups of four warps take the tiles
+//     in turn, each with an A buffer of its own;
+//   * one thread of warp 17 of the pair's first CTA issues the products, eight for each 128 of the inner dimension;
+//   * warps 0-15 read D back, multiply by the row's power of two and x's scale in 32 bits, and write.
+// The CTAs stay and take tile after tile; the first A buffers of a tile are filled before the tile before it is read back.
 //
-// A weight is held in 16 bits as S 2^-e (Q - Z) (e: llm.h, w4_pack.cu): this rounding, to bf16 beside bf16 rows and to f16 beside f16 and
-// e4m3 rows, is the price of one product per 128-deep tile over a group's sums being scaled apart in 32 bits, which would double
-// the traffic of tensor memory.  It is as large as the rounding of the result to the same type.  As in the kernel for few rows, a masked nibble
-// is a subnormal number: without zero points S (q - 8) is ONE packed multiply-add, S q - 8 S, with 8 S exact; with zero points S z
-// need not be exact, so (q - z) comes first, exactly, and the scale second.
+// A weight is held in 16 bits as S 2^-e (Q - Z) (e: w4_pack.cu): this rounding, to bf16 beside bf16 rows and to f16 beside f16 and
+// e4m3 rows, is the price of one chain of products over the whole inner dimension; sums of a group scaled apart in 32 bits would
+// cross tensor memory once per group.  It is as large as the rounding of the result to the same type.  As in the kernel for few rows, a masked
+// nibble is a subnormal number: without zero points S (q - 8) is ONE packed multiply-add, S q - 8 S, with 8 S exact; with zero points
+// S z need not be exact, so (q - z) comes first, exactly, and the scale second.
 //
-// Where tiles are too few to fill the GPU, the CTAs of a cluster split the inner dimension and add their sums in a fixed order over
-// distributed shared memory.  Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
+// Where tiles are too few to fill the GPU, up to four pairs of a cluster split the inner dimension and add their sums in a fixed
+// order over distributed shared memory.  Rows of x that a tensor map cannot take as they are (e4m3, other alignments, the rows of an
+// expert's tokens) are first written to the workspace in order, in 16 bits (rows_kernel).
+//
+// Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
 #include <cooperative_groups.h>
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+
+#include <atomic>
 
 #include "llm.h"
 #include "strassen_b200.h"
@@ -33,14 +42,14 @@ namespace strassen {
 
 namespace {
 
-enum { XBF16 = 0, XF16 = 1, XE4M3 = 2 };
-
-constexpr int TOKENS = 128;                 // most rows of x in a tile
-constexpr int DEQUANT_WARPS = 8, LOAD_WARPS = 8, THREADS = 32 * (DEQUANT_WARPS + LOAD_WARPS + 2);
-constexpr int MMA_WARP = 16, COPY_WARP = 17;
+constexpr int TOKENS = 256;                 // most rows of x in a tile
+constexpr int BOX = 16;                     // rows of x in one copy; a tile has a multiple of 2 * BOX
+constexpr int GROUPS = 4;                   // groups of four warps that turn weights, and A buffers
+constexpr int TURN_WARPS = 4 * GROUPS, COPY_WARP = TURN_WARPS, MMA_WARP = TURN_WARPS + 1, THREADS = 32 * (TURN_WARPS + 2);
 constexpr int MAX_STAGES = 8;
 constexpr int A_COLUMN = 256;               // first tensor-memory column of the A buffers; D is below
 constexpr int A_WIDTH = 64;                 // columns of 128 rows x 128 values of 16 bits
+constexpr int W_BYTES = kW4TileBytes + 1024 + 512;      // of a stage: weights, scales, zero points
 constexpr uint32_t kWaitLimit = 1u << 22;   // tries of a wait; each may sleep for a while
 
 // Set by a CTA that gave up on a wait; read and cleared by strassen_device_status.
@@ -50,28 +59,40 @@ struct Args {
     const uint8_t *packed, *zeros;
     const uint16_t *scales;
     const float *exponents;
-    const void *x;
     const float *x_scale;
     void *out;
-    int64_t n, k, m, ldx_bytes, ldo, depth_tiles, row_tiles;
+    int64_t n, m, ldo, depth_tiles;
+    int row_tiles;           // of one matrix
     int group_words;
-    int x_align;
-    int tokens;              // rows of x in a tile, a multiple of 16
-    int stages, stage_bytes, x_bytes;
+    int tokens;              // rows of x in a tile, a multiple of 2 * BOX
+    int stages, stage_bytes;
     int out_type;
-    bool scale_bf16, out_wide;
+    bool scale_bf16, out_pairs;
+    const W4Tile *table;     // experts: the tiles of rows and their number; NULL: every `tokens` rows a tile
+    const int *table_size;
+    const int *order;        // experts: which pair a row of x is
+    int scale_div;           // experts: x_scale of pair i is x_scale[i / scale_div]
 };
 
+// full_w / empty_w: weights of a ring stage have arrived / have been read; full_x: the pair's rows of x are in place; used: the products that
+// read the stage and the A buffer of its tile are done; full_a: the pair's A buffers are written; done: all products of a tile of
+// results are; d_free: the pair has read them back.  full_x, full_a and d_free count in the pair's first CTA.
 struct Shared {
-    uint64_t full_w[MAX_STAGES], empty_w[MAX_STAGES], full_x[MAX_STAGES], empty_x[MAX_STAGES], full_a[4], empty_a[4], done;
+    uint64_t full_w[MAX_STAGES], empty_w[MAX_STAGES], full_x[MAX_STAGES], used[MAX_STAGES], full_a[GROUPS], done, d_free;
     uint32_t tmem;
     int dead;
-    int64_t row_at[TOKENS];          // byte offset of each row of x; -1: none
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint32_t of_rank(const void *p, uint32_t rank)
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count)); }
 __device__ __forceinline__ void bar_arrive(uint64_t *b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory"); }
+__device__ __forceinline__ void bar_arrive_at(uint32_t b) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(b) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
@@ -79,12 +100,9 @@ __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
 }
-// For whole warps: the same answer in every lane, so that a warp leaves its loop as one.
-__device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *sh);
-__device__ __forceinline__ bool warp_wait_for(uint64_t *b, uint32_t parity, Shared *sh) { return __all_sync(~0u, wait_for(b, parity, sh)); }
 // Waits until phase `parity` of the barrier is over.  False: the limit was reached, here or elsewhere in the CTA, and the caller leaves
 // its loop; nothing that comes later waits long, and the results of the call are not valid.
 __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *sh)
@@ -97,22 +115,41 @@ __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *s
     g_gave_up = 1;
     return false;
 }
+// For whole warps: the same answer in every lane, so that a warp leaves its loop as one.
+__device__ __forceinline__ bool warp_wait_for(uint64_t *b, uint32_t parity, Shared *sh) { return __all_sync(~0u, wait_for(b, parity, sh)); }
+// One lane of a whole warp, known as such to the compiler: tensor instructions and bulk copies issued by a lane that a comparison
+// picked cost 105 clocks each and more, whatever their size; by an elected one, what the tensor cores take.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+    return ok != 0;
+}
 __device__ __forceinline__ void bulk_copy(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void commit(uint64_t *bar)
+// A box of 64 values x BOX rows; the barrier may be the other CTA's of the pair.  k is a multiple of 64 (128 bytes).
+__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap *map, int k, int row, uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(k), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t *bar, uint16_t mask)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"(mask) : "memory");
 }
 __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 // Shared-memory descriptor of a K-major operand whose rows of 64 values (128 bytes) are swizzled in groups of 8 (1024 bytes).
 __device__ __forceinline__ uint64_t operand(uint32_t addr)
 {
     return uint64_t((addr & 0x3ffff) >> 4) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void st_tmem32(uint32_t at, const uint32_t (&v)[32])
 {
@@ -186,97 +223,162 @@ __device__ __forceinline__ float scale_value(uint32_t bits, bool bf16)
     return bf16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half(uint16_t(bits)));
 }
 
-// 8 values of a row of x from k on, as 16 bits each.
-template <int XT> __device__ __forceinline__ uint4 load_x(const char *row, int64_t k, int64_t size, int align)
+
+__device__ __forceinline__ uint32_t to_16_bits(float v, int type)
 {
-    uint32_t v[4] = {0, 0, 0, 0};
-    if constexpr (XT == XE4M3) {
-        const uint8_t *p = reinterpret_cast<const uint8_t *>(row) + k;
-        uint32_t w[2] = {0, 0};
-        if (align >= 8 && k + 8 <= size) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(p);
-            w[0] = u.x;
-            w[1] = u.y;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < size) w[i >> 2] |= uint32_t(p[i]) << (8 * (i & 3));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-            v[i] = uint32_t(h.x) | (uint32_t(h.y) << 16);
-        }
-    } else {
-        const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + k;
-        if (align >= 16 && k + 8 <= size) return *reinterpret_cast<const uint4 *>(p);
-        if (align >= 4 && k + 8 <= size) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const uint32_t *>(p)[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = k + 2 * i < size ? p[2 * i] : 0, hi = k + 2 * i + 1 < size ? p[2 * i + 1] : 0;
-                v[i] = lo | (hi << 16);
-            }
-        }
-    }
-    return make_uint4(v[0], v[1], v[2], v[3]);
+    return type == STRASSEN_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
 }
 
-template <int XT, int HALVES, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p)
+// BF16: x and weights are bf16, else f16.
+template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
 {
-    using N = Num<XT == XBF16>;
-    constexpr int A_BUFFERS = HALVES == 2 ? 2 : 4, ROWS = 128 * HALVES;
+    using N = Num<BF16>;
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
-    uint8_t *const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);      // the swizzle's groups start at multiples of 1024
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t nt0 = int64_t(blockIdx.x) * HALVES, row0 = nt0 * kW4Rows, t0 = int64_t(blockIdx.z) * p.tokens;
-    const int splits = int(gridDim.y);
-    const int kb0 = int(p.depth_tiles * blockIdx.y / splits), tiles = int(p.depth_tiles * (blockIdx.y + 1) / splits) - kb0;
+    uint8_t *const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);      // the swizzle's groups start at multiples of 1024; the same place in every CTA
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;     // the shuffle: known to be one value per warp
+    const int side = blockIdx.x & 1, splits = int(gridDim.y);
+    const uint32_t first_rank = 2 * blockIdx.y;                                // cluster rank of the pair's first CTA
+    const int kb0 = int(p.depth_tiles * blockIdx.y / splits), depth = int(p.depth_tiles * (blockIdx.y + 1) / splits) - kb0;
     const int per_tile = 4 / p.group_words;                                   // groups of a 128-deep tile
+    const int row_pairs = (p.row_tiles + 1) / 2;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
             bar_init(&sh.full_w[i], 1);
-            bar_init(&sh.empty_w[i], HALVES == 2 ? 8 : 4);
-            bar_init(&sh.full_x[i], LOAD_WARPS);
-            bar_init(&sh.empty_x[i], 1);
+            bar_init(&sh.empty_w[i], 4);
+            bar_init(&sh.full_x[i], 1);
+            bar_init(&sh.used[i], 1);
         }
-        for (int i = 0; i < A_BUFFERS; ++i) {
-            bar_init(&sh.full_a[i], HALVES == 2 ? 8 : 4);
-            bar_init(&sh.empty_a[i], 1);
-        }
+        for (int i = 0; i < GROUPS; ++i) bar_init(&sh.full_a[i], 8);
         bar_init(&sh.done, 1);
+        bar_init(&sh.d_free, 2 * TURN_WARPS);
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh.tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    for (int i = threadIdx.x; i < p.tokens; i += THREADS) sh.row_at[i] = t0 + i < p.m ? (t0 + i) * p.ldx_bytes : -1;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh.tmem;
-    const int w_at = p.x_bytes, s_at = w_at + HALVES * kW4TileBytes, z_at = s_at + HALVES * 1024;    // sections of a stage
 
-    if (warp < DEQUANT_WARPS) {
-        // ---- weights to tensor memory --------------------------------------------------------------------------------
+    // tiles of results: those of one run of rows of x side by side, so that its CTAs share the rows in L2
+    const int64_t tile_count = int64_t(row_pairs) * (p.table ? *p.table_size : int((p.m + p.tokens - 1) / p.tokens));
+    const int64_t first = blockIdx.x >> 1, stride = gridDim.x >> 1;
+    const int mine = first < tile_count ? int((tile_count - first + stride - 1) / stride) : 0;
+    struct Tile {
+        int64_t nt;              // this CTA's tile of 128 rows of weights, over all matrices; one past the last: the last again, not written
+        int64_t row0;            // its first row in its matrix
+        int64_t t0;              // first row of x
+        int count, tokens;       // rows of x, and what they are padded to
+    };
+    auto tile_at = [&](int i) {
+        const int64_t at = first + i * stride, run = at / row_pairs;
+        const int pair = int(at % row_pairs), rt = 2 * pair + side;
+        Tile t;
+        int64_t matrix = 0;
+        if (p.table) {
+            const W4Tile e = p.table[run];
+            matrix = e.expert;
+            t.t0 = e.first;
+            t.count = e.count;
+            t.tokens = (e.count + 2 * BOX - 1) / (2 * BOX) * (2 * BOX);
+        } else {
+            t.t0 = run * p.tokens;
+            t.count = int(p.m - t.t0 < p.tokens ? p.m - t.t0 : p.tokens);
+            t.tokens = p.tokens;
+        }
+        t.row0 = int64_t(rt) * kW4Rows;
+        t.nt = matrix * p.row_tiles + (rt < p.row_tiles ? rt : p.row_tiles - 1);
+        return t;
+    };
+    const int w_at = p.tokens * 128, s_at = w_at + kW4TileBytes, z_at = s_at + 1024;      // sections of a stage; this CTA's rows of x come first
+
+    if (warp < TURN_WARPS) {
         const int group = warp >> 2, r = (warp & 3) * 32 + lane;
-        const int half = HALVES == 2 ? group : 0;
-        const float down = 1.f / p.exponents[(nt0 + half < p.row_tiles ? nt0 + half : p.row_tiles - 1) * kW4Rows + r];      // 2^-e
+        const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
         const int place = W4Layout::row_place(r);
-        for (int t = HALVES == 2 ? 0 : group; t < tiles; t += HALVES == 2 ? 1 : 2) {
-            const int s = t % p.stages, a = t % A_BUFFERS;
-            if (!warp_wait_for(&sh.full_w[s], (t / p.stages) & 1, &sh)) break;
+        const uint32_t full_a = of_rank(&sh.full_a[group], first_rank), d_free = of_rank(&sh.d_free, first_rank);
+
+        // ---- results of tile i; with splits this CTA's part of the sums stays in the ring ------------------------------------
+        auto read_back = [&](int i) {
+            if (!warp_wait_for(&sh.done, i & 1, &sh)) return false;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const Tile t = tile_at(i);
+            const int64_t row = t.row0 + r;
+            const float back = N::BACK * p.exponents[t.nt * kW4Rows + r];
+            for (int c = 16 * group; c < t.tokens; c += 16 * GROUPS) {
+                uint32_t v[16];
+                ld_tmem16(v, lanes + c);
+                if (splits > 1) {
+                    float *sums = reinterpret_cast<float *>(ring);
+#pragma unroll
+                    for (int b = 0; b < 16; ++b) sums[(c + b) * kW4Rows + r] = __uint_as_float(v[b]);
+                    continue;
+                }
+                int to[16];          // row of the result; -1: none
+#pragma unroll
+                for (int b = 0; b < 16; ++b) {
+                    const int at = int(t.t0) + c + b;
+                    to[b] = c + b >= t.count ? -1 : p.order ? p.order[at] : at;
+                    float y = __uint_as_float(v[b]) * back;
+                    if (p.x_scale && to[b] >= 0) y *= p.x_scale[p.order ? to[b] / p.scale_div : to[b]];
+                    v[b] = __float_as_uint(y);
+                }
+                if (p.out_type == STRASSEN_F32) {
+#pragma unroll
+                    for (int b = 0; b < 16; ++b)
+                        if (to[b] >= 0 && row < p.n) static_cast<float *>(p.out)[int64_t(to[b]) * p.ldo + row] = __uint_as_float(v[b]);
+                } else if (p.out_pairs) {
+                    // neighbouring rows of weights are neighbours in memory: two lanes trade so that each writes two of them, one its row of x, one the next
+#pragma unroll
+                    for (int b = 0; b < 16; b += 2) {
+                        const uint32_t lo = to_16_bits(__uint_as_float(v[b]), p.out_type), hi = to_16_bits(__uint_as_float(v[b + 1]), p.out_type);
+                        const uint32_t got = __shfl_xor_sync(~0u, lane & 1 ? lo : hi, 1);
+                        const uint32_t word = lane & 1 ? got | (hi << 16) : lo | (got << 16);
+                        const int64_t at = lane & 1 ? to[b + 1] : to[b];
+                        const int64_t even = row & ~int64_t(1);
+                        uint16_t *o = static_cast<uint16_t *>(p.out) + at * p.ldo + even;
+                        if (at >= 0 && even + 1 < p.n) *reinterpret_cast<uint32_t *>(o) = word;
+                        else if (at >= 0 && even < p.n) *o = uint16_t(word);
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 16; ++b)
+                        if (to[b] >= 0 && row < p.n) static_cast<uint16_t *>(p.out)[int64_t(to[b]) * p.ldo + row] = uint16_t(to_16_bits(__uint_as_float(v[b]), p.out_type));
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive_at(d_free);
+            return true;
+        };
+
+        // ---- weights to tensor memory: every GROUPS-th of the 128-deep tiles g of all tiles of results --------------------------
+        int read = 0;            // tiles of results read back
+        bool alive = true;
+        float down = 0.f;
+        int down_of = -1;
+        for (int64_t g = group; alive && g < int64_t(mine) * depth; g += GROUPS) {
+            const int i = int(g / depth), j = int(g % depth);
+            // the first A buffers of a tile are filled before the tile before it is read back
+            while (alive && read < i && (j >= GROUPS - 1 || read < i - 1)) alive = read_back(read++);
+            if (!alive) break;
+            if (down_of != i) {
+                down = 1.f / p.exponents[tile_at(i).nt * kW4Rows + r];      // 2^-e
+                down_of = i;
+            }
+            const int s = int(g % p.stages);
+            if (!warp_wait_for(&sh.full_w[s], uint32_t(g / p.stages) & 1, &sh)) break;
             const uint8_t *stage = ring + s * p.stage_bytes;
             uint32_t w[4][4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(stage + w_at + half * kW4TileBytes + c * 2048 + r * 16);
+                const uint4 u = *reinterpret_cast<const uint4 *>(stage + w_at + c * 2048 + r * 16);
                 w[c][0] = u.x;
                 w[c][1] = u.y;
                 w[c][2] = u.z;
@@ -285,287 +387,292 @@ template <int XT, int HALVES, bool ZEROS> __global__ void __launch_bounds__(THRE
             uint16_t sc[4];
             uint8_t z[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = (i / p.group_words) * kW4Rows + place;
-                sc[i] = *reinterpret_cast<const uint16_t *>(stage + s_at + half * 1024 + at * 2);
-                if (ZEROS) z[i] = stage[z_at + half * 512 + at];
+            for (int b = 0; b < 4; ++b) {
+                const int at = (b / p.group_words) * kW4Rows + place;
+                sc[b] = *reinterpret_cast<const uint16_t *>(stage + s_at + at * 2);
+                if (ZEROS) z[b] = stage[z_at + at];
             }
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.empty_w[s]);
-            if (!warp_wait_for(&sh.empty_a[a], ((t / A_BUFFERS) & 1) ^ 1, &sh)) break;
+            // the buffer is free when the products of the tile that used it are done
+            const int64_t before = g - GROUPS;
+            if (before >= 0 && !warp_wait_for(&sh.used[before % p.stages], uint32_t(before / p.stages) & 1, &sh)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = tmem + (uint32_t((warp & 3) * 32) << 16) + A_COLUMN + (a * HALVES + half) * A_WIDTH;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t v[32];                      // column 16 w + 4 c + pair
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int i = 2 * h + j;
-                    const float sn = scale_value(sc[i], p.scale_bf16) * down;
+                for (int jj = 0; jj < 2; ++jj) {
+                    const int b = 2 * h + jj;
+                    const float sn = scale_value(sc[b], p.scale_bf16) * down;
                     if (ZEROS) {
-                        const uint32_t minus = N::both(-N::STEP * float(z[i])), scale = N::both(sn * (N::UNIT / N::STEP));
+                        const uint32_t minus = N::both(-N::STEP * float(z[b])), scale = N::both(sn * (N::UNIT / N::STEP));
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t u = w[c][i], uu = u >> 8;
-                            v[16 * j + 4 * c + 0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), scale);
-                            v[16 * j + 4 * c + 1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), scale);
-                            v[16 * j + 4 * c + 2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), scale);
-                            v[16 * j + 4 * c + 3] = N::mul(N::fma(uu & 0x00f000f0, N::SMALL, minus), scale);
+                            const uint32_t u = w[c][b], uu = u >> 8;
+                            v[16 * jj + 4 * c + 0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), scale);
+                            v[16 * jj + 4 * c + 1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), scale);
+                            v[16 * jj + 4 * c + 2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), scale);
+                            v[16 * jj + 4 * c + 3] = N::mul(N::fma(uu & 0x00f000f0, N::SMALL, minus), scale);
                         }
                     } else {
                         const uint32_t big = N::both(sn * N::FACTOR), small = N::both(sn * (N::FACTOR / 16)), minus = N::both(sn * (-8 * N::UNIT));
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t u = w[c][i], uu = u >> 8;
-                            v[16 * j + 4 * c + 0] = N::fma(u & 0x000f000f, big, minus);
-                            v[16 * j + 4 * c + 1] = N::fma(u & 0x00f000f0, small, minus);
-                            v[16 * j + 4 * c + 2] = N::fma(uu & 0x000f000f, big, minus);
-                            v[16 * j + 4 * c + 3] = N::fma(uu & 0x00f000f0, small, minus);
+                            const uint32_t u = w[c][b], uu = u >> 8;
+                            v[16 * jj + 4 * c + 0] = N::fma(u & 0x000f000f, big, minus);
+                            v[16 * jj + 4 * c + 1] = N::fma(u & 0x00f000f0, small, minus);
+                            v[16 * jj + 4 * c + 2] = N::fma(uu & 0x000f000f, big, minus);
+                            v[16 * jj + 4 * c + 3] = N::fma(uu & 0x00f000f0, small, minus);
                         }
                     }
                 }
-                st_tmem32(at + 32 * h, v);
+                st_tmem32(lanes + A_COLUMN + group * A_WIDTH + 32 * h, v);
             }
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive(&sh.full_a[a]);
+            if (lane == 0) bar_arrive_at(full_a);
         }
-    } else if (warp < DEQUANT_WARPS + LOAD_WARPS) {
-        // ---- rows of x to the swizzled operand: 16 lanes a row, 8 values a lane ---------------------------------------
-        const int j = lane & 15, first = (warp - DEQUANT_WARPS) * 2 + (lane >> 4);
-        const int swizzled = (j >> 3) * (p.tokens * 128);            // which 64 of the 128
-        const char *x = static_cast<const char *>(p.x);
-        constexpr int PASSES = TOKENS / (2 * LOAD_WARPS);
-        uint4 v[PASSES];
-        auto fetch = [&](int t) {
-            const int64_t k = int64_t(kb0 + t) * kW4Depth + 8 * j;
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int row = first + i * 2 * LOAD_WARPS;
-                const int64_t at = row < p.tokens ? sh.row_at[row] : -1;
-                v[i] = at >= 0 ? load_x<XT>(x + at, k, p.k, p.x_align) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        if (tiles > 0) fetch(0);
-        for (int t = 0; t < tiles; ++t) {
-            const int s = t % p.stages;
-            if (!warp_wait_for(&sh.empty_x[s], ((t / p.stages) & 1) ^ 1, &sh)) break;
-            uint8_t *stage = ring + s * p.stage_bytes + swizzled;
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int row = first + i * 2 * LOAD_WARPS;
-                if (row < p.tokens) *reinterpret_cast<uint4 *>(stage + row * 128 + (((j & 7) ^ (row & 7)) << 4)) = v[i];
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive(&sh.full_x[s]);
-            if (t + 1 < tiles) fetch(t + 1);
-        }
-    } else if (warp == MMA_WARP) {
-        // ---- products ---------------------------------------------------------------------------------------------------
-        if (lane == 0) {
-            const uint32_t format = XT == XBF16 ? 1 : 0;
-            const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(p.tokens >> 3) << 17) | (uint32_t(128 >> 4) << 24);
+        while (alive && read < mine) alive = read_back(read++);
+    } else if (warp == COPY_WARP) {
+        // ---- weights and rows of x to shared memory ---------------------------------------------------------------------------
+        if (elected()) {
+            const uint32_t scale_bytes = uint32_t(per_tile) * 256, zero_bytes = ZEROS ? uint32_t(per_tile) * 128 : 0;
+            const uint32_t ring_at = smem_addr(ring);
+            int64_t g = 0;
             bool alive = true;
-            for (int t = 0; t < tiles && alive; ++t) {
-                const int s = t % p.stages, a = t % A_BUFFERS;
-                alive = wait_for(&sh.full_x[s], (t / p.stages) & 1, &sh) && wait_for(&sh.full_a[a], (t / A_BUFFERS) & 1, &sh);
+            for (int i = 0; i < mine && alive; ++i) {
+                const Tile t = tile_at(i);
+                const int rows = t.tokens / 2, row = int(t.t0) + side * rows;
+                for (int j = 0; j < depth; ++j, ++g) {
+                    const int s = int(g % p.stages);
+                    const uint32_t again = (uint32_t(g / p.stages) & 1) ^ 1;
+                    if (!(alive = wait_for(&sh.empty_w[s], again, &sh))) break;
+                    uint8_t *stage = ring + s * p.stage_bytes;
+                    const int64_t tile = t.nt * p.depth_tiles + kb0 + j;
+                    bar_expect(&sh.full_w[s], kW4TileBytes + scale_bytes + zero_bytes);
+                    bulk_copy(stage + w_at, p.packed + tile * kW4TileBytes, kW4TileBytes, &sh.full_w[s]);
+                    bulk_copy(stage + s_at, p.scales + tile * per_tile * kW4Rows, scale_bytes, &sh.full_w[s]);
+                    if (ZEROS) bulk_copy(stage + z_at, p.zeros + tile * per_tile * kW4Rows, zero_bytes, &sh.full_w[s]);
+                    if (!(alive = wait_for(&sh.used[s], again, &sh))) break;
+                    const uint32_t full_x = of_rank(&sh.full_x[s], first_rank), to = ring_at + s * p.stage_bytes;
+                    if (side == 0) bar_expect(&sh.full_x[s], uint32_t(t.tokens) * 256);       // of both CTAs
+                    const int k = (kb0 + j) * kW4Depth;
+                    for (int b = 0; b < rows; b += BOX) {
+                        box_copy(to + b * 128, &map, k, row + b, full_x);
+                        box_copy(to + rows * 128 + b * 128, &map, k + 64, row + b, full_x);
+                    }
+                }
+            }
+            if (!alive) {
+                // given up: the copies that are under way end before the CTA does
+                for (int s = 0; s < p.stages; ++s)
+                    for (uint32_t w = 0; w < 1024; ++w) {
+                        bar_try(&sh.full_w[s], 0);
+                        if (side == 0) bar_try(&sh.full_x[s], 0);
+                        __nanosleep(100);
+                    }
+            }
+        }
+    } else if (side == 0 && elected()) {
+        // ---- products -----------------------------------------------------------------------------------------------------------
+        constexpr uint32_t format = BF16 ? 1 : 0;
+        const uint16_t both = uint16_t(3u << first_rank);
+        int64_t g = 0;
+        bool alive = true;
+        for (int i = 0; i < mine && alive; ++i) {
+            const int tokens = tile_at(i).tokens;
+            const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(tokens >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+            if (i > 0 && !(alive = wait_for(&sh.d_free, (i - 1) & 1, &sh))) break;
+            for (int j = 0; j < depth; ++j, ++g) {
+                const int s = int(g % p.stages), a = int(g % GROUPS);
+                alive = wait_for(&sh.full_x[s], uint32_t(g / p.stages) & 1, &sh) && wait_for(&sh.full_a[a], uint32_t(g / GROUPS) & 1, &sh);
                 if (!alive) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t x_addr = smem_addr(ring + s * p.stage_bytes);
+                const uint32_t x_addr = smem_addr(ring) + s * p.stage_bytes;
+                const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + tokens * 64);
+                const uint32_t from = tmem + A_COLUMN + a * A_WIDTH;
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint64_t b = operand(x_addr + (kk >> 2) * (p.tokens * 128) + (kk & 3) * 32);
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
-                        mma(tmem + h * TOKENS, tmem + A_COLUMN + (a * HALVES + h) * A_WIDTH + kk * 8, b, idesc, t > 0 || kk > 0);
-                }
-                commit(&sh.empty_x[s]);
-                commit(&sh.empty_a[a]);
+                for (int kk = 0; kk < 8; ++kk) mma(tmem, from + kk * 8, (kk < 4 ? b0 : b1) + (kk & 3) * 2, idesc, j > 0 || kk > 0);
+                commit_pair(&sh.used[s], both);
             }
-            commit(&sh.done);
+            commit_pair(&sh.done, both);
         }
-    } else if (lane == 0) {
-        // ---- weights to shared memory -----------------------------------------------------------------------------------
-        const uint32_t scale_bytes = uint32_t(per_tile) * 256, zero_bytes = ZEROS ? uint32_t(per_tile) * 128 : 0;
-        int issued = 0;
-        for (; issued < tiles; ++issued) {
-            const int s = issued % p.stages;
-            if (!wait_for(&sh.empty_w[s], ((issued / p.stages) & 1) ^ 1, &sh)) break;
-            bar_expect(&sh.full_w[s], HALVES * (kW4TileBytes + scale_bytes + zero_bytes));
-            uint8_t *stage = ring + s * p.stage_bytes;
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                const int64_t nt = nt0 + h < p.row_tiles ? nt0 + h : p.row_tiles - 1;      // past the last tile: the last one again, its results not written
-                const int64_t tile = nt * p.depth_tiles + kb0 + issued;
-                bulk_copy(stage + w_at + h * kW4TileBytes, p.packed + tile * kW4TileBytes, kW4TileBytes, &sh.full_w[s]);
-                bulk_copy(stage + s_at + h * 1024, p.scales + tile * per_tile * kW4Rows, scale_bytes, &sh.full_w[s]);
-                if (ZEROS) bulk_copy(stage + z_at + h * 512, p.zeros + tile * per_tile * kW4Rows, zero_bytes, &sh.full_w[s]);
-            }
-        }
-        // no copy may be in flight when the ring is used for the results or the CTA ends
-        for (int t = issued > p.stages ? issued - p.stages : 0; t < issued; ++t)
-            for (uint32_t i = 0; i < kWaitLimit && !bar_try(&sh.full_w[t % p.stages], (t / p.stages) & 1); ++i) {}
     }
     __syncwarp();
-
-    // ---- results ------------------------------------------------------------------------------------------------------------
-    const bool finished = warp_wait_for(&sh.done, 0, &sh);
-    __syncthreads();                 // every role is through with the ring
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const int group = warp >> 2, r = (warp & 3) * 32 + lane;
-    if (splits == 1) {
-        constexpr int PITCH = ROWS * 2 + 16;          // bytes of one row of x's results in shared memory
-        if (warp < DEQUANT_WARPS && finished) {
-            const int half = HALVES == 2 ? group : 0;
-            const int64_t row = row0 + half * kW4Rows + r;
-            const float back = row < p.row_tiles * kW4Rows ? N::BACK * p.exponents[row] : 0.f;
-            for (int c = HALVES == 2 ? 0 : 16 * group; c < p.tokens; c += HALVES == 2 ? 16 : 32) {
-                uint32_t v[16];
-                ld_tmem16(v, tmem + (uint32_t((warp & 3) * 32) << 16) + half * TOKENS + c);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float y = __uint_as_float(v[i]) * back;
-                    if (p.x_scale) y *= t0 + c + i < p.m ? p.x_scale[t0 + c + i] : 0.f;
-                    uint16_t *to = reinterpret_cast<uint16_t *>(ring + (c + i) * PITCH) + half * kW4Rows + r;
-                    *to = p.out_type == STRASSEN_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
+    __syncthreads();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_barrier();               // the pair is through with its shared and tensor memory; the sums of all splits are in place
+    if (splits > 1) {
+        if (mine > 0) {
+            const Tile t = tile_at(0);
+            cg::cluster_group cluster = cg::this_cluster();
+            float *sums = reinterpret_cast<float *>(ring);
+            for (int e = threadIdx.x + int(blockIdx.y) * THREADS; e < t.count * kW4Rows; e += THREADS * splits) {
+                const int i = e / kW4Rows, c = e % kW4Rows;
+                float y = 0.f;
+                for (int b = 0; b < splits; ++b) y += cluster.map_shared_rank(sums, unsigned(2 * b + side))[e];
+                if (t.row0 + c < p.n) {
+                    y *= N::BACK * p.exponents[t.nt * kW4Rows + c];
+                    if (p.x_scale) y *= p.x_scale[t.t0 + i];
+                    static_cast<uint16_t *>(p.out)[(t.t0 + i) * p.ldo + t.row0 + c] = uint16_t(to_16_bits(y, p.out_type));
                 }
             }
         }
-        __syncthreads();
-        const int tokens = int(p.m - t0 < p.tokens ? p.m - t0 : p.tokens);
-        const int rows = int(p.n - row0 < ROWS ? p.n - row0 : ROWS);
-        uint16_t *out = static_cast<uint16_t *>(p.out) + t0 * p.ldo + row0;
-        if (p.out_wide) {
-            for (int e = threadIdx.x; e < tokens * (ROWS / 8); e += THREADS) {
-                const int i = e / (ROWS / 8), c = e % (ROWS / 8) * 8;
-                const uint16_t *from = reinterpret_cast<const uint16_t *>(ring + i * PITCH) + c;
-                if (c + 8 <= rows) *reinterpret_cast<uint4 *>(out + i * p.ldo + c) = *reinterpret_cast<const uint4 *>(from);
-                else
-                    for (int b = 0; c + b < rows; ++b) out[i * p.ldo + c + b] = from[b];
-            }
-        } else {
-            for (int e = threadIdx.x; e < tokens * ROWS; e += THREADS) {
-                const int i = e / ROWS, c = e % ROWS;
-                if (c < rows) out[i * p.ldo + c] = reinterpret_cast<const uint16_t *>(ring + i * PITCH)[c];
-            }
-        }
-    } else {
-        // partial sums side by side in the cluster: [row of x][row of weights], 32 bits
-        float *sums = reinterpret_cast<float *>(ring);
-        if (warp < DEQUANT_WARPS && finished) {
-            const int half = HALVES == 2 ? group : 0;
-            for (int c = HALVES == 2 ? 0 : 16 * group; c < p.tokens; c += HALVES == 2 ? 16 : 32) {
-                uint32_t v[16];
-                ld_tmem16(v, tmem + (uint32_t((warp & 3) * 32) << 16) + half * TOKENS + c);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sums[(c + i) * ROWS + half * kW4Rows + r] = __uint_as_float(v[i]);
-            }
-        }
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
-        const int tokens = int(p.m - t0 < p.tokens ? p.m - t0 : p.tokens);
-        for (int e = threadIdx.x + int(blockIdx.y) * THREADS; e < tokens * ROWS; e += THREADS * splits) {
-            const int i = e / ROWS, c = e % ROWS;
-            float y = 0.f;
-            for (int b = 0; b < splits; ++b) y += cluster.map_shared_rank(sums, b)[e];
-            if (row0 + c < p.n) {
-                y *= N::BACK * p.exponents[row0 + c];
-                if (p.x_scale) y *= p.x_scale[t0 + i];
-                static_cast<uint16_t *>(p.out)[(t0 + i) * p.ldo + row0 + c] =
-                    p.out_type == STRASSEN_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
-            }
-        }
-        cluster.sync();              // no CTA leaves while another reads its sums
+        cluster_barrier();           // no CTA leaves while another reads its sums
     }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-constexpr int kDynamicLimit = 222 * 1024;         // of 227 KB: the rest holds Shared
-
-template <int XT, int HALVES, bool ZEROS> cudaError_t launch_one(Args p, int splits, cudaStream_t stream)
+// Rows of x in 16 bits, one after another, `width` (a multiple of 8) values apart, zeros past the inner size: e4m3 becomes f16, exactly.
+__global__ void __launch_bounds__(256) rows_kernel(const char *x, int64_t ldx_bytes, int64_t rows, int64_t k, int64_t width, bool e4m3, bool wide, const int *order, int order_div, uint16_t *out)
 {
-    p.x_bytes = p.tokens * 256;
-    p.stage_bytes = (p.x_bytes + HALVES * (kW4TileBytes + 1024 + 512) + 1023) / 1024 * 1024;
-    int stages = (kDynamicLimit - 1024) / p.stage_bytes;
-    p.stages = stages > MAX_STAGES ? MAX_STAGES : stages;
-    int bytes = p.stages * p.stage_bytes;
-    const int rows = 128 * HALVES, results = splits == 1 ? p.tokens * (rows * 2 + 16) : p.tokens * rows * 4;
-    if (results > bytes) bytes = results;
-    bytes += 1024;
-    cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<XT, HALVES, ZEROS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
+    const int64_t chunks = width / 8, total = rows * chunks;
+    for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
+        const int64_t i = e / chunks, c = e % chunks * 8;
+        const int64_t row = order ? order[i] / order_div : i;
+        uint32_t v[4] = {0, 0, 0, 0};
+        if (e4m3) {
+            const uint8_t *p = reinterpret_cast<const uint8_t *>(x + row * ldx_bytes) + c;
+            uint32_t w[2] = {0, 0};
+            if (wide && c + 8 <= k) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(p);
+                w[0] = u.x;
+                w[1] = u.y;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 8; ++b)
+                    if (c + b < k) w[b >> 2] |= uint32_t(p[b]) << (8 * (b & 3));
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w[b >> 1] >> (16 * (b & 1))), __NV_E4M3);
+                v[b] = uint32_t(h.x) | (uint32_t(h.y) << 16);
+            }
+        } else {
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(x + row * ldx_bytes) + c;
+            if (wide && c + 8 <= k) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(p);
+                v[0] = u.x;
+                v[1] = u.y;
+                v[2] = u.z;
+                v[3] = u.w;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 8; ++b)
+                    if (c + b < k) v[b >> 1] |= uint32_t(p[b]) << (16 * (b & 1));
+            }
+        }
+        *reinterpret_cast<uint4 *>(out + i * width + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+
+constexpr int kDynamicLimit = 225 * 1024;         // of 227 KB: the rest holds Shared
+
+template <bool BF16, bool ZEROS> cudaError_t launch_one(const Args &p, const CUtensorMap &map, int pairs, int splits, int bytes, cudaStream_t stream)
+{
+    cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZEROS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((p.row_tiles + HALVES - 1) / HALVES), unsigned(splits), unsigned((p.m + p.tokens - 1) / p.tokens));
+    cfg.gridDim = dim3(unsigned(2 * pairs), unsigned(splits));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = size_t(bytes);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1;
+    attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = unsigned(splits);
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, w4_tile_kernel<XT, HALVES, ZEROS>, p);
+    return cudaLaunchKernelEx(&cfg, w4_tile_kernel<BF16, ZEROS>, p, map);
 }
 
-template <int XT> cudaError_t launch_type(const Args &p, bool zeros, int sm_count, cudaStream_t stream)
+using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
+
+// The driver's function that fills a tensor map, looked up once.
+EncodeTiled encode_tiled()
 {
-    const int64_t token_tiles = (p.m + p.tokens - 1) / p.tokens;
-    // two row tiles share the rows of x that a CTA brings in: taken where that leaves enough CTAs
-    if ((p.row_tiles + 1) / 2 * token_tiles >= sm_count) return zeros ? launch_one<XT, 2, true>(p, 1, stream) : launch_one<XT, 2, false>(p, 1, stream);
-    int splits = 1;
-    while (splits < 8 && p.row_tiles * token_tiles * (splits + 1) <= sm_count && p.depth_tiles >= 2 * (splits + 1)) ++splits;
-    return zeros ? launch_one<XT, 1, true>(p, splits, stream) : launch_one<XT, 1, false>(p, splits, stream);
+    static std::atomic<EncodeTiled> found{nullptr};
+    EncodeTiled f = found.load(std::memory_order_acquire);
+    if (!f) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+        f = reinterpret_cast<EncodeTiled>(p);
+        found.store(f, std::memory_order_release);
+    }
+    return f;
 }
 
-int alignment(uintptr_t bits)
+bool map_takes(const W4Args &a)
 {
-    int a = 16;
-    while (bits % a) a /= 2;
-    return a;
+    return a.type != STRASSEN_E4M3 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx % 8 == 0;
 }
 
 }  // namespace
 
+int64_t w4_tiles_workspace(const W4Args &a) { return map_takes(a) ? 0 : a.m * ((a.lay.k + 7) / 8 * 8) * 2; }
+
 cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
 {
-    const int size = a.type == STRASSEN_E4M3 ? 1 : 2;
-    constexpr int64_t most = int64_t(65535) * TOKENS;            // rows of x in one launch: the grid's z
-    for (int64_t m0 = 0; m0 < a.m; m0 += most) {
-        Args p = {};
-        p.packed = a.packed;
-        p.zeros = a.packed + a.lay.zero_off;
-        p.scales = reinterpret_cast<const uint16_t *>(a.packed + a.lay.scale_off);
-        p.exponents = reinterpret_cast<const float *>(a.packed + a.lay.exponent_off);
-        p.x = static_cast<const char *>(a.x) + m0 * a.ldx * size;
-        p.x_scale = a.x_scale ? a.x_scale + m0 : nullptr;
-        p.out = static_cast<char *>(a.out) + m0 * a.ldo * 2;
-        p.n = a.lay.n;
-        p.k = a.lay.k;
-        p.m = a.m - m0 < most ? a.m - m0 : most;
-        p.ldx_bytes = a.ldx * size;
-        p.ldo = a.ldo;
-        p.depth_tiles = a.lay.depth_tiles;
-        p.row_tiles = a.lay.row_tiles;
-        p.group_words = a.lay.group / 32;
-        p.x_align = alignment(reinterpret_cast<uintptr_t>(p.x) | uintptr_t(p.m > 1 ? p.ldx_bytes : 0));
-        p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
-        p.out_type = a.out_type;
-        p.out_wide = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && (p.m == 1 || p.ldo % 8 == 0);
-        const int64_t tiles = (p.m + TOKENS - 1) / TOKENS;
-        p.tokens = int(((p.m + tiles - 1) / tiles + 15) / 16 * 16);
-        cudaError_t e;
-        if (a.type == STRASSEN_BF16) e = launch_type<XBF16>(p, a.lay.has_zeros, sm_count, stream);
-        else if (a.type == STRASSEN_F16) e = launch_type<XF16>(p, a.lay.has_zeros, sm_count, stream);
-        else e = launch_type<XE4M3>(p, a.lay.has_zeros, sm_count, stream);
+    const bool bf16 = a.type == STRASSEN_BF16;
+    const void *x = a.x;
+    int64_t ldx = a.ldx;
+    if (!map_takes(a)) {
+        const int size = a.type == STRASSEN_E4M3 ? 1 : 2;
+        ldx = (a.lay.k + 7) / 8 * 8;
+        const bool wide = (reinterpret_cast<uintptr_t>(a.x) | uintptr_t(a.ldx * size)) % (8 * size) == 0;
+        const int64_t blocks = (a.m * (ldx / 8) + 255) / 256, most = int64_t(sm_count) * 32;
+        rows_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(static_cast<const char *>(a.x), a.ldx * size, a.m, a.lay.k, ldx, a.type == STRASSEN_E4M3, wide, nullptr, 1, static_cast<uint16_t *>(a.workspace));
+        const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
+        x = a.workspace;
     }
-    return cudaSuccess;
+    Args p = {};
+    p.packed = a.packed;
+    p.zeros = a.packed + a.lay.zero_off;
+    p.scales = reinterpret_cast<const uint16_t *>(a.packed + a.lay.scale_off);
+    p.exponents = reinterpret_cast<const float *>(a.packed + a.lay.exponent_off);
+    p.x_scale = a.x_scale;
+    p.out = a.out;
+    p.n = a.lay.n;
+    p.m = a.m;
+    p.ldo = a.ldo;
+    p.depth_tiles = a.lay.depth_tiles;
+    p.row_tiles = int(a.lay.row_tiles);
+    p.group_words = a.lay.group / 32;
+    p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
+    p.out_type = a.out_type;
+    p.out_pairs = reinterpret_cast<uintptr_t>(p.out) % 4 == 0 && p.ldo % 2 == 0;
+    p.scale_div = 1;
+    // rows of x: as few tiles as hold them, evenly filled
+    const int64_t runs = (p.m + TOKENS - 1) / TOKENS;
+    p.tokens = int(((p.m + runs - 1) / runs + 2 * BOX - 1) / (2 * BOX) * (2 * BOX));
+    p.stage_bytes = (p.tokens * 128 + W_BYTES + 1023) / 1024 * 1024;
+    const int64_t tiles = (int64_t(p.row_tiles) + 1) / 2 * ((p.m + p.tokens - 1) / p.tokens);
+    const int most = sm_count / 2;
+    int splits = 1;
+    while (splits < 4 && tiles * (splits + 1) <= most && p.depth_tiles >= 2 * (splits + 1)) ++splits;
+    const int stages = (kDynamicLimit - 1024) / p.stage_bytes;
+    p.stages = stages > MAX_STAGES ? MAX_STAGES : stages;
+    int bytes = p.stages * p.stage_bytes;
+    if (splits > 1 && bytes < p.tokens * kW4Rows * 4) bytes = p.tokens * kW4Rows * 4;
+    bytes += 1024;
+
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorSymbolNotFound;
+    CUtensorMap map;
+    const cuuint64_t dims[2] = {cuuint64_t(a.lay.k), cuuint64_t(a.m)}, strides[1] = {cuuint64_t(ldx) * 2};
+    const cuuint32_t box[2] = {64, BOX}, steps[2] = {1, 1};
+    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    const int pairs = int(splits > 1 || tiles < most ? tiles : most);
+    if (bf16) return a.lay.has_zeros ? launch_one<true, true>(p, map, pairs, splits, bytes, stream) : launch_one<true, false>(p, map, pairs, splits, bytes, stream);
+    return a.lay.has_zeros ? launch_one<false, true>(p, map, pairs, splits, bytes, stream) : launch_one<false, false>(p, map, pairs, splits, bytes, stream);
 }
 
 cudaError_t read_gave_up(int *flag)

@@ -155,7 +155,13 @@ class W4Matrix:
             raise ValueError("the result is bfloat16 or float16, not %s" % out.dtype)
         ldx, ldo = _rows("x", x, (m, self.k), x.dtype, device), _rows("out", out, (m, self.n), out.dtype, device)
         xs = 0 if x_scale is None else _vector("x_scale", x_scale, m, torch.float32, device)
-        _call(device, binding.strassen_w4_matmul, self._h, m, _TYPES[x.dtype], x.data_ptr(), ldx, xs, _TYPES[out.dtype], out.data_ptr(), ldo)
+        at, kind, ws, need = x.data_ptr(), _TYPES[x.dtype], 0, 0
+        if m > binding.STRASSEN_W4_THIN_ROWS:
+            need = binding.strassen_w4_workspace_bytes(self._h, m, kind, at, ldx)
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)      # of the current stream, like the call
+                ws = workspace.data_ptr()
+        _call(device, binding.strassen_w4_matmul, self._h, m, kind, at, ldx, xs, _TYPES[out.dtype], out.data_ptr(), ldo, ws, need)
         return out
 
     def close(self):

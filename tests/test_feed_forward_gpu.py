@@ -191,6 +191,16 @@ W4_SHAPES = [(1, 1, 1), (1, 128, 128), (2, 16, 130), (1, 4096, 4096), (3, 100, 1
 @pytest.mark.parametrize("group,zeros", [(32, False), (32, True), (64, True), (128, False), (128, True)])
 @pytest.mark.parametrize("m,n,k", W4_SHAPES)
 def test_w4_product(m, n, k, group, zeros):
+    products(m, n, k, group, zeros)
+
+
+@pytest.mark.parametrize("m,n,k", [(3000, 4000, 100), (2100, 2600, 200), (1100, 5000, 300), (1300, 4200, 500), (700, 9000, 1500)])
+def test_w4_product_of_more_tiles_than_the_gpu_holds(m, n, k):
+    """Tiles of one, two and more steps of the inner dimension, taken by CTAs that stay."""
+    products(m, n, k, 64, True)
+
+
+def products(m, n, k, group, zeros):
     for dtype, out_dtype, sdtype in ((BF16, BF16, BF16), (F16, F16, F16), (E4M3, BF16, BF16), (E4M3, F16, F16), (BF16, F16, F16)):
         q, s, z = weights(n, k, group, zeros, sdtype, n + k)
         W, A = dense64(q, s, z, k, group)
