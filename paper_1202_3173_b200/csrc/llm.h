@@ -35,7 +35,9 @@ cudaError_t launch_silu_mul_quant(const RowArgs &a, cudaStream_t stream);
 // k = 32 w + 8 c + (0..7), w = 0..3, in the nibble order 0, 2, 4, 6, 1, 3, 5, 7 from the lowest nibble up, so that (word & 0x000f000f)
 // is the pair k = 0, 1, ((word >> 4) & 0x000f000f) the pair 2, 3, and so on.  A 16 x 128 piece is then the operand of
 // eight m16n8k16 products with one 16-byte load per lane and row, 32 rows x 128 are the rows of 32 lanes of tensor memory.
-constexpr int kW4Rows = 128, kW4Depth = 128, kW4TileBytes = kW4Rows * kW4Depth / 2;
+// The nibbles are followed by the tile's scales (128 of 16 bits for each group) and its zero points (128 bytes for each group), so that a tile is
+// one piece of memory.
+constexpr int kW4Rows = 128, kW4Depth = 128, kW4NibbleBytes = kW4Rows * kW4Depth / 2;
 
 struct W4Layout {
     int64_t n, k;
@@ -43,9 +45,11 @@ struct W4Layout {
     int scale_type;              // STRASSEN_BF16 / F16
     int has_zeros;
     int64_t row_tiles, depth_tiles;
-    // byte offsets of the sections of the packed memory
-    size_t scale_off, zero_off, exponent_off, bytes;
+    int tile_bytes;
+    // byte offset of the rows' exponents (w4_pack.cu) in the packed memory, and its size
+    size_t exponent_off, bytes;
 
+    __host__ __device__ int zero_off() const { return kW4NibbleBytes + kW4Depth / group * kW4Rows * 2; }     // within a tile
     // position of row r (0..127) of a tile in the scale and zero sections: rows g and g + 8 of a 16-row piece are neighbours
     __host__ __device__ static int row_place(int r) { return (r & ~15) | ((r & 7) << 1) | ((r >> 3) & 1); }
 };

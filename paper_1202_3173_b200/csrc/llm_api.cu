@@ -167,10 +167,8 @@ extern "C" strassen_w4 *strassen_w4_create(int64_t n, int64_t k, int group, int 
         fail(STRASSEN_INVALID_ARG, "the matrix is too large (2^31 tiles of 128 x 128)");
         return nullptr;
     }
-    const int64_t places = tiles * (kW4Depth / group) * kW4Rows;
-    l.scale_off = size_t(tiles) * kW4TileBytes;
-    l.zero_off = l.scale_off + size_t(round_up(places * 2, 256));
-    l.exponent_off = l.zero_off + size_t(l.has_zeros ? round_up(places, 256) : 0);
+    l.tile_bytes = kW4NibbleBytes + kW4Depth / group * kW4Rows * (l.has_zeros ? 3 : 2);
+    l.exponent_off = size_t(round_up(tiles * l.tile_bytes, 256));
     l.bytes = l.exponent_off + size_t(l.row_tiles) * kW4Rows * 4;
     strassen_w4 *w = new (std::nothrow) strassen_w4;
     if (!w) {

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
         }
         out[w] = word;
     }
-    uint4 *dst = reinterpret_cast<uint4 *>(p.packed + tile * kW4TileBytes);
+    uint4 *dst = reinterpret_cast<uint4 *>(p.packed + tile * p.lay.tile_bytes);
     dst[c * kW4Rows + r] = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
@@ -54,15 +54,16 @@ __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
     const int lane = threadIdx.x & 31;
     const int64_t nt = row / kW4Rows;
     const int place = W4Layout::row_place(int(row % kW4Rows));
-    const int64_t groups = (p.lay.k + p.lay.group - 1) / p.lay.group, places = p.lay.depth_tiles * (kW4Depth / p.lay.group);
-    uint16_t *scales = reinterpret_cast<uint16_t *>(p.packed + p.lay.scale_off) + nt * places * kW4Rows + place;
-    uint8_t *zeros = p.packed + p.lay.zero_off + nt * places * kW4Rows + place;
+    const int64_t groups = (p.lay.k + p.lay.group - 1) / p.lay.group;
+    const int per_tile = kW4Depth / p.lay.group;
     float mx = 0.f;
-    for (int64_t g = lane; g < places; g += 32) {
+    for (int64_t g = lane; g < p.lay.depth_tiles * per_tile; g += 32) {
         const bool on = row < p.lay.n && g < groups;
+        uint8_t *tile = p.packed + (nt * p.lay.depth_tiles + g / per_tile) * p.lay.tile_bytes;
+        const int at = int(g % per_tile) * kW4Rows + place;
         const uint16_t s = on ? static_cast<const uint16_t *>(p.scales)[row * p.lds + g] : uint16_t(0);
-        scales[g * kW4Rows] = s;
-        if (p.lay.has_zeros) zeros[g * kW4Rows] = on ? uint8_t(p.zeros[row * p.ldz + g] & 15) : uint8_t(8);
+        reinterpret_cast<uint16_t *>(tile + kW4NibbleBytes)[at] = s;
+        if (p.lay.has_zeros) tile[p.lay.zero_off() + at] = on ? uint8_t(p.zeros[row * p.ldz + g] & 15) : uint8_t(8);
         const float v = fabsf(scale_value(s, p.lay.scale_type));
         if (isfinite(v)) mx = fmaxf(mx, v);
     }

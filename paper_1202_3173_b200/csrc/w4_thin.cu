@@ -125,13 +125,13 @@ __device__ __forceinline__ float scale_value(uint32_t bits, bool bf16)
 }
 
 struct Ptrs {
-    const uint8_t *packed, *zeros;
-    const uint16_t *scales;
+    const uint8_t *packed;
     const void *x;
     const float *x_scale;
     void *out;
     int64_t n, k, m, ldx_bytes, ldo, depth_tiles;
     int group_words;         // words of a row's 16 bytes in one group: 1, 2 or 4
+    int tile_bytes, zero_off;
     int x_align;
     bool scale_bf16, out_bf16;
 };
@@ -146,7 +146,6 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
     const int64_t row0 = int64_t(blockIdx.x) * ROWS, nt = row0 / kW4Rows;
     const int r_in = int(row0 % kW4Rows);
     const int64_t t0 = int64_t(blockIdx.z) * TOKENS;
-    const int per_tile = 4 / p.group_words;       // groups of a 128-deep tile
 
     float acc[RT][TT][4] = {};
     const void *xrow[TT];
@@ -154,7 +153,8 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
     for (int t = 0; t < TT; ++t) xrow[t] = t0 + 8 * t + g < p.m ? static_cast<const char *>(p.x) + (t0 + 8 * t + g) * p.ldx_bytes : nullptr;
 
     for (int64_t kb = blockIdx.y * WARPS + warp; kb < p.depth_tiles; kb += int64_t(gridDim.y) * WARPS) {
-        const uint4 *tile = reinterpret_cast<const uint4 *>(p.packed + (nt * p.depth_tiles + kb) * kW4TileBytes) + c * kW4Rows + r_in + g;
+        const uint8_t *const packed = p.packed + (nt * p.depth_tiles + kb) * p.tile_bytes;
+        const uint4 *tile = reinterpret_cast<const uint4 *>(packed) + c * kW4Rows + r_in + g;
         uint32_t w[RT][2][4];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -172,14 +172,14 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
 #pragma unroll
         for (int gg = 0; gg < 4; ++gg) {
             if (gg % p.group_words == 0) {
-                const int64_t at = ((nt * p.depth_tiles + kb) * per_tile + gg / p.group_words) * kW4Rows + r_in + 2 * g;
+                const int at = gg / p.group_words * kW4Rows + r_in + 2 * g;
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    const uint32_t s = *reinterpret_cast<const uint32_t *>(p.scales + at + 16 * r);
+                    const uint32_t s = *reinterpret_cast<const uint32_t *>(packed + kW4NibbleBytes + 2 * (at + 16 * r));
                     scale[r][0] = scale_value(s & 0xffff, p.scale_bf16);
                     scale[r][1] = scale_value(s >> 16, p.scale_bf16);
                     uint32_t z = 0x0808;
-                    if (ZEROS) z = *reinterpret_cast<const uint16_t *>(p.zeros + at + 16 * r);
+                    if (ZEROS) z = *reinterpret_cast<const uint16_t *>(packed + p.zero_off + at + 16 * r);
                     minus[r][0] = N::both(-N::UNIT * float(z & 0xff));
                     minus[r][1] = N::both(-N::UNIT * float(z >> 8));
                 }
@@ -305,8 +305,8 @@ cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream)
     for (int64_t m0 = 0; m0 < a.m; m0 += most) {
         Ptrs p;
         p.packed = a.packed;
-        p.zeros = a.packed + a.lay.zero_off;
-        p.scales = reinterpret_cast<const uint16_t *>(a.packed + a.lay.scale_off);
+        p.tile_bytes = a.lay.tile_bytes;
+        p.zero_off = a.lay.zero_off();
         p.x = static_cast<const char *>(a.x) + m0 * a.ldx * size;
         p.x_scale = a.x_scale ? a.x_scale + m0 : nullptr;
         p.out = static_cast<char *>(a.out) + m0 * a.ldo * 2;

@@ -1,16 +1,17 @@
 // Products of many rows with a matrix of 4-bit weights on the fifth-generation tensor cores.
 //
 // The weights are the rows of the product, so few rows of x make a narrow product and not a padded one:
-//     D (256 rows of weights x up to 256 rows of x, 32 bits, tensor memory) += A (tensor memory) . B (shared memory)
-// A pair of CTAs (tcgen05 cta_group::2) owns such a tile: each holds 128 rows of weights, and HALF of the rows of x, which both
-// tensor cores read: with 128 x 256 tiles of single CTAs the rows of x alone would cross L2 -> SM at 64 bytes a clock and SM.
-// A CTA of 18 warps:
-//   * warp 16 streams the laid-out weights with their scales (bulk copies) and its half of the rows of x (tensor-map copies, which swizzle
-//     and fill with zeros past the inner size and the last row) into a ring of shared memory;
+//     D (128 rows of weights a CTA x up to 256 rows of x, 32 bits, tensor memory) += A (tensor memory) . B (shared memory)
+// Where there are tiles enough, a pair of CTAs (CTAS = 2, tcgen05 cta_group::2) owns 256 rows of weights, and each of the two brings in
+// HALF of the rows of x, which both tensor cores read: for single CTAs the rows of x alone would cross L2 -> SM at 64 bytes a clock and
+// SM.  Where there are few, single CTAs (CTAS = 1) spread over more of the GPU.  A CTA of 19 warps:
+//   * warp 16 streams the laid-out weights with their scales into a ring of shared memory (bulk copies), from before the CTA is set up;
+//   * warp 18 brings its part of the rows of x to the same ring (tensor-map copies, which swizzle and fill with zeros past the inner size
+//     and the last row);
 //   * warps 0-15 turn weights into 16-bit floats in registers, a thread one row of a 128 x 128 tile, and store them to tensor memory as
 //     the A operand: they never go back to shared memory, whose bandwidth the B operand needs.  Four groups of four warps take the tiles
 //     in turn, each with an A buffer of its own;
-//   * one thread of warp 17 of the pair's first CTA issues the products, eight for each 128 of the inner dimension;
+//   * one thread of warp 17 (of the pair's first CTA) issues the products, eight for each 128 of the inner dimension;
 //   * warps 0-15 read D back, multiply by the row's power of two and x's scale in 32 bits, and write.
 // The CTAs stay and take tile after tile; the first A buffers of a tile are filled before the tile before it is read back.
 //
@@ -20,12 +21,11 @@
 // nibble is a subnormal number: without zero points S (q - 8) is ONE packed multiply-add, S q - 8 S, with 8 S exact; with zero points
 // S z need not be exact, so (q - z) comes first, exactly, and the scale second.
 //
-// Where tiles are too few to fill the GPU, up to four pairs of a cluster split the inner dimension and add their sums in a fixed
-// order over distributed shared memory.  Rows of x that a tensor map cannot take as they are (e4m3, other alignments, the rows of an
+// Where even single CTAs' tiles are too few to fill the GPU, the CTAs of a cluster split the inner dimension and add their sums in a
+// fixed order over distributed shared memory.  Rows of x that a tensor map cannot take as they are (e4m3, other alignments, the rows of an
 // expert's tokens) are first written to the workspace in order, in 16 bits (rows_kernel).
 //
 // Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
-#include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -36,36 +36,36 @@
 #include "llm.h"
 #include "strassen_b200.h"
 
-namespace cg = cooperative_groups;
-
 namespace strassen {
 
 namespace {
 
-constexpr int TOKENS = 256;                 // most rows of x in a tile
-constexpr int BOX = 16;                     // rows of x in one copy; a tile has a multiple of 2 * BOX
+constexpr int TOKENS = 256;                 // most rows of x in a tile of a pair
+constexpr int ALONE_TOKENS = 176;           // ... of a single CTA: the ring has to keep as many stages as there are A buffers
+constexpr int STEP = 16;                    // rows of x that a CTA brings in: a multiple of this
 constexpr int GROUPS = 4;                   // groups of four warps that turn weights, and A buffers
-constexpr int TURN_WARPS = 4 * GROUPS, COPY_WARP = TURN_WARPS, MMA_WARP = TURN_WARPS + 1, THREADS = 32 * (TURN_WARPS + 2);
-constexpr int MAX_STAGES = 8;
+constexpr int TURN_WARPS = 4 * GROUPS, WEIGHT_WARP = TURN_WARPS, MMA_WARP = TURN_WARPS + 1, X_WARP = TURN_WARPS + 2, THREADS = 32 * (TURN_WARPS + 3);
+constexpr int MAX_STAGES = 8, MAX_SPLITS = 8;
 constexpr int A_COLUMN = 256;               // first tensor-memory column of the A buffers; D is below
 constexpr int A_WIDTH = 64;                 // columns of 128 rows x 128 values of 16 bits
-constexpr int W_BYTES = kW4TileBytes + 1024 + 512;      // of a stage: weights, scales, zero points
-constexpr uint32_t kWaitLimit = 1u << 22;   // tries of a wait; each may sleep for a while
+constexpr int64_t kWaitLimit = int64_t(1) << 31;      // clocks of a wait, about a second
 
 // Set by a CTA that gave up on a wait; read and cleared by strassen_device_status.
 __device__ int g_gave_up;
 
 struct Args {
-    const uint8_t *packed, *zeros;
-    const uint16_t *scales;
+    const uint8_t *packed;
     const float *exponents;
     const float *x_scale;
     void *out;
-    int64_t n, m, ldo, depth_tiles;
+    int64_t ldo, depth_tiles;
+    int n, m;
     int row_tiles;           // of one matrix
     int group_words;
-    int tokens;              // rows of x in a tile, a multiple of 2 * BOX
-    int stages, stage_bytes;
+    int tile_bytes, zero_off;
+    int tokens;              // rows of x in a tile, a multiple of CTAS * STEP
+    int box;                 // rows of x in one copy
+    int stages, stage_bytes, x_bytes;
     int out_type;
     bool scale_bf16, out_pairs;
     const W4Tile *table;     // experts: the tiles of rows and their number; NULL: every `tokens` rows a tile
@@ -74,11 +74,11 @@ struct Args {
     int scale_div;           // experts: x_scale of pair i is x_scale[i / scale_div]
 };
 
-// full_w / empty_w: weights of a ring stage have arrived / have been read; full_x: the pair's rows of x are in place; used: the products that
-// read the stage and the A buffer of its tile are done; full_a: the pair's A buffers are written; done: all products of a tile of
-// results are; d_free: the pair has read them back.  full_x, full_a and d_free count in the pair's first CTA.
+// full_w / empty_w: weights of a ring stage have arrived / have been read; ready: the pair's rows of x of the stage are in place, and its
+// weights are in their A buffers; used: the products that read those are done; done: all products of a tile of results are; d_free: the
+// pair has read them back.  ready and d_free count in the pair's first CTA.
 struct Shared {
-    uint64_t full_w[MAX_STAGES], empty_w[MAX_STAGES], full_x[MAX_STAGES], used[MAX_STAGES], full_a[GROUPS], done, d_free;
+    uint64_t full_w[MAX_STAGES], empty_w[MAX_STAGES], ready[MAX_STAGES], used[MAX_STAGES], done, d_free;
     uint32_t tmem;
     int dead;
 };
@@ -89,6 +89,24 @@ __device__ __forceinline__ uint32_t of_rank(const void *p, uint32_t rank)
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
+}
+__device__ __forceinline__ uint32_t of_address(uint32_t at, uint32_t rank)
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ float4 remote_float4(uint32_t at)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
 }
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count)); }
 __device__ __forceinline__ void bar_arrive(uint64_t *b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory"); }
@@ -107,9 +125,12 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 // its loop; nothing that comes later waits long, and the results of the call are not valid.
 __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *sh)
 {
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
-        if (bar_try(b, parity)) return true;
-        if ((i & 255) == 255 && *reinterpret_cast<volatile int *>(&sh->dead)) return false;
+    if (bar_try(b, parity)) return true;
+    for (const int64_t start = clock64(); clock64() - start < kWaitLimit;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (bar_try(b, parity)) return true;
+        if (*reinterpret_cast<volatile int *>(&sh->dead)) return false;
     }
     *reinterpret_cast<volatile int *>(&sh->dead) = 1;
     g_gave_up = 1;
@@ -129,18 +150,48 @@ __device__ __forceinline__ void bulk_copy(void *dst, const void *src, uint32_t b
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
 }
-// A box of 64 values x BOX rows; the barrier may be the other CTA's of the pair.  k is a multiple of 64 (128 bytes).
-__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap *map, int k, int row, uint32_t bar)
+// A box of 64 values x p.box rows; the barrier may be the other CTA's of the pair.  k is a multiple of 64 (128 bytes).
+template <int CTAS> __device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap *map, int k, int row, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(k), "r"(row), "r"(bar) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(k), "r"(row), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(k), "r"(row), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void commit_pair(uint64_t *bar, uint16_t mask)
+// Arrives at the barrier, in both CTAs of a pair, when the products issued so far are done.
+template <int CTAS> __device__ __forceinline__ void commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"(mask) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"(uint16_t(3)) : "memory");
 }
-__device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+template <int CTAS> __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+template <int CTAS> __device__ __forceinline__ void tmem_alloc(uint32_t *to)
+{
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(to)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(to)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+// After giving up: the copies that are under way end before the CTA does.
+__device__ __noinline__ void give_copies_time()
+{
+    for (int i = 0; i < 10000; ++i) __nanosleep(100);
+}
+template <int CTAS> __device__ __forceinline__ void tmem_free(uint32_t at)
+{
+    if constexpr (CTAS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
 }
 // Shared-memory descriptor of a K-major operand whose rows of 64 values (128 bytes) are swizzled in groups of 8 (1024 bytes).
 __device__ __forceinline__ uint64_t operand(uint32_t addr)
@@ -224,132 +275,152 @@ __device__ __forceinline__ float scale_value(uint32_t bits, bool bf16)
 }
 
 
-__device__ __forceinline__ uint32_t to_16_bits(float v, int type)
+// Two values as 16 bits each, the first in the low half.
+__device__ __forceinline__ uint32_t two_16_bits(float lo, float hi, bool bf16)
 {
-    return type == STRASSEN_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+    uint32_t d;
+    if (bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
 }
 
+enum { PLAIN = 0, SPLIT = 1, EXPERTS = 2 };
+
 // BF16: x and weights are bf16, else f16.
-template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
+template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
 {
     using N = Num<BF16>;
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t *const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);      // the swizzle's groups start at multiples of 1024; the same place in every CTA
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;     // the shuffle: known to be one value per warp
-    const int side = blockIdx.x & 1, splits = int(gridDim.y);
-    const uint32_t first_rank = 2 * blockIdx.y;                                // cluster rank of the pair's first CTA
-    const int kb0 = int(p.depth_tiles * blockIdx.y / splits), depth = int(p.depth_tiles * (blockIdx.y + 1) / splits) - kb0;
-    const int per_tile = 4 / p.group_words;                                   // groups of a 128-deep tile
-    const int row_pairs = (p.row_tiles + 1) / 2;
-
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) {
-            bar_init(&sh.full_w[i], 1);
-            bar_init(&sh.empty_w[i], 4);
-            bar_init(&sh.full_x[i], 1);
-            bar_init(&sh.used[i], 1);
-        }
-        for (int i = 0; i < GROUPS; ++i) bar_init(&sh.full_a[i], 8);
-        bar_init(&sh.done, 1);
-        bar_init(&sh.d_free, 2 * TURN_WARPS);
-        sh.dead = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == MMA_WARP) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh.tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    cluster_barrier();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = sh.tmem;
+    const int side = CTAS == 2 ? blockIdx.x & 1 : 0, splits = MODE == SPLIT ? int(gridDim.y) : 1;
+    const int kb0 = MODE == SPLIT ? int(p.depth_tiles * blockIdx.y / splits) : 0;
+    const int depth = (MODE == SPLIT ? int(p.depth_tiles * (blockIdx.y + 1) / splits) : int(p.depth_tiles)) - kb0;
+    const int columns = (p.row_tiles + CTAS - 1) / CTAS;                      // tiles of results side by side
 
     // tiles of results: those of one run of rows of x side by side, so that its CTAs share the rows in L2
-    const int64_t tile_count = int64_t(row_pairs) * (p.table ? *p.table_size : int((p.m + p.tokens - 1) / p.tokens));
-    const int64_t first = blockIdx.x >> 1, stride = gridDim.x >> 1;
-    const int mine = first < tile_count ? int((tile_count - first + stride - 1) / stride) : 0;
+    const int runs = MODE == EXPERTS ? *p.table_size : (p.m + p.tokens - 1) / p.tokens;
+    const int first = int(blockIdx.x) / CTAS, stride = int(gridDim.x) / CTAS, tile_count = columns * runs;
+    const int mine = first < tile_count ? (tile_count - first + stride - 1) / stride : 0;
     struct Tile {
-        int64_t nt;              // this CTA's tile of 128 rows of weights, over all matrices; one past the last: the last again, not written
-        int64_t row0;            // its first row in its matrix
-        int64_t t0;              // first row of x
+        int64_t nt;              // this CTA's tile of 128 rows of weights, over all matrices; past the last: the last again, not written
+        int row0;                // its first row in its matrix
+        int t0;                  // first row of x
         int count, tokens;       // rows of x, and what they are padded to
     };
     auto tile_at = [&](int i) {
-        const int64_t at = first + i * stride, run = at / row_pairs;
-        const int pair = int(at % row_pairs), rt = 2 * pair + side;
+        const int at = first + i * stride, run = at / columns, rt = (at - run * columns) * CTAS + side;
         Tile t;
-        int64_t matrix = 0;
-        if (p.table) {
+        t.nt = rt < p.row_tiles ? rt : p.row_tiles - 1;
+        if (MODE == EXPERTS) {
             const W4Tile e = p.table[run];
-            matrix = e.expert;
+            t.nt += int64_t(e.expert) * p.row_tiles;
             t.t0 = e.first;
             t.count = e.count;
-            t.tokens = (e.count + 2 * BOX - 1) / (2 * BOX) * (2 * BOX);
+            t.tokens = (e.count + CTAS * STEP - 1) / (CTAS * STEP) * (CTAS * STEP);
         } else {
             t.t0 = run * p.tokens;
-            t.count = int(p.m - t.t0 < p.tokens ? p.m - t.t0 : p.tokens);
+            t.count = p.m - t.t0 < p.tokens ? p.m - t.t0 : p.tokens;
             t.tokens = p.tokens;
         }
-        t.row0 = int64_t(rt) * kW4Rows;
-        t.nt = matrix * p.row_tiles + (rt < p.row_tiles ? rt : p.row_tiles - 1);
+        t.row0 = rt * kW4Rows;
         return t;
     };
-    const int w_at = p.tokens * 128, s_at = w_at + kW4TileBytes, z_at = s_at + 1024;      // sections of a stage; this CTA's rows of x come first
+    // the weights of the first tile's first steps are on their way before anything else is
+    const auto weights = [&](int64_t tile, int s) {
+        bar_expect(&sh.full_w[s], uint32_t(p.tile_bytes));
+        bulk_copy(ring + s * p.stage_bytes + p.x_bytes, p.packed + tile * p.tile_bytes, uint32_t(p.tile_bytes), &sh.full_w[s]);
+    };
+    const int ahead = mine == 0 ? 0 : depth < p.stages ? depth : p.stages;
+    if (warp == WEIGHT_WARP && elected()) {
+        for (int i = 0; i < p.stages; ++i) {
+            bar_init(&sh.full_w[i], 1);
+            bar_init(&sh.empty_w[i], 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (ahead > 0) {
+            const int64_t from = tile_at(0).nt * p.depth_tiles + kb0;
+            for (int j = 0; j < ahead; ++j) weights(from + j, j);
+        }
+    }
+    if (warp == X_WARP && elected()) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+        for (int i = 0; i < p.stages; ++i) {
+            bar_init(&sh.ready[i], 4 * CTAS + 1);
+            bar_init(&sh.used[i], 1);
+        }
+        bar_init(&sh.done, 1);
+        bar_init(&sh.d_free, TURN_WARPS * CTAS);
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MMA_WARP) tmem_alloc<CTAS>(&sh.tmem);
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CTAS == 2) cluster_barrier();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = sh.tmem;
+
+    const int w_at = p.x_bytes, s_at = w_at + kW4NibbleBytes, z_at = w_at + p.zero_off;      // sections of a stage; this CTA's rows of x come first
 
     if (warp < TURN_WARPS) {
         const int group = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
         const int place = W4Layout::row_place(r);
-        const uint32_t full_a = of_rank(&sh.full_a[group], first_rank), d_free = of_rank(&sh.d_free, first_rank);
+        const uint32_t ready = of_rank(sh.ready, CTAS == 2 ? 0 : cluster_rank()), d_free = of_rank(&sh.d_free, CTAS == 2 ? 0 : cluster_rank());
+        const bool bf16_out = p.out_type == STRASSEN_BF16;
 
         // ---- results of tile i; with splits this CTA's part of the sums stays in the ring ------------------------------------
         auto read_back = [&](int i) {
+            const Tile t = tile_at(i);
+            const int row = t.row0 + r;
+            const float back = N::BACK * p.exponents[t.nt * kW4Rows + r];
             if (!warp_wait_for(&sh.done, i & 1, &sh)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const Tile t = tile_at(i);
-            const int64_t row = t.row0 + r;
-            const float back = N::BACK * p.exponents[t.nt * kW4Rows + r];
             for (int c = 16 * group; c < t.tokens; c += 16 * GROUPS) {
+                if (MODE != SPLIT && c >= t.count) break;
                 uint32_t v[16];
                 ld_tmem16(v, lanes + c);
-                if (splits > 1) {
-                    float *sums = reinterpret_cast<float *>(ring);
+                if (MODE == SPLIT) {
+                    float *sums = reinterpret_cast<float *>(ring) + c * kW4Rows + r;
 #pragma unroll
-                    for (int b = 0; b < 16; ++b) sums[(c + b) * kW4Rows + r] = __uint_as_float(v[b]);
+                    for (int b = 0; b < 16; ++b) sums[b * kW4Rows] = __uint_as_float(v[b]);
                     continue;
                 }
-                int to[16];          // row of the result; -1: none
+                const int left = t.count - c;            // rows of x from here on
+                int to[16];                              // where they go
+                float y[16];
 #pragma unroll
                 for (int b = 0; b < 16; ++b) {
-                    const int at = int(t.t0) + c + b;
-                    to[b] = c + b >= t.count ? -1 : p.order ? p.order[at] : at;
-                    float y = __uint_as_float(v[b]) * back;
-                    if (p.x_scale && to[b] >= 0) y *= p.x_scale[p.order ? to[b] / p.scale_div : to[b]];
-                    v[b] = __float_as_uint(y);
+                    to[b] = t.t0 + c + (b < left ? b : 0);
+                    if (MODE == EXPERTS) to[b] = p.order[to[b]];
+                    y[b] = __uint_as_float(v[b]) * back;
                 }
-                if (p.out_type == STRASSEN_F32) {
+                if (p.x_scale) {
+#pragma unroll
+                    for (int b = 0; b < 16; ++b) y[b] *= p.x_scale[MODE == EXPERTS ? to[b] / p.scale_div : to[b]];
+                }
+                if (MODE == EXPERTS && p.out_type == STRASSEN_F32) {
 #pragma unroll
                     for (int b = 0; b < 16; ++b)
-                        if (to[b] >= 0 && row < p.n) static_cast<float *>(p.out)[int64_t(to[b]) * p.ldo + row] = __uint_as_float(v[b]);
-                } else if (p.out_pairs) {
-                    // neighbouring rows of weights are neighbours in memory: two lanes trade so that each writes two of them, one its row of x, one the next
+                        if (b < left && row < p.n) static_cast<float *>(p.out)[to[b] * p.ldo + row] = y[b];
+                } else if (p.out_pairs && row - r + kW4Rows <= p.n) {
+                    // neighbouring rows of weights are neighbours in memory: two lanes trade halves so that each writes two of them in one
+                    // word, the even lane for one row of x, the odd lane for the next
+                    const int odd = lane & 1;
+                    uint16_t *const out = static_cast<uint16_t *>(p.out) + (row & ~1);
 #pragma unroll
                     for (int b = 0; b < 16; b += 2) {
-                        const uint32_t lo = to_16_bits(__uint_as_float(v[b]), p.out_type), hi = to_16_bits(__uint_as_float(v[b + 1]), p.out_type);
-                        const uint32_t got = __shfl_xor_sync(~0u, lane & 1 ? lo : hi, 1);
-                        const uint32_t word = lane & 1 ? got | (hi << 16) : lo | (got << 16);
-                        const int64_t at = lane & 1 ? to[b + 1] : to[b];
-                        const int64_t even = row & ~int64_t(1);
-                        uint16_t *o = static_cast<uint16_t *>(p.out) + at * p.ldo + even;
-                        if (at >= 0 && even + 1 < p.n) *reinterpret_cast<uint32_t *>(o) = word;
-                        else if (at >= 0 && even < p.n) *o = uint16_t(word);
+                        const uint32_t own = two_16_bits(y[b], y[b + 1], bf16_out), got = __shfl_xor_sync(~0u, own, 1);
+                        const uint32_t word = odd ? __byte_perm(got, own, 0x7632) : __byte_perm(own, got, 0x5410);
+                        if (b + odd < left) *reinterpret_cast<uint32_t *>(out + (odd ? to[b + 1] : to[b]) * p.ldo) = word;
                     }
-                } else {
+                } else if (row < p.n) {
 #pragma unroll
                     for (int b = 0; b < 16; ++b)
-                        if (to[b] >= 0 && row < p.n) static_cast<uint16_t *>(p.out)[int64_t(to[b]) * p.ldo + row] = uint16_t(to_16_bits(__uint_as_float(v[b]), p.out_type));
+                        if (b < left) static_cast<uint16_t *>(p.out)[to[b] * p.ldo + row] = uint16_t(two_16_bits(y[b], 0.f, bf16_out));
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -358,13 +429,15 @@ template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w
             return true;
         };
 
-        // ---- weights to tensor memory: every GROUPS-th of the 128-deep tiles g of all tiles of results --------------------------
+        // ---- weights to tensor memory: every GROUPS-th of the 128-deep tiles of all tiles of results ------------------------------
         int read = 0;            // tiles of results read back
+        int i = group / depth, j = group % depth;        // tile of results, and its step
+        int s = group % p.stages, s_phase = (group / p.stages) & 1;
+        int before = -1, before_phase = 0;               // the stage that this group's A buffer was used with
         bool alive = true;
         float down = 0.f;
         int down_of = -1;
-        for (int64_t g = group; alive && g < int64_t(mine) * depth; g += GROUPS) {
-            const int i = int(g / depth), j = int(g % depth);
+        while (alive && i < mine) {
             // the first A buffers of a tile are filled before the tile before it is read back
             while (alive && read < i && (j >= GROUPS - 1 || read < i - 1)) alive = read_back(read++);
             if (!alive) break;
@@ -372,8 +445,7 @@ template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w
                 down = 1.f / p.exponents[tile_at(i).nt * kW4Rows + r];      // 2^-e
                 down_of = i;
             }
-            const int s = int(g % p.stages);
-            if (!warp_wait_for(&sh.full_w[s], uint32_t(g / p.stages) & 1, &sh)) break;
+            if (!warp_wait_for(&sh.full_w[s], s_phase, &sh)) break;
             const uint8_t *stage = ring + s * p.stage_bytes;
             uint32_t w[4][4];
 #pragma unroll
@@ -395,8 +467,7 @@ template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.empty_w[s]);
             // the buffer is free when the products of the tile that used it are done
-            const int64_t before = g - GROUPS;
-            if (before >= 0 && !warp_wait_for(&sh.used[before % p.stages], uint32_t(before / p.stages) & 1, &sh)) break;
+            if (before >= 0 && !warp_wait_for(&sh.used[before], before_phase, &sh)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -432,98 +503,130 @@ template <bool BF16, bool ZEROS> __global__ void __launch_bounds__(THREADS, 1) w
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive_at(full_a);
+            if (lane == 0) {
+                if (CTAS == 2) bar_arrive_at(ready + 8 * s);
+                else bar_arrive(&sh.ready[s]);
+            }
+            before = s;
+            before_phase = s_phase;
+            for (s += GROUPS; s >= p.stages; s -= p.stages) s_phase ^= 1;
+            for (j += GROUPS; j >= depth; j -= depth) ++i;
         }
         while (alive && read < mine) alive = read_back(read++);
-    } else if (warp == COPY_WARP) {
-        // ---- weights and rows of x to shared memory ---------------------------------------------------------------------------
+    } else if (warp == WEIGHT_WARP) {
+        // ---- weights to shared memory -------------------------------------------------------------------------------------------
         if (elected()) {
-            const uint32_t scale_bytes = uint32_t(per_tile) * 256, zero_bytes = ZEROS ? uint32_t(per_tile) * 128 : 0;
-            const uint32_t ring_at = smem_addr(ring);
-            int64_t g = 0;
+            int s = ahead == p.stages ? 0 : ahead, again = ahead == p.stages ? 0 : 1;
             bool alive = true;
             for (int i = 0; i < mine && alive; ++i) {
-                const Tile t = tile_at(i);
-                const int rows = t.tokens / 2, row = int(t.t0) + side * rows;
-                for (int j = 0; j < depth; ++j, ++g) {
-                    const int s = int(g % p.stages);
-                    const uint32_t again = (uint32_t(g / p.stages) & 1) ^ 1;
+                const int64_t from = tile_at(i).nt * p.depth_tiles + kb0;
+                for (int j = i == 0 ? ahead : 0; j < depth; ++j) {
                     if (!(alive = wait_for(&sh.empty_w[s], again, &sh))) break;
-                    uint8_t *stage = ring + s * p.stage_bytes;
-                    const int64_t tile = t.nt * p.depth_tiles + kb0 + j;
-                    bar_expect(&sh.full_w[s], kW4TileBytes + scale_bytes + zero_bytes);
-                    bulk_copy(stage + w_at, p.packed + tile * kW4TileBytes, kW4TileBytes, &sh.full_w[s]);
-                    bulk_copy(stage + s_at, p.scales + tile * per_tile * kW4Rows, scale_bytes, &sh.full_w[s]);
-                    if (ZEROS) bulk_copy(stage + z_at, p.zeros + tile * per_tile * kW4Rows, zero_bytes, &sh.full_w[s]);
-                    if (!(alive = wait_for(&sh.used[s], again, &sh))) break;
-                    const uint32_t full_x = of_rank(&sh.full_x[s], first_rank), to = ring_at + s * p.stage_bytes;
-                    if (side == 0) bar_expect(&sh.full_x[s], uint32_t(t.tokens) * 256);       // of both CTAs
-                    const int k = (kb0 + j) * kW4Depth;
-                    for (int b = 0; b < rows; b += BOX) {
-                        box_copy(to + b * 128, &map, k, row + b, full_x);
-                        box_copy(to + rows * 128 + b * 128, &map, k + 64, row + b, full_x);
+                    weights(from + j, s);
+                    if (++s == p.stages) {
+                        s = 0;
+                        again ^= 1;
                     }
                 }
             }
-            if (!alive) {
-                // given up: the copies that are under way end before the CTA does
-                for (int s = 0; s < p.stages; ++s)
-                    for (uint32_t w = 0; w < 1024; ++w) {
-                        bar_try(&sh.full_w[s], 0);
-                        if (side == 0) bar_try(&sh.full_x[s], 0);
-                        __nanosleep(100);
+            if (!alive) give_copies_time();
+        }
+    } else if (warp == X_WARP) {
+        // ---- rows of x to shared memory -----------------------------------------------------------------------------------------
+        if (elected()) {
+            const uint32_t ring_at = smem_addr(ring);
+            int s = 0, again = 1;
+            bool alive = true;
+            for (int i = 0; i < mine && alive; ++i) {
+                const Tile t = tile_at(i);
+                const int rows = t.tokens / CTAS, row = t.t0 + side * rows;
+                for (int j = 0; j < depth; ++j) {
+                    if (!(alive = wait_for(&sh.used[s], again, &sh))) break;
+                    const uint32_t ready = CTAS == 2 ? of_rank(&sh.ready[s], 0) : smem_addr(&sh.ready[s]), to = ring_at + s * p.stage_bytes;
+                    if (side == 0) bar_expect(&sh.ready[s], uint32_t(t.tokens) * 256);       // of both CTAs
+                    const int k = (kb0 + j) * kW4Depth;
+                    for (int b = 0; b < rows; b += p.box) {
+                        box_copy<CTAS>(to + b * 128, &map, k, row + b, ready);
+                        box_copy<CTAS>(to + rows * 128 + b * 128, &map, k + 64, row + b, ready);
                     }
+                    if (++s == p.stages) {
+                        s = 0;
+                        again ^= 1;
+                    }
+                }
             }
+            if (!alive) give_copies_time();
         }
     } else if (side == 0 && elected()) {
         // ---- products -----------------------------------------------------------------------------------------------------------
         constexpr uint32_t format = BF16 ? 1 : 0;
-        const uint16_t both = uint16_t(3u << first_rank);
-        int64_t g = 0;
-        bool alive = true;
+        int s = 0, s_phase = 0, a = 0;
+        bool alive = true, here = false;         // here: the next stage was found ready while products were being issued
         for (int i = 0; i < mine && alive; ++i) {
             const int tokens = tile_at(i).tokens;
-            const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(tokens >> 3) << 17) | (uint32_t(256 >> 4) << 24);
+            const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(tokens >> 3) << 17) | (uint32_t(128 * CTAS >> 4) << 24);
             if (i > 0 && !(alive = wait_for(&sh.d_free, (i - 1) & 1, &sh))) break;
-            for (int j = 0; j < depth; ++j, ++g) {
-                const int s = int(g % p.stages), a = int(g % GROUPS);
-                alive = wait_for(&sh.full_x[s], uint32_t(g / p.stages) & 1, &sh) && wait_for(&sh.full_a[a], uint32_t(g / GROUPS) & 1, &sh);
-                if (!alive) break;
+            for (int j = 0; j < depth; ++j) {
+                if (!here && !(alive = wait_for(&sh.ready[s], s_phase, &sh))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t x_addr = smem_addr(ring) + s * p.stage_bytes;
-                const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + tokens * 64);
+                const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + tokens * (128 / CTAS));
                 const uint32_t from = tmem + A_COLUMN + a * A_WIDTH;
+                const int next = s + 1 == p.stages ? 0 : s + 1, next_phase = next == 0 ? s_phase ^ 1 : s_phase;
+                here = bar_try(&sh.ready[next], next_phase);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) mma(tmem, from + kk * 8, (kk < 4 ? b0 : b1) + (kk & 3) * 2, idesc, j > 0 || kk > 0);
-                commit_pair(&sh.used[s], both);
+                for (int kk = 0; kk < 8; ++kk) mma<CTAS>(tmem, from + kk * 8, (kk < 4 ? b0 : b1) + (kk & 3) * 2, idesc, j > 0 || kk > 0);
+                commit<CTAS>(&sh.used[s]);
+                s = next;
+                s_phase = next_phase;
+                a = (a + 1) % GROUPS;
             }
-            commit_pair(&sh.done, both);
+            commit<CTAS>(&sh.done);
         }
     }
     __syncwarp();
     __syncthreads();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    cluster_barrier();               // the pair is through with its shared and tensor memory; the sums of all splits are in place
-    if (splits > 1) {
-        if (mine > 0) {
-            const Tile t = tile_at(0);
-            cg::cluster_group cluster = cg::this_cluster();
-            float *sums = reinterpret_cast<float *>(ring);
-            for (int e = threadIdx.x + int(blockIdx.y) * THREADS; e < t.count * kW4Rows; e += THREADS * splits) {
-                const int i = e / kW4Rows, c = e % kW4Rows;
-                float y = 0.f;
-                for (int b = 0; b < splits; ++b) y += cluster.map_shared_rank(sums, unsigned(2 * b + side))[e];
-                if (t.row0 + c < p.n) {
-                    y *= N::BACK * p.exponents[t.nt * kW4Rows + c];
-                    if (p.x_scale) y *= p.x_scale[t.t0 + i];
-                    static_cast<uint16_t *>(p.out)[(t.t0 + i) * p.ldo + t.row0 + c] = uint16_t(to_16_bits(y, p.out_type));
+    if (CTAS == 2 || MODE == SPLIT) cluster_barrier();       // the pair is through with its shared and tensor memory; the sums of all splits are in place
+    if (MODE == SPLIT) {
+        const Tile t = mine > 0 ? tile_at(0) : Tile{};
+        // CTA y of the cluster writes every splits-th row of x, a thread four rows of weights
+        if (mine > 0 && threadIdx.x < TURN_WARPS * 32) {
+            const int c = (threadIdx.x & 31) * 4;
+            const float4 back = *reinterpret_cast<const float4 *>(p.exponents + t.nt * kW4Rows + c);
+            const bool bf16_out = p.out_type == STRASSEN_BF16;
+            const bool wide = p.out_pairs && p.ldo % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % 8 == 0 && t.row0 + c + 4 <= p.n;
+            for (int i = int(blockIdx.y) + splits * int(threadIdx.x / 32); i < t.count; i += splits * TURN_WARPS) {
+                float4 part[MAX_SPLITS];
+#pragma unroll
+                for (int b = 0; b < MAX_SPLITS; ++b)
+                    if (b < splits) part[b] = remote_float4(of_address(smem_addr(ring) + uint32_t(i * kW4Rows + c) * 4, uint32_t(b)));
+                float4 y = part[0];
+#pragma unroll
+                for (int b = 1; b < MAX_SPLITS; ++b)
+                    if (b < splits) {
+                        y.x += part[b].x;
+                        y.y += part[b].y;
+                        y.z += part[b].z;
+                        y.w += part[b].w;
+                    }
+                const float factor = p.x_scale ? N::BACK * p.x_scale[t.t0 + i] : N::BACK;
+                const uint32_t lo = two_16_bits(y.x * back.x * factor, y.y * back.y * factor, bf16_out), hi = two_16_bits(y.z * back.z * factor, y.w * back.w * factor, bf16_out);
+                uint16_t *out = static_cast<uint16_t *>(p.out) + (t.t0 + i) * p.ldo + t.row0 + c;
+                if (wide) {
+                    *reinterpret_cast<uint2 *>(out) = make_uint2(lo, hi);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (t.row0 + c + b < p.n) out[b] = uint16_t((b < 2 ? lo : hi) >> (16 * (b & 1)));
                 }
             }
         }
+        __syncwarp();
         cluster_barrier();           // no CTA leaves while another reads its sums
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == MMA_WARP) tmem_free<CTAS>(tmem);
 }
 
 // Rows of x in 16 bits, one after another, `width` (a multiple of 8) values apart, zeros past the inner size: e4m3 becomes f16, exactly.
@@ -571,23 +674,66 @@ __global__ void __launch_bounds__(256) rows_kernel(const char *x, int64_t ldx_by
 
 constexpr int kDynamicLimit = 225 * 1024;         // of 227 KB: the rest holds Shared
 
-template <bool BF16, bool ZEROS> cudaError_t launch_one(const Args &p, const CUtensorMap &map, int pairs, int splits, int bytes, cudaStream_t stream)
+// What a launch is made of beside the kernel's arguments.
+struct Shape {
+    int ctas, mode, columns, splits, bytes;
+};
+
+template <bool BF16, bool ZEROS, int CTAS, int MODE> cudaError_t launch_one(const Args &p, const CUtensorMap &map, const Shape &shape, cudaStream_t stream)
 {
-    cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZEROS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
+    static std::atomic<uint64_t> opted_in{0};        // devices that this kernel has been given its shared memory on
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (!(opted_in.load(std::memory_order_relaxed) >> dev & 1)) {
+        e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
+        if (e != cudaSuccess) return e;
+        opted_in.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(2 * pairs), unsigned(splits));
+    cfg.gridDim = dim3(unsigned(shape.columns * CTAS), unsigned(shape.splits));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = size_t(bytes);
+    cfg.dynamicSmemBytes = size_t(shape.bytes);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = unsigned(splits);
+    attr[0].val.clusterDim.x = CTAS;
+    attr[0].val.clusterDim.y = unsigned(shape.splits);
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, w4_tile_kernel<BF16, ZEROS>, p, map);
+    return cudaLaunchKernelEx(&cfg, w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, p, map);
+}
+
+template <bool BF16, bool ZEROS> cudaError_t launch_shape(const Args &p, const CUtensorMap &map, const Shape &s, cudaStream_t stream)
+{
+    if (s.ctas == 2) return launch_one<BF16, ZEROS, 2, PLAIN>(p, map, s, stream);
+    return s.mode == SPLIT ? launch_one<BF16, ZEROS, 1, SPLIT>(p, map, s, stream) : launch_one<BF16, ZEROS, 1, PLAIN>(p, map, s, stream);
+}
+
+// How many clusters of `size` of these CTAs, one to an SM, the device holds at a time: less than SMs / size, since a cluster lies within
+// one group of SMs (33 of 4 and 15 of 8 on a B200 with 148 SMs).
+int clusters_of(int size)
+{
+    static std::atomic<int> known[MAX_SPLITS + 1];
+    int n = known[size].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    const auto kernel = w4_tile_kernel<true, false, 1, SPLIT>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(64, unsigned(size));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = kDynamicLimit;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1;
+    attr[0].val.clusterDim.y = unsigned(size);
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
+    known[size].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
@@ -633,13 +779,13 @@ cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
     }
     Args p = {};
     p.packed = a.packed;
-    p.zeros = a.packed + a.lay.zero_off;
-    p.scales = reinterpret_cast<const uint16_t *>(a.packed + a.lay.scale_off);
+    p.tile_bytes = a.lay.tile_bytes;
+    p.zero_off = a.lay.zero_off();
     p.exponents = reinterpret_cast<const float *>(a.packed + a.lay.exponent_off);
     p.x_scale = a.x_scale;
     p.out = a.out;
-    p.n = a.lay.n;
-    p.m = a.m;
+    p.n = int(a.lay.n);
+    p.m = int(a.m);
     p.ldo = a.ldo;
     p.depth_tiles = a.lay.depth_tiles;
     p.row_tiles = int(a.lay.row_tiles);
@@ -649,30 +795,39 @@ cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
     p.out_pairs = reinterpret_cast<uintptr_t>(p.out) % 4 == 0 && p.ldo % 2 == 0;
     p.scale_div = 1;
     // rows of x: as few tiles as hold them, evenly filled
-    const int64_t runs = (p.m + TOKENS - 1) / TOKENS;
-    p.tokens = int(((p.m + runs - 1) / runs + 2 * BOX - 1) / (2 * BOX) * (2 * BOX));
-    p.stage_bytes = (p.tokens * 128 + W_BYTES + 1023) / 1024 * 1024;
-    const int64_t tiles = (int64_t(p.row_tiles) + 1) / 2 * ((p.m + p.tokens - 1) / p.tokens);
-    const int most = sm_count / 2;
-    int splits = 1;
-    while (splits < 4 && tiles * (splits + 1) <= most && p.depth_tiles >= 2 * (splits + 1)) ++splits;
+    Shape shape = {2, PLAIN, 0, 1, 0};
+    if (int64_t(p.row_tiles) * ((p.m + ALONE_TOKENS - 1) / ALONE_TOKENS) <= sm_count) shape.ctas = 1;
+    const int full = shape.ctas == 1 ? ALONE_TOKENS : TOKENS, runs = (p.m + full - 1) / full, even = (p.m + runs - 1) / runs;
+    const int step = shape.ctas * STEP;
+    p.tokens = (even + step - 1) / step * step;
+    const int64_t tiles = int64_t(p.row_tiles + shape.ctas - 1) / shape.ctas * runs;
+    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
+    if (shape.ctas == 1)
+        while (shape.splits < MAX_SPLITS && tiles <= clusters_of(shape.splits + 1) && p.depth_tiles >= 2 * (shape.splits + 1)) ++shape.splits;
+    if (shape.splits > 1) shape.mode = SPLIT;
+    shape.columns = int(tiles < sm_count / shape.ctas ? tiles : sm_count / shape.ctas);
+    p.box = p.tokens / shape.ctas;
+    p.x_bytes = p.tokens * 256 / shape.ctas;
+    p.stage_bytes = (p.x_bytes + p.tile_bytes + 1023) / 1024 * 1024;
     const int stages = (kDynamicLimit - 1024) / p.stage_bytes;
     p.stages = stages > MAX_STAGES ? MAX_STAGES : stages;
-    int bytes = p.stages * p.stage_bytes;
-    if (splits > 1 && bytes < p.tokens * kW4Rows * 4) bytes = p.tokens * kW4Rows * 4;
-    bytes += 1024;
+    constexpr int most_w = kW4NibbleBytes + 4 * kW4Rows * 3;
+    static_assert((kDynamicLimit - 1024) / ((TOKENS * 128 + most_w + 1023) / 1024 * 1024) >= GROUPS && (kDynamicLimit - 1024) / ((ALONE_TOKENS * 256 + most_w + 1023) / 1024 * 1024) >= GROUPS,
+                  "a group's wait for its A buffer tells two phases of a stage apart, not three");
+    shape.bytes = p.stages * p.stage_bytes;
+    if (shape.mode == SPLIT && shape.bytes < p.tokens * kW4Rows * 4) shape.bytes = p.tokens * kW4Rows * 4;
+    shape.bytes += 1024;
 
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorSymbolNotFound;
     CUtensorMap map;
     const cuuint64_t dims[2] = {cuuint64_t(a.lay.k), cuuint64_t(a.m)}, strides[1] = {cuuint64_t(ldx) * 2};
-    const cuuint32_t box[2] = {64, BOX}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {64, cuuint32_t(p.box)}, steps[2] = {1, 1};
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    const int pairs = int(splits > 1 || tiles < most ? tiles : most);
-    if (bf16) return a.lay.has_zeros ? launch_one<true, true>(p, map, pairs, splits, bytes, stream) : launch_one<true, false>(p, map, pairs, splits, bytes, stream);
-    return a.lay.has_zeros ? launch_one<false, true>(p, map, pairs, splits, bytes, stream) : launch_one<false, false>(p, map, pairs, splits, bytes, stream);
+    if (bf16) return a.lay.has_zeros ? launch_shape<true, true>(p, map, shape, stream) : launch_shape<true, false>(p, map, shape, stream);
+    return a.lay.has_zeros ? launch_shape<false, true>(p, map, shape, stream) : launch_shape<false, false>(p, map, shape, stream);
 }
 
 cudaError_t read_gave_up(int *flag)

@@ -8,9 +8,8 @@ def test_layout_sizes():
     for n, k, group, zeros in ((1, 1, 128, False), (128, 128, 128, True), (129, 257, 32, True), (4096, 12345, 64, False)):
         h = binding.strassen_w4_create(n, k, group, binding.STRASSEN_BF16, zeros)
         tiles = -(-n // 128) * -(-k // 128)
-        places = tiles * (128 // group) * 128
-        pad = lambda v: -(-v // 256) * 256  # noqa: E731
-        assert binding.strassen_w4_bytes(h) == tiles * 8192 + pad(2 * places) + (pad(places) if zeros else 0) + -(-n // 128) * 512
+        tile = 8192 + 128 // group * 128 * (3 if zeros else 2)          # nibbles, 16-bit scales, zero points
+        assert binding.strassen_w4_bytes(h) == -(-tiles * tile // 256) * 256 + -(-n // 128) * 512
         binding.strassen_w4_destroy(h)
 
 
