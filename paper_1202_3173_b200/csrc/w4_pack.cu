@@ -1,9 +1,9 @@
 // Laying out 4-bit weights, once for a matrix: from rows of packed nibbles to the tiles that the products read (llm.h).
 //
 // Positions past the inner size hold the row's zero point (their value is 0), rows past the matrix the nibble 8 with a scale of 0.
-// The exponent section holds, for each row, the power of two 2^e with 1 <= max_g |S_g| 2^-e < 2: the tiled product holds
-// its weights in 16 bits as S 2^-e (Q - Z), so that small scales do not fall into the subnormal range of f16, and multiplies its
-// 32-bit sums by 2^e, both exactly.
+// Scales are held as S 2^-e with e such that 1 <= max_g |S_g| 2^-e < 2 in each row, and 2^e (32 bits) apart, in the exponent section: 16-bit weights
+// S 2^-e (Q - Z) then keep clear of the subnormal range of f16, and the products multiply their 32-bit sums by 2^e.  Both steps are exact,
+// except that f16 scales below 2^-14 of their row's largest lose bits, never more than 2^-25 of that.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
     dst[c * kW4Rows + r] = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// One warp per row: its scales and zero points to their places, and its exponent.
+// One warp per row: its exponent, and its scales and zero points to their places.
 __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
 {
     const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
@@ -56,23 +56,26 @@ __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
     const int place = W4Layout::row_place(int(row % kW4Rows));
     const int64_t groups = (p.lay.k + p.lay.group - 1) / p.lay.group;
     const int per_tile = kW4Depth / p.lay.group;
+    const bool real = row < p.lay.n;
+    const uint16_t *scales = static_cast<const uint16_t *>(p.scales) + (real ? row : 0) * p.lds;
     float mx = 0.f;
-    for (int64_t g = lane; g < p.lay.depth_tiles * per_tile; g += 32) {
-        const bool on = row < p.lay.n && g < groups;
-        uint8_t *tile = p.packed + (nt * p.lay.depth_tiles + g / per_tile) * p.lay.tile_bytes;
-        const int at = int(g % per_tile) * kW4Rows + place;
-        const uint16_t s = on ? static_cast<const uint16_t *>(p.scales)[row * p.lds + g] : uint16_t(0);
-        reinterpret_cast<uint16_t *>(tile + kW4NibbleBytes)[at] = s;
-        if (p.lay.has_zeros) tile[p.lay.zero_off() + at] = on ? uint8_t(p.zeros[row * p.ldz + g] & 15) : uint8_t(8);
-        const float v = fabsf(scale_value(s, p.lay.scale_type));
+    for (int64_t g = lane; g < groups && real; g += 32) {
+        const float v = fabsf(scale_value(scales[g], p.lay.scale_type));
         if (isfinite(v)) mx = fmaxf(mx, v);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
-    if (lane == 0) {
-        int e = mx > 0.f ? ilogbf(mx) : 0;
-        e = e < -126 ? -126 : e;
-        reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[row] = ldexpf(1.f, e);
+    int e = mx > 0.f ? ilogbf(mx) : 0;
+    e = e < -126 ? -126 : e;
+    if (lane == 0) reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[row] = ldexpf(1.f, e);
+    for (int64_t g = lane; g < p.lay.depth_tiles * per_tile; g += 32) {
+        const bool on = real && g < groups;
+        uint8_t *tile = p.packed + (nt * p.lay.depth_tiles + g / per_tile) * p.lay.tile_bytes;
+        const int at = int(g % per_tile) * kW4Rows + place;
+        const float v = on ? ldexpf(scale_value(scales[g], p.lay.scale_type), -e) : 0.f;
+        reinterpret_cast<uint16_t *>(tile + kW4NibbleBytes)[at] =
+            p.lay.scale_type == STRASSEN_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+        if (p.lay.has_zeros) tile[p.lay.zero_off() + at] = on ? uint8_t(p.zeros[row * p.ldz + g] & 15) : uint8_t(8);
     }
 }
 

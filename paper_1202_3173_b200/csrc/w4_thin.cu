@@ -9,7 +9,7 @@
 // Nibbles in bits 4..7 are 16 q in the same unit and take a sixteenth of the factor, so two pairs need no shift: 9 instructions for 8 weights.
 //
 // Products are summed over one group in the 32-bit accumulators of the tensor instructions and only then multiplied by the group's
-// scale, in 32 bits: no weight is ever rounded.
+// scale, in 32 bits: no weight is ever rounded.  (Scales are held as S 2^-e; the row's power of two joins at the end: w4_pack.cu.)
 //
 // The warps of a CTA hold the same rows of weights and take the 128-deep tiles of the inner dimension in turn; their sums meet in
 // shared memory and are added in a fixed order.  Where the rows are too few to fill the GPU, the CTAs of a cluster split the inner
@@ -126,6 +126,7 @@ __device__ __forceinline__ float scale_value(uint32_t bits, bool bf16)
 
 struct Ptrs {
     const uint8_t *packed;
+    const float *exponents;
     const void *x;
     const float *x_scale;
     void *out;
@@ -249,7 +250,7 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
         }
         const int64_t n = row0 + e % ROWS, t = t0 + e / ROWS;
         if (n < p.n && t < p.m) {
-            s *= N::BACK;
+            s *= N::BACK * p.exponents[n];
             if (p.x_scale) s *= p.x_scale[t];
             if (p.out_bf16) static_cast<__nv_bfloat16 *>(p.out)[t * p.ldo + n] = __float2bfloat16_rn(s);
             else static_cast<__half *>(p.out)[t * p.ldo + n] = __float2half_rn(s);
@@ -305,6 +306,7 @@ cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream)
     for (int64_t m0 = 0; m0 < a.m; m0 += most) {
         Ptrs p;
         p.packed = a.packed;
+        p.exponents = reinterpret_cast<const float *>(a.packed + a.lay.exponent_off);
         p.tile_bytes = a.lay.tile_bytes;
         p.zero_off = a.lay.zero_off();
         p.x = static_cast<const char *>(a.x) + m0 * a.ldx * size;

@@ -10,7 +10,7 @@
 //     and the last row);
 //   * warps 0-15 turn weights into 16-bit floats in registers, a thread one row of a 128 x 128 tile, and store them to tensor memory as
 //     the A operand: they never go back to shared memory, whose bandwidth the B operand needs.  Four groups of four warps take the tiles
-//     in turn, each with an A buffer of its own;
+//     in turn; four to seven A buffers, as many as D leaves room for;
 //   * one thread of warp 17 (of the pair's first CTA) issues the products, eight for each 128 of the inner dimension;
 //   * warps 0-15 read D back, multiply by the row's power of two and x's scale in 32 bits, and write.
 // The CTAs stay and take tile after tile; the first A buffers of a tile are filled before the tile before it is read back.
@@ -41,13 +41,16 @@ namespace strassen {
 namespace {
 
 constexpr int TOKENS = 256;                 // most rows of x in a tile of a pair
-constexpr int ALONE_TOKENS = 176;           // ... of a single CTA: the ring has to keep as many stages as there are A buffers
+constexpr int ALONE_TOKENS = 176;           // ... of a single CTA, which brings them all in: three steps fit in shared memory
 constexpr int STEP = 16;                    // rows of x that a CTA brings in: a multiple of this
-constexpr int GROUPS = 4;                   // groups of four warps that turn weights, and A buffers
+constexpr int GROUPS = 4;                   // groups of four warps that turn weights; at least as many A buffers
 constexpr int TURN_WARPS = 4 * GROUPS, WEIGHT_WARP = TURN_WARPS, MMA_WARP = TURN_WARPS + 1, X_WARP = TURN_WARPS + 2, THREADS = 32 * (TURN_WARPS + 3);
-constexpr int MAX_STAGES = 8, MAX_SPLITS = 8;
-constexpr int A_COLUMN = 256;               // first tensor-memory column of the A buffers; D is below
-constexpr int A_WIDTH = 64;                 // columns of 128 rows x 128 values of 16 bits
+// 128-deep steps g = 0, 1, .. over all tiles of a CTA: their weights and their barriers are in rings of RING, at g % RING.  A group sees every
+// RING / GROUPS-th of them, always at the same places, so it never takes a phase of a barrier for the one two later.  The rows of x, which are
+// larger, have a ring of x_stages, and the A buffers one of a_buffers.
+constexpr int RING = 8, MAX_SPLITS = 8;
+static_assert(RING % GROUPS == 0, "");
+constexpr int A_WIDTH = 64;                 // tensor-memory columns of an A buffer: 128 rows x 128 values of 16 bits; the last of 512, D comes first
 constexpr int64_t kWaitLimit = int64_t(1) << 31;      // clocks of a wait, about a second
 
 // Set by a CTA that gave up on a wait; read and cleared by strassen_device_status.
@@ -61,11 +64,12 @@ struct Args {
     int64_t ldo, depth_tiles;
     int n, m;
     int row_tiles;           // of one matrix
-    int group_words;
+    int group_shift;         // a group is 1 << group_shift words of a row's 16 bytes
     int tile_bytes, zero_off;
     int tokens;              // rows of x in a tile, a multiple of CTAS * STEP
     int box;                 // rows of x in one copy
-    int stages, stage_bytes, x_bytes;
+    int x_stages, x_bytes;   // up to RING
+    int a_buffers;           // GROUPS .. RING
     int out_type;
     bool scale_bf16, out_pairs;
     const W4Tile *table;     // experts: the tiles of rows and their number; NULL: every `tokens` rows a tile
@@ -74,11 +78,11 @@ struct Args {
     int scale_div;           // experts: x_scale of pair i is x_scale[i / scale_div]
 };
 
-// full_w / empty_w: weights of a ring stage have arrived / have been read; ready: the pair's rows of x of the stage are in place, and its
-// weights are in their A buffers; used: the products that read those are done; done: all products of a tile of results are; d_free: the
+// Barriers of step g: full_w / empty_w: its weights have arrived / have been read; ready: the pair's rows of x are in place, and its
+// weights are in their A buffers; used: the products that read those are done.  done: all products of a tile of results are; d_free: the
 // pair has read them back.  ready and d_free count in the pair's first CTA.
 struct Shared {
-    uint64_t full_w[MAX_STAGES], empty_w[MAX_STAGES], ready[MAX_STAGES], used[MAX_STAGES], done, d_free;
+    uint64_t full_w[RING], empty_w[RING], ready[RING], used[RING], done, d_free;
     uint32_t tmem;
     int dead;
 };
@@ -119,6 +123,13 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 {
     uint32_t ok;
     asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Whether it is over, without waiting.
+__device__ __forceinline__ bool bar_test(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
 }
 // Waits until phase `parity` of the barrier is over.  False: the limit was reached, here or elsewhere in the CTA, and the caller leaves
@@ -220,13 +231,16 @@ __device__ __forceinline__ void ld_tmem16(uint32_t (&v)[16], uint32_t at)
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// What a 16-bit weight is made of: w = FMA(nibble pair, big or small, add) without zero points, FMA(FMA(pair, BIG or SMALL, -z), scale, 0) with them.
+// What a 16-bit weight is made of, from the pairs of a masked nibble and the scale S 2^-e, at most 2:
+//   without zero points  FMA(pair, scale FACTOR, scale -8 UNIT): one step of q becomes scale UNIT
+//   with zero points     MUL(FMA(pair, BIG or SMALL, -z STEP), scale RATIO): steps of STEP first, exactly, and of scale UNIT then
+// Nibbles in bits 4..7 take a sixteenth of the factor.
 template <bool BF16> struct Num;
 template <> struct Num<true> {
-    // a masked nibble is q 2^-133; the scale arrives as S 2^-e < 2; one step of q becomes S 2^-e UNIT
-    static constexpr float FACTOR = 8.507059173023462e37f /* 2^126 */, UNIT = 1.f / 128, BACK = 128.f;
-    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00;       // 2^127, 2^123: steps of 2^-6
-    static constexpr float STEP = 1.f / 64;
+    // a masked nibble is q 2^-133; UNIT 2^-7, STEP 2^-6
+    static constexpr float BACK = 128.f, STEP = 1.f / 64;
+    static constexpr uint32_t BIG_FACTOR = 0x7e807e80, SMALL_FACTOR = 0x7c807c80, MINUS_EIGHT = 0xbd80bd80;       // 2^126, 2^122, -2^-4
+    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00, RATIO = 0x3f003f00;                           // 2^127, 2^123, 2^-1
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rn(v));
@@ -246,10 +260,10 @@ template <> struct Num<true> {
     }
 };
 template <> struct Num<false> {
-    // a masked nibble is q 2^-24
-    static constexpr float FACTOR = 16384.f, UNIT = 1.f / 1024, BACK = 1024.f;
-    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800;       // 2^15, 2^11: steps of 2^-9
-    static constexpr float STEP = 1.f / 512;
+    // a masked nibble is q 2^-24; UNIT 2^-10, STEP 2^-9
+    static constexpr float BACK = 1024.f, STEP = 1.f / 512;
+    static constexpr uint32_t BIG_FACTOR = 0x74007400, SMALL_FACTOR = 0x64006400, MINUS_EIGHT = 0xa000a000;       // 2^14, 2^10, -2^-7
+    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800, RATIO = 0x38003800;                           // 2^15, 2^11, 2^-1
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __half_as_ushort(__float2half_rn(v));
@@ -293,6 +307,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t *const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);      // the swizzle's groups start at multiples of 1024; the same place in every CTA
+    uint8_t *const weight_ring = ring + p.x_stages * p.x_bytes;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;     // the shuffle: known to be one value per warp
     const int side = CTAS == 2 ? blockIdx.x & 1 : 0, splits = MODE == SPLIT ? int(gridDim.y) : 1;
     const int kb0 = MODE == SPLIT ? int(p.depth_tiles * blockIdx.y / splits) : 0;
@@ -330,11 +345,11 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     // the weights of the first tile's first steps are on their way before anything else is
     const auto weights = [&](int64_t tile, int s) {
         bar_expect(&sh.full_w[s], uint32_t(p.tile_bytes));
-        bulk_copy(ring + s * p.stage_bytes + p.x_bytes, p.packed + tile * p.tile_bytes, uint32_t(p.tile_bytes), &sh.full_w[s]);
+        bulk_copy(weight_ring + s * p.tile_bytes, p.packed + tile * p.tile_bytes, uint32_t(p.tile_bytes), &sh.full_w[s]);
     };
-    const int ahead = mine == 0 ? 0 : depth < p.stages ? depth : p.stages;
+    const int ahead = mine == 0 ? 0 : depth < RING ? depth : RING;
     if (warp == WEIGHT_WARP && elected()) {
-        for (int i = 0; i < p.stages; ++i) {
+        for (int i = 0; i < RING; ++i) {
             bar_init(&sh.full_w[i], 1);
             bar_init(&sh.empty_w[i], 4);
         }
@@ -346,7 +361,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     }
     if (warp == X_WARP && elected()) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
-        for (int i = 0; i < p.stages; ++i) {
+        for (int i = 0; i < RING; ++i) {
             bar_init(&sh.ready[i], 4 * CTAS + 1);
             bar_init(&sh.used[i], 1);
         }
@@ -362,8 +377,6 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     if (CTAS == 2) cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh.tmem;
-
-    const int w_at = p.x_bytes, s_at = w_at + kW4NibbleBytes, z_at = w_at + p.zero_off;      // sections of a stage; this CTA's rows of x come first
 
     if (warp < TURN_WARPS) {
         const int group = warp >> 2, r = (warp & 3) * 32 + lane;
@@ -432,74 +445,79 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
         // ---- weights to tensor memory: every GROUPS-th of the 128-deep tiles of all tiles of results ------------------------------
         int read = 0;            // tiles of results read back
         int i = group / depth, j = group % depth;        // tile of results, and its step
-        int s = group % p.stages, s_phase = (group / p.stages) & 1;
-        int before = -1, before_phase = 0;               // the stage that this group's A buffer was used with
+        int a = group;                                   // A buffer (a_buffers >= GROUPS)
+        int g = group;
         bool alive = true;
-        float down = 0.f;
-        int down_of = -1;
         while (alive && i < mine) {
             // the first A buffers of a tile are filled before the tile before it is read back
             while (alive && read < i && (j >= GROUPS - 1 || read < i - 1)) alive = read_back(read++);
             if (!alive) break;
-            if (down_of != i) {
-                down = 1.f / p.exponents[tile_at(i).nt * kW4Rows + r];      // 2^-e
-                down_of = i;
-            }
-            if (!warp_wait_for(&sh.full_w[s], s_phase, &sh)) break;
-            const uint8_t *stage = ring + s * p.stage_bytes;
+            const int s = g % RING;
+            if (!warp_wait_for(&sh.full_w[s], (g / RING) & 1, &sh)) break;
+            const uint8_t *stage = weight_ring + s * p.tile_bytes;
             uint32_t w[4][4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(stage + w_at + c * 2048 + r * 16);
+                const uint4 u = *reinterpret_cast<const uint4 *>(stage + c * 2048 + r * 16);
                 w[c][0] = u.x;
                 w[c][1] = u.y;
                 w[c][2] = u.z;
                 w[c][3] = u.w;
             }
-            uint16_t sc[4];
-            uint8_t z[4];
+            uint32_t sc[4], z[4];                    // of each word's group
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const int at = (b / p.group_words) * kW4Rows + place;
-                sc[b] = *reinterpret_cast<const uint16_t *>(stage + s_at + at * 2);
-                if (ZEROS) z[b] = stage[z_at + at];
+                if (b & ((1 << p.group_shift) - 1)) {
+                    sc[b] = sc[b - 1];
+                    z[b] = z[b - 1];
+                } else {
+                    const int at = (b >> p.group_shift) * kW4Rows + place;
+                    sc[b] = *reinterpret_cast<const uint16_t *>(stage + kW4NibbleBytes + at * 2);
+                    z[b] = ZEROS ? stage[p.zero_off + at] : 0;
+                }
             }
             __syncwarp();
             if (lane == 0) bar_arrive(&sh.empty_w[s]);
-            // the buffer is free when the products of the tile that used it are done
-            if (before >= 0 && !warp_wait_for(&sh.used[before], before_phase, &sh)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t v[2][32];                       // column 16 w + 4 c + pair
+            uint32_t big = 0, small = 0, minus = 0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t v[32];                      // column 16 w + 4 c + pair
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                    const int b = 2 * h + jj;
-                    const float sn = scale_value(sc[b], p.scale_bf16) * down;
+            for (int b = 0; b < 4; ++b) {
+                if (!(b & ((1 << p.group_shift) - 1))) {
+                    if (p.scale_bf16 == BF16) big = sc[b] | sc[b] << 16;
+                    else big = N::both(scale_value(sc[b], p.scale_bf16));
                     if (ZEROS) {
-                        const uint32_t minus = N::both(-N::STEP * float(z[b])), scale = N::both(sn * (N::UNIT / N::STEP));
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const uint32_t u = w[c][b], uu = u >> 8;
-                            v[16 * jj + 4 * c + 0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), scale);
-                            v[16 * jj + 4 * c + 1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), scale);
-                            v[16 * jj + 4 * c + 2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), scale);
-                            v[16 * jj + 4 * c + 3] = N::mul(N::fma(uu & 0x00f000f0, N::SMALL, minus), scale);
-                        }
+                        minus = N::both(-N::STEP * float(z[b]));
+                        big = N::mul(big, N::RATIO);
                     } else {
-                        const uint32_t big = N::both(sn * N::FACTOR), small = N::both(sn * (N::FACTOR / 16)), minus = N::both(sn * (-8 * N::UNIT));
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const uint32_t u = w[c][b], uu = u >> 8;
-                            v[16 * jj + 4 * c + 0] = N::fma(u & 0x000f000f, big, minus);
-                            v[16 * jj + 4 * c + 1] = N::fma(u & 0x00f000f0, small, minus);
-                            v[16 * jj + 4 * c + 2] = N::fma(uu & 0x000f000f, big, minus);
-                            v[16 * jj + 4 * c + 3] = N::fma(uu & 0x00f000f0, small, minus);
-                        }
+                        small = N::mul(big, N::SMALL_FACTOR);
+                        minus = N::mul(big, N::MINUS_EIGHT);
+                        big = N::mul(big, N::BIG_FACTOR);
                     }
                 }
-                st_tmem32(lanes + A_COLUMN + group * A_WIDTH + 32 * h, v);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t *const to = v[b >> 1] + 16 * (b & 1) + 4 * c;
+                    const uint32_t u = w[c][b], uu = u >> 8;
+                    if (ZEROS) {
+                        to[0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), big);
+                        to[1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), big);
+                        to[2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), big);
+                        to[3] = N::mul(N::fma(uu & 0x00f000f0, N::SMALL, minus), big);
+                    } else {
+                        to[0] = N::fma(u & 0x000f000f, big, minus);
+                        to[1] = N::fma(u & 0x00f000f0, small, minus);
+                        to[2] = N::fma(uu & 0x000f000f, big, minus);
+                        to[3] = N::fma(uu & 0x00f000f0, small, minus);
+                    }
+                }
             }
+            // the buffer is free when the products of the step that used it are done
+            const int before = g - p.a_buffers;
+            if (before >= 0 && !warp_wait_for(&sh.used[before % RING], (before / RING) & 1, &sh)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t to = lanes + 512 - (p.a_buffers - a) * A_WIDTH;
+            st_tmem32(to, v[0]);
+            st_tmem32(to + 32, v[1]);
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -507,26 +525,22 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                 if (CTAS == 2) bar_arrive_at(ready + 8 * s);
                 else bar_arrive(&sh.ready[s]);
             }
-            before = s;
-            before_phase = s_phase;
-            for (s += GROUPS; s >= p.stages; s -= p.stages) s_phase ^= 1;
+            g += GROUPS;
+            a += GROUPS;
+            if (a >= p.a_buffers) a -= p.a_buffers;
             for (j += GROUPS; j >= depth; j -= depth) ++i;
         }
         while (alive && read < mine) alive = read_back(read++);
     } else if (warp == WEIGHT_WARP) {
         // ---- weights to shared memory -------------------------------------------------------------------------------------------
         if (elected()) {
-            int s = ahead == p.stages ? 0 : ahead, again = ahead == p.stages ? 0 : 1;
+            int g = ahead;
             bool alive = true;
             for (int i = 0; i < mine && alive; ++i) {
                 const int64_t from = tile_at(i).nt * p.depth_tiles + kb0;
-                for (int j = i == 0 ? ahead : 0; j < depth; ++j) {
-                    if (!(alive = wait_for(&sh.empty_w[s], again, &sh))) break;
-                    weights(from + j, s);
-                    if (++s == p.stages) {
-                        s = 0;
-                        again ^= 1;
-                    }
+                for (int j = i == 0 ? ahead : 0; j < depth; ++j, ++g) {
+                    if (g >= RING && !(alive = wait_for(&sh.empty_w[g % RING], (g / RING - 1) & 1, &sh))) break;
+                    weights(from + j, g % RING);
                 }
             }
             if (!alive) give_copies_time();
@@ -535,24 +549,22 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
         // ---- rows of x to shared memory -----------------------------------------------------------------------------------------
         if (elected()) {
             const uint32_t ring_at = smem_addr(ring);
-            int s = 0, again = 1;
+            int g = 0, at = 0;                       // step, and its place in the ring of rows of x
             bool alive = true;
             for (int i = 0; i < mine && alive; ++i) {
                 const Tile t = tile_at(i);
                 const int rows = t.tokens / CTAS, row = t.t0 + side * rows;
-                for (int j = 0; j < depth; ++j) {
-                    if (!(alive = wait_for(&sh.used[s], again, &sh))) break;
-                    const uint32_t ready = CTAS == 2 ? of_rank(&sh.ready[s], 0) : smem_addr(&sh.ready[s]), to = ring_at + s * p.stage_bytes;
+                for (int j = 0; j < depth; ++j, ++g) {
+                    const int before = g - p.x_stages, s = g % RING;
+                    if (before >= 0 && !(alive = wait_for(&sh.used[before % RING], (before / RING) & 1, &sh))) break;
+                    const uint32_t ready = CTAS == 2 ? of_rank(&sh.ready[s], 0) : smem_addr(&sh.ready[s]), to = ring_at + at * p.x_bytes;
                     if (side == 0) bar_expect(&sh.ready[s], uint32_t(t.tokens) * 256);       // of both CTAs
                     const int k = (kb0 + j) * kW4Depth;
                     for (int b = 0; b < rows; b += p.box) {
                         box_copy<CTAS>(to + b * 128, &map, k, row + b, ready);
                         box_copy<CTAS>(to + rows * 128 + b * 128, &map, k + 64, row + b, ready);
                     }
-                    if (++s == p.stages) {
-                        s = 0;
-                        again ^= 1;
-                    }
+                    at = at + 1 == p.x_stages ? 0 : at + 1;
                 }
             }
             if (!alive) give_copies_time();
@@ -560,26 +572,24 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     } else if (side == 0 && elected()) {
         // ---- products -----------------------------------------------------------------------------------------------------------
         constexpr uint32_t format = BF16 ? 1 : 0;
-        int s = 0, s_phase = 0, a = 0;
-        bool alive = true, here = false;         // here: the next stage was found ready while products were being issued
+        int g = 0, at = 0, a = 0;
+        bool alive = true, here = false;         // here: the next step was found ready while products were being issued
         for (int i = 0; i < mine && alive; ++i) {
             const int tokens = tile_at(i).tokens;
             const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(tokens >> 3) << 17) | (uint32_t(128 * CTAS >> 4) << 24);
             if (i > 0 && !(alive = wait_for(&sh.d_free, (i - 1) & 1, &sh))) break;
-            for (int j = 0; j < depth; ++j) {
-                if (!here && !(alive = wait_for(&sh.ready[s], s_phase, &sh))) break;
+            for (int j = 0; j < depth; ++j, ++g) {
+                if (!here && !(alive = wait_for(&sh.ready[g % RING], (g / RING) & 1, &sh))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t x_addr = smem_addr(ring) + s * p.stage_bytes;
+                const uint32_t x_addr = smem_addr(ring) + at * p.x_bytes;
                 const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + tokens * (128 / CTAS));
-                const uint32_t from = tmem + A_COLUMN + a * A_WIDTH;
-                const int next = s + 1 == p.stages ? 0 : s + 1, next_phase = next == 0 ? s_phase ^ 1 : s_phase;
-                here = bar_try(&sh.ready[next], next_phase);
+                const uint32_t from = tmem + 512 - (p.a_buffers - a) * A_WIDTH;
+                here = bar_test(&sh.ready[(g + 1) % RING], ((g + 1) / RING) & 1);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) mma<CTAS>(tmem, from + kk * 8, (kk < 4 ? b0 : b1) + (kk & 3) * 2, idesc, j > 0 || kk > 0);
-                commit<CTAS>(&sh.used[s]);
-                s = next;
-                s_phase = next_phase;
-                a = (a + 1) % GROUPS;
+                commit<CTAS>(&sh.used[g % RING]);
+                at = at + 1 == p.x_stages ? 0 : at + 1;
+                a = a + 1 == p.a_buffers ? 0 : a + 1;
             }
             commit<CTAS>(&sh.done);
         }
@@ -789,7 +799,7 @@ cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
     p.ldo = a.ldo;
     p.depth_tiles = a.lay.depth_tiles;
     p.row_tiles = int(a.lay.row_tiles);
-    p.group_words = a.lay.group / 32;
+    p.group_shift = a.lay.group == 32 ? 0 : a.lay.group == 64 ? 1 : 2;
     p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
     p.out_type = a.out_type;
     p.out_pairs = reinterpret_cast<uintptr_t>(p.out) % 4 == 0 && p.ldo % 2 == 0;
@@ -808,13 +818,15 @@ cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
     shape.columns = int(tiles < sm_count / shape.ctas ? tiles : sm_count / shape.ctas);
     p.box = p.tokens / shape.ctas;
     p.x_bytes = p.tokens * 256 / shape.ctas;
-    p.stage_bytes = (p.x_bytes + p.tile_bytes + 1023) / 1024 * 1024;
-    const int stages = (kDynamicLimit - 1024) / p.stage_bytes;
-    p.stages = stages > MAX_STAGES ? MAX_STAGES : stages;
-    constexpr int most_w = kW4NibbleBytes + 4 * kW4Rows * 3;
-    static_assert((kDynamicLimit - 1024) / ((TOKENS * 128 + most_w + 1023) / 1024 * 1024) >= GROUPS && (kDynamicLimit - 1024) / ((ALONE_TOKENS * 256 + most_w + 1023) / 1024 * 1024) >= GROUPS,
-                  "a group's wait for its A buffer tells two phases of a stage apart, not three");
-    shape.bytes = p.stages * p.stage_bytes;
+    const int stages = (kDynamicLimit - 1024 - RING * p.tile_bytes) / p.x_bytes;
+    p.x_stages = stages > RING ? RING : stages;
+    p.a_buffers = (512 - p.tokens) / A_WIDTH;
+    if (p.a_buffers > RING) p.a_buffers = RING;
+    static_assert((512 - TOKENS) / A_WIDTH >= GROUPS, "at least an A buffer for each group");
+    static_assert((kDynamicLimit - 1024 - RING * (kW4NibbleBytes + 4 * kW4Rows * 3)) / (ALONE_TOKENS * 256) >= 3 &&
+                      (kDynamicLimit - 1024 - RING * (kW4NibbleBytes + 4 * kW4Rows * 3)) / (TOKENS * 128) >= 3,
+                  "rows of x three steps deep at least");
+    shape.bytes = p.x_stages * p.x_bytes + RING * p.tile_bytes;
     if (shape.mode == SPLIT && shape.bytes < p.tokens * kW4Rows * 4) shape.bytes = p.tokens * kW4Rows * 4;
     shape.bytes += 1024;
 

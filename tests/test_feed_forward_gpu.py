@@ -437,3 +437,18 @@ def test_device_status_is_clean():
     q, s, z = weights(256, 1024, 128, False, BF16, 2)
     sw().W4Matrix(q, s)(rows(64, 1024, BF16, 1)[0])
     binding.strassen_device_status()
+
+
+@pytest.mark.parametrize("m,n,k", [(20, 4096, 8192), (60, 4096, 8192), (112, 4096, 16384), (130, 512, 20000), (200, 4096, 16384), (900, 4096, 3000), (300, 2100, 256)])
+def test_w4_many_launches(m, n, k):
+    """Every number of rows has rings of its own depths: the same result from each of many launches, and no wait that ran out."""
+    q, s, z = weights(n, k, 64, True, BF16, 3)
+    matrix = sw().W4Matrix(q, s, z, group=64)
+    x, _ = rows(m, k, BF16, 4)
+    want, out = matrix(x), torch.empty(m, n, device="cuda", dtype=BF16)
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(300):
+        matrix(x, out=out)
+        bad += (out != want).sum()
+    assert int(bad) == 0
+    binding.strassen_device_status()
