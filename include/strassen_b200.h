@@ -481,7 +481,44 @@ int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x,
 size_t strassen_w4_workspace_bytes(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx);
 
 /*
- * strassen_device_status -- wait for the current device and say whether a kernel of strassen_w4_matmul has given up since
+ * strassen_route_experts -- which experts a token goes to, and with what weight.
+ *   score   STRASSEN_SOFTMAX: softmax of the token's logits; STRASSEN_SIGMOID: 1 / (1 + exp(-logit))
+ *   bias    `experts` floats added to the scores for the choice alone (balance), or NULL
+ *   groups  1 .. 32, neighbouring experts / groups each (1: no groups): only the experts of the top_groups groups of the highest
+ *           rating can be chosen; a group's rating is its largest score + bias (softmax), or the sum of its two largest (sigmoid)
+ *   top     1 .. 32: ids (tokens x top) receives the experts of the largest score + bias, in order, the lowest index first among equals;
+ *           weights (tokens x top) their scores, divided by their sum if `renormalize`, times `factor`
+ * experts 1 .. 1024; type of the logits (leading dimension ld): STRASSEN_BF16, STRASSEN_F16 or STRASSEN_F32; scores in 32 bits.  A logit of -inf
+ * or NaN leaves the expert out: it takes no part in the softmax and is never chosen.  Where fewer than `top` are left the ids end in
+ * -1 with weight 0.
+ */
+#define STRASSEN_SOFTMAX 0
+#define STRASSEN_SIGMOID 1
+int strassen_route_experts(int64_t tokens, int64_t experts, int type, const void *logits, int64_t ld, const float *bias, int score, int groups,
+                           int top_groups, int top, int renormalize, float factor, int *ids, float *weights, void *stream);
+
+/*
+ * Matrices of experts: `experts` (1 .. 1024) matrices of one size, laid out together.  As strassen_w4_create and strassen_w4_pack, with
+ * q, scales and zeros holding the rows of the first matrix, then those of the second, and so on.
+ *
+ * strassen_w4_experts -- products of rows with the matrices that ids name; ids (tokens x top) and weights as strassen_route_experts gives them.
+ *   x         without `each`: a row for each token; with it: a row for each of its ids (row token * top + j)
+ *   weights   NULL: out has tokens * top rows, row token * top + j = W[ids[token][j]] x;
+ *             else: out has a row for each token, the sum over j of weights[token][j] W[ids[token][j]] x, held in 32 bits and rounded once
+ *   x_scale   floats, one for each row of x, or NULL
+ * An id outside 0 .. experts - 1 is no expert: its row is zeros, and it adds nothing to a sum.  For more than STRASSEN_W4_THIN_IDS ids the
+ * rows are put in order of their experts in the workspace (strassen_w4_experts_workspace_bytes; 0 up to there), and the weights are rounded to
+ * 16 bits as for many rows above.
+ */
+#define STRASSEN_W4_THIN_IDS 32
+strassen_w4 *strassen_w4_create_experts(int64_t experts, int64_t n, int64_t k, int group, int scale_type, int has_zeros);
+size_t strassen_w4_experts_workspace_bytes(const strassen_w4 *w, int64_t tokens, int64_t top, int weighted);
+int strassen_w4_experts(const strassen_w4 *w, int64_t tokens, int64_t top, const int *ids, int type, const void *x, int64_t ldx, int each,
+                        const float *x_scale, const float *weights, int out_type, void *out, int64_t ldo, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * strassen_device_status -- wait for the current device and say whether a kernel of strassen_w4_matmul or strassen_w4_experts has given up since
  * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
  * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else
  * STRASSEN_CUDA_ERROR, and the flag is cleared.

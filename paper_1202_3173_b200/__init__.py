@@ -10,9 +10,8 @@ from __future__ import annotations
 from . import binding
 from .binding import StrassenError  # noqa: F401
 
-__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError", "W4Matrix", "FeedForward", "rms_norm_quant", "silu_mul_quant",
-           "quant_rows"]
-_FEED_FORWARD = ("W4Matrix", "FeedForward", "rms_norm_quant", "silu_mul_quant", "quant_rows")
+_FEED_FORWARD = ("W4Matrix", "W4Experts", "FeedForward", "ExpertsFeedForward", "rms_norm_quant", "silu_mul_quant", "route_experts", "quant_rows")
+__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError", *_FEED_FORWARD]
 
 
 def __getattr__(name):

@@ -96,11 +96,17 @@ SYMBOLS = [
     ("strassen_w4_destroy", None, [_vp]),
     ("strassen_w4_matmul", _int, [_vp, _i64, _int, _vp, _i64, _vp, _int, _vp, _i64, _vp, _sz, _vp]),
     ("strassen_w4_workspace_bytes", _sz, [_vp, _i64, _int, _vp, _i64]),
+    ("strassen_route_experts", _int, [_i64, _i64, _int, _vp, _i64, _vp, _int, _int, _int, _int, _int, ctypes.c_float, _vp, _vp, _vp]),
+    ("strassen_w4_create_experts", _vp, [_i64, _i64, _i64, _int, _int, _int]),
+    ("strassen_w4_experts_workspace_bytes", _sz, [_vp, _i64, _i64, _int]),
+    ("strassen_w4_experts", _int, [_vp, _i64, _i64, _vp, _int, _vp, _i64, _int, _vp, _vp, _int, _vp, _i64, _vp, _sz, _vp]),
     ("strassen_device_status", _int, []),
     ("strassen_last_error", _cp, []),
 ]
 STRASSEN_STATIC_MAX_N = 512
 STRASSEN_W4_THIN_ROWS = 16
+STRASSEN_W4_THIN_IDS = 32
+STRASSEN_SOFTMAX, STRASSEN_SIGMOID = 0, 1
 
 _lib = None
 
@@ -345,3 +351,26 @@ def strassen_w4_workspace_bytes(matrix: int, m: int, type: int, x: int, ldx: int
 
 def strassen_device_status() -> None:
     _check(lib().strassen_device_status())
+
+
+def strassen_route_experts(tokens: int, experts: int, type: int, logits: int, ld: int, bias: int, score: int, groups: int, top_groups: int,
+                           top: int, renormalize: bool, factor: float, ids: int, weights: int, stream: int = 0) -> None:
+    _check(lib().strassen_route_experts(tokens, experts, type, logits, ld, bias, score, groups, top_groups, top, int(renormalize), factor, ids,
+                                        weights, stream))
+
+
+def strassen_w4_create_experts(experts: int, n: int, k: int, group: int, scale_type: int, has_zeros: bool) -> int:
+    h = lib().strassen_w4_create_experts(experts, n, k, group, scale_type, int(has_zeros))
+    if not h:
+        raise StrassenError(-1, strassen_last_error())
+    return h
+
+
+def strassen_w4_experts_workspace_bytes(matrices: int, tokens: int, top: int, weighted: bool) -> int:
+    return lib().strassen_w4_experts_workspace_bytes(matrices, tokens, top, int(weighted))
+
+
+def strassen_w4_experts(matrices: int, tokens: int, top: int, ids: int, type: int, x: int, ldx: int, each: bool, x_scale: int, weights: int,
+                        out_type: int, out: int, ldo: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().strassen_w4_experts(matrices, tokens, top, ids, type, x, ldx, int(each), x_scale, weights, out_type, out, ldo, workspace,
+                                     workspace_bytes, stream))

@@ -29,6 +29,22 @@ struct RowArgs {
 cudaError_t launch_rms_norm_quant(const RowArgs &a, cudaStream_t stream);
 cudaError_t launch_silu_mul_quant(const RowArgs &a, cudaStream_t stream);
 
+// ---- routing (route.cu) -------------------------------------------------------------------------------------------
+struct RouteArgs {
+    int64_t tokens;
+    int experts, type;
+    const void *logits;
+    int64_t ld;
+    const float *bias;
+    int softmax, groups, top_groups, top, renormalize;
+    float factor;
+    int *ids;
+    float *weights;
+    uint32_t size_magic;
+};
+constexpr int kMostExperts = 1024, kMostTop = 32, kMostGroups = 32;
+cudaError_t launch_route(RouteArgs p, cudaStream_t stream);
+
 // ---- 4-bit weights (w4_pack.cu, w4_thin.cu, w4_tiles.cu) -----------------------------------------------------------
 // Laid-out weights: tiles of 128 rows x 128 inner positions, one after another along the inner dimension, then along the
 // rows.  A tile is four chunks c = 0..3 of 128 rows x 16 bytes; the four 32-bit words of a row's 16 bytes hold
@@ -41,10 +57,11 @@ constexpr int kW4Rows = 128, kW4Depth = 128, kW4NibbleBytes = kW4Rows * kW4Depth
 
 struct W4Layout {
     int64_t n, k;
+    int64_t experts;             // matrices of this size, one after another
     int group;                   // 32, 64 or 128
     int scale_type;              // STRASSEN_BF16 / F16
     int has_zeros;
-    int64_t row_tiles, depth_tiles;
+    int64_t row_tiles, depth_tiles;      // of one matrix
     int tile_bytes;
     // byte offset of the rows' exponents (w4_pack.cu) in the packed memory, and its size
     size_t exponent_off, bytes;
@@ -66,6 +83,11 @@ struct W4Args {
     void *out;
     int64_t ldo;
     void *workspace;
+    // products of experts: m tokens, `top` rows of ids each; x has a row for each token, or with `each` for each of its ids
+    const int *ids;
+    int64_t top;
+    bool each;
+    const float *weights;        // NULL: a row of results for each id
 };
 
 struct W4PackArgs {
@@ -88,6 +110,10 @@ struct W4Tile {
 int64_t w4_tiles_workspace(const W4Args &a);        // bytes; 0: none is needed
 cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream);
 cudaError_t read_gave_up(int *flag);        // reads and clears the flag of w4_tiles.cu
+// Most ids for which every id's matrix is read by itself (w4_thin.cu); beyond that the rows are put in order of their experts.
+constexpr int64_t kThinIds = STRASSEN_W4_THIN_IDS;
+int64_t w4_experts_workspace(const W4Args &a);
+cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t stream);
 cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream);
 
 }  // namespace strassen

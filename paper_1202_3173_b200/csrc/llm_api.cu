@@ -139,11 +139,50 @@ extern "C" int strassen_silu_mul_quant(int64_t m, int64_t k, int type, const voi
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
 }
 
+extern "C" int strassen_route_experts(int64_t tokens, int64_t experts, int type, const void *logits, int64_t ld, const float *bias, int score, int groups,
+                                      int top_groups, int top, int renormalize, float factor, int *ids, float *weights, void *stream)
+{
+    set_last_error("");
+    if (tokens < 0 || tokens > kMaxExtent) return fail(STRASSEN_INVALID_ARG, "tokens must be 0 .. 2^30");
+    if (experts < 1 || experts > kMostExperts) return fail(STRASSEN_INVALID_ARG, "experts must be 1 .. 1024");
+    if (type != STRASSEN_BF16 && type != STRASSEN_F16 && type != STRASSEN_F32)
+        return fail(STRASSEN_INVALID_ARG, "the logits' type must be STRASSEN_BF16, STRASSEN_F16 or STRASSEN_F32");
+    if (score != STRASSEN_SOFTMAX && score != STRASSEN_SIGMOID) return fail(STRASSEN_INVALID_ARG, "the score must be STRASSEN_SOFTMAX or STRASSEN_SIGMOID");
+    if (groups < 1 || groups > kMostGroups || experts % groups != 0 || top_groups < 1 || top_groups > groups)
+        return fail(STRASSEN_INVALID_ARG, "groups must be 1 .. 32, divide the experts, and top_groups 1 .. groups");
+    if (top < 1 || top > kMostTop || top > experts / groups * top_groups)
+        return fail(STRASSEN_INVALID_ARG, "top must be 1 .. 32 and no more than the experts of top_groups groups");
+    if (!(factor == factor)) return fail(STRASSEN_INVALID_ARG, "factor must be a number");
+    if (tokens == 0) return STRASSEN_OK;
+    if (!logits || !ids || !weights) return fail(STRASSEN_INVALID_ARG, "logits, ids and weights must be non-NULL");
+    if (tokens > 1 && (ld < experts || ld > kMaxLd)) return fail(STRASSEN_INVALID_ARG, "leading dimensions must be at least the rows' length");
+    const int t = type_size(type);
+    if (misaligned(logits, t) || misaligned(bias, 4) || misaligned(ids, 4) || misaligned(weights, 4))
+        return fail(STRASSEN_MISALIGNED, "logits, bias, ids and weights must be aligned to their elements");
+    const Range l = rows_of(logits, tokens, experts, ld, t), b = rows_of(bias, bias ? 1 : 0, experts, experts, 4), i = rows_of(ids, tokens, top, top, 4),
+                w = rows_of(weights, tokens, top, top, 4);
+    if (overlap(i, l) || overlap(i, b) || overlap(w, l) || overlap(w, b) || overlap(i, w)) return fail(STRASSEN_ALIAS, "ids and weights must not overlap the inputs or each other");
+    int sms = 0, rc = current_device(&sms);
+    if (rc != STRASSEN_OK) return rc;
+    const RouteArgs a = {tokens, int(experts), type, logits, ld, bias, score == STRASSEN_SOFTMAX, groups, top_groups, top, renormalize != 0, factor, ids, weights, 0};
+    const cudaError_t e = launch_route(a, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
+}
+
 extern "C" strassen_w4 *strassen_w4_create(int64_t n, int64_t k, int group, int scale_type, int has_zeros)
+{
+    return strassen_w4_create_experts(1, n, k, group, scale_type, has_zeros);
+}
+
+extern "C" strassen_w4 *strassen_w4_create_experts(int64_t experts, int64_t n, int64_t k, int group, int scale_type, int has_zeros)
 {
     set_last_error("");
     if (n < 1 || k < 1 || n > kMaxExtent || k > kMaxExtent) {
         fail(STRASSEN_INVALID_ARG, "n and k must be 1 .. 2^30");
+        return nullptr;
+    }
+    if (experts < 1 || experts > kMostExperts) {
+        fail(STRASSEN_INVALID_ARG, "experts must be 1 .. 1024");
         return nullptr;
     }
     if (group != 32 && group != 64 && group != 128) {
@@ -157,19 +196,20 @@ extern "C" strassen_w4 *strassen_w4_create(int64_t n, int64_t k, int group, int 
     W4Layout l;
     l.n = n;
     l.k = k;
+    l.experts = experts;
     l.group = group;
     l.scale_type = scale_type;
     l.has_zeros = has_zeros != 0;
     l.row_tiles = round_up(n, kW4Rows) / kW4Rows;
     l.depth_tiles = round_up(k, kW4Depth) / kW4Depth;
-    const int64_t tiles = l.row_tiles * l.depth_tiles;
+    const int64_t tiles = experts * l.row_tiles * l.depth_tiles;
     if (tiles > 0x7fffffff) {
-        fail(STRASSEN_INVALID_ARG, "the matrix is too large (2^31 tiles of 128 x 128)");
+        fail(STRASSEN_INVALID_ARG, "the matrices are too large (2^31 tiles of 128 x 128)");
         return nullptr;
     }
     l.tile_bytes = kW4NibbleBytes + kW4Depth / group * kW4Rows * (l.has_zeros ? 3 : 2);
     l.exponent_off = size_t(round_up(tiles * l.tile_bytes, 256));
-    l.bytes = l.exponent_off + size_t(l.row_tiles) * kW4Rows * 4;
+    l.bytes = l.exponent_off + size_t(experts * l.row_tiles) * kW4Rows * 4;
     strassen_w4 *w = new (std::nothrow) strassen_w4;
     if (!w) {
         fail(STRASSEN_OUT_OF_MEMORY, "out of host memory");
@@ -191,13 +231,14 @@ extern "C" int strassen_w4_pack(strassen_w4 *w, const uint8_t *q, int64_t ldq, c
     const W4Layout &l = w->lay;
     if (!zeros != !l.has_zeros) return fail(STRASSEN_INVALID_ARG, "zero points must be given if, and only if, the matrix was created with them");
     const int64_t half = (l.k + 1) / 2, groups = (l.k + l.group - 1) / l.group;
-    if (l.n > 1 && (ldq < half || lds < groups || (zeros && ldz < groups) || ldq > kMaxLd || lds > kMaxLd || ldz > kMaxLd))
+    const int64_t rows = l.experts * l.n;
+    if (rows > 1 && (ldq < half || lds < groups || (zeros && ldz < groups) || ldq > kMaxLd || lds > kMaxLd || ldz > kMaxLd))
         return fail(STRASSEN_INVALID_ARG, "leading dimensions must be at least the rows' length");
     if (misaligned(scales, 2)) return fail(STRASSEN_MISALIGNED, "scales must be 2-byte aligned");
     if (misaligned(packed, 256)) return fail(STRASSEN_MISALIGNED, "packed must be 256-byte aligned");
     const Range out = {reinterpret_cast<uintptr_t>(packed), reinterpret_cast<uintptr_t>(packed) + l.bytes};
-    if (overlap(out, rows_of(q, l.n, half, ldq, 1)) || overlap(out, rows_of(scales, l.n, groups, lds, 2)) ||
-        overlap(out, rows_of(zeros, zeros ? l.n : 0, groups, ldz, 1)))
+    if (overlap(out, rows_of(q, rows, half, ldq, 1)) || overlap(out, rows_of(scales, rows, groups, lds, 2)) ||
+        overlap(out, rows_of(zeros, zeros ? rows : 0, groups, ldz, 1)))
         return fail(STRASSEN_ALIAS, "packed overlaps an input");
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
@@ -227,6 +268,7 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
     if (!w) return fail(STRASSEN_INVALID_ARG, "the matrix must be non-NULL");
     if (!w->packed) return fail(STRASSEN_INVALID_ARG, "the matrix has not been laid out (strassen_w4_pack)");
     const W4Layout &l = w->lay;
+    if (l.experts != 1) return fail(STRASSEN_INVALID_ARG, "several matrices: strassen_w4_experts multiplies by those that ids name");
     if (m < 0 || m > kMaxExtent) return fail(STRASSEN_INVALID_ARG, "m must be 0 .. 2^30");
     if (type != STRASSEN_BF16 && type != STRASSEN_F16 && type != STRASSEN_E4M3)
         return fail(STRASSEN_INVALID_ARG, "the type of x must be STRASSEN_BF16, STRASSEN_F16 or STRASSEN_E4M3");
@@ -243,7 +285,7 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
         return fail(STRASSEN_ALIAS, "out overlaps an input");
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
-    const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, workspace};
+    const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, workspace, nullptr, 0, false, nullptr};
     const int64_t need = m > kThinRows ? w4_tiles_workspace(a) : 0;
     if (need > 0) {
         if (!workspace || workspace_bytes < size_t(need))
@@ -255,6 +297,65 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
     }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = m <= kThinRows ? launch_w4_thin(a, sms, st) : launch_w4_tiles(a, sms, st);
+    return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
+}
+
+extern "C" size_t strassen_w4_experts_workspace_bytes(const strassen_w4 *w, int64_t tokens, int64_t top, int weighted)
+{
+    if (!w || tokens < 0 || top < 1 || top > kMostTop || tokens * top <= kThinIds || tokens > kMaxExtent / kMostTop) return 0;
+    W4Args a = {};
+    a.lay = w->lay;
+    a.m = tokens;
+    a.top = top;
+    static const float some = 0.f;
+    a.weights = weighted ? &some : nullptr;
+    return size_t(w4_experts_workspace(a));
+}
+
+extern "C" int strassen_w4_experts(const strassen_w4 *w, int64_t tokens, int64_t top, const int *ids, int type, const void *x, int64_t ldx, int each,
+                                   const float *x_scale, const float *weights, int out_type, void *out, int64_t ldo, void *workspace,
+                                   size_t workspace_bytes, void *stream)
+{
+    set_last_error("");
+    if (!w) return fail(STRASSEN_INVALID_ARG, "the matrices must be non-NULL");
+    if (!w->packed) return fail(STRASSEN_INVALID_ARG, "the matrices have not been laid out (strassen_w4_pack)");
+    const W4Layout &l = w->lay;
+    if (tokens < 0 || tokens > kMaxExtent / kMostTop) return fail(STRASSEN_INVALID_ARG, "tokens must be 0 .. 2^25");
+    if (top < 1 || top > kMostTop) return fail(STRASSEN_INVALID_ARG, "top must be 1 .. 32");
+    if (type != STRASSEN_BF16 && type != STRASSEN_F16 && type != STRASSEN_E4M3)
+        return fail(STRASSEN_INVALID_ARG, "the type of x must be STRASSEN_BF16, STRASSEN_F16 or STRASSEN_E4M3");
+    if (out_type != STRASSEN_BF16 && out_type != STRASSEN_F16) return fail(STRASSEN_INVALID_ARG, "the output type must be STRASSEN_BF16 or STRASSEN_F16");
+    if (tokens == 0) return STRASSEN_OK;
+    if (!ids || !x || !out) return fail(STRASSEN_INVALID_ARG, "ids, x and out must be non-NULL");
+    const int64_t pairs = tokens * top, x_rows = each ? pairs : tokens, out_rows = weights ? tokens : pairs;
+    if ((x_rows > 1 && (ldx < l.k || ldx > kMaxLd)) || (out_rows > 1 && (ldo < l.n || ldo > kMaxLd)))
+        return fail(STRASSEN_INVALID_ARG, "leading dimensions must be at least the rows' length");
+    const int t = type_size(type);
+    if (misaligned(x, t) || misaligned(x_scale, 4) || misaligned(out, 2) || misaligned(ids, 4) || misaligned(weights, 4))
+        return fail(STRASSEN_MISALIGNED, "ids, x, x_scale, weights and out must be aligned to their elements");
+    const Range inputs[] = {rows_of(x, x_rows, l.k, ldx, t), rows_of(x_scale, x_scale ? 1 : 0, x_rows, x_rows, 4), rows_of(ids, 1, pairs, pairs, 4),
+                            rows_of(weights, weights ? 1 : 0, pairs, pairs, 4), {reinterpret_cast<uintptr_t>(w->packed), reinterpret_cast<uintptr_t>(w->packed) + l.bytes}};
+    const Range o = rows_of(out, out_rows, l.n, ldo, 2);
+    for (const Range &r : inputs)
+        if (overlap(o, r)) return fail(STRASSEN_ALIAS, "out overlaps an input");
+    int sms = 0, rc = current_device(&sms);
+    if (rc != STRASSEN_OK) return rc;
+    const W4Args a = {l, w->packed, tokens, type, x, ldx, x_scale, out_type, out, ldo, workspace, ids, top, each != 0, weights};
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (pairs <= kThinIds) {
+        e = launch_w4_thin(a, sms, st);
+    } else {
+        const size_t need = size_t(w4_experts_workspace(a));
+        if (!workspace || workspace_bytes < need)
+            return fail(STRASSEN_WORKSPACE_TOO_SMALL, "these rows need a workspace of " + std::to_string(need) + " bytes (strassen_w4_experts_workspace_bytes)");
+        if (misaligned(workspace, 256)) return fail(STRASSEN_MISALIGNED, "workspace must be 256-byte aligned");
+        const Range ws = {reinterpret_cast<uintptr_t>(workspace), reinterpret_cast<uintptr_t>(workspace) + need};
+        if (overlap(ws, o)) return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
+        for (const Range &r : inputs)
+            if (overlap(ws, r)) return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
+        e = launch_w4_experts_tiles(a, sms, st);
+    }
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
 }
 

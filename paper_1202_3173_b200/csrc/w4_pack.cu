@@ -25,20 +25,21 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
     const int64_t tile = blockIdx.x;
     const int64_t nt = tile / p.lay.depth_tiles, kb = tile % p.lay.depth_tiles;
     const int c = threadIdx.x >> 7, r = threadIdx.x & 127;
-    const int64_t row = nt * kW4Rows + r;
+    const int64_t matrix = nt / p.lay.row_tiles, in = (nt - matrix * p.lay.row_tiles) * kW4Rows + r, row = matrix * p.lay.n + in;
+    const bool real = in < p.lay.n;
     const uint8_t *src = p.q + row * p.ldq;
     uint32_t out[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const int64_t k0 = kb * kW4Depth + 32 * w + 8 * c;
         uint32_t pad = 8;
-        if (p.lay.has_zeros && row < p.lay.n && k0 < p.lay.k) pad = p.zeros[row * p.ldz + k0 / p.lay.group] & 15;
+        if (p.lay.has_zeros && real && k0 < p.lay.k) pad = p.zeros[row * p.ldz + k0 / p.lay.group] & 15;
         uint32_t word = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t k = k0 + i;
             uint32_t v = pad;
-            if (row < p.lay.n && k < p.lay.k) v = (src[k >> 1] >> (4 * (i & 1))) & 15;
+            if (real && k < p.lay.k) v = (src[k >> 1] >> (4 * (i & 1))) & 15;
             word |= v << (4 * (i >> 1) + 16 * (i & 1));
         }
         out[w] = word;
@@ -50,14 +51,15 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
 // One warp per row: its exponent, and its scales and zero points to their places.
 __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
 {
-    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
+    const int64_t slot = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);         // row among the padded rows of all matrices
     const int lane = threadIdx.x & 31;
-    const int64_t nt = row / kW4Rows;
-    const int place = W4Layout::row_place(int(row % kW4Rows));
+    const int64_t nt = slot / kW4Rows, matrix = nt / p.lay.row_tiles, in = slot - matrix * p.lay.row_tiles * kW4Rows;
+    const int place = W4Layout::row_place(int(slot % kW4Rows));
     const int64_t groups = (p.lay.k + p.lay.group - 1) / p.lay.group;
     const int per_tile = kW4Depth / p.lay.group;
-    const bool real = row < p.lay.n;
-    const uint16_t *scales = static_cast<const uint16_t *>(p.scales) + (real ? row : 0) * p.lds;
+    const bool real = in < p.lay.n;
+    const int64_t row = real ? matrix * p.lay.n + in : 0;
+    const uint16_t *scales = static_cast<const uint16_t *>(p.scales) + row * p.lds;
     float mx = 0.f;
     for (int64_t g = lane; g < groups && real; g += 32) {
         const float v = fabsf(scale_value(scales[g], p.lay.scale_type));
@@ -67,7 +69,7 @@ __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
     int e = mx > 0.f ? ilogbf(mx) : 0;
     e = e < -126 ? -126 : e;
-    if (lane == 0) reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[row] = ldexpf(1.f, e);
+    if (lane == 0) reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[slot] = ldexpf(1.f, e);
     for (int64_t g = lane; g < p.lay.depth_tiles * per_tile; g += 32) {
         const bool on = real && g < groups;
         uint8_t *tile = p.packed + (nt * p.lay.depth_tiles + g / per_tile) * p.lay.tile_bytes;
@@ -83,8 +85,8 @@ __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
 
 cudaError_t launch_w4_pack(const W4PackArgs &p, cudaStream_t stream)
 {
-    pack_weights_kernel<<<unsigned(p.lay.row_tiles * p.lay.depth_tiles), 512, 0, stream>>>(p);
-    pack_scales_kernel<<<unsigned(p.lay.row_tiles * kW4Rows / 4), 128, 0, stream>>>(p);
+    pack_weights_kernel<<<unsigned(p.lay.experts * p.lay.row_tiles * p.lay.depth_tiles), 512, 0, stream>>>(p);
+    pack_scales_kernel<<<unsigned(p.lay.experts * p.lay.row_tiles * kW4Rows / 4), 128, 0, stream>>>(p);
     return cudaGetLastError();
 }
 

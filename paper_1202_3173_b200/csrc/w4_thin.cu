@@ -135,10 +135,20 @@ struct Ptrs {
     int tile_bytes, zero_off;
     int x_align;
     bool scale_bf16, out_bf16;
+    // experts: m tokens with `top` ids each
+    const int *ids;
+    const float *weights;
+    int64_t row_tiles;       // of one matrix
+    int top, experts;
+    bool each;
 };
 
+enum { ONE = 0, EACH_ID = 1, SUM_OF_IDS = 2 };
+
 // RT pieces of 16 rows, TT pieces of 8 tokens.
-template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(WARPS * 32) w4_thin_kernel(const Ptrs p)
+// With experts a CTA has a single row of x at a time: MODE EACH_ID that of one id, its row of results; MODE SUM_OF_IDS those of all ids of
+// a token one after another, their sums multiplied by the ids' weights on the way.
+template <int XT, int RT, int TT, bool ZEROS, int MODE> __global__ void __launch_bounds__(WARPS * 32) w4_thin_kernel(const Ptrs p)
 {
     using N = Num<XT>;
     constexpr int ROWS = 16 * RT, TOKENS = 8 * TT, CELLS = ROWS * TOKENS;
@@ -146,15 +156,32 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int64_t row0 = int64_t(blockIdx.x) * ROWS, nt = row0 / kW4Rows;
     const int r_in = int(row0 % kW4Rows);
-    const int64_t t0 = int64_t(blockIdx.z) * TOKENS;
+    const int64_t t0 = MODE == ONE ? int64_t(blockIdx.z) * TOKENS : int64_t(blockIdx.z);        // first row of x; with experts, of the result
 
     float acc[RT][TT][4] = {};
     const void *xrow[TT];
+    const int choices = MODE == SUM_OF_IDS ? p.top : 1;
+    for (int choice = 0; choice < choices; ++choice) {
+    int64_t matrix_tile = nt;
+    float factor[RT][2];
+    if (MODE == ONE) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xrow[t] = t0 + 8 * t + g < p.m ? static_cast<const char *>(p.x) + (t0 + 8 * t + g) * p.ldx_bytes : nullptr;
+        for (int t = 0; t < TT; ++t) xrow[t] = t0 + 8 * t + g < p.m ? static_cast<const char *>(p.x) + (t0 + 8 * t + g) * p.ldx_bytes : nullptr;
+    } else {
+        const int64_t at = MODE == SUM_OF_IDS ? t0 * p.top + choice : t0, from = p.each ? at : at / p.top;
+        const int id = p.ids[at];
+        if (id < 0 || id >= p.experts) continue;         // no expert: adds nothing
+        matrix_tile += id * p.row_tiles;
+        xrow[0] = g == 0 ? static_cast<const char *>(p.x) + from * p.ldx_bytes : nullptr;
+        const float f = (p.x_scale ? p.x_scale[from] : 1.f) * (MODE == SUM_OF_IDS ? p.weights[at] : 1.f);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) factor[r][h] = f * p.exponents[matrix_tile * kW4Rows + r_in + 16 * r + 8 * h + g];
+    }
 
     for (int64_t kb = blockIdx.y * WARPS + warp; kb < p.depth_tiles; kb += int64_t(gridDim.y) * WARPS) {
-        const uint8_t *const packed = p.packed + (nt * p.depth_tiles + kb) * p.tile_bytes;
+        const uint8_t *const packed = p.packed + (matrix_tile * p.depth_tiles + kb) * p.tile_bytes;
         const uint4 *tile = reinterpret_cast<const uint4 *>(packed) + c * kW4Rows + r_in + g;
         uint32_t w[RT][2][4];
 #pragma unroll
@@ -177,8 +204,8 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     const uint32_t s = *reinterpret_cast<const uint32_t *>(packed + kW4NibbleBytes + 2 * (at + 16 * r));
-                    scale[r][0] = scale_value(s & 0xffff, p.scale_bf16);
-                    scale[r][1] = scale_value(s >> 16, p.scale_bf16);
+                    scale[r][0] = scale_value(s & 0xffff, p.scale_bf16) * (MODE == ONE ? 1.f : factor[r][0]);
+                    scale[r][1] = scale_value(s >> 16, p.scale_bf16) * (MODE == ONE ? 1.f : factor[r][1]);
                     uint32_t z = 0x0808;
                     if (ZEROS) z = *reinterpret_cast<const uint16_t *>(packed + p.zero_off + at + 16 * r);
                     minus[r][0] = N::both(-N::UNIT * float(z & 0xff));
@@ -220,6 +247,7 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
             }
         }
     }
+    }
     // cell (row, token) at token * ROWS + row: accumulator i is row g + 8 (i / 2), token 2 c + i % 2
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -249,9 +277,9 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
             for (int w = 0; w < WARPS; ++w) s += red[w][e];
         }
         const int64_t n = row0 + e % ROWS, t = t0 + e / ROWS;
-        if (n < p.n && t < p.m) {
-            s *= N::BACK * p.exponents[n];
-            if (p.x_scale) s *= p.x_scale[t];
+        if (n < p.n && (MODE == ONE ? t < p.m : e < ROWS)) {
+            s *= N::BACK;
+            if (MODE == ONE) s *= p.x_scale ? p.x_scale[t] * p.exponents[n] : p.exponents[n];
             if (p.out_bf16) static_cast<__nv_bfloat16 *>(p.out)[t * p.ldo + n] = __float2bfloat16_rn(s);
             else static_cast<__half *>(p.out)[t * p.ldo + n] = __float2half_rn(s);
         }
@@ -259,9 +287,9 @@ template <int XT, int RT, int TT, bool ZEROS> __global__ void __launch_bounds__(
     if (splits > 1) cluster.sync();         // no CTA leaves while another reads its sums
 }
 
-template <int XT, int RT, int TT, bool ZEROS> cudaError_t launch_one(const Ptrs &p, int sm_count, cudaStream_t stream)
+template <int XT, int RT, int TT, bool ZEROS, int MODE> cudaError_t launch_one(const Ptrs &p, int sm_count, cudaStream_t stream)
 {
-    const int64_t rows = (p.n + 16 * RT - 1) / (16 * RT), tokens = (p.m + 8 * TT - 1) / (8 * TT);
+    const int64_t rows = (p.n + 16 * RT - 1) / (16 * RT), tokens = MODE == ONE ? (p.m + 8 * TT - 1) / (8 * TT) : MODE == EACH_ID ? p.m * p.top : p.m;
     int splits = 1;
     while (splits < 8 && rows * tokens * splits * 2 <= 2 * sm_count && p.depth_tiles >= int64_t(splits) * 2 * WARPS) splits *= 2;
     cudaLaunchConfig_t cfg = {};
@@ -275,14 +303,15 @@ template <int XT, int RT, int TT, bool ZEROS> cudaError_t launch_one(const Ptrs 
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, w4_thin_kernel<XT, RT, TT, ZEROS>, p);
+    return cudaLaunchKernelEx(&cfg, w4_thin_kernel<XT, RT, TT, ZEROS, MODE>, p);
 }
 
 template <int XT, bool ZEROS> cudaError_t launch_shape(const Ptrs &p, int sm_count, cudaStream_t stream)
 {
-    if (p.m <= 2) return launch_one<XT, 1, 1, ZEROS>(p, sm_count, stream);
-    if (p.m <= 8) return launch_one<XT, 2, 1, ZEROS>(p, sm_count, stream);
-    return launch_one<XT, 4, 2, ZEROS>(p, sm_count, stream);
+    if (p.ids) return p.weights ? launch_one<XT, 1, 1, ZEROS, SUM_OF_IDS>(p, sm_count, stream) : launch_one<XT, 1, 1, ZEROS, EACH_ID>(p, sm_count, stream);
+    if (p.m <= 2) return launch_one<XT, 1, 1, ZEROS, ONE>(p, sm_count, stream);
+    if (p.m <= 8) return launch_one<XT, 2, 1, ZEROS, ONE>(p, sm_count, stream);
+    return launch_one<XT, 4, 2, ZEROS, ONE>(p, sm_count, stream);
 }
 
 template <int XT> cudaError_t launch_type(const Ptrs &p, bool zeros, int sm_count, cudaStream_t stream)
@@ -319,9 +348,15 @@ cudaError_t launch_w4_thin(const W4Args &a, int sm_count, cudaStream_t stream)
         p.ldo = a.ldo;
         p.depth_tiles = a.lay.depth_tiles;
         p.group_words = a.lay.group / 32;
-        p.x_align = alignment(reinterpret_cast<uintptr_t>(p.x) | uintptr_t(p.m > 1 ? p.ldx_bytes : 0));
+        p.x_align = alignment(reinterpret_cast<uintptr_t>(p.x) | uintptr_t(p.m > 1 || a.each ? p.ldx_bytes : 0));
         p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
         p.out_bf16 = a.out_type == STRASSEN_BF16;
+        p.ids = a.ids;
+        p.weights = a.weights;
+        p.row_tiles = a.lay.row_tiles;
+        p.top = int(a.top);
+        p.experts = int(a.lay.experts);
+        p.each = a.each;
         cudaError_t e;
         if (a.type == STRASSEN_BF16) e = launch_type<XBF16>(p, a.lay.has_zeros, sm_count, stream);
         else if (a.type == STRASSEN_F16) e = launch_type<XF16>(p, a.lay.has_zeros, sm_count, stream);

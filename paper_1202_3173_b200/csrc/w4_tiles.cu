@@ -640,24 +640,37 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
 }
 
 // Rows of x in 16 bits, one after another, `width` (a multiple of 8) values apart, zeros past the inner size: e4m3 becomes f16, exactly.
-__global__ void __launch_bounds__(256) rows_kernel(const char *x, int64_t ldx_bytes, int64_t rows, int64_t k, int64_t width, bool e4m3, bool wide, const int *order, int order_div, uint16_t *out)
+struct RowsArgs {
+    const char *x;
+    int64_t ldx_bytes, rows, k, width;
+    bool e4m3, wide;         // wide: rows of x allow 16-byte (e4m3: 8-byte) accesses
+    uint16_t *out;
+    // experts: the pair of each row in order, pairs per row of x; the pairs' ids, to write zeros to the results of those without an expert
+    const int *order, *count, *ids;
+    int per_row, experts;
+    uint16_t *results;       // NULL: not those
+    int64_t ldo, n;
+};
+
+__global__ void __launch_bounds__(256) rows_kernel(const RowsArgs p)
 {
-    const int64_t chunks = width / 8, total = rows * chunks;
-    for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
-        const int64_t i = e / chunks, c = e % chunks * 8;
-        const int64_t row = order ? order[i] / order_div : i;
+    const int64_t chunks = p.width / 8, total = (p.count ? int64_t(*p.count) : p.rows) * chunks, step = int64_t(gridDim.x) * blockDim.x;
+    const int64_t me = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+    for (int64_t e = me; e < total; e += step) {
+        const int64_t i = e / chunks, c = (e - i * chunks) * 8;
+        const int64_t row = p.order ? p.order[i] / p.per_row : i;
         uint32_t v[4] = {0, 0, 0, 0};
-        if (e4m3) {
-            const uint8_t *p = reinterpret_cast<const uint8_t *>(x + row * ldx_bytes) + c;
+        if (p.e4m3) {
+            const uint8_t *x = reinterpret_cast<const uint8_t *>(p.x + row * p.ldx_bytes) + c;
             uint32_t w[2] = {0, 0};
-            if (wide && c + 8 <= k) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(p);
+            if (p.wide && c + 8 <= p.k) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(x);
                 w[0] = u.x;
                 w[1] = u.y;
             } else {
 #pragma unroll
                 for (int b = 0; b < 8; ++b)
-                    if (c + b < k) w[b >> 2] |= uint32_t(p[b]) << (8 * (b & 3));
+                    if (c + b < p.k) w[b >> 2] |= uint32_t(x[b]) << (8 * (b & 3));
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -665,9 +678,9 @@ __global__ void __launch_bounds__(256) rows_kernel(const char *x, int64_t ldx_by
                 v[b] = uint32_t(h.x) | (uint32_t(h.y) << 16);
             }
         } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(x + row * ldx_bytes) + c;
-            if (wide && c + 8 <= k) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(p);
+            const uint16_t *x = reinterpret_cast<const uint16_t *>(p.x + row * p.ldx_bytes) + c;
+            if (p.wide && c + 8 <= p.k) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(x);
                 v[0] = u.x;
                 v[1] = u.y;
                 v[2] = u.z;
@@ -675,10 +688,107 @@ __global__ void __launch_bounds__(256) rows_kernel(const char *x, int64_t ldx_by
             } else {
 #pragma unroll
                 for (int b = 0; b < 8; ++b)
-                    if (c + b < k) v[b >> 1] |= uint32_t(p[b]) << (16 * (b & 1));
+                    if (c + b < p.k) v[b >> 1] |= uint32_t(x[b]) << (16 * (b & 1));
             }
         }
-        *reinterpret_cast<uint4 *>(out + i * width + c) = make_uint4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<uint4 *>(p.out + i * p.width + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    if (p.results && *p.count < p.rows)
+        for (int64_t i = me >> 5; i < p.rows; i += step >> 5)
+            if (p.ids[i] < 0 || p.ids[i] >= p.experts)
+                for (int64_t c = threadIdx.x & 31; c < p.n; c += 32) p.results[i * p.ldo + c] = 0;
+}
+
+// Pairs (a token and one of its ids) in order of their experts, pairs of one expert in their own order: CTA e counts the ids of all experts,
+// and with them knows where its own begin.  Every CTA reads all ids, a few kilobytes from L2, and nothing has to be waited for.
+__global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, int experts, int most, int *order, int *count, int *table_size, W4Tile *table)
+{
+    __shared__ int counts[kMostExperts], part[2][32];
+    __shared__ int start, tiles;
+    const int e = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < experts; i += blockDim.x) counts[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+        const int id = ids[i];
+        if (id >= 0 && id < experts) atomicAdd(&counts[id], 1);
+    }
+    __syncthreads();
+    // rows and tiles of rows before this expert, and of all
+    int before[2] = {0, 0}, all[2] = {0, 0};
+    if (int(threadIdx.x) < experts) {
+        const int n = counts[threadIdx.x], t = (n + most - 1) / most;
+        all[0] = n;
+        all[1] = t;
+        if (int(threadIdx.x) < e) {
+            before[0] = n;
+            before[1] = t;
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        before[b] = __reduce_add_sync(~0u, before[b]);
+        all[b] = __reduce_add_sync(~0u, all[b]);
+        if (lane == 0) part[b][warp] = before[b];
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const int rows = __reduce_add_sync(~0u, part[0][lane]), t = __reduce_add_sync(~0u, part[1][lane]);
+        if (lane == 0) {
+            start = rows;
+            tiles = t;
+        }
+    }
+    __syncthreads();
+    if (lane == 0) {
+        part[0][warp] = all[0];
+        part[1][warp] = all[1];
+    }
+    __syncthreads();
+    if (e == 0 && warp == 0) {
+        const int rows = __reduce_add_sync(~0u, part[0][lane]), t = __reduce_add_sync(~0u, part[1][lane]);
+        if (lane == 0) {
+            *count = rows;
+            *table_size = t;
+        }
+    }
+    // rows of x: as few tiles as hold them, evenly filled
+    const int mine = counts[e], runs = (mine + most - 1) / most, even = runs ? (mine + runs - 1) / runs : 0;
+    for (int i = threadIdx.x; i < runs; i += blockDim.x) table[tiles + i] = {e, start + i * even, mine - i * even < even ? mine - i * even : even, 0};
+    __syncthreads();
+    int at = start;
+    for (int i0 = 0; i0 < pairs; i0 += blockDim.x) {
+        const int i = i0 + threadIdx.x;
+        const bool on = i < pairs && ids[i] == e;
+        const uint32_t here = __ballot_sync(~0u, on);
+        if (lane == 0) part[0][warp] = __popc(here);
+        __syncthreads();
+        const int n = part[0][lane], below = __reduce_add_sync(~0u, lane < warp ? n : 0), total = __reduce_add_sync(~0u, n);
+        if (on) order[at + below + __popc(here & ((1u << lane) - 1))] = i;
+        at += total;
+        __syncthreads();
+    }
+}
+
+// out_t = sum_j weights_tj part_tj, in the order of j; pairs without an expert add nothing.
+__global__ void __launch_bounds__(256) weighted_sum_kernel(const float *part, const int *ids, const float *weights, int64_t tokens, int top, int experts, int64_t n, int64_t width, void *out, int64_t ldo, bool bf16)
+{
+    const int64_t chunks = width / 4, total = tokens * chunks;
+    for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
+        const int64_t t = e / chunks, c = (e - t * chunks) * 4;
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < top; ++j) {
+            const int id = ids[t * top + j];
+            if (id < 0 || id >= experts) continue;
+            const float w = weights[t * top + j];
+            const float4 v = *reinterpret_cast<const float4 *>(part + (t * top + j) * width + c);
+            y[0] += w * v.x;
+            y[1] += w * v.y;
+            y[2] += w * v.z;
+            y[3] += w * v.w;
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            if (c + b < n) static_cast<uint16_t *>(out)[t * ldo + c + b] = uint16_t(two_16_bits(y[b], 0.f, bf16));
     }
 }
 
@@ -717,6 +827,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> cudaError_t launch_one(cons
 
 template <bool BF16, bool ZEROS> cudaError_t launch_shape(const Args &p, const CUtensorMap &map, const Shape &s, cudaStream_t stream)
 {
+    if (s.mode == EXPERTS) return launch_one<BF16, ZEROS, 2, EXPERTS>(p, map, s, stream);
     if (s.ctas == 2) return launch_one<BF16, ZEROS, 2, PLAIN>(p, map, s, stream);
     return s.mode == SPLIT ? launch_one<BF16, ZEROS, 1, SPLIT>(p, map, s, stream) : launch_one<BF16, ZEROS, 1, PLAIN>(p, map, s, stream);
 }
@@ -768,55 +879,54 @@ bool map_takes(const W4Args &a)
     return a.type != STRASSEN_E4M3 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx % 8 == 0;
 }
 
-}  // namespace
-
-int64_t w4_tiles_workspace(const W4Args &a) { return map_takes(a) ? 0 : a.m * ((a.lay.k + 7) / 8 * 8) * 2; }
-
-cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
+RowsArgs rows_args(const W4Args &a, void *to)
 {
-    const bool bf16 = a.type == STRASSEN_BF16;
-    const void *x = a.x;
-    int64_t ldx = a.ldx;
-    if (!map_takes(a)) {
-        const int size = a.type == STRASSEN_E4M3 ? 1 : 2;
-        ldx = (a.lay.k + 7) / 8 * 8;
-        const bool wide = (reinterpret_cast<uintptr_t>(a.x) | uintptr_t(a.ldx * size)) % (8 * size) == 0;
-        const int64_t blocks = (a.m * (ldx / 8) + 255) / 256, most = int64_t(sm_count) * 32;
-        rows_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(static_cast<const char *>(a.x), a.ldx * size, a.m, a.lay.k, ldx, a.type == STRASSEN_E4M3, wide, nullptr, 1, static_cast<uint16_t *>(a.workspace));
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-        x = a.workspace;
-    }
+    const int size = a.type == STRASSEN_E4M3 ? 1 : 2;
+    RowsArgs r = {};
+    r.x = static_cast<const char *>(a.x);
+    r.ldx_bytes = a.ldx * size;
+    r.rows = a.m;
+    r.k = a.lay.k;
+    r.width = (a.lay.k + 7) / 8 * 8;
+    r.e4m3 = a.type == STRASSEN_E4M3;
+    r.wide = (reinterpret_cast<uintptr_t>(a.x) | uintptr_t(r.ldx_bytes)) % (8 * size) == 0;
+    r.out = static_cast<uint16_t *>(to);
+    r.per_row = 1;
+    return r;
+}
+
+cudaError_t launch_rows(const RowsArgs &r, int sm_count, cudaStream_t stream)
+{
+    const int64_t blocks = (r.rows * (r.width / 8) + 255) / 256, most = int64_t(sm_count) * 32;
+    rows_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(r);
+    return cudaGetLastError();
+}
+
+// What does not depend on how the rows of x are cut into tiles.
+Args common_args(const W4Args &a)
+{
     Args p = {};
     p.packed = a.packed;
-    p.tile_bytes = a.lay.tile_bytes;
-    p.zero_off = a.lay.zero_off();
     p.exponents = reinterpret_cast<const float *>(a.packed + a.lay.exponent_off);
     p.x_scale = a.x_scale;
     p.out = a.out;
     p.n = int(a.lay.n);
-    p.m = int(a.m);
     p.ldo = a.ldo;
     p.depth_tiles = a.lay.depth_tiles;
     p.row_tiles = int(a.lay.row_tiles);
     p.group_shift = a.lay.group == 32 ? 0 : a.lay.group == 64 ? 1 : 2;
+    p.tile_bytes = a.lay.tile_bytes;
+    p.zero_off = a.lay.zero_off();
     p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
     p.out_type = a.out_type;
     p.out_pairs = reinterpret_cast<uintptr_t>(p.out) % 4 == 0 && p.ldo % 2 == 0;
     p.scale_div = 1;
-    // rows of x: as few tiles as hold them, evenly filled
-    Shape shape = {2, PLAIN, 0, 1, 0};
-    if (int64_t(p.row_tiles) * ((p.m + ALONE_TOKENS - 1) / ALONE_TOKENS) <= sm_count) shape.ctas = 1;
-    const int full = shape.ctas == 1 ? ALONE_TOKENS : TOKENS, runs = (p.m + full - 1) / full, even = (p.m + runs - 1) / runs;
-    const int step = shape.ctas * STEP;
-    p.tokens = (even + step - 1) / step * step;
-    const int64_t tiles = int64_t(p.row_tiles + shape.ctas - 1) / shape.ctas * runs;
-    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
-    if (shape.ctas == 1)
-        while (shape.splits < MAX_SPLITS && tiles <= clusters_of(shape.splits + 1) && p.depth_tiles >= 2 * (shape.splits + 1)) ++shape.splits;
-    if (shape.splits > 1) shape.mode = SPLIT;
-    shape.columns = int(tiles < sm_count / shape.ctas ? tiles : sm_count / shape.ctas);
-    p.box = p.tokens / shape.ctas;
+    return p;
+}
+
+// Rings and shared memory for p.tokens rows of x, and the launch.
+cudaError_t launch_tiles(Args p, Shape shape, const W4Args &a, const void *x, int64_t ldx, int64_t rows, cudaStream_t stream)
+{
     p.x_bytes = p.tokens * 256 / shape.ctas;
     const int stages = (kDynamicLimit - 1024 - RING * p.tile_bytes) / p.x_bytes;
     p.x_stages = stages > RING ? RING : stages;
@@ -833,13 +943,119 @@ cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorSymbolNotFound;
     CUtensorMap map;
-    const cuuint64_t dims[2] = {cuuint64_t(a.lay.k), cuuint64_t(a.m)}, strides[1] = {cuuint64_t(ldx) * 2};
+    const cuuint64_t dims[2] = {cuuint64_t(a.lay.k), cuuint64_t(rows)}, strides[1] = {cuuint64_t(ldx) * 2};
     const cuuint32_t box[2] = {64, cuuint32_t(p.box)}, steps[2] = {1, 1};
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    if (bf16) return a.lay.has_zeros ? launch_shape<true, true>(p, map, shape, stream) : launch_shape<true, false>(p, map, shape, stream);
+    if (a.type == STRASSEN_BF16) return a.lay.has_zeros ? launch_shape<true, true>(p, map, shape, stream) : launch_shape<true, false>(p, map, shape, stream);
     return a.lay.has_zeros ? launch_shape<false, true>(p, map, shape, stream) : launch_shape<false, false>(p, map, shape, stream);
+}
+
+// Workspace of the products of experts: the order and its tables, the rows of x in order, and with weights the pairs' results in 32 bits.
+struct ExpertsSpace {
+    int64_t pairs, most_tiles;
+    size_t count_off, table_off, rows_off, part_off, bytes;
+    int64_t width;           // of the pairs' results
+};
+ExpertsSpace experts_space(const W4Args &a)
+{
+    const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    ExpertsSpace s;
+    s.pairs = a.m * a.top;
+    s.most_tiles = s.pairs / TOKENS + (s.pairs < a.lay.experts ? s.pairs : a.lay.experts);
+    s.width = (a.lay.n + 3) / 4 * 4;
+    s.count_off = up(size_t(s.pairs) * 4);
+    s.table_off = s.count_off + 256;
+    s.rows_off = s.table_off + up(size_t(s.most_tiles) * sizeof(W4Tile));
+    s.part_off = s.rows_off + up(size_t(s.pairs) * size_t((a.lay.k + 7) / 8 * 8) * 2);
+    s.bytes = s.part_off + (a.weights ? up(size_t(s.pairs) * size_t(s.width) * 4) : 0);
+    return s;
+}
+
+}  // namespace
+
+int64_t w4_tiles_workspace(const W4Args &a) { return map_takes(a) ? 0 : a.m * ((a.lay.k + 7) / 8 * 8) * 2; }
+
+cudaError_t launch_w4_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
+{
+    const void *x = a.x;
+    int64_t ldx = a.ldx;
+    if (!map_takes(a)) {
+        const RowsArgs r = rows_args(a, a.workspace);
+        const cudaError_t e = launch_rows(r, sm_count, stream);
+        if (e != cudaSuccess) return e;
+        x = a.workspace;
+        ldx = r.width;
+    }
+    Args p = common_args(a);
+    p.m = int(a.m);
+    // rows of x: as few tiles as hold them, evenly filled
+    Shape shape = {2, PLAIN, 0, 1, 0};
+    if (int64_t(p.row_tiles) * ((p.m + ALONE_TOKENS - 1) / ALONE_TOKENS) <= sm_count) shape.ctas = 1;
+    const int full = shape.ctas == 1 ? ALONE_TOKENS : TOKENS, runs = (p.m + full - 1) / full, even = (p.m + runs - 1) / runs;
+    const int step = shape.ctas * STEP;
+    p.tokens = (even + step - 1) / step * step;
+    p.box = p.tokens / shape.ctas;
+    const int64_t tiles = int64_t(p.row_tiles + shape.ctas - 1) / shape.ctas * runs;
+    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
+    if (shape.ctas == 1)
+        while (shape.splits < MAX_SPLITS && tiles <= clusters_of(shape.splits + 1) && p.depth_tiles >= 2 * (shape.splits + 1)) ++shape.splits;
+    if (shape.splits > 1) shape.mode = SPLIT;
+    shape.columns = int(tiles < sm_count / shape.ctas ? tiles : sm_count / shape.ctas);
+    return launch_tiles(p, shape, a, x, ldx, a.m, stream);
+}
+
+int64_t w4_experts_workspace(const W4Args &a) { return int64_t(experts_space(a).bytes); }
+
+cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t stream)
+{
+    const ExpertsSpace s = experts_space(a);
+    uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
+    int *const order = reinterpret_cast<int *>(ws), *const count = reinterpret_cast<int *>(ws + s.count_off);
+    W4Tile *const table = reinterpret_cast<W4Tile *>(ws + s.table_off);
+    const int experts = int(a.lay.experts);
+    order_kernel<<<unsigned(experts), 1024, 0, stream>>>(a.ids, int(s.pairs), experts, TOKENS, order, count, count + 1, table);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+
+    RowsArgs r = rows_args(a, ws + s.rows_off);
+    r.rows = s.pairs;
+    r.order = order;
+    r.count = count;
+    r.ids = a.ids;
+    r.per_row = a.each ? 1 : int(a.top);
+    r.experts = experts;
+    if (!a.weights) r.results = static_cast<uint16_t *>(a.out);
+    r.ldo = a.ldo;
+    r.n = a.lay.n;
+    e = launch_rows(r, sm_count, stream);
+    if (e != cudaSuccess) return e;
+
+    Args p = common_args(a);
+    p.m = int(s.pairs);
+    p.table = table;
+    p.table_size = count + 1;
+    p.order = order;
+    p.scale_div = r.per_row;
+    if (a.weights) {
+        p.out = ws + s.part_off;
+        p.out_type = STRASSEN_F32;
+        p.ldo = s.width;
+    }
+    // no tile has more rows than there are pairs
+    p.tokens = int(s.pairs < TOKENS ? (s.pairs + 2 * STEP - 1) / (2 * STEP) * (2 * STEP) : TOKENS);
+    p.box = STEP;
+    Shape shape = {2, EXPERTS, 0, 1, 0};
+    const int64_t tiles = int64_t(p.row_tiles + 1) / 2 * s.most_tiles;
+    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
+    shape.columns = int(tiles < sm_count / 2 ? tiles : sm_count / 2);
+    e = launch_tiles(p, shape, a, r.out, r.width, s.pairs, stream);
+    if (e != cudaSuccess || !a.weights) return e;
+    const int64_t blocks = (a.m * (s.width / 4) + 255) / 256, most = int64_t(sm_count) * 16;
+    weighted_sum_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(reinterpret_cast<const float *>(ws + s.part_off), a.ids, a.weights, a.m, int(a.top), experts, a.lay.n, s.width, a.out,
+                                                                                     a.ldo, a.out_type == STRASSEN_BF16);
+    return cudaGetLastError();
 }
 
 cudaError_t read_gave_up(int *flag)

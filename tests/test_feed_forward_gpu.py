@@ -452,3 +452,270 @@ def test_w4_many_launches(m, n, k):
         bad += (out != want).sum()
     assert int(bad) == 0
     binding.strassen_device_status()
+
+
+# ---- routing ---------------------------------------------------------------------------------------------------------
+
+def route64(logits, top, score, bias, groups, top_groups, renormalize, factor):
+    """(ids, weights, margin): the definition in 64 bits; margin: by how much the closest choice of each token was made."""
+    l = logits.double().cpu()
+    tokens, e = l.shape
+    left_out = ~(l > -float("inf"))
+    if score == "softmax":
+        s = torch.softmax(l.masked_fill(left_out, -float("inf")), 1).nan_to_num(0.0)
+        key = s + bias.double().cpu() if bias is not None else l
+    else:
+        s = torch.special.expit(l)
+        key = s + bias.double().cpu() if bias is not None else s
+    ids, weights, margin = torch.full((tokens, top), -1), torch.zeros(tokens, top, dtype=torch.float64), torch.full((tokens,), float("inf"), dtype=torch.float64)
+    size = e // groups
+    for t in range(tokens):
+        keys = {i: float(key[t, i]) for i in range(e) if not left_out[t, i] and float(key[t, i]) > -float("inf")}
+
+        def pick(rated, n):
+            order = sorted(rated, key=lambda i: (-rated[i], i))
+            for a, b in zip(order[:n], order[1:n + 1]):
+                if rated[a] != rated[b]:
+                    margin[t] = min(margin[t], rated[a] - rated[b])
+            return order[:n]
+        if groups > 1:
+            rated = {}
+            for g in range(groups):
+                k = sorted((v for i, v in keys.items() if i // size == g), reverse=True)
+                if k:
+                    rated[g] = k[0] if score == "softmax" or len(k) == 1 else k[0] + k[1]
+            kept = pick(rated, top_groups)
+            keys = {i: v for i, v in keys.items() if i // size in kept}
+        chosen = pick(keys, top)
+        for j, i in enumerate(chosen):
+            ids[t, j], weights[t, j] = i, s[t, i]
+    if renormalize:
+        total = weights.sum(1, keepdim=True)
+        weights = torch.where(total > 0, weights / total, torch.zeros_like(weights))
+    return ids, weights * factor, margin
+
+
+def check_route(logits, top, score="softmax", bias=None, groups=1, top_groups=1, renormalize=True, factor=1.0):
+    ids, weights = sw().route_experts(logits, top, score=score, bias=bias, groups=groups, top_groups=top_groups, renormalize=renormalize, factor=factor)
+    want, w64, margin = route64(logits, top, score, bias, groups, top_groups, renormalize, factor)
+    clear = margin > 2e-6                        # scores in 32 bits: errors of a few 2^-24, of a sum of two twice that
+    assert clear.any()
+    assert torch.equal(ids.cpu()[clear].long(), want[clear])
+    assert ((weights.double().cpu()[clear] - w64[clear]).abs() <= 1e-5 * w64[clear] + 1e-12).all()
+    # every token's ids are distinct and in range, clear or not
+    for row in ids.cpu()[~clear].tolist():
+        got = [i for i in row if i >= 0]
+        assert len(set(got)) == len(got) and all(i < logits.shape[1] for i in got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("tokens,experts,top", [(1, 1, 1), (1, 8, 2), (5, 31, 4), (9, 32, 32), (7, 33, 5), (64, 64, 8), (3, 100, 6), (130, 128, 8), (2, 256, 8), (17, 257, 16), (5, 512, 10), (4, 1000, 32), (2, 1024, 8)])
+def test_route(tokens, experts, top, dtype):
+    g = gen(experts + tokens)
+    logits = (torch.randn(tokens, experts, device="cuda", generator=g) * 2).to(dtype)
+    bias = 0.1 * torch.randn(experts, device="cuda", generator=g)
+    for score in ("softmax", "sigmoid"):
+        for b in (None, bias):
+            check_route(logits, top, score, b, renormalize=b is None, factor=2.5 if b is None else 1.0)
+
+
+@pytest.mark.parametrize("experts,groups,top_groups,top", [(8, 8, 3, 3), (32, 32, 5, 5), (64, 8, 4, 8), (256, 8, 4, 8), (96, 3, 2, 6), (160, 16, 1, 10), (1024, 32, 7, 32), (60, 2, 2, 7), (512, 4, 3, 16)])
+def test_route_groups(experts, groups, top_groups, top):
+    g = gen(experts + groups)
+    logits = torch.randn(40, experts, device="cuda", generator=g)
+    bias = 0.2 * torch.randn(experts, device="cuda", generator=g)
+    for score in ("softmax", "sigmoid"):
+        for b in (None, bias):
+            check_route(logits, top, score, b, groups, top_groups)
+
+
+def test_route_ties_go_to_the_lowest_index():
+    logits = torch.zeros(3, 70, device="cuda")
+    logits[1, 40:] = 1.0
+    logits[2, ::7] = -0.0
+    ids, weights = sw().route_experts(logits, 4)
+    assert ids.tolist() == [[0, 1, 2, 3], [40, 41, 42, 43], [0, 1, 2, 3]]
+    assert torch.allclose(weights, torch.full_like(weights, 0.25))
+    ids, _ = sw().route_experts(torch.zeros(2, 64, device="cuda"), 3, score="sigmoid", groups=8, top_groups=2)
+    assert ids.tolist() == [[0, 1, 2]] * 2
+
+
+def test_route_experts_left_out():
+    inf = float("inf")
+    logits = torch.randn(6, 40, device="cuda", generator=gen(1))
+    logits[0, 3:] = -inf                          # three left for five
+    logits[1] = -inf                              # none
+    logits[2, 5], logits[2, 6] = float("nan"), -inf
+    logits[3, 7] = inf
+    for score in ("softmax", "sigmoid"):
+        for groups in (1, 4):
+            check_route(logits[[0, 1, 2, 4, 5]], 5, score, groups=groups, top_groups=min(groups, 2))
+            ids, weights = sw().route_experts(logits, 5, score=score, groups=groups, top_groups=min(groups, 2))
+            assert (ids[1] == -1).all() and (weights[1] == 0).all() and ids[3, 0] == 7
+            assert (ids[0] >= 0).sum() == 3 and torch.isfinite(weights).all()
+    ids, weights = sw().route_experts(torch.full((1, 16), -200.0, device="cuda"), 4, score="sigmoid")      # scores that are all 0
+    assert ids.tolist() == [[0, 1, 2, 3]] and (weights == 0).all()
+
+
+def test_route_strides_and_no_tokens():
+    wide = torch.randn(9, 77, device="cuda", generator=gen(3)).to(BF16)
+    check_route(wide[:, 3:69], 6)
+    ids, weights = sw().route_experts(wide[:0, :64], 6)
+    assert ids.shape == (0, 6) and weights.shape == (0, 6)
+
+
+# ---- products of experts ---------------------------------------------------------------------------------------------
+
+def experts_case(experts, n, k, group, zeros, sdtype, seed):
+    q, s, z = weights(experts * n, k, group, zeros, sdtype, seed)
+    W, A = dense64(q, s, z, k, group)
+    shape = lambda t: t.view(experts, n, -1)  # noqa: E731
+    matrices = sw().W4Experts(shape(q), shape(s), shape(z) if z is not None else None, k=k, group=group)
+    return matrices, W.view(experts, n, k), A.view(experts, n, k)
+
+
+def check_experts(matrices, W, A, x, xs, ids, factor, out_dtype, y):
+    """y against the sums, with the tolerances of the products; a sum of ids adds the rounding of its own."""
+    tokens, top = ids.shape
+    experts, n, k = W.shape
+    xd = x.double() if xs is None else x.double() * xs.double()[:, None]
+    if x.shape[0] == tokens and top > 1 or x.shape[0] == tokens:
+        xd = xd.repeat_interleave(top, 0) if x.shape[0] != tokens * top else xd
+    want = torch.zeros(tokens * top, n, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(want)
+    flat = ids.flatten().long()
+    for e in range(experts):
+        at = (flat == e).nonzero()[:, 0]
+        want[at], size[at] = xd[at] @ W[e].t(), xd[at].abs() @ A[e].t()
+    if factor is not None:
+        f = factor.double()[..., None]
+        want, size = (want.view(tokens, top, n) * f).sum(1), (size.view(tokens, top, n) * f.abs()).sum(1)
+    w = 0.0 if tokens * top <= 32 else U[BF16] if x.dtype == BF16 else U[F16]
+    assert y.dtype == out_dtype and y.shape == want.shape and torch.isfinite(y).all()
+    err = (y.double() - want).abs()
+    lim = U[out_dtype] * want.abs() + ((k + top) * 2.0 ** -23 + w) * size + (6e-8 if out_dtype == F16 else 0)
+    assert (err <= lim).all(), float((err - lim).max())
+    assert err.norm() <= (2 * U[out_dtype] + 2 * w + k * 2.0 ** -23) * want.norm() + 6e-8 * err.numel() ** 0.5
+
+
+EXPERT_SHAPES = [(1, 1, 4, 16, 64), (1, 8, 16, 200, 300), (4, 2, 3, 129, 257), (3, 8, 64, 128, 512), (2, 16, 40, 100, 1000), (5, 8, 10, 130, 200), (33, 1, 7, 64, 96),
+                 (40, 4, 6, 300, 140), (200, 2, 3, 257, 400), (700, 3, 20, 130, 256), (300, 8, 300, 40, 64), (64, 32, 40, 96, 128)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("tokens,top,experts,n,k", EXPERT_SHAPES)
+def test_experts(tokens, top, experts, n, k, group, zeros):
+    g = gen(tokens + k)
+    ids = torch.rand(tokens, experts, device="cuda", generator=g).pow(3).argsort(1)[:, :top].to(torch.int32).contiguous() if top <= experts else \
+        torch.randint(0, experts, (tokens, top), device="cuda", generator=g, dtype=torch.int32)
+    factor = torch.rand(tokens, top, device="cuda", generator=g)
+    for dtype, out_dtype, sdtype in ((BF16, BF16, BF16), (F16, F16, F16), (E4M3, BF16, BF16)):
+        matrices, W, A = experts_case(experts, n, k, group, zeros, sdtype, n + k)
+        for m in (tokens, tokens * top):
+            x, xs = rows(m, k, dtype, m)
+            for f in (None, factor):
+                check_experts(matrices, W, A, x, xs, ids, f, out_dtype, matrices(x, ids, xs, weights=f, dtype=out_dtype))
+
+
+@pytest.mark.parametrize("tokens", [3, 50])
+def test_experts_ids_that_name_none(tokens):
+    n, k, experts, top = 150, 300, 5, 4
+    matrices, W, A = experts_case(experts, n, k, 64, True, BF16, 3)
+    g = gen(tokens)
+    ids = torch.randint(-2, experts + 2, (tokens, top), device="cuda", generator=g, dtype=torch.int32)
+    ids[1] = -1                                  # a token without any
+    ids[2, 0] = 2 ** 31 - 1
+    factor = torch.rand(tokens, top, device="cuda", generator=g)
+    x, _ = rows(tokens, k, BF16, 5)
+    for f in (None, factor):
+        y = matrices(x, ids, weights=f)
+        check_experts(matrices, W, A, x, None, ids, f, BF16, y)
+        assert (y.view(tokens, -1)[1] == 0).all()
+    y = matrices(x, torch.full_like(ids, -1))
+    assert (y == 0).all()
+
+
+@pytest.mark.parametrize("tokens", [2, 60])
+def test_experts_strides(tokens):
+    n, k, experts, top = 140, 333, 6, 3
+    q, s, z = weights(experts * n, k, 64, True, BF16, 9)
+    W, A = dense64(q, s, z, k, 64)
+    qs, ss, zs = (strided(t, 5, 1, 0).unflatten(0, (experts, n)) for t in (q, s, z))
+    matrices = sw().W4Experts(qs, ss, zs, k=k, group=64)
+    ids = torch.randint(0, experts, (tokens, top), device="cuda", generator=gen(2), dtype=torch.int32)
+    for dtype in (BF16, E4M3):
+        x, xs = rows(tokens * top, k, dtype, 3)
+        out = strided(torch.zeros(tokens * top, n, device="cuda").to(BF16), 3, 1, 7.0)
+        matrices(strided(x, 3, 1), ids, xs, out=out)
+        check_experts(matrices, W.view(experts, n, k), A.view(experts, n, k), x, xs, ids, None, BF16, out)
+        assert (out.as_strided((tokens * top - 1, 3), (n + 3, 1), out.storage_offset() + n) == 7).all()
+
+
+def test_experts_many_launches_and_special_rows():
+    """The same bits each time; a NaN in one row of x stays in that row's results, although other rows share its tile."""
+    experts, top, tokens = 8, 2, 300
+    matrices, W, A = experts_case(experts, 512, 1024, 128, False, BF16, 3)
+    g = gen(1)
+    ids = torch.rand(tokens, experts, device="cuda", generator=g).argsort(1)[:, :top].to(torch.int32).contiguous()
+    factor = torch.rand(tokens, top, device="cuda", generator=g)
+    x, _ = rows(tokens, 1024, BF16, 3)
+    x[17, 5] = float("nan")
+    fine = torch.arange(tokens, device="cuda") != 17
+    want = matrices(x, ids, weights=factor)
+    assert torch.isnan(want[17]).all() and torch.isfinite(want[fine]).all()
+    for _ in range(100):
+        assert torch.equal(matrices(x, ids, weights=factor)[fine], want[fine])
+    binding.strassen_device_status()
+
+
+def test_experts_block():
+    from paper_1202_3173_b200.feed_forward import ExpertsFeedForward
+    width, inner, experts, top = 128, 192, 6, 2
+    up, W1, _ = experts_case(experts, 2 * inner, width, 64, True, BF16, 3)
+    down, W2, _ = experts_case(experts, width, inner, 64, True, BF16, 4)
+    g = gen(3)
+    norm = (1 + 0.1 * torch.randn(width, device="cuda", generator=g)).to(BF16)
+    router = torch.randn(experts, width, device="cuda", generator=g).to(BF16)
+    block_ = ExpertsFeedForward(norm, router, up, down, top, score="sigmoid")
+    for tokens in (1, 70):
+        x, r = (torch.randn(tokens, width, device="cuda", generator=g).to(BF16) for _ in range(2))
+        y, h = block_(x, r)
+        q, s, _ = sw().rms_norm_quant(x, norm, EPS, residual=r)
+        v = q.double() * s.double()[:, None]
+        ids, f = sw().route_experts((v @ router.double().t()).float(), top, score="sigmoid")
+        want = torch.zeros(tokens, width, dtype=torch.float64, device="cuda")
+        for t in range(tokens):
+            for j in range(top):
+                e = int(ids[t, j])
+                a, b = (W1[e] @ v[t]).split(inner)
+                want[t] += float(f[t, j]) * (W2[e] @ (a * torch.special.expit(a) * b))
+        # the inner rows are rounded to bf16 and then to e4m3
+        assert (y.double() - want).norm() <= 2.0 ** -4 * want.norm()
+
+
+def test_refusals_of_routing_and_experts():
+    m = sw()
+    l = torch.randn(4, 64, device="cuda")
+    ids, f = m.route_experts(l, 4)
+    q, s, z = weights(6 * 32, 64, 32, True, BF16, 1)
+    E = m.W4Experts(q.view(6, 32, -1), s.view(6, 32, -1), z.view(6, 32, -1), group=32)
+    x = torch.randn(4, 64, device="cuda").to(BF16)
+    bad = [lambda: m.route_experts(l.cpu(), 4), lambda: m.route_experts(l.double(), 4), lambda: m.route_experts(l[0], 4), lambda: m.route_experts(l, 4, score="tanh"),
+           lambda: m.route_experts(l, 4, bias=l[0, :63]), lambda: m.route_experts(l, 4, bias=l[0].half()), lambda: m.route_experts(l, 4, out=(ids.long(), f)),
+           lambda: m.route_experts(l, 4, out=(ids, f[:, :3])), lambda: m.route_experts(l.t(), 4),
+           lambda: E(x, ids.long()), lambda: E(x, ids[0]), lambda: E(x[:3], ids), lambda: E(x[:, :63], ids), lambda: E(x, ids, weights=f[:, :3]), lambda: E(x, ids, weights=f.double()),
+           lambda: E(x, ids, f[:, 0]), lambda: E(x, ids, out=torch.empty(4, 32, device="cuda", dtype=BF16)), lambda: E(x, ids, weights=f, out=torch.empty(16, 32, device="cuda", dtype=BF16)),
+           lambda: E(x.float(), ids), lambda: E(x, ids.cpu()), lambda: m.W4Experts(q, s, z, group=32), lambda: m.W4Experts(q.view(6, 32, -1), s.view(3, 64, -1), None, group=32),
+           lambda: m.W4Experts(q.view(6, 32, -1).transpose(0, 1), s.view(6, 32, -1).transpose(0, 1), None, group=32)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("refusal %d" % i)
+    many, xs, ys = torch.zeros(100, 4, device="cuda", dtype=torch.int32), torch.zeros(100, 64, device="cuda", dtype=BF16), torch.zeros(400, 32, device="cuda", dtype=BF16)
+    for call in (lambda: m.route_experts(l, 65), lambda: m.route_experts(l, 33), lambda: m.route_experts(l, 4, groups=7), lambda: m.route_experts(l, 9, groups=8, top_groups=1),
+                 lambda: binding.strassen_w4_matmul(E.handle, 4, 0, x.data_ptr(), 64, 0, 0, l.data_ptr(), 32),
+                 lambda: binding.strassen_w4_experts(E.handle, 4, 33, ids.data_ptr(), 0, x.data_ptr(), 64, False, 0, 0, 0, l.data_ptr(), 32),
+                 lambda: binding.strassen_w4_experts(E.handle, 100, 4, many.data_ptr(), 0, xs.data_ptr(), 64, False, 0, 0, 0, ys.data_ptr(), 32)):
+        with pytest.raises(StrassenError) as e:
+            call()
+        assert e.value.status in (-1, -3)
