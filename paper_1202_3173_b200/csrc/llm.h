@@ -9,6 +9,35 @@
 
 namespace strassen {
 
+// Programmatic dependent launch: the kernels below may be placed on the GPU while the one before them in the stream drains, and let the one
+// behind them do the same; every CTA waits here, before its first access to memory, until the work before it is done and visible.
+__device__ __forceinline__ void after_work_before()
+{
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// Launches `kernel` so; cluster: CTAs of a cluster along x and y.
+template <class... Parameters, class... Arguments>
+cudaError_t launch_after(void (*kernel)(Parameters...), dim3 grid, dim3 block, size_t bytes, cudaStream_t stream, dim3 cluster, const Arguments &...arguments)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster.x;
+    attr[1].val.clusterDim.y = cluster.y;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster.x * cluster.y > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, arguments...);
+}
+
 constexpr float kE4M3Max = 448.f;                    // largest finite e4m3
 constexpr float kMinRowScale = 5.421010862427522e-20f;   // 2^-64: scale of a row of zeros; its reciprocal is finite
 
