@@ -518,7 +518,7 @@ int strassen_w4_experts(const strassen_w4 *w, int64_t tokens, int64_t top, const
                         size_t workspace_bytes, void *stream);
 
 /*
- * strassen_device_status -- wait for the current device and say whether a kernel of strassen_w4_matmul or strassen_w4_experts has given up since
+ * strassen_device_status -- wait for the current device and say whether one of the feed-forward operators' kernels has given up since
  * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
  * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else
  * STRASSEN_CUDA_ERROR, and the flag is cleared.

@@ -55,8 +55,9 @@ struct RowArgs {
     int64_t ldq;
     float *scale;
 };
-cudaError_t launch_rms_norm_quant(const RowArgs &a, cudaStream_t stream);
-cudaError_t launch_silu_mul_quant(const RowArgs &a, cudaStream_t stream);
+cudaError_t launch_rms_norm_quant(const RowArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t launch_silu_mul_quant(const RowArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t rows8_gave_up(int *flag);        // reads and clears the flag of a copy that did not come
 
 // ---- routing (route.cu) -------------------------------------------------------------------------------------------
 struct RouteArgs {

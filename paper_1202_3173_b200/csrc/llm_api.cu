@@ -120,7 +120,7 @@ extern "C" int strassen_rms_norm_quant(int64_t m, int64_t k, int type, const voi
         return fail(STRASSEN_ALIAS, "sum may take the place of x or of residual, but not overlap them otherwise");
     int sms = 0;
     if ((rc = current_device(&sms)) != STRASSEN_OK) return rc;
-    const cudaError_t e = launch_rms_norm_quant(a, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_rms_norm_quant(a, sms, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
 }
 
@@ -135,7 +135,7 @@ extern "C" int strassen_silu_mul_quant(int64_t m, int64_t k, int type, const voi
     if (!up) return fail(STRASSEN_INVALID_ARG, "up must be non-NULL");
     int sms = 0;
     if ((rc = current_device(&sms)) != STRASSEN_OK) return rc;
-    const cudaError_t e = launch_silu_mul_quant(a, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_silu_mul_quant(a, sms, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
 }
 
@@ -365,9 +365,10 @@ extern "C" int strassen_device_status(void)
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
     cudaError_t e = cudaDeviceSynchronize();
-    int flag = 0;
-    if (e == cudaSuccess) e = read_gave_up(&flag);
+    int tiles = 0, rows = 0;
+    if (e == cudaSuccess) e = read_gave_up(&tiles);
+    if (e == cudaSuccess) e = rows8_gave_up(&rows);
     if (e != cudaSuccess) return cuda_fail(e, "reading the device's status");
-    if (flag) return fail(STRASSEN_CUDA_ERROR, "a product gave up waiting for its own copies or tensor instructions; its results are not valid");
+    if (tiles || rows) return fail(STRASSEN_CUDA_ERROR, "a kernel gave up waiting for its own copies or tensor instructions; its results are not valid");
     return STRASSEN_OK;
 }

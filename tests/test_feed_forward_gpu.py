@@ -102,6 +102,32 @@ def test_norm_sum_in_place(k):
         check_rows(q, s, v)
 
 
+@pytest.mark.parametrize("pad,shift", [(0, 0), (7, 0), (1, 3), (8, 8)])
+@pytest.mark.parametrize("k", [1, 7, 31, 64, 100, 128, 200, 256, 300, 511, 777, 1024, 1025, 2049, 4096, 6001, 8192, 12345, 16383, 16384])
+def test_many_rows(k, pad, shift):
+    """Rows enough for CTAs that stay and copy ahead: each alignment, the first and last row of the matrix included, sums in place too."""
+    g = gen(k + pad)
+    for dtype in (BF16, F16, F32):
+        m = 700
+        x, r = (strided(torch.randn(m, k, device="cuda", generator=g).to(dtype), pad, shift) for _ in range(2))
+        w = (1 + 0.3 * torch.randn(k, device="cuda", generator=g)).to(dtype)
+        q, s = sw().quant_rows(m, k)
+        sw().rms_norm_quant(x, w, EPS, out=(q, s))
+        check_rows(q, s, norm64(x, w))
+        want, v = (x.float() + r.float()).to(dtype), norm64(x, w, r)
+        total = torch.empty(m, k, device="cuda", dtype=dtype)
+        sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, total))
+        check_rows(q, s, v)
+        assert torch.equal(total, want)
+        a, b = x.double(), r.double()
+        sw().silu_mul_quant(x, r, out=(q, s))
+        check_rows(q, s, a * torch.special.expit(a) * b)
+        sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, r))
+        check_rows(q, s, v)
+        assert torch.equal(r, want)
+    binding.strassen_device_status()
+
+
 def test_norm_rows_of_zeros_nan_and_infinity():
     for k in (96, 40000):
         x = torch.randn(6, k, device="cuda")
