@@ -131,7 +131,8 @@ template <class T, int W> __device__ __forceinline__ void store(const Words<T> &
 {
     constexpr int N = Words<T>::N;
     const int lane = threadIdx.x & (W - 1);
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + k), off = at & 15;        // off: the same in all lanes
+    const uint32_t row_lanes = W == 32 ? ~0u : ((1u << (W & 31)) - 1) << (threadIdx.x & 31 & ~(W - 1));     // other rows of the warp may take another way
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + k), off = at & 15;        // off: the same in all lanes of the row
     const bool full = k + 8 <= size;
     bool whole = !full;                                                             // to be written element by element
     if (off == 0) {
@@ -143,10 +144,10 @@ template <class T, int W> __device__ __forceinline__ void store(const Words<T> &
         // aligned words that end within this piece: the last `off` bytes of the lane below's, then this lane's own
         uint32_t b[N + 4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = __shfl_up_sync(~0u, p.w[N - 4 + i], 1, W);
+        for (int i = 0; i < 4; ++i) b[i] = __shfl_up_sync(row_lanes, p.w[N - 4 + i], 1, W);
 #pragma unroll
         for (int i = 0; i < N; ++i) b[i + 4] = p.w[i];
-        const bool above = __shfl_down_sync(~0u, int(full), 1, W) && lane < W - 1;   // the lane above writes this one's last bytes
+        const bool above = __shfl_down_sync(row_lanes, int(full), 1, W) && lane < W - 1;   // the lane above writes this one's last bytes
         const uint32_t up = 16 - uint32_t(off);                                     // how far the piece moves up from an aligned place
         if (up & 8) {
 #pragma unroll
@@ -206,24 +207,6 @@ template <class T, int W> __device__ __forceinline__ void store(const Words<T> &
     }
 }
 
-__device__ __forceinline__ void store_e4m3(uint8_t *row, int64_t k, int64_t size, const float (&v)[8])
-{
-    uint32_t w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i], v[4 * i + 1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
-        w[i] = lo | (hi << 16);
-    }
-    if (reinterpret_cast<uintptr_t>(row) % 8 == 0 && k + 8 <= size) {
-        *reinterpret_cast<uint2 *>(row + k) = make_uint2(w[0], w[1]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < size) row[k + i] = uint8_t(w[i / 4] >> (8 * (i & 3)));
-    }
-}
-
 // Sum and maximum over the CTA, the same bits in every thread (each adds the warps' values in the same order).
 __device__ __forceinline__ void reduce_row(float &sum, float &mx, float (*part)[32])
 {
@@ -256,30 +239,108 @@ template <class T> struct Range {
     __device__ Range(const void *p, int64_t m, int64_t k, int64_t ld) : lo(reinterpret_cast<uintptr_t>(p)), hi(lo + uintptr_t((m - 1) * ld + k) * sizeof(T)) {}
 };
 
-// The values of a piece before the row's factor: h w for the norm, silu(g) u for the gate, and what they add to the row's sum and maximum.
-// exp and the quotient are the fast forms: some 2^-21 of a value, against 2^-5 of its rounding to e4m3.
-template <int MODE> __device__ __forceinline__ void values(float (&x)[8], const float (&y)[8], const float (&w)[8], float (&v)[8], float &sq, float &mx)
+// Two f32 in a register pair: Blackwell adds and multiplies them in one instruction.
+struct Pair {
+    uint64_t v;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Pair operator+(Pair a, Pair b)
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (MODE == GATE) {
-            v[i] = __fdividef(x[i], 1.f + __expf(-x[i])) * y[i];
-        } else {
-            if (MODE == NORM_RESIDUAL) x[i] += y[i];
-            sq += x[i] * x[i];
-            v[i] = x[i] * w[i];
-        }
-        mx = max_nan(mx, fabsf(v[i]));
-    }
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b)
+{
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+__device__ __forceinline__ float max_abs(float m, Pair v)
+{
+    float a, b, d;
+    v.get(a, b);
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(a), "f"(b));
+    return d;
 }
 
-// The row's scale, and the factor that takes a value before the row's factor to the e4m3 range.
-template <int MODE> __device__ __forceinline__ float row_factor(float sq, float mx, int64_t k, float eps, float &scale)
+// A piece's values before the row's factor, v = h w for the norm, silu(g) u for the gate; what they add to the row's sum of squares and maximum; and
+// for a norm with a residual h itself, in its type.  exp and the reciprocal are the approximate instructions: some 2^-21 of a value, against 2^-5 of its
+// rounding to e4m3.
+template <class T, int MODE> __device__ __forceinline__ void values(const Words<T> &pa, const Words<T> &pb, const Words<T> &pw, Pair (&v)[4], Words<T> &sum, Pair &sq, float &mx)
 {
-    const float inv = MODE == GATE ? 1.f : 1.f / sqrtf(sq / float(k) + eps);
-    const float s = mx * inv / kE4M3Max;
+    float x[8], y[8], w[8];
+    unpack(pa, x);
+    if (MODE != NORM) unpack(pb, y);
+    if (MODE != GATE) unpack(pw, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        Pair h(x[2 * i], x[2 * i + 1]);
+        if (MODE == GATE) {
+            // one by one: the two special-function instructions of each decide, and pairs would have to be taken apart for them
+            float t[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) t[j] = __fdividef(x[2 * i + j], 1.f + __expf(-x[2 * i + j])) * y[2 * i + j];
+            v[i] = Pair(t[0], t[1]);
+        } else {
+            if (MODE == NORM_RESIDUAL) {
+                h = h + Pair(y[2 * i], y[2 * i + 1]);
+                h.get(x[2 * i], x[2 * i + 1]);
+            }
+            sq = fma(h, h, sq);
+            v[i] = h * Pair(w[2 * i], w[2 * i + 1]);
+        }
+        mx = max_abs(mx, v[i]);
+    }
+    if (MODE == NORM_RESIDUAL) pack(sum, x);
+}
+__device__ __forceinline__ float both(Pair v)
+{
+    float a, b;
+    v.get(a, b);
+    return a + b;
+}
+
+// The row's scale, and the factor that takes a value before the row's factor to the e4m3 range.  The quotients of two values and the root are the
+// approximate instructions here too, within two units of the last place.
+template <int MODE> __device__ __forceinline__ float row_factor(float sq, float mx, float over_k, float eps, float &scale)
+{
+    const float inv = MODE == GATE ? 1.f : rsqrtf(sq * over_k + eps);
+    const float s = mx * inv * (1.f / kE4M3Max);
     scale = s <= kMinRowScale ? kMinRowScale : s;        // NaN stays NaN
-    return inv / scale;
+    return __fdividef(inv, scale);
+}
+
+// v factor as e4m3; `wide`: rows of q start at multiples of 8 bytes.
+__device__ __forceinline__ void store_e4m3(uint8_t *row, int64_t k, int64_t size, const Pair (&v)[4], float factor, bool wide)
+{
+    uint32_t w[2];
+    const Pair f(factor, factor);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float a, b, c, d;
+        (v[2 * i] * f).get(a, b);
+        (v[2 * i + 1] * f).get(c, d);
+        uint16_t lo, hi;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+        asm("mov.b32 %0, {%1, %2};" : "=r"(w[i]) : "h"(lo), "h"(hi));
+    }
+    if (wide && k + 8 <= size) {
+        *reinterpret_cast<uint2 *>(row + k) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < size) row[k + i] = uint8_t(w[i / 4] >> (8 * (i & 3)));
+    }
 }
 
 // One CTA per row, the row in registers: ITEMS pieces a thread, their loads all under way before the first is used.
@@ -303,34 +364,25 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
             for (int j = 0; j < Words<T>::N; ++j) pa[i].w[j] = pb[i].w[j] = pw[i].w[j] = 0;
         }
     }
-    // kept until the row's factor is known: h of a norm, v of a gate (the norm's weights stay as they came)
-    float kept[ITEMS][8];
-    float sq = 0.f, mx = 0.f;
+    // v is kept until the row's factor is known; the sum goes out at once: what a thread, or the lane beside it, writes over has been read
+    Pair v[ITEMS][4], squares(0.f, 0.f);
+    float mx = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        float y[8], f[8], v[8];
-        unpack(pa[i], kept[i]);
-        if (MODE != NORM) unpack(pb[i], y);
-        if (MODE != GATE) unpack(pw[i], f);
-        values<MODE>(kept[i], y, f, v, sq, mx);
-        if (MODE == GATE) memcpy(kept[i], v, sizeof(v));
+        Words<T> sum;
+        values<T, MODE>(pa[i], pb[i], pw[i], v[i], sum, squares, mx);
+        if (MODE == NORM_RESIDUAL) store<T, 32>(sum, static_cast<T *>(p.sum) + r * p.lds, (i * int64_t(blockDim.x) + threadIdx.x) * 8, p.k);
     }
+    float sq = both(squares);
     reduce_row(sq, mx, part);
     float scale;
-    const float factor = row_factor<MODE>(sq, mx, p.k, p.eps, scale);
+    const float factor = row_factor<MODE>(sq, mx, 1.f / float(p.k), p.eps, scale);
+    uint8_t *const q = p.q + r * p.ldq;
+    const bool wide = reinterpret_cast<uintptr_t>(q) % 8 == 0;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int64_t c = (i * int64_t(blockDim.x) + threadIdx.x) * 8;
-        if (MODE == NORM_RESIDUAL) {
-            Words<T> ps;
-            pack(ps, kept[i]);
-            store<T, 32>(ps, static_cast<T *>(p.sum) + r * p.lds, c, p.k);
-        }
-        float f[8], v[8];
-        if (MODE != GATE) unpack(pw[i], f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = kept[i][j] * (MODE == GATE ? factor : f[j] * factor);
-        if (c < p.k) store_e4m3(p.q + r * p.ldq, c, p.k, v);
+        if (c < p.k) store_e4m3(q, c, p.k, v[i], factor, wide);
     }
     if (threadIdx.x == 0) p.scale[r] = scale;
 }
@@ -355,70 +407,91 @@ __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity)
     return false;
 }
 
-// The 16-byte words that a row lies in, and whether they are all memory of the matrix.
-template <class T> struct Window {
-    uintptr_t from;
-    uint32_t bytes, off;
-    bool inside;
-    __device__ __forceinline__ Window(const T *row, int64_t k, const Range<T> &range)
-    {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(row), end = (at + uintptr_t(k) * sizeof(T) + 15) & ~uintptr_t(15);
-        off = uint32_t(at & 15);
-        from = at - off;
-        bytes = uint32_t(end - from);
-        inside = from >= range.lo && end <= range.hi;
+// 8 elements at `at` in shared memory, `off` bytes past a multiple of 16 (the same for all pieces of a row); what lies around them may be read.
+template <class T> __device__ __forceinline__ void load_shared(Words<T> &p, const uint8_t *at, uint32_t off)
+{
+    constexpr int N = Words<T>::N;
+    if (off == 0) {
+        load_words<N>(p.w, at);
+    } else {
+        uint32_t a[N + 4];
+        load_words<N + 4>(a, at - off);
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < N + 2; ++i) a[i] = a[i + 2];
+        }
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < N + 1; ++i) a[i] = a[i + 1];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.w[i] = __funnelshift_r(a[i], a[i + 1], 8 * (off & 3));
     }
-};
+}
+// Zeros in the place of the elements from `count` on.
+template <class T> __device__ __forceinline__ void cut(Words<T> &p, int count)
+{
+    constexpr int N = Words<T>::N, PER = 8 / N;              // elements of a word
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i * PER >= count) p.w[i] = 0;
+        else if (PER == 2 && i * PER + 1 == count) p.w[i] &= 0xffffu;
+    }
+}
 
 template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) stream_kernel(const RowArgs p, int slots, int slot_bytes)
 {
     extern __shared__ __align__(16) uint8_t memory[];            // the weights of a norm, then the ring
+    constexpr bool TWO = MODE != NORM;                           // two inputs
     uint8_t *const ring = memory + (MODE == GATE ? 0 : int(blockDim.x) * ITEMS * 8 * int(sizeof(T)));
-    __shared__ float part[2][32];
+    __shared__ float2 part[2][THREADS / 32];
     __shared__ uint64_t full[MOST_SLOTS];
+    __shared__ int dead;
     if (threadIdx.x == 0) {
         for (int i = 0; i < slots; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&full[i])));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        dead = 0;
     }
     after_work_before();
     __syncthreads();
-    const int k = int(p.k);
-    const Range<T> range_a(p.a, p.m, p.k, p.lda), range_b(p.b, p.m, p.k, p.ldb), range_w(p.weight, 1, p.k, p.k);
-    const auto row_a = [&](int64_t r) { return static_cast<const T *>(p.a) + r * p.lda; };
-    const auto row_b = [&](int64_t r) { return static_cast<const T *>(p.b) + r * p.ldb; };
-    const auto copied = [&](int64_t r) { return Window<T>(row_a(r), k, range_a).inside && (MODE == NORM || Window<T>(row_b(r), k, range_b).inside); };
-    const int half = MODE == NORM ? slot_bytes : slot_bytes / 2;
-    const auto fetch = [&](int64_t r, int slot) {                // by thread 0
-        if (r >= p.m || !copied(r)) return;
-        const Window<T> a(row_a(r), k, range_a);
+    const int k = int(p.k), rows = int(p.m), step = int(gridDim.x);
+    const uint32_t row_bytes = uint32_t(k) * uint32_t(sizeof(T));
+    const uintptr_t base_a = reinterpret_cast<uintptr_t>(p.a), base_b = reinterpret_cast<uintptr_t>(p.b);
+    const uintptr_t ld_a = uintptr_t(p.lda) * sizeof(T), ld_b = uintptr_t(p.ldb) * sizeof(T);
+    const int half = TWO ? slot_bytes / 2 : slot_bytes;
+    // the 16-byte words of a row: those of the first row may begin before the matrix, those of the last end after it
+    const auto copied = [&](int r) {
+        bool in = r > 0 || (((base_a | (TWO ? base_b : 0)) & 15) == 0);
+        if (r == rows - 1) in = in && ((base_a + r * ld_a + row_bytes) & 15) == 0 && (!TWO || ((base_b + r * ld_b + row_bytes) & 15) == 0);
+        return in;
+    };
+    const auto fetch = [&](int r, int slot) {                    // by one thread
+        if (r >= rows || !copied(r)) return;
         const uint32_t bar = smem_addr(&full[slot]), to = smem_addr(ring + slot * slot_bytes);
-        uint32_t bytes = a.bytes;
-        if (MODE != NORM) bytes += Window<T>(row_b(r), k, range_b).bytes;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(a.from), "r"(a.bytes), "r"(bar) : "memory");
-        if (MODE != NORM) {
-            const Window<T> b(row_b(r), k, range_b);
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + half), "l"(b.from), "r"(b.bytes), "r"(bar) : "memory");
-        }
+        const uintptr_t a = base_a + r * ld_a, b = base_b + r * ld_b;
+        const uint32_t bytes_a = (uint32_t(a & 15) + row_bytes + 15) & ~15u, bytes_b = TWO ? (uint32_t(b & 15) + row_bytes + 15) & ~15u : 0;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes_a + bytes_b) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(a & ~uintptr_t(15)), "r"(bytes_a), "r"(bar) : "memory");
+        if (TWO)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + half), "l"(b & ~uintptr_t(15)), "r"(bytes_b), "r"(bar) : "memory");
     };
     if (threadIdx.x == 0)
-        for (int i = 0; i < slots; ++i) fetch(blockIdx.x + int64_t(i) * gridDim.x, i);
+        for (int i = 0; i < slots; ++i) fetch(int(blockIdx.x) + i * step, i);
     // weights: each thread's own pieces, 16 bytes of all threads side by side
     constexpr int N16 = Words<T>::N / 4;
-    uint4 *const weights = reinterpret_cast<uint4 *>(memory);
-    const auto weight = [&](int i, float (&f)[8]) {
-        Words<T> w;
+    uint4 *const weights = reinterpret_cast<uint4 *>(memory) + threadIdx.x;
+    const auto weight = [&](int i, Words<T> &w) {
 #pragma unroll
         for (int j = 0; j < N16; ++j) {
-            const uint4 u = weights[(i * N16 + j) * int(blockDim.x) + int(threadIdx.x)];
+            const uint4 u = weights[(i * N16 + j) * int(blockDim.x)];
             w.w[4 * j] = u.x;
             w.w[4 * j + 1] = u.y;
             w.w[4 * j + 2] = u.z;
             w.w[4 * j + 3] = u.w;
         }
-        unpack(w, f);
     };
     if (MODE != GATE) {
+        const Range<T> range_w(p.weight, 1, p.k, p.k);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
@@ -426,78 +499,94 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
             memset(&w, 0, sizeof(w));
             if (c < k) load(w, static_cast<const T *>(p.weight), c, k, range_w.lo, range_w.hi);
 #pragma unroll
-            for (int j = 0; j < N16; ++j) weights[(i * N16 + j) * int(blockDim.x) + int(threadIdx.x)] = make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]);
+            for (int j = 0; j < N16; ++j) weights[(i * N16 + j) * int(blockDim.x)] = make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]);
         }
     }
-    int slot = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const float over_k = 1.f / float(k);
+    int slot = 0, turn = 0;
     uint32_t phases = 0;                                         // of each slot's barrier
-    bool alive = true;
-    for (int64_t r = blockIdx.x; r < p.m && alive; r += gridDim.x) {
+    for (int r = blockIdx.x; r < rows; r += step) {
         Words<T> pa[ITEMS], pb[ITEMS];
-        const T *a = row_a(r), *b = row_b(r);
-        uintptr_t lo_a = range_a.lo, hi_a = range_a.hi, lo_b = range_b.lo, hi_b = range_b.hi;
         if (copied(r)) {
-            alive = wait_for(&full[slot], phases >> slot & 1);
+            if (!wait_for(&full[slot], phases >> slot & 1)) dead = 1;
             phases ^= 1u << slot;
-            // the row's place in the ring, in which wider accesses stay inside what was copied and its margin
-            uint8_t *const at = ring + slot * slot_bytes;
-            a = reinterpret_cast<const T *>(at + (reinterpret_cast<uintptr_t>(a) & 15));
-            lo_a = reinterpret_cast<uintptr_t>(at);
-            hi_a = lo_a + half;
-            b = reinterpret_cast<const T *>(at + half + (reinterpret_cast<uintptr_t>(b) & 15));
-            lo_b = lo_a + half;
-            hi_b = lo_b + half;
-        }
+            const uint32_t off_a = uint32_t(base_a + r * ld_a) & 15, off_b = uint32_t(base_b + r * ld_b) & 15;
+            const uint8_t *const at = ring + slot * slot_bytes;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
-            if (c < k) {
-                load(pa[i], a, c, k, lo_a, hi_a);
-                if (MODE != NORM) load(pb[i], b, c, k, lo_b, hi_b);
-            } else {
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
+                if (c < k) {
+                    load_shared(pa[i], at + off_a + c * int(sizeof(T)), off_a);
+                    if (TWO) load_shared(pb[i], at + half + off_b + c * int(sizeof(T)), off_b);
+                    if (c + 8 > k) {
+                        cut(pa[i], k - c);
+                        if (TWO) cut(pb[i], k - c);
+                    }
+                } else {
+                    memset(&pa[i], 0, sizeof(pa[i]));
+                    memset(&pb[i], 0, sizeof(pb[i]));
+                }
+            }
+        } else {
+            const Range<T> range_a(p.a, p.m, p.k, p.lda), range_b(p.b, p.m, p.k, p.ldb);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
                 memset(&pa[i], 0, sizeof(pa[i]));
                 memset(&pb[i], 0, sizeof(pb[i]));
+                if (c < k) {
+                    load(pa[i], reinterpret_cast<const T *>(base_a + r * ld_a), c, k, range_a.lo, range_a.hi);
+                    if (TWO) load(pb[i], reinterpret_cast<const T *>(base_b + r * ld_b), c, k, range_b.lo, range_b.hi);
+                }
             }
         }
-        alive = __syncthreads_and(alive);
-        if (!alive) break;
-        if (threadIdx.x == 0) fetch(r + int64_t(slots) * gridDim.x, slot);
-        slot = slot + 1 == slots ? 0 : slot + 1;
-        float kept[ITEMS][8];
-        float sq = 0.f, mx = 0.f;
+        // the sum goes out at once: its row is in shared memory, or in the registers of the threads beside it, whatever it is written over
+        Pair v[ITEMS][4], squares(0.f, 0.f);
+        float mx = 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            float y[8], f[8], v[8];
-            unpack(pa[i], kept[i]);
-            if (MODE != NORM) unpack(pb[i], y);
-            if (MODE != GATE) weight(i, f);
-            values<MODE>(kept[i], y, f, v, sq, mx);
-            if (MODE == GATE) memcpy(kept[i], v, sizeof(v));
+            Words<T> w, sum;
+            if (MODE != GATE) weight(i, w);
+            values<T, MODE>(pa[i], pb[i], w, v[i], sum, squares, mx);
+            if (MODE == NORM_RESIDUAL) store<T, 32>(sum, static_cast<T *>(p.sum) + r * p.lds, (i * int(blockDim.x) + int(threadIdx.x)) * 8, k);
         }
-        reduce_row(sq, mx, part);
+        float sq = both(squares);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            if (MODE != GATE) sq += __shfl_xor_sync(~0u, sq, o);
+            mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
+        }
+        if (lane == 0) part[turn][warp] = make_float2(sq, mx);
+        __syncthreads();
+        // every thread has its part of the row: its place is free
+        if (dead) break;
+        if (threadIdx.x == 0) fetch(r + slots * step, slot);
+        slot = slot + 1 == slots ? 0 : slot + 1;
+        sq = mx = 0.f;
+        for (int w = 0; w < warps; ++w) {
+            const float2 v = part[turn][w];
+            sq += v.x;
+            mx = max_nan(mx, v.y);
+        }
+        turn ^= 1;
         float scale;
-        const float factor = row_factor<MODE>(sq, mx, p.k, p.eps, scale);
+        const float factor = row_factor<MODE>(sq, mx, over_k, p.eps, scale);
+        uint8_t *const q = p.q + r * p.ldq;
+        const bool wide = reinterpret_cast<uintptr_t>(q) % 8 == 0;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
-            if (MODE == NORM_RESIDUAL) {
-                Words<T> ps;
-                pack(ps, kept[i]);
-                store<T, 32>(ps, static_cast<T *>(p.sum) + r * p.lds, c, k);
-            }
-            float f[8], v[8];
-            if (MODE != GATE) weight(i, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = kept[i][j] * (MODE == GATE ? factor : f[j] * factor);
-            if (c < k) store_e4m3(p.q + r * p.ldq, c, k, v);
+            if (c < k) store_e4m3(q, c, k, v[i], factor, wide);
         }
         if (threadIdx.x == 0) p.scale[r] = scale;
     }
     // given up: the copies that are under way end before the CTA does
-    if (!alive)
+    if (dead)
         for (int i = 0; i < 10000; ++i) __nanosleep(100);
 }
 
+// cudaErrorNotSupported, with nothing launched, where not one row fits the CTA's shared memory.
 template <class T, int MODE, int ITEMS, int THREADS> cudaError_t launch_stream(const RowArgs &p, int sm_count, cudaStream_t stream)
 {
     static std::atomic<uint64_t> opted_in{0};                // devices that this kernel has been given its shared memory on
@@ -514,6 +603,7 @@ template <class T, int MODE, int ITEMS, int THREADS> cudaError_t launch_stream(c
     const int half = int((p.k * int64_t(sizeof(T)) + 15) / 16 * 16 + 48);        // the words it lies in, and what a piece's window may read beyond
     const int slot_bytes = MODE == NORM ? half : 2 * half;
     int slots = (most - weights) / slot_bytes;
+    if (slots < 1) return cudaErrorNotSupported;
     if (slots > MOST_SLOTS) slots = MOST_SLOTS;
     const int ctas = 1024 / THREADS * sm_count;
     return launch_after(stream_kernel<T, MODE, ITEMS, THREADS>, dim3(unsigned(p.m < ctas ? p.m : ctas)), dim3(unsigned(threads)), size_t(weights + slots * slot_bytes), stream, dim3(1, 1), p, slots, slot_bytes);
@@ -542,37 +632,28 @@ template <class T, int MODE, int W, int ITEMS> __global__ void __launch_bounds__
             for (int j = 0; j < Words<T>::N; ++j) pa[i].w[j] = pb[i].w[j] = pw[i].w[j] = 0;
         }
     }
-    float kept[ITEMS][8];
-    float sq = 0.f, mx = 0.f;
+    Pair v[ITEMS][4], squares(0.f, 0.f);
+    float mx = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        float y[8], f[8], v[8];
-        unpack(pa[i], kept[i]);
-        if (MODE != NORM) unpack(pb[i], y);
-        if (MODE != GATE) unpack(pw[i], f);
-        values<MODE>(kept[i], y, f, v, sq, mx);
-        if (MODE == GATE) memcpy(kept[i], v, sizeof(v));
+        Words<T> sum;
+        values<T, MODE>(pa[i], pb[i], pw[i], v[i], sum, squares, mx);
+        if (MODE == NORM_RESIDUAL) store<T, W>(sum, static_cast<T *>(p.sum) + r * p.lds, (i * W + lane) * 8, size);
     }
+    float sq = both(squares);
 #pragma unroll
     for (int o = W / 2; o > 0; o >>= 1) {
         sq += __shfl_xor_sync(~0u, sq, o);
         mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
     }
     float scale;
-    const float factor = row_factor<MODE>(sq, mx, p.k, p.eps, scale);
+    const float factor = row_factor<MODE>(sq, mx, 1.f / float(p.k), p.eps, scale);
+    uint8_t *const q = p.q + r * p.ldq;
+    const bool wide = reinterpret_cast<uintptr_t>(q) % 8 == 0;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int64_t c = (i * W + lane) * 8;
-        if (MODE == NORM_RESIDUAL) {
-            Words<T> ps;
-            pack(ps, kept[i]);
-            store<T, W>(ps, static_cast<T *>(p.sum) + r * p.lds, c, size);
-        }
-        float f[8], v[8];
-        if (MODE != GATE) unpack(pw[i], f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = kept[i][j] * (MODE == GATE ? factor : f[j] * factor);
-        if (c < size) store_e4m3(p.q + r * p.ldq, c, size, v);
+        if (c < size) store_e4m3(q, c, size, v[i], factor, wide);
     }
     if (lane == 0 && on) p.scale[r] = scale;
 }
@@ -592,39 +673,31 @@ template <class T, int MODE> __global__ void __launch_bounds__(1024) long_row_ke
     const T *const a = static_cast<const T *>(p.a) + r * p.lda, *const b = static_cast<const T *>(p.b) + r * p.ldb, *const w = static_cast<const T *>(p.weight);
     const Range<T> range_a(p.a, p.m, p.k, p.lda), range_b(p.b, p.m, p.k, p.ldb), range_w(p.weight, 1, p.k, p.k);
     float sq = 0.f, mx = 0.f, scale = 0.f, factor = 0.f;
+    uint8_t *const q = p.q + r * p.ldq;
+    const bool wide = reinterpret_cast<uintptr_t>(q) % 8 == 0;
     for (int pass = 0; pass < 2; ++pass) {
+        Pair squares(0.f, 0.f);
         for (int64_t c0 = 0; c0 < p.k; c0 += int64_t(blockDim.x) * 8) {
             const int64_t c = c0 + int64_t(threadIdx.x) * 8;
-            float x[8] = {}, y[8] = {}, f[8] = {}, v[8];
+            Words<T> pa, pb, pw, sum;
+            memset(&pa, 0, sizeof(pa));
+            memset(&pb, 0, sizeof(pb));
+            memset(&pw, 0, sizeof(pw));
             if (c < p.k) {
-                Words<T> t;
-                load(t, a, c, p.k, range_a.lo, range_a.hi);
-                unpack(t, x);
-                if (MODE != NORM) {
-                    load(t, b, c, p.k, range_b.lo, range_b.hi);
-                    unpack(t, y);
-                }
-                if (MODE != GATE) {
-                    load(t, w, c, p.k, range_w.lo, range_w.hi);
-                    unpack(t, f);
-                }
+                load(pa, a, c, p.k, range_a.lo, range_a.hi);
+                if (MODE != NORM) load(pb, b, c, p.k, range_b.lo, range_b.hi);
+                if (MODE != GATE) load(pw, w, c, p.k, range_w.lo, range_w.hi);
             }
-            values<MODE>(x, y, f, v, sq, mx);
+            Pair v[4];
+            values<T, MODE>(pa, pb, pw, v, sum, squares, mx);
             if (pass == 0) continue;
-            if (MODE == NORM_RESIDUAL) {
-                // a piece of a misaligned row is read with its neighbours' bytes: all reads of these pieces come before the writes
-                __syncthreads();
-                Words<T> t;
-                pack(t, x);
-                store<T, 32>(t, static_cast<T *>(p.sum) + r * p.lds, c, p.k);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= factor;
-            if (c < p.k) store_e4m3(p.q + r * p.ldq, c, p.k, v);
+            if (MODE == NORM_RESIDUAL) store<T, 32>(sum, static_cast<T *>(p.sum) + r * p.lds, c, p.k);
+            if (c < p.k) store_e4m3(q, c, p.k, v, factor, wide);
         }
         if (pass == 0) {
+            sq = both(squares);
             reduce_row(sq, mx, part);
-            factor = row_factor<MODE>(sq, mx, p.k, p.eps, scale);
+            factor = row_factor<MODE>(sq, mx, 1.f / float(p.k), p.eps, scale);
         }
     }
     if (threadIdx.x == 0) p.scale[r] = scale;
@@ -644,10 +717,13 @@ template <class T, int MODE> cudaError_t launch_type(const RowArgs &p, int sm_co
     }
     // Rows enough for CTAs that stay.  Two pieces a thread, so that an SM has several rows at a time in different steps, four where a row would
     // need more than half of its threads.
-    if (p.m >= 4 * sm_count && pieces > 128 && pieces <= 2048 && p.k * int64_t(sizeof(T)) <= 32 * 1024) {
-        if (pieces <= 512) return launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
-        if (pieces <= 1024) return launch_stream<T, MODE, 2, 512>(p, sm_count, stream);
-        return launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
+    if (p.m >= 4 * sm_count && pieces > 128 && pieces <= 2048) {
+        cudaError_t e = cudaErrorNotSupported;
+        if (pieces <= 256) e = launch_stream<T, MODE, 2, 128>(p, sm_count, stream);
+        else if (pieces <= 512) e = launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
+        else if (pieces <= 1024) e = launch_stream<T, MODE, 2, 512>(p, sm_count, stream);
+        else e = launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
+        if (e != cudaErrorNotSupported) return e;
     }
     const dim3 grid(unsigned(p.m));
     const auto threads = [&](int items) { return dim3(unsigned((pieces + 32 * items - 1) / (32 * items) * 32)); };
