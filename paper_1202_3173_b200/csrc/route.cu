@@ -52,6 +52,7 @@ template <class T, int V> __global__ void __launch_bounds__(WARPS * 32) route_ke
     extern __shared__ float keys_of[];           // groups only: the keys of each warp's token
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t token = int64_t(blockIdx.x) * WARPS + warp;
+    after_work_before();
     if (token >= p.tokens) return;
     const T *logits = static_cast<const T *>(p.logits) + token * p.ld;
     float score[V], key[V];
@@ -168,8 +169,7 @@ template <class T, int V> __global__ void __launch_bounds__(WARPS * 32) route_ke
 template <class T, int V> cudaError_t launch_as(const RouteArgs &p, cudaStream_t stream)
 {
     const size_t bytes = p.groups > 1 ? size_t(WARPS) * p.experts * sizeof(float) : 0;
-    route_kernel<T, V><<<unsigned((p.tokens + WARPS - 1) / WARPS), WARPS * 32, bytes, stream>>>(p);
-    return cudaGetLastError();
+    return launch_after(route_kernel<T, V>, dim3(unsigned((p.tokens + WARPS - 1) / WARPS)), dim3(WARPS * 32), bytes, stream, dim3(1, 1), p);
 }
 
 template <class T> cudaError_t launch_type(const RouteArgs &p, cudaStream_t stream)

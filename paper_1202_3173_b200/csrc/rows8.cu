@@ -20,6 +20,7 @@
 #include <atomic>
 
 #include "llm.h"
+#include "pieces.cuh"
 #include "strassen_b200.h"
 
 namespace strassen {
@@ -32,12 +33,6 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-
-// A piece of 8 elements in 32-bit words, as they lie in memory.
-template <class T> struct Words {
-    static constexpr int N = 8 * int(sizeof(T)) / 4;
-    uint32_t w[N];
-};
 
 __device__ __forceinline__ void unpack(const Words<float> &p, float (&v)[8])
 {
@@ -75,51 +70,6 @@ __device__ __forceinline__ void pack(Words<__half> &p, const float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-}
-
-template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void *at)
-{
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const uint4 u = static_cast<const uint4 *>(at)[i];
-        w[4 * i] = u.x;
-        w[4 * i + 1] = u.y;
-        w[4 * i + 2] = u.z;
-        w[4 * i + 3] = u.w;
-    }
-}
-
-// Elements k .. k + 7 of a row of `size`; zeros past its end.  lo, hi: the memory of the whole matrix, which wider accesses do not leave.
-template <class T> __device__ __forceinline__ void load(Words<T> &p, const T *row, int64_t k, int64_t size, uintptr_t lo, uintptr_t hi)
-{
-    constexpr int N = Words<T>::N;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + k), off = at & 15, from = at - off;
-    if (k + 8 <= size && off == 0) {
-        load_words<N>(p.w, reinterpret_cast<const void *>(at));
-    } else if (k + 8 <= size && from >= lo && from + 4 * N + 16 <= hi) {
-        // the aligned words around the piece, moved down by `off` bytes
-        uint32_t a[N + 4];
-        load_words<N + 4>(a, reinterpret_cast<const void *>(from));
-        if (off & 8) {
-#pragma unroll
-            for (int i = 0; i < N + 2; ++i) a[i] = a[i + 2];
-        }
-        if (off & 4) {
-#pragma unroll
-            for (int i = 0; i < N + 1; ++i) a[i] = a[i + 1];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) p.w[i] = __funnelshift_r(a[i], a[i + 1], 8 * (off & 3));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) p.w[i] = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < size) {
-                if (sizeof(T) == 4) p.w[i] = reinterpret_cast<const uint32_t *>(row)[k + i];
-                else p.w[i / 2] |= uint32_t(reinterpret_cast<const uint16_t *>(row)[k + i]) << (16 * (i & 1));
-            }
-    }
 }
 
 // The 32 bits that start `bytes` (0..3 of them into w[0]) into two words.
@@ -233,11 +183,6 @@ __device__ __forceinline__ void reduce_row(float &sum, float &mx, float (*part)[
 }
 
 enum { GATE = 0, NORM = 1, NORM_RESIDUAL = 2 };
-
-template <class T> struct Range {
-    uintptr_t lo, hi;
-    __device__ Range(const void *p, int64_t m, int64_t k, int64_t ld) : lo(reinterpret_cast<uintptr_t>(p)), hi(lo + uintptr_t((m - 1) * ld + k) * sizeof(T)) {}
-};
 
 // Two f32 in a register pair: Blackwell adds and multiplies them in one instruction.
 struct Pair {

@@ -34,6 +34,7 @@
 #include <atomic>
 
 #include "llm.h"
+#include "pieces.cuh"
 #include "strassen_b200.h"
 
 namespace strassen {
@@ -314,6 +315,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
     const int depth = (MODE == SPLIT ? int(p.depth_tiles * (blockIdx.y + 1) / splits) : int(p.depth_tiles)) - kb0;
     const int columns = (p.row_tiles + CTAS - 1) / CTAS;                      // tiles of results side by side
 
+    after_work_before();
     // tiles of results: those of one run of rows of x side by side, so that its CTAs share the rows in L2
     const int runs = MODE == EXPERTS ? *p.table_size : (p.m + p.tokens - 1) / p.tokens;
     const int first = int(blockIdx.x) / CTAS, stride = int(gridDim.x) / CTAS, tile_count = columns * runs;
@@ -643,7 +645,8 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
 struct RowsArgs {
     const char *x;
     int64_t ldx_bytes, rows, k, width;
-    bool e4m3, wide;         // wide: rows of x allow 16-byte (e4m3: 8-byte) accesses
+    bool e4m3;
+    uintptr_t x_end;         // of the memory of x
     uint16_t *out;
     // experts: the pair of each row in order, pairs per row of x; the pairs' ids, to write zeros to the results of those without an expert
     const int *order, *count, *ids;
@@ -654,42 +657,26 @@ struct RowsArgs {
 
 __global__ void __launch_bounds__(256) rows_kernel(const RowsArgs p)
 {
+    after_work_before();
     const int64_t chunks = p.width / 8, total = (p.count ? int64_t(*p.count) : p.rows) * chunks, step = int64_t(gridDim.x) * blockDim.x;
     const int64_t me = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p.x);
     for (int64_t e = me; e < total; e += step) {
         const int64_t i = e / chunks, c = (e - i * chunks) * 8;
         const int64_t row = p.order ? p.order[i] / p.per_row : i;
-        uint32_t v[4] = {0, 0, 0, 0};
+        uint32_t v[4];
         if (p.e4m3) {
-            const uint8_t *x = reinterpret_cast<const uint8_t *>(p.x + row * p.ldx_bytes) + c;
-            uint32_t w[2] = {0, 0};
-            if (p.wide && c + 8 <= p.k) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(x);
-                w[0] = u.x;
-                w[1] = u.y;
-            } else {
-#pragma unroll
-                for (int b = 0; b < 8; ++b)
-                    if (c + b < p.k) w[b >> 2] |= uint32_t(x[b]) << (8 * (b & 3));
-            }
+            const uint2 u = load_bytes8(reinterpret_cast<const uint8_t *>(p.x + row * p.ldx_bytes), c, p.k, lo, p.x_end);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(w[b >> 1] >> (16 * (b & 1))), __NV_E4M3);
+                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t((b < 2 ? u.x : u.y) >> (16 * (b & 1))), __NV_E4M3);
                 v[b] = uint32_t(h.x) | (uint32_t(h.y) << 16);
             }
         } else {
-            const uint16_t *x = reinterpret_cast<const uint16_t *>(p.x + row * p.ldx_bytes) + c;
-            if (p.wide && c + 8 <= p.k) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(x);
-                v[0] = u.x;
-                v[1] = u.y;
-                v[2] = u.z;
-                v[3] = u.w;
-            } else {
+            Words<__half> w;
+            load(w, reinterpret_cast<const __half *>(p.x + row * p.ldx_bytes), c, p.k, lo, p.x_end);
 #pragma unroll
-                for (int b = 0; b < 8; ++b)
-                    if (c + b < p.k) v[b >> 1] |= uint32_t(x[b]) << (16 * (b & 1));
-            }
+            for (int b = 0; b < 4; ++b) v[b] = w.w[b];
         }
         *reinterpret_cast<uint4 *>(p.out + i * p.width + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
@@ -706,6 +693,7 @@ __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, 
     __shared__ int counts[kMostExperts], part[2][32];
     __shared__ int start, tiles;
     const int e = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    after_work_before();
     for (int i = threadIdx.x; i < experts; i += blockDim.x) counts[i] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
@@ -772,6 +760,7 @@ __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, 
 // out_t = sum_j weights_tj part_tj, in the order of j; pairs without an expert add nothing.
 __global__ void __launch_bounds__(256) weighted_sum_kernel(const float *part, const int *ids, const float *weights, int64_t tokens, int top, int experts, int64_t n, int64_t width, void *out, int64_t ldo, bool bf16)
 {
+    after_work_before();
     const int64_t chunks = width / 4, total = tokens * chunks;
     for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
         const int64_t t = e / chunks, c = (e - t * chunks) * 4;
@@ -810,19 +799,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> cudaError_t launch_one(cons
         if (e != cudaSuccess) return e;
         opted_in.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(shape.columns * CTAS), unsigned(shape.splits));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = size_t(shape.bytes);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CTAS;
-    attr[0].val.clusterDim.y = unsigned(shape.splits);
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, p, map);
+    return launch_after(w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, dim3(unsigned(shape.columns * CTAS), unsigned(shape.splits)), dim3(THREADS), size_t(shape.bytes), stream, dim3(CTAS, unsigned(shape.splits)), p, map);
 }
 
 template <bool BF16, bool ZEROS> cudaError_t launch_shape(const Args &p, const CUtensorMap &map, const Shape &s, cudaStream_t stream)
@@ -889,7 +866,7 @@ RowsArgs rows_args(const W4Args &a, void *to)
     r.k = a.lay.k;
     r.width = (a.lay.k + 7) / 8 * 8;
     r.e4m3 = a.type == STRASSEN_E4M3;
-    r.wide = (reinterpret_cast<uintptr_t>(a.x) | uintptr_t(r.ldx_bytes)) % (8 * size) == 0;
+    r.x_end = reinterpret_cast<uintptr_t>(a.x) + uintptr_t(((a.ids && a.each ? a.m * a.top : a.m) - 1) * r.ldx_bytes + a.lay.k * size);
     r.out = static_cast<uint16_t *>(to);
     r.per_row = 1;
     return r;
@@ -898,8 +875,7 @@ RowsArgs rows_args(const W4Args &a, void *to)
 cudaError_t launch_rows(const RowsArgs &r, int sm_count, cudaStream_t stream)
 {
     const int64_t blocks = (r.rows * (r.width / 8) + 255) / 256, most = int64_t(sm_count) * 32;
-    rows_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(r);
-    return cudaGetLastError();
+    return launch_after(rows_kernel, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, stream, dim3(1, 1), r);
 }
 
 // What does not depend on how the rows of x are cut into tiles.
@@ -1015,8 +991,7 @@ cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t 
     int *const order = reinterpret_cast<int *>(ws), *const count = reinterpret_cast<int *>(ws + s.count_off);
     W4Tile *const table = reinterpret_cast<W4Tile *>(ws + s.table_off);
     const int experts = int(a.lay.experts);
-    order_kernel<<<unsigned(experts), 1024, 0, stream>>>(a.ids, int(s.pairs), experts, TOKENS, order, count, count + 1, table);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = launch_after(order_kernel, dim3(unsigned(experts)), dim3(1024), 0, stream, dim3(1, 1), a.ids, int(s.pairs), experts, TOKENS, order, count, count + 1, table);
     if (e != cudaSuccess) return e;
 
     RowsArgs r = rows_args(a, ws + s.rows_off);
@@ -1053,9 +1028,8 @@ cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t 
     e = launch_tiles(p, shape, a, r.out, r.width, s.pairs, stream);
     if (e != cudaSuccess || !a.weights) return e;
     const int64_t blocks = (a.m * (s.width / 4) + 255) / 256, most = int64_t(sm_count) * 16;
-    weighted_sum_kernel<<<unsigned(blocks < most ? blocks : most), 256, 0, stream>>>(reinterpret_cast<const float *>(ws + s.part_off), a.ids, a.weights, a.m, int(a.top), experts, a.lay.n, s.width, a.out,
-                                                                                     a.ldo, a.out_type == STRASSEN_BF16);
-    return cudaGetLastError();
+    return launch_after(weighted_sum_kernel, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, stream, dim3(1, 1), reinterpret_cast<const float *>(ws + s.part_off), a.ids, a.weights, a.m, int(a.top), experts,
+                        a.lay.n, s.width, a.out, a.ldo, a.out_type == STRASSEN_BF16);
 }
 
 cudaError_t read_gave_up(int *flag)
