@@ -1,0 +1,4 @@
+// Products of a few rows with a matrix of 4-bit weights: kernels for bf16 rows.
+#include "w4_thin.cuh"
+
+cudaError_t strassen::thin::launch_bf16(const Ptrs &p, int group, bool zeros, int sm_count, cudaStream_t stream) { return launch_type<XBF16>(p, group, zeros, sm_count, stream); }
