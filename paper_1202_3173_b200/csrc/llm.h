@@ -77,10 +77,11 @@ cudaError_t launch_route(RouteArgs p, cudaStream_t stream);
 
 // ---- 4-bit weights (w4_pack.cu, w4_thin.cu, w4_tiles.cu) -----------------------------------------------------------
 // Laid-out weights: tiles of 128 rows x 128 inner positions, one after another along the inner dimension, then along the
-// rows.  A tile is four chunks c = 0..3 of 128 rows x 16 bytes; the four 32-bit words of a row's 16 bytes hold
-// k = 32 w + 8 c + (0..7), w = 0..3, in the nibble order 0, 2, 4, 6, 1, 3, 5, 7 from the lowest nibble up, so that (word & 0x000f000f)
-// is the pair k = 0, 1, ((word >> 4) & 0x000f000f) the pair 2, 3, and so on.  A 16 x 128 piece is then the operand of
-// eight m16n8k16 products with one 16-byte load per lane and row, 32 rows x 128 are the rows of 32 lanes of tensor memory.
+// rows.  A tile is eight pieces of 16 rows, 1 KB each, in which the 64 bytes of rows g = 0..7 come first and those of rows g + 8 second.  The four
+// 16-byte chunks c of a row hold k = 32 w + 8 c + (0..7), w = 0..3 their 32-bit words, in the nibble order 0, 2, 4, 6, 1, 3, 5, 7 from the lowest nibble up,
+// so that (word & 0x000f000f) is the pair k = 0, 1, ((word >> 4) & 0x000f000f) the pair 2, 3, and so on.  A piece is then the operand of eight
+// m16n8k16 products with two 16-byte loads of a lane, 512 neighbouring bytes of the warp each; and the rows of 32 lanes of tensor memory are in pieces
+// too: chunk c of row r is in place c ^ (r / 2 & 3), so that neighbouring rows' are in different banks.
 // The nibbles are followed by the tile's scales (128 of 16 bits for each group) and its zero points (128 bytes for each group), so that a tile is
 // one piece of memory.
 constexpr int kW4Rows = 128, kW4Depth = 128, kW4NibbleBytes = kW4Rows * kW4Depth / 2;
@@ -97,6 +98,8 @@ struct W4Layout {
     size_t exponent_off, bytes;
 
     __host__ __device__ int zero_off() const { return kW4NibbleBytes + kW4Depth / group * kW4Rows * 2; }     // within a tile
+    // byte of chunk c of row r (0..127) of a tile
+    __host__ __device__ static int chunk_place(int r, int c) { return (r >> 3) * 512 + (r & 7) * 64 + (c ^ (r >> 1 & 3)) * 16; }
     // position of row r (0..127) of a tile in the scale and zero sections: rows g and g + 8 of a 16-row piece are neighbours
     __host__ __device__ static int row_place(int r) { return (r & ~15) | ((r & 7) << 1) | ((r >> 3) & 1); }
 };

@@ -44,8 +44,7 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
         }
         out[w] = word;
     }
-    uint4 *dst = reinterpret_cast<uint4 *>(p.packed + tile * p.lay.tile_bytes);
-    dst[c * kW4Rows + r] = make_uint4(out[0], out[1], out[2], out[3]);
+    *reinterpret_cast<uint4 *>(p.packed + tile * p.lay.tile_bytes + W4Layout::chunk_place(r, c)) = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 // One warp per row: its exponent, and its scales and zero points to their places.

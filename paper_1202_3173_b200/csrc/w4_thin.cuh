@@ -141,7 +141,7 @@ template <int RT, int U> struct Batch {
 // With experts a CTA has a single row of x at a time: MODE EACH_ID that of one id, its row of results; MODE SUM_OF_IDS those of all ids of
 // a token one after another, their sums multiplied by the ids' weights on the way.
 // A group is 1 << GS words of a row's 16 bytes.
-template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> __global__ void __launch_bounds__(WARPS * 32, 2) w4_thin_kernel(const Ptrs p)
+template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> __global__ void __launch_bounds__(WARPS * 32, RT == 1 ? 4 : 2) w4_thin_kernel(const Ptrs p)
 {
     using N = Num<XT>;
     constexpr int ROWS = 16 * RT, TOKENS = 8 * TT, CELLS = ROWS * TOKENS;
@@ -159,6 +159,7 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> __global_
     const int pitch = p.chunk * (kW4Depth * 2) + 64;        // + 64: two rows' 64 bytes, which 8 lanes read at a time, in different banks
     const int splits = int(gridDim.y);
 
+    const int chunk = W4Layout::chunk_place(r_in + g, c);
     // where this lane's rows of x are; past the last row, that one again: a column of sums that is not written
     int mine[TT];
 #pragma unroll
@@ -188,11 +189,11 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> __global_
             for (int u = 0; u < U; ++u)
                 if (kb + u * wk_count < stop) {
                     const uint8_t *const packed = matrix + int64_t(kb + u * wk_count) * p.tile_bytes;
-                    const uint4 *tile = reinterpret_cast<const uint4 *>(packed) + c * kW4Rows + r_in + g;
+                    const uint8_t *const tile = packed + chunk;
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) b.w[u][r][h] = __ldg(tile + 16 * r + 8 * h);
+                        for (int h = 0; h < 2; ++h) b.w[u][r][h] = __ldg(reinterpret_cast<const uint4 *>(tile + 1024 * r + 512 * h));
 #pragma unroll
                     for (int gg = 0; gg < 4; ++gg)
                         if ((gg & in_group) == 0) {
@@ -349,7 +350,7 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> __global_
 
 template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> cudaError_t launch_one(Ptrs p, int sm_count, cudaStream_t stream)
 {
-    constexpr int SUMS = WARPS * 16 * RT * 8 * TT * 4, MOST = 104 * 1024;        // of shared memory: two CTAs to an SM
+    constexpr int SUMS = WARPS * 16 * RT * 8 * TT * 4, MOST = 208 / (RT == 1 ? 4 : 2) * 1024;        // of shared memory, for the CTAs that an SM's registers hold
     static std::atomic<uint64_t> opted_in{0};                // devices that this kernel has been given its shared memory on
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -360,7 +361,7 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> cudaError
         opted_in.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
     const int64_t rows = (p.n + 16 * RT - 1) / (16 * RT), tokens = MODE == ONE ? (p.m + 8 * TT - 1) / (8 * TT) : MODE == EACH_ID ? p.m * p.top : p.m;
-    const int64_t room = int64_t(2) * WARPS * sm_count;      // warps that the GPU holds
+    const int64_t room = int64_t(RT == 1 ? 4 : 2) * WARPS * sm_count;      // warps that the GPU holds
     const int64_t tiles = rows * tokens;                     // that need a warp at least
     // the ids of a token go to different CTAs of a cluster, the inner dimension to the warps of a CTA and then to CTAs
     int splits = 1;
@@ -381,8 +382,8 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> cudaError
 
 template <int XT, int GS, bool ZEROS> cudaError_t launch_shape(const Ptrs &p, int sm_count, cudaStream_t stream)
 {
-    if (p.ids) return p.weights ? launch_one<XT, GS, 1, 1, 2, ZEROS, SUM_OF_IDS>(p, sm_count, stream) : launch_one<XT, GS, 1, 1, 2, ZEROS, EACH_ID>(p, sm_count, stream);
-    if (p.m <= 2) return launch_one<XT, GS, 1, 1, 2, ZEROS, ONE>(p, sm_count, stream);
+    if (p.ids) return p.weights ? launch_one<XT, GS, 1, 1, 1, ZEROS, SUM_OF_IDS>(p, sm_count, stream) : launch_one<XT, GS, 1, 1, 1, ZEROS, EACH_ID>(p, sm_count, stream);
+    if (p.m <= 2) return launch_one<XT, GS, 1, 1, 1, ZEROS, ONE>(p, sm_count, stream);
     if (p.m <= 8) return launch_one<XT, GS, 2, 1, 1, ZEROS, ONE>(p, sm_count, stream);
     return launch_one<XT, GS, 2, 2, 1, ZEROS, ONE>(p, sm_count, stream);
 }

@@ -460,7 +460,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
             uint32_t w[4][4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(stage + c * 2048 + r * 16);
+                const uint4 u = *reinterpret_cast<const uint4 *>(stage + W4Layout::chunk_place(r, c));
                 w[c][0] = u.x;
                 w[c][1] = u.y;
                 w[c][2] = u.z;
