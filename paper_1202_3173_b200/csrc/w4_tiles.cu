@@ -68,7 +68,7 @@ struct Args {
     int group_shift;         // a group is 1 << group_shift words of a row's 16 bytes
     int tile_bytes, zero_off;
     int tokens;              // rows of x in a tile, a multiple of CTAS * STEP
-    int box;                 // rows of x in one copy
+    int box;                 // rows of x in one copy; a CTA brings in whole boxes
     int x_stages, x_bytes;   // up to RING
     int a_buffers;           // GROUPS .. RING
     int out_type;
@@ -392,10 +392,26 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
             const Tile t = tile_at(i);
             const int row = t.row0 + r;
             const float back = N::BACK * p.exponents[t.nt * kW4Rows + r];
+            // where this group's rows of x (16 of every 64) go and their scales, two a lane, read before the wait
+            int place[2] = {0, 0};
+            float scale[2] = {1.f, 1.f};
+            if (MODE != SPLIT) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int at = 16 * group + 128 * b + (lane >> 4) * 64 + (lane & 15);
+                    if (at < t.count) {
+                        place[b] = t.t0 + at;
+                        if (MODE == EXPERTS) place[b] = p.order[place[b]];
+                        if (p.x_scale) scale[b] = p.x_scale[MODE == EXPERTS ? place[b] / p.scale_div : place[b]];
+                    }
+                }
+            }
             if (!warp_wait_for(&sh.done, i & 1, &sh)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int c = 16 * group; c < t.tokens; c += 16 * GROUPS) {
-                if (MODE != SPLIT && c >= t.count) break;
+#pragma unroll
+            for (int q = 0; q < TOKENS / (16 * GROUPS); ++q) {
+                const int c = 16 * group + 16 * GROUPS * q;
+                if (c >= (MODE == SPLIT ? t.tokens : t.count)) break;
                 uint32_t v[16];
                 ld_tmem16(v, lanes + c);
                 if (MODE == SPLIT) {
@@ -409,13 +425,9 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                 float y[16];
 #pragma unroll
                 for (int b = 0; b < 16; ++b) {
-                    to[b] = t.t0 + c + (b < left ? b : 0);
-                    if (MODE == EXPERTS) to[b] = p.order[to[b]];
+                    to[b] = MODE == EXPERTS ? __shfl_sync(~0u, place[q >> 1], 16 * (q & 1) + b) : t.t0 + c + b;
                     y[b] = __uint_as_float(v[b]) * back;
-                }
-                if (p.x_scale) {
-#pragma unroll
-                    for (int b = 0; b < 16; ++b) y[b] *= p.x_scale[MODE == EXPERTS ? to[b] / p.scale_div : to[b]];
+                    if (p.x_scale) y[b] *= __shfl_sync(~0u, scale[q >> 1], 16 * (q & 1) + b);
                 }
                 if (MODE == EXPERTS && p.out_type == STRASSEN_F32) {
 #pragma unroll
@@ -555,16 +567,16 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
             bool alive = true;
             for (int i = 0; i < mine && alive; ++i) {
                 const Tile t = tile_at(i);
-                const int rows = t.tokens / CTAS, row = t.t0 + side * rows;
+                const int rows = t.tokens / CTAS, row = t.t0 + side * rows, brought = (rows + p.box - 1) / p.box * p.box;
                 for (int j = 0; j < depth; ++j, ++g) {
                     const int before = g - p.x_stages, s = g % RING;
                     if (before >= 0 && !(alive = wait_for(&sh.used[before % RING], (before / RING) & 1, &sh))) break;
                     const uint32_t ready = CTAS == 2 ? of_rank(&sh.ready[s], 0) : smem_addr(&sh.ready[s]), to = ring_at + at * p.x_bytes;
-                    if (side == 0) bar_expect(&sh.ready[s], uint32_t(t.tokens) * 256);       // of both CTAs
+                    if (side == 0) bar_expect(&sh.ready[s], uint32_t(brought * CTAS) * 256);       // of both CTAs
                     const int k = (kb0 + j) * kW4Depth;
                     for (int b = 0; b < rows; b += p.box) {
                         box_copy<CTAS>(to + b * 128, &map, k, row + b, ready);
-                        box_copy<CTAS>(to + rows * 128 + b * 128, &map, k + 64, row + b, ready);
+                        box_copy<CTAS>(to + brought * 128 + b * 128, &map, k + 64, row + b, ready);
                     }
                     at = at + 1 == p.x_stages ? 0 : at + 1;
                 }
@@ -577,14 +589,14 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
         int g = 0, at = 0, a = 0;
         bool alive = true, here = false;         // here: the next step was found ready while products were being issued
         for (int i = 0; i < mine && alive; ++i) {
-            const int tokens = tile_at(i).tokens;
+            const int tokens = tile_at(i).tokens, brought = (tokens / CTAS + p.box - 1) / p.box * p.box;
             const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(tokens >> 3) << 17) | (uint32_t(128 * CTAS >> 4) << 24);
             if (i > 0 && !(alive = wait_for(&sh.d_free, (i - 1) & 1, &sh))) break;
             for (int j = 0; j < depth; ++j, ++g) {
                 if (!here && !(alive = wait_for(&sh.ready[g % RING], (g / RING) & 1, &sh))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t x_addr = smem_addr(ring) + at * p.x_bytes;
-                const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + tokens * (128 / CTAS));
+                const uint64_t b0 = operand(x_addr), b1 = operand(x_addr + brought * 128);
                 const uint32_t from = tmem + 512 - (p.a_buffers - a) * A_WIDTH;
                 here = bar_test(&sh.ready[(g + 1) % RING], ((g + 1) / RING) & 1);
 #pragma unroll
@@ -743,18 +755,22 @@ __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, 
     const int mine = counts[e], runs = (mine + most - 1) / most, even = runs ? (mine + runs - 1) / runs : 0;
     for (int i = threadIdx.x; i < runs; i += blockDim.x) table[tiles + i] = {e, start + i * even, mine - i * even < even ? mine - i * even : even, 0};
     __syncthreads();
-    int at = start;
-    for (int i0 = 0; i0 < pairs; i0 += blockDim.x) {
-        const int i = i0 + threadIdx.x;
-        const bool on = i < pairs && ids[i] == e;
-        const uint32_t here = __ballot_sync(~0u, on);
-        if (lane == 0) part[0][warp] = __popc(here);
-        __syncthreads();
-        const int n = part[0][lane], below = __reduce_add_sync(~0u, lane < warp ? n : 0), total = __reduce_add_sync(~0u, n);
-        if (on) order[at + below + __popc(here & ((1u << lane) - 1))] = i;
-        at += total;
-        __syncthreads();
+    // each thread has neighbouring ids; it counts its own, and with those of the threads before it knows its place
+    const int each = (pairs + int(blockDim.x) - 1) / int(blockDim.x), from = int(threadIdx.x) * each, to = from + each < pairs ? from + each : pairs;
+    int own = 0;
+    for (int i = from; i < to; ++i) own += ids[i] == e;
+    int upto = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += v;
     }
+    if (lane == 31) part[0][warp] = upto;
+    __syncthreads();
+    const int below = __reduce_add_sync(~0u, lane < warp ? part[0][lane] : 0);
+    int at = start + below + upto - own;
+    for (int i = from; i < to && own > 0; ++i)
+        if (ids[i] == e) order[at++] = i;
 }
 
 // out_t = sum_j weights_tj part_tj, in the order of j; pairs without an expert add nothing.
@@ -1020,7 +1036,11 @@ cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t 
     }
     // no tile has more rows than there are pairs
     p.tokens = int(s.pairs < TOKENS ? (s.pairs + 2 * STEP - 1) / (2 * STEP) * (2 * STEP) : TOKENS);
+    // Boxes as large as the runs are on average: a copy costs the thread that issues it more than the rows that it brings in beyond a run's end cost L2.
+    const int64_t average = s.pairs / experts / 2;
     p.box = STEP;
+    while (p.box < 64 && p.box * 2 <= average && p.box * 4 <= p.tokens) p.box *= 2;
+    p.tokens = (p.tokens + 2 * p.box - 1) / (2 * p.box) * (2 * p.box);
     Shape shape = {2, EXPERTS, 0, 1, 0};
     const int64_t tiles = int64_t(p.row_tiles + 1) / 2 * s.most_tiles;
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
