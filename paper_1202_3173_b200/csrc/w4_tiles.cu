@@ -667,39 +667,59 @@ struct RowsArgs {
     int64_t ldo, n;
 };
 
+// A warp has a row's piece of PIECES x 256 values at a time, all its loads under way at once: what a row's place costs (order, divisions) is paid once for them.
+// 16384 rows of 2048 out of 2048 in e4m3: 17.6 us, 23 us with a division for every 8 values.
+constexpr int PIECES = 4;
 __global__ void __launch_bounds__(256) rows_kernel(const RowsArgs p)
 {
     after_work_before();
-    const int64_t chunks = p.width / 8, total = (p.count ? int64_t(*p.count) : p.rows) * chunks, step = int64_t(gridDim.x) * blockDim.x;
-    const int64_t me = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int64_t count = p.count ? int64_t(*p.count) : p.rows;
+    const int warp = int(threadIdx.x >> 5), lane = int(threadIdx.x & 31);
     const uintptr_t lo = reinterpret_cast<uintptr_t>(p.x);
-    for (int64_t e = me; e < total; e += step) {
-        const int64_t i = e / chunks, c = (e - i * chunks) * 8;
-        const int64_t row = p.order ? p.order[i] / p.per_row : i;
-        uint32_t v[4];
-        if (p.e4m3) {
-            const uint2 u = load_bytes8(reinterpret_cast<const uint8_t *>(p.x + row * p.ldx_bytes), c, p.k, lo, p.x_end);
+    for (int64_t i = int64_t(blockIdx.x) * 8 + warp; i < count; i += int64_t(gridDim.x) * 8) {
+        const char *const x = p.x + (p.order ? int64_t(p.order[i] / p.per_row) : i) * p.ldx_bytes;
+        uint16_t *const out = p.out + i * p.width;
+        for (int64_t piece = blockIdx.y; piece * (PIECES * 256) < p.width; piece += gridDim.y) {
+            const int64_t c0 = piece * (PIECES * 256) + lane * 8;
+            uint4 v[PIECES];
+            if (p.e4m3) {
+                uint2 u[PIECES];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t((b < 2 ? u.x : u.y) >> (16 * (b & 1))), __NV_E4M3);
-                v[b] = uint32_t(h.x) | (uint32_t(h.y) << 16);
+                for (int j = 0; j < PIECES; ++j)
+                    if (c0 + j * 256 < p.width) u[j] = load_bytes8(reinterpret_cast<const uint8_t *>(x), c0 + j * 256, p.k, lo, p.x_end);
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t((b < 2 ? u[j].x : u[j].y) >> (16 * (b & 1))), __NV_E4M3);
+                        w[b] = uint32_t(h.x) | (uint32_t(h.y) << 16);
+                    }
+                    v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j)
+                    if (c0 + j * 256 < p.width) {
+                        Words<__half> w;
+                        load(w, reinterpret_cast<const __half *>(x), c0 + j * 256, p.k, lo, p.x_end);
+                        v[j] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+                    }
             }
-        } else {
-            Words<__half> w;
-            load(w, reinterpret_cast<const __half *>(p.x + row * p.ldx_bytes), c, p.k, lo, p.x_end);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) v[b] = w.w[b];
+            for (int j = 0; j < PIECES; ++j)
+                if (c0 + j * 256 < p.width) *reinterpret_cast<uint4 *>(out + c0 + j * 256) = v[j];
         }
-        *reinterpret_cast<uint4 *>(p.out + i * p.width + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
     if (p.results && *p.count < p.rows)
-        for (int64_t i = me >> 5; i < p.rows; i += step >> 5)
+        for (int64_t i = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * 8 + warp; i < p.rows; i += int64_t(gridDim.x) * gridDim.y * 8)
             if (p.ids[i] < 0 || p.ids[i] >= p.experts)
-                for (int64_t c = threadIdx.x & 31; c < p.n; c += 32) p.results[i * p.ldo + c] = 0;
+                for (int64_t c = lane; c < p.n; c += 32) p.results[i * p.ldo + c] = 0;
 }
 
 // Pairs (a token and one of its ids) in order of their experts, pairs of one expert in their own order: CTA e counts the ids of all experts,
 // and with them knows where its own begin.  Every CTA reads all ids, a few kilobytes from L2, and nothing has to be waited for.
+// 16384 ids of 64 experts: 7 us, 17 us with one load at a time.
 __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, int experts, int most, int *order, int *count, int *table_size, W4Tile *table)
 {
     __shared__ int counts[kMostExperts], part[2][32];
@@ -708,9 +728,19 @@ __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, 
     after_work_before();
     for (int i = threadIdx.x; i < experts; i += blockDim.x) counts[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
-        const int id = ids[i];
-        if (id >= 0 && id < experts) atomicAdd(&counts[id], 1);
+    // a warp has neighbouring ids, 32 * EACH of them at a time, whose loads are all under way at once
+    constexpr int EACH = 16;
+    const int share = (pairs + 32 * 32 - 1) / (32 * 32) * 32, from = warp * share, to = from + share < pairs ? from + share : pairs;
+    int own = 0;
+    for (int i = from; i < to; i += 32 * EACH) {
+        int id[EACH];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) id[j] = i + 32 * j + lane < to ? ids[i + 32 * j + lane] : -1;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            if (id[j] >= 0 && id[j] < experts) atomicAdd(&counts[id[j]], 1);
+            own += __popc(__ballot_sync(~0u, id[j] == e));
+        }
     }
     __syncthreads();
     // rows and tiles of rows before this expert, and of all
@@ -755,22 +785,22 @@ __global__ void __launch_bounds__(1024) order_kernel(const int *ids, int pairs, 
     const int mine = counts[e], runs = (mine + most - 1) / most, even = runs ? (mine + runs - 1) / runs : 0;
     for (int i = threadIdx.x; i < runs; i += blockDim.x) table[tiles + i] = {e, start + i * even, mine - i * even < even ? mine - i * even : even, 0};
     __syncthreads();
-    // each thread has neighbouring ids; it counts its own, and with those of the threads before it knows its place
-    const int each = (pairs + int(blockDim.x) - 1) / int(blockDim.x), from = int(threadIdx.x) * each, to = from + each < pairs ? from + each : pairs;
-    int own = 0;
-    for (int i = from; i < to; ++i) own += ids[i] == e;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(~0u, upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 31) part[0][warp] = upto;
+    // its own ids' places: after those of the warps before it, of its ids before and of the lanes below
+    if (lane == 0) part[0][warp] = own;
     __syncthreads();
-    const int below = __reduce_add_sync(~0u, lane < warp ? part[0][lane] : 0);
-    int at = start + below + upto - own;
-    for (int i = from; i < to && own > 0; ++i)
-        if (ids[i] == e) order[at++] = i;
+    int at = start + __reduce_add_sync(~0u, lane < warp ? part[0][lane] : 0);
+    if (own > 0)
+        for (int i = from; i < to; i += 32 * EACH) {
+            int id[EACH];
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) id[j] = i + 32 * j + lane < to ? ids[i + 32 * j + lane] : -1;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const uint32_t those = __ballot_sync(~0u, id[j] == e);
+                if (id[j] == e) order[at + __popc(those & ((1u << lane) - 1))] = i + 32 * j + lane;
+                at += __popc(those);
+            }
+        }
 }
 
 // out_t = sum_j weights_tj part_tj, in the order of j; pairs without an expert add nothing.
@@ -890,8 +920,9 @@ RowsArgs rows_args(const W4Args &a, void *to)
 
 cudaError_t launch_rows(const RowsArgs &r, int sm_count, cudaStream_t stream)
 {
-    const int64_t blocks = (r.rows * (r.width / 8) + 255) / 256, most = int64_t(sm_count) * 32;
-    return launch_after(rows_kernel, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, stream, dim3(1, 1), r);
+    const int64_t pieces = (r.width + PIECES * 256 - 1) / (PIECES * 256), y = pieces < 65535 ? pieces : 65535;
+    const int64_t blocks = (r.rows + 7) / 8, most = (int64_t(sm_count) * 32 + y - 1) / y;
+    return launch_after(rows_kernel, dim3(unsigned(blocks < most ? blocks : most), unsigned(y)), dim3(256), 0, stream, dim3(1, 1), r);
 }
 
 // What does not depend on how the rows of x are cut into tiles.
