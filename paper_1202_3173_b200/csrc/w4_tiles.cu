@@ -115,7 +115,10 @@ __device__ __forceinline__ float4 remote_float4(uint32_t at)
 }
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count)); }
 __device__ __forceinline__ void bar_arrive(uint64_t *b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory"); }
-__device__ __forceinline__ void bar_arrive_at(uint32_t b) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(b) : "memory"); }
+// At the pair's first CTA, after tcgen05 loads and stores that tcgen05.fence::before_thread_sync orders.  Relaxed: a release at cluster scope waits for
+// all that the thread has under way, its results' stores among them, and took some thousand clocks of each step (64 tokens, 8 of 64 experts of
+// 2048 x 2048: 80 us, 54 without; 4096 x 16384 x 4096: 372 and 360).
+__device__ __forceinline__ void bar_arrive_at(uint32_t b) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(b) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
@@ -123,14 +126,14 @@ __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes)
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
 }
 // Whether it is over, without waiting.
 __device__ __forceinline__ bool bar_test(uint64_t *b, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
     return ok != 0;
 }
 // Waits until phase `parity` of the barrier is over.  False: the limit was reached, here or elsewhere in the CTA, and the caller leaves
@@ -978,15 +981,20 @@ cudaError_t launch_tiles(Args p, Shape shape, const W4Args &a, const void *x, in
 // Workspace of the products of experts: the order and its tables, the rows of x in order, and with weights the pairs' results in 32 bits.
 struct ExpertsSpace {
     int64_t pairs, most_tiles;
+    int tokens;              // most rows of x in a tile
     size_t count_off, table_off, rows_off, part_off, bytes;
     int64_t width;           // of the pairs' results
 };
 ExpertsSpace experts_space(const W4Args &a)
 {
+    constexpr int LEAST = 64;
     const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     ExpertsSpace s;
     s.pairs = a.m * a.top;
-    s.most_tiles = s.pairs / TOKENS + (s.pairs < a.lay.experts ? s.pairs : a.lay.experts);
+    // Twice the average run, so that few runs take two tiles, and however uneven they are, there are at most half as many tiles again as experts.
+    const int64_t twice = (2 * s.pairs / a.lay.experts + 2 * STEP - 1) / (2 * STEP) * (2 * STEP);
+    s.tokens = int(twice < LEAST ? LEAST : twice > TOKENS ? TOKENS : twice);
+    s.most_tiles = s.pairs / s.tokens + (s.pairs < a.lay.experts ? s.pairs : a.lay.experts);
     s.width = (a.lay.n + 3) / 4 * 4;
     s.count_off = up(size_t(s.pairs) * 4);
     s.table_off = s.count_off + 256;
@@ -1038,7 +1046,7 @@ cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t 
     int *const order = reinterpret_cast<int *>(ws), *const count = reinterpret_cast<int *>(ws + s.count_off);
     W4Tile *const table = reinterpret_cast<W4Tile *>(ws + s.table_off);
     const int experts = int(a.lay.experts);
-    cudaError_t e = launch_after(order_kernel, dim3(unsigned(experts)), dim3(1024), 0, stream, dim3(1, 1), a.ids, int(s.pairs), experts, TOKENS, order, count, count + 1, table);
+    cudaError_t e = launch_after(order_kernel, dim3(unsigned(experts)), dim3(1024), 0, stream, dim3(1, 1), a.ids, int(s.pairs), experts, s.tokens, order, count, count + 1, table);
     if (e != cudaSuccess) return e;
 
     RowsArgs r = rows_args(a, ws + s.rows_off);
@@ -1065,8 +1073,7 @@ cudaError_t launch_w4_experts_tiles(const W4Args &a, int sm_count, cudaStream_t 
         p.out_type = STRASSEN_F32;
         p.ldo = s.width;
     }
-    // no tile has more rows than there are pairs
-    p.tokens = int(s.pairs < TOKENS ? (s.pairs + 2 * STEP - 1) / (2 * STEP) * (2 * STEP) : TOKENS);
+    p.tokens = s.tokens;
     // Boxes as large as the runs are on average: a copy costs the thread that issues it more than the rows that it brings in beyond a run's end cost L2.
     const int64_t average = s.pairs / experts / 2;
     p.box = STEP;
