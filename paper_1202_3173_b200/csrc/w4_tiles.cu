@@ -411,12 +411,21 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
             }
             if (!warp_wait_for(&sh.done, i & 1, &sh)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const int end = MODE == SPLIT ? t.tokens : t.count;
+            // D is free for the products of the next tile as soon as its last rows are in registers
+            const auto free_d = [&] {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_at(d_free);
+            };
+            if (16 * group >= end) free_d();
 #pragma unroll
             for (int q = 0; q < TOKENS / (16 * GROUPS); ++q) {
                 const int c = 16 * group + 16 * GROUPS * q;
-                if (c >= (MODE == SPLIT ? t.tokens : t.count)) break;
+                if (c >= end) break;
                 uint32_t v[16];
                 ld_tmem16(v, lanes + c);
+                if (c + 16 * GROUPS >= end) free_d();
                 if (MODE == SPLIT) {
                     float *sums = reinterpret_cast<float *>(ring) + c * kW4Rows + r;
 #pragma unroll
@@ -453,9 +462,6 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                         if (b < left) static_cast<uint16_t *>(p.out)[to[b] * p.ldo + row] = uint16_t(two_16_bits(y[b], 0.f, bf16_out));
                 }
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive_at(d_free);
             return true;
         };
 
