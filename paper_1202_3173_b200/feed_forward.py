@@ -227,7 +227,8 @@ class W4Matrix(_W4):
         out, out_kind, ldo = self._output(x, m, out, dtype)
         xs = 0 if x_scale is None else _packed("x_scale", x_scale, (m,), torch.float32, index)
         at, ws, need = x.data_ptr(), 0, 0
-        if m > binding.STRASSEN_W4_THIN_ROWS:
+        # rows in 16 bits that start at multiples of 16 bytes need no workspace: not asked for them, a call in itself
+        if m > binding.STRASSEN_W4_THIN_ROWS and (kind == binding.STRASSEN_E4M3 or at % 16 or ldx % 8):
             need = binding.strassen_w4_workspace_bytes(self._h, m, kind, at, ldx)
             if need:
                 workspace = self._workspace(need)
