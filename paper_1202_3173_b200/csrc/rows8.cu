@@ -391,9 +391,9 @@ template <class T> __device__ __forceinline__ void cut(Words<T> &p, int count)
 
 template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) stream_kernel(const RowArgs p, int slots, int slot_bytes, int stage_at)
 {
-    extern __shared__ __align__(16) uint8_t memory[];            // the weights of a norm, then the ring
+    extern __shared__ __align__(16) uint8_t memory[];            // the norm's weights, then the ring
     constexpr bool TWO = MODE != NORM;                           // two inputs
-    uint8_t *const ring = memory + (MODE == GATE ? 0 : int(blockDim.x) * ITEMS * 8 * int(sizeof(T)));
+    uint8_t *const ring = memory + int(blockDim.x) * ITEMS * 8 * int(sizeof(T));
     __shared__ float2 part[2][THREADS / 32];
     __shared__ uint64_t full[MOST_SLOTS];
     __shared__ int dead;
@@ -440,17 +440,15 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
             w.w[4 * j + 3] = u.w;
         }
     };
-    if (MODE != GATE) {
-        const Range<T> range_w(p.weight, 1, p.k, p.k);
+    const Range<T> range_w(p.weight, 1, p.k, p.k);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
-            Words<T> w;
-            memset(&w, 0, sizeof(w));
-            if (c < k) load(w, static_cast<const T *>(p.weight), c, k, range_w.lo, range_w.hi);
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
+        Words<T> w;
+        memset(&w, 0, sizeof(w));
+        if (c < k) load(w, static_cast<const T *>(p.weight), c, k, range_w.lo, range_w.hi);
 #pragma unroll
-            for (int j = 0; j < N16; ++j) weights[(i * N16 + j) * int(blockDim.x)] = make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]);
-        }
+        for (int j = 0; j < N16; ++j) weights[(i * N16 + j) * int(blockDim.x)] = make_uint4(w.w[4 * j], w.w[4 * j + 1], w.w[4 * j + 2], w.w[4 * j + 3]);
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const float over_k = 1.f / float(k);
@@ -497,7 +495,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             Words<T> w, sum;
-            if (MODE != GATE) weight(i, w);
+            weight(i, w);
             values<T, MODE>(pa[i], pb[i], w, v[i], sum, squares, mx);
             if (MODE == NORM_RESIDUAL) {
                 const int c = (i * int(blockDim.x) + int(threadIdx.x)) * 8;
@@ -513,7 +511,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
         float sq = both(squares);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            if (MODE != GATE) sq += __shfl_xor_sync(~0u, sq, o);
+            sq += __shfl_xor_sync(~0u, sq, o);
             mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
         }
         if (lane == 0) part[turn][warp] = make_float2(sq, mx);
@@ -575,7 +573,7 @@ template <class T, int MODE, int ITEMS, int THREADS> cudaError_t launch_stream(c
         if (e != cudaSuccess) return e;
         opted_in.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
-    const int threads = int((p.k + 256 * ITEMS - 1) / (256 * ITEMS) * 32), weights = MODE == GATE ? 0 : threads * ITEMS * 8 * int(sizeof(T));
+    const int threads = int((p.k + 256 * ITEMS - 1) / (256 * ITEMS) * 32), weights = threads * ITEMS * 8 * int(sizeof(T));
     const int half = int((p.k * int64_t(sizeof(T)) + 15) / 16 * 16 + 48);        // the words it lies in, and what a piece's window may read beyond
     const int slot_bytes = MODE == NORM ? half : 2 * half;
     int slots = (most - weights) / slot_bytes;
@@ -692,23 +690,33 @@ template <class T, int MODE> cudaError_t launch_type(const RowArgs &p, int sm_co
 {
     const int64_t pieces = (p.k + 7) / 8;
     // Short rows, where there are enough of them for the lanes to be all in use; a CTA for each row would spend its time on its launch and its
-    // reduction (128 bf16 values: 310 us for 300000 rows).
-    if (pieces <= 128 && p.m >= 2 * sm_count) {
+    // reduction.  30000 rows of 512 bf16 values: 11.6 us, 32 with a CTA for each (gate: 13.8 and 32); 1000 rows of 256: 1.9 and 2.0.  Longer ones only without a
+    // sum to write, and where they are very many: gate 30000 x 1024 25 and 33 us, but 1000 x 1024 3.7 and 2.6; with the sum 42 and 39 us.
+    if (p.m >= 2 * sm_count && (pieces <= 64 || (MODE != NORM_RESIDUAL && pieces <= 128 && p.m >= 32 * sm_count))) {
         if (pieces <= 8) return launch_short<T, MODE, 8, 1>(p, stream);
         if (pieces <= 16) return launch_short<T, MODE, 16, 1>(p, stream);
         if (pieces <= 32) return launch_short<T, MODE, 32, 1>(p, stream);
         if (pieces <= 64) return launch_short<T, MODE, 32, 2>(p, stream);
-        return launch_short<T, MODE, 32, 4>(p, stream);
+        if constexpr (MODE != NORM_RESIDUAL) return launch_short<T, MODE, 32, 4>(p, stream);
     }
-    // Rows enough for CTAs that stay.  Two pieces a thread, so that an SM has several rows at a time in different steps, four where a row would
-    // need more than half of its threads.
-    if (p.m >= 4 * sm_count && pieces > 128 && pieces <= 2048) {
-        cudaError_t e = cudaErrorNotSupported;
-        if (pieces <= 256) e = launch_stream<T, MODE, 2, 128>(p, sm_count, stream);
-        else if (pieces <= 512) e = launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
-        else if (pieces <= 1024) e = launch_stream<T, MODE, 2, 512>(p, sm_count, stream);
-        else e = launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
-        if (e != cudaErrorNotSupported) return e;
+    // CTAs that stay, for norms with enough to do (half a megabyte of x an SM; residual, 8192 bf16: 1200 rows 16.1 us with them and 14.5 without, 9600 rows 93 and 96):
+    // with a residual at any length (4099 x 12345 f16, misaligned: 84 and 112 us; 4800 x 16384 bf16: 96 and 107), without one in 32 bits (4096 x 8192:
+    // 31 and 41) and for the longest rows (4800 x 16384 bf16: 50 and 56, but 9600 x 4096: 32 and 26).  Never for gates, whose
+    // arithmetic wants more warps than that leaves (4800 x 16384 bf16: 78 and 67 us, 9600 x 8192: 85 and 59).  Two pieces a thread, so that
+    // an SM has several rows at a time in different steps, four where a row would need more than half of its threads.
+    if constexpr (MODE != GATE) {
+        if (p.m * p.k * int64_t(sizeof(T)) >= int64_t(sm_count) << 19 && pieces > 128 && pieces <= 2048) {
+            cudaError_t e = cudaErrorNotSupported;
+            if constexpr (MODE == NORM_RESIDUAL || sizeof(T) == 4) {
+                if (pieces <= 256) e = launch_stream<T, MODE, 2, 128>(p, sm_count, stream);
+                else if (pieces <= 512) e = launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
+                else if (pieces <= 1024) e = launch_stream<T, MODE, 2, 512>(p, sm_count, stream);
+                else e = launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
+            } else if (pieces > 1536) {
+                e = launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
+            }
+            if (e != cudaErrorNotSupported) return e;
+        }
     }
     const dim3 grid(unsigned(p.m));
     const auto threads = [&](int items) { return dim3(unsigned((pieces + 32 * items - 1) / (32 * items) * 32)); };
