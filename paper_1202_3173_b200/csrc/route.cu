@@ -9,7 +9,8 @@
 // of large negative numbers) stay 0 when they are renormalised.
 //
 // One warp a token, expert i * 32 + lane in register i.  Keys become unsigned numbers of the same order, so that the warp's largest is one
-// reduction instruction and the lowest index among equals another.  A few kilobytes a token: bound by launch and latency.
+// reduction instruction and the lowest index among equals another.  A few kilobytes a token: bound by launch and latency
+// (16384 tokens, 64 experts of which 8: 9.4 us, 3.1 MB; one token: the launch).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

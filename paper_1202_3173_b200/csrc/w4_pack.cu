@@ -3,7 +3,8 @@
 // Positions past the inner size hold the row's zero point (their value is 0), rows past the matrix the nibble 8 with a scale of 0.
 // Scales are held as S 2^-e with e such that 1 <= max_g |S_g| 2^-e < 2 in each row, and 2^e (32 bits) apart, in the exponent section: 16-bit weights
 // S 2^-e (Q - Z) then keep clear of the subnormal range of f16, and the products multiply their 32-bit sums by 2^e.  Both steps are exact,
-// except that f16 scales below 2^-14 of their row's largest lose bits, never more than 2^-25 of that.
+// except that f16 scales below 2^-14 of their row's largest lose bits, never more than 2^-25 of that.  A thread writes one 16-byte piece: once for
+// a matrix, at the rate of scattered reads of nibbles; nothing that a product waits for.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
