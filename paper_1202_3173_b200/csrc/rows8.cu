@@ -12,8 +12,8 @@
 //
 // A thread has pieces of 8 neighbouring elements.  Rows that do not start at a multiple of 16 bytes (odd lengths, halves of odd rows) are read and
 // written in the same 16-byte accesses: two aligned words around a piece are shifted into place, and on the way out neighbouring lanes pass
-// each other the bytes that belong to the other's word.  Bound by HBM for many rows (norm with residual 19200 x 4096 bf16: 92 us, 6.0 TB/s; without 50 us,
-// 4.7 TB/s, gate 57 us, 6.9 TB/s), by shifting and staging where rows are misaligned (4099 x 12345 f16: 85 us, 4.2 TB/s), by launch and latency for few.
+// each other the bytes that belong to the other's word.  Bound by HBM for many rows (norm with residual 9600 x 8192 bf16: 90 us, 6.1 TB/s; without 48 us,
+// 4.9 TB/s, gate 57 us, 6.9 TB/s), by shifting and staging where rows are misaligned (4099 x 12345 f16: 78 us, 4.5 TB/s), by launch and latency for few.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -158,32 +158,37 @@ template <class T, int W> __device__ __forceinline__ void store(const Words<T> &
     }
 }
 
-// Sum and maximum over the CTA, the same bits in every thread (each adds the warps' values in the same order).
-__device__ __forceinline__ void reduce_row(float &sum, float &mx, float (*part)[32])
+enum { GATE = 0, NORM = 1, NORM_RESIDUAL = 2 };
+
+// Sum (of a norm) and maximum over a warp.  The maximum is of absolute values, so its bits have the order of unsigned numbers, NaN (0x7fffffff) above
+// infinity: one reduction instruction.
+template <int MODE> __device__ __forceinline__ void reduce_warp(float &sum, float &mx)
 {
+    if (MODE != GATE) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        sum += __shfl_xor_sync(~0u, sum, o);
-        mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     }
+    mx = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(mx)));
+}
+// ... of the warps' values in `part` (sum, maximum), the same bits in every thread: each adds them in the same order.
+template <int MODE> __device__ __forceinline__ void reduce_warps(float &sum, float &mx, const float2 *part, int warps)
+{
+    const int lane = threadIdx.x & 31;
+    const float2 v = lane < warps ? part[lane] : make_float2(0.f, 0.f);
+    sum = v.x;
+    mx = v.y;
+    reduce_warp<MODE>(sum, mx);
+}
+// ... over the CTA.
+template <int MODE> __device__ __forceinline__ void reduce_row(float &sum, float &mx, float2 *part)
+{
+    reduce_warp<MODE>(sum, mx);
     const int warps = blockDim.x >> 5;
     if (warps == 1) return;
-    if ((threadIdx.x & 31) == 0) {
-        part[0][threadIdx.x >> 5] = sum;
-        part[1][threadIdx.x >> 5] = mx;
-    }
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(sum, mx);
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    sum = lane < warps ? part[0][lane] : 0.f;
-    mx = lane < warps ? part[1][lane] : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        sum += __shfl_xor_sync(~0u, sum, o);
-        mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
-    }
+    reduce_warps<MODE>(sum, mx, part, warps);
 }
-
-enum { GATE = 0, NORM = 1, NORM_RESIDUAL = 2 };
 
 // Two f32 in a register pair: Blackwell adds and multiplies them in one instruction.
 struct Pair {
@@ -297,7 +302,7 @@ __device__ __forceinline__ void store_e4m3(uint8_t *row, int64_t k, int64_t size
 // One CTA per row, the row in registers: ITEMS pieces a thread, their loads all under way before the first is used.
 template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bounds__(THREADS) row_kernel(const RowArgs p)
 {
-    __shared__ float part[2][32];
+    __shared__ float2 part[32];
     after_work_before();
     const int64_t r = blockIdx.x;
     const T *const a = static_cast<const T *>(p.a) + r * p.lda, *const b = static_cast<const T *>(p.b) + r * p.ldb, *const w = static_cast<const T *>(p.weight);
@@ -325,7 +330,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
         if (MODE == NORM_RESIDUAL) store<T, 32>(sum, static_cast<T *>(p.sum) + r * p.lds, (i * int64_t(blockDim.x) + threadIdx.x) * 8, p.k);
     }
     float sq = both(squares);
-    reduce_row(sq, mx, part);
+    reduce_row<MODE>(sq, mx, part);
     float scale;
     const float factor = row_factor<MODE>(sq, mx, 1.f / float(p.k), p.eps, scale);
     uint8_t *const q = p.q + r * p.ldq;
@@ -510,23 +515,14 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
             }
         }
         float sq = both(squares);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            sq += __shfl_xor_sync(~0u, sq, o);
-            mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
-        }
+        reduce_warp<MODE>(sq, mx);
         if (lane == 0) part[turn][warp] = make_float2(sq, mx);
         __syncthreads();
         // every thread has its part of the row: its place is free
         if (dead) break;
         if (threadIdx.x == 0) fetch(r + slots * step, slot);
         slot = slot + 1 == slots ? 0 : slot + 1;
-        sq = mx = 0.f;
-        for (int w = 0; w < warps; ++w) {
-            const float2 v = part[turn][w];
-            sq += v.x;
-            mx = max_nan(mx, v.y);
-        }
+        reduce_warps<MODE>(sq, mx, part[turn], warps);
         turn ^= 1;
         float scale;
         const float factor = row_factor<MODE>(sq, mx, over_k, p.eps, scale);
@@ -579,7 +575,7 @@ template <class T, int MODE, int ITEMS, int THREADS> cudaError_t launch_stream(c
     const int slot_bytes = MODE == NORM ? half : 2 * half;
     int slots = (most - weights) / slot_bytes;
     if (slots < 1) return cudaErrorNotSupported;
-    // A sum whose rows do not start at multiples of 16 bytes goes through shared memory where a row of it fits: 4099 x 12345 f16 in 86 us, against 116 us
+    // A sum whose rows do not start at multiples of 16 bytes goes through shared memory where a row of it fits: 4099 x 12345 f16 in 78 us, against 113 us
     // by exchanges between the lanes.
     int stage_at = 0;
     const int stage_bytes = int((p.k * int64_t(sizeof(T)) + 15) / 16 * 16 + 32);
@@ -627,7 +623,7 @@ template <class T, int MODE, int W, int ITEMS> __global__ void __launch_bounds__
     float sq = both(squares);
 #pragma unroll
     for (int o = W / 2; o > 0; o >>= 1) {
-        sq += __shfl_xor_sync(~0u, sq, o);
+        if (MODE != GATE) sq += __shfl_xor_sync(~0u, sq, o);
         mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
     }
     float scale;
@@ -651,7 +647,7 @@ template <class T, int MODE, int W, int ITEMS> cudaError_t launch_short(const Ro
 // beside it writes the sum there, so the sum may take the residual's place here too.
 template <class T, int MODE> __global__ void __launch_bounds__(1024) long_row_kernel(const RowArgs p)
 {
-    __shared__ float part[2][32];
+    __shared__ float2 part[32];
     after_work_before();
     const int64_t r = blockIdx.x;
     const T *const a = static_cast<const T *>(p.a) + r * p.lda, *const b = static_cast<const T *>(p.b) + r * p.ldb, *const w = static_cast<const T *>(p.weight);
@@ -680,7 +676,7 @@ template <class T, int MODE> __global__ void __launch_bounds__(1024) long_row_ke
         }
         if (pass == 0) {
             sq = both(squares);
-            reduce_row(sq, mx, part);
+            reduce_row<MODE>(sq, mx, part);
             factor = row_factor<MODE>(sq, mx, 1.f / float(p.k), p.eps, scale);
         }
     }
@@ -700,17 +696,19 @@ template <class T, int MODE> cudaError_t launch_type(const RowArgs &p, int sm_co
         if (pieces <= 64) return launch_short<T, MODE, 32, 2>(p, stream);
         if constexpr (MODE != NORM_RESIDUAL) return launch_short<T, MODE, 32, 4>(p, stream);
     }
-    // CTAs that stay, for norms with enough to do (half a megabyte of x an SM; residual, 8192 bf16: 1200 rows 16.1 us with them and 14.5 without, 9600 rows 93 and 96):
-    // with a residual at any length (4099 x 12345 f16, misaligned: 84 and 112 us; 4800 x 16384 bf16: 96 and 107), without one in 32 bits (4096 x 8192:
-    // 31 and 41) and for the longest rows (4800 x 16384 bf16: 50 and 56, but 9600 x 4096: 32 and 26).  Never for gates, whose
-    // arithmetic wants more warps than that leaves (4800 x 16384 bf16: 78 and 67 us, 9600 x 8192: 85 and 59).  Two pieces a thread, so that
+    // CTAs that stay, for norms with enough to do.  With a residual: half a megabyte of x an SM (1200 x 8192 bf16 16.1 us with them and 14.5 without, 9600 x 8192 90 and
+    // 97, 4800 x 16384 96 and 108, 19200 x 2048 50 and 55, but f32 16384 x 2048 77 and 64), an eighth of a megabyte where the sum is misaligned and staged (8192 x 2047: 34 and 39 us, 4099 x 12345 f16 78 and 113).  Without
+    // one: in 32 bits (4096 x 8192: 28 and 41) and for the longest rows (4800 x 16384 bf16: 47 and 56, but 19200 x 4096: 58 and 50).  Never for gates,
+    // whose arithmetic wants more warps than that leaves (4800 x 16384 bf16: 78 and 67 us, 9600 x 8192: 85 and 59).  Two pieces a thread, so that
     // an SM has several rows at a time in different steps, four where a row would need more than half of its threads.
     if constexpr (MODE != GATE) {
-        if (p.m * p.k * int64_t(sizeof(T)) >= int64_t(sm_count) << 19 && pieces > 128 && pieces <= 2048) {
+        const bool staged = MODE == NORM_RESIDUAL && (reinterpret_cast<uintptr_t>(p.sum) | uintptr_t(p.lds * int64_t(sizeof(T)))) % 16 != 0;
+        if (p.m * p.k * int64_t(sizeof(T)) >= int64_t(sm_count) << (staged ? 17 : 19) && pieces > 128 && pieces <= 2048) {
             cudaError_t e = cudaErrorNotSupported;
             if constexpr (MODE == NORM_RESIDUAL || sizeof(T) == 4) {
-                if (pieces <= 256) e = launch_stream<T, MODE, 2, 128>(p, sm_count, stream);
-                else if (pieces <= 512) e = launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
+                if (pieces <= 256) {
+                    if (MODE == NORM || staged || sizeof(T) == 2) e = launch_stream<T, MODE, 2, 128>(p, sm_count, stream);
+                } else if (pieces <= 512) e = launch_stream<T, MODE, 2, 256>(p, sm_count, stream);
                 else if (pieces <= 1024) e = launch_stream<T, MODE, 2, 512>(p, sm_count, stream);
                 else e = launch_stream<T, MODE, 4, 512>(p, sm_count, stream);
             } else if (pieces > 1536) {
