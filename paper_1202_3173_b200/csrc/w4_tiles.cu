@@ -26,7 +26,7 @@
 // expert's tokens) are first written to the workspace in order, in 16 bits (rows_kernel).
 //
 // Bound by the tensor cores for prompts (4096 x 16384 x 4096, e4m3 with zero points: 342 us with the rows' conversion in a run of calls on one input, 1.6 PFLOP/s,
-// 413 where the inputs change from call to call, 1.33 PFLOP/s); for tens of rows by what a step costs besides (turning the weights takes a
+// 410 to 422 where the inputs change from call to call, 1.3 PFLOP/s); for tens of rows by what a step costs besides (turning the weights takes a
 // group some 1000 clocks of latency, four groups at a time: 48 x 4096 x 16384 in 16.2 us, 2.4 TB/s).
 //
 // Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
