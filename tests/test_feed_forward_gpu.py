@@ -128,6 +128,31 @@ def test_many_rows(k, pad, shift):
     binding.strassen_device_status()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (7, 0), (1, 3)])
+@pytest.mark.parametrize("k", [600, 1025, 2047, 2048, 4096, 4099, 8192, 12345, 16384])
+def test_matrices_of_many_megabytes(k, pad, shift, dtype):
+    """Norms with enough to do for CTAs that stay and copy ahead, each number of threads and pieces, sums staged or not and in place; gates of as much."""
+    g = gen(k + pad)
+    m = 90000000 // (k * dtype.itemsize)
+    x, r = (strided(torch.randn(m, k, device="cuda", generator=g).to(dtype), pad, shift) for _ in range(2))
+    w = (1 + 0.3 * torch.randn(k, device="cuda", generator=g)).to(dtype)
+    q, s = sw().quant_rows(m, k)
+    sw().rms_norm_quant(x, w, EPS, out=(q, s))
+    check_rows(q, s, norm64(x, w))
+    sw().silu_mul_quant(x, r, out=(q, s))
+    check_rows(q, s, x.double() * torch.special.expit(x.double()) * r.double())
+    want, v = (x.float() + r.float()).to(dtype), norm64(x, w, r)
+    total = torch.empty(m, k, device="cuda", dtype=dtype)
+    sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, total))
+    check_rows(q, s, v)
+    assert torch.equal(total, want)
+    sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, r))
+    check_rows(q, s, v)
+    assert torch.equal(r, want)
+    binding.strassen_device_status()
+
+
 def test_norm_rows_of_zeros_nan_and_infinity():
     for k in (96, 40000):
         x = torch.randn(6, k, device="cuda")
