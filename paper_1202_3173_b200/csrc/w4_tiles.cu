@@ -600,6 +600,8 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                     at = at + 1 == p.x_stages ? 0 : at + 1;
                 }
             }
+            // the last products' arrivals at `used`, which may come from the other CTA, are here before this one leaves
+            for (int before = g > p.x_stages ? g - p.x_stages : 0; before < g && alive; ++before) alive = wait_for(&sh.used[before % RING], (before / RING) & 1, &sh);
             if (!alive) give_copies_time();
         }
     } else if (side == 0 && elected()) {
