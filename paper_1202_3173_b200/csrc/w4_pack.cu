@@ -1,10 +1,10 @@
 // Laying out 4-bit weights, once for a matrix: from rows of packed nibbles to the tiles that the products read (llm.h).
 //
 // Positions past the inner size hold the row's zero point (their value is 0), rows past the matrix the nibble 8 with a scale of 0.
-// Scales are held as S 2^-e with e such that 1 <= max_g |S_g| 2^-e < 2 in each row, and 2^e (32 bits) apart, in the exponent section: 16-bit weights
-// S 2^-e (Q - Z) then keep clear of the subnormal range of f16, and the products multiply their 32-bit sums by 2^e.  Both steps are exact,
-// except that f16 scales below 2^-14 of their row's largest lose bits, never more than 2^-25 of that.  A thread writes one 16-byte piece: once for
-// a matrix, at the rate of scattered reads of nibbles; nothing that a product waits for.
+// Scales are held as S 2^-e with e such that 2^15 <= max_g |S_g| 2^-e < 2^16 in each row (the upper end of f16), and 2^e (32 bits) apart, in the exponent
+// section; the products multiply their 32-bit sums by 2^e.  Both steps are exact: f16 scales only ever move up.  (Of bf16 scales only those below 2^-141 of
+// their row's largest lose bits.)  A thread writes one 16-byte piece: once for a matrix, at the rate of scattered reads of nibbles; nothing that a
+// product waits for.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(128) pack_scales_kernel(const W4PackArgs p)
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
-    int e = mx > 0.f ? ilogbf(mx) : 0;
+    int e = mx > 0.f ? ilogbf(mx) - 15 : 0;
     e = e < -126 ? -126 : e;
     if (lane == 0) reinterpret_cast<float *>(p.packed + p.lay.exponent_off)[slot] = ldexpf(1.f, e);
     for (int64_t g = lane; g < p.lay.depth_tiles * per_tile; g += 32) {

@@ -239,16 +239,16 @@ __device__ __forceinline__ void ld_tmem16(uint32_t (&v)[16], uint32_t at)
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// What a 16-bit weight is made of, from the pairs of a masked nibble and the scale S 2^-e, at most 2:
+// What a 16-bit weight is made of, from the pairs of a masked nibble and the scale S 2^-e, below 2^16:
 //   without zero points  FMA(pair, scale FACTOR, scale -8 UNIT): one step of q becomes scale UNIT
 //   with zero points     MUL(FMA(pair, BIG or SMALL, -z STEP), scale RATIO): steps of STEP first, exactly, and of scale UNIT then
 // Nibbles in bits 4..7 take a sixteenth of the factor.
 template <bool BF16> struct Num;
 template <> struct Num<true> {
-    // a masked nibble is q 2^-133; UNIT 2^-7, STEP 2^-6
-    static constexpr float BACK = 128.f, STEP = 1.f / 64;
-    static constexpr uint32_t BIG_FACTOR = 0x7e807e80, SMALL_FACTOR = 0x7c807c80, MINUS_EIGHT = 0xbd80bd80;       // 2^126, 2^122, -2^-4
-    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00, RATIO = 0x3f003f00;                           // 2^127, 2^123, 2^-1
+    // a masked nibble is q 2^-133; UNIT 2^-22, STEP 2^-6
+    static constexpr float BACK = 4194304.f, STEP = 1.f / 64;
+    static constexpr uint32_t BIG_FACTOR = 0x77007700, SMALL_FACTOR = 0x75007500, MINUS_EIGHT = 0xb600b600;       // 2^111, 2^107, -2^-19
+    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00, RATIO = 0x37803780;                           // 2^127, 2^123, 2^-16
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rn(v));
@@ -268,10 +268,10 @@ template <> struct Num<true> {
     }
 };
 template <> struct Num<false> {
-    // a masked nibble is q 2^-24; UNIT 2^-10, STEP 2^-9
-    static constexpr float BACK = 1024.f, STEP = 1.f / 512;
-    static constexpr uint32_t BIG_FACTOR = 0x74007400, SMALL_FACTOR = 0x64006400, MINUS_EIGHT = 0xa000a000;       // 2^14, 2^10, -2^-7
-    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800, RATIO = 0x38003800;                           // 2^15, 2^11, 2^-1
+    // a masked nibble is q 2^-24; UNIT 2^-25, STEP 2^-9
+    static constexpr float BACK = 33554432.f, STEP = 1.f / 512;
+    static constexpr uint32_t BIG_FACTOR = 0x38003800, SMALL_FACTOR = 0x28002800, MINUS_EIGHT = 0x80048004;       // 2^-1, 2^-5, -2^-22
+    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800, RATIO = 0x01000100;                           // 2^15, 2^11, 2^-16
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __half_as_ushort(__float2half_rn(v));
