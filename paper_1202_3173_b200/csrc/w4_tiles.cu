@@ -17,9 +17,9 @@
 //
 // A weight is held in 16 bits as S 2^-e (Q - Z) (e: w4_pack.cu): this rounding, to bf16 beside bf16 rows and to f16 beside f16 and
 // e4m3 rows, is the price of one chain of products over the whole inner dimension; sums of a group scaled apart in 32 bits would
-// cross tensor memory once per group.  It is as large as the rounding of the result to the same type.  As in the kernel for few rows, a masked
-// nibble is a subnormal number: without zero points S (q - 8) is ONE packed multiply-add, S q - 8 S, with 8 S exact; with zero points
-// S z need not be exact, so (q - z) comes first, exactly, and the scale second.
+// cross tensor memory once per group.  It is one rounding of each weight, as large as that of the result to the same type (in f16 down to weights of
+// 2^-20 of their row's largest scale).  As in the kernel for few rows, a masked nibble is a subnormal number, and one or two packed instructions
+// make a pair of weights of two of them (Num).
 //
 // Where even single CTAs' tiles are too few to fill the GPU, the CTAs of a cluster split the inner dimension and add their sums in a
 // fixed order over distributed shared memory.  Rows of x that a tensor map cannot take as they are (e4m3, other alignments, the rows of an
@@ -239,16 +239,18 @@ __device__ __forceinline__ void ld_tmem16(uint32_t (&v)[16], uint32_t at)
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-// What a 16-bit weight is made of, from the pairs of a masked nibble and the scale S 2^-e, below 2^16:
-//   without zero points  FMA(pair, scale FACTOR, scale -8 UNIT): one step of q becomes scale UNIT
-//   with zero points     MUL(FMA(pair, BIG or SMALL, -z STEP), scale RATIO): steps of STEP first, exactly, and of scale UNIT then
+// What a 16-bit weight is made of, from the pairs of a masked nibble and the scale S 2^-e, below 2^16 and near it for the row's largest (w4_pack.cu):
+//   one step   FMA(pair, scale FACTOR, scale -8 UNIT): one step of q becomes scale UNIT.  For bf16 without zero points, where 8 S is exact
+//   two steps  MUL(FMA(pair, BIG or SMALL, -z STEP), scale): (q - z) STEP first, exactly.  With zero points S z need not be exact; and in f16 the scale
+//              has to stay at the upper end of the range (one step leaves UNIT at 2^-10 of it, where scales below a sixteenth of the row's largest
+//              make subnormal weights): so it does down to 2^-20 of the row's largest
 // Nibbles in bits 4..7 take a sixteenth of the factor.
 template <bool BF16> struct Num;
 template <> struct Num<true> {
-    // a masked nibble is q 2^-133; UNIT 2^-22, STEP 2^-6
-    static constexpr float BACK = 4194304.f, STEP = 1.f / 64;
+    // a masked nibble is q 2^-133
+    static constexpr float UNIT = 1.f / 4194304, STEP = 1.f / 64;
     static constexpr uint32_t BIG_FACTOR = 0x77007700, SMALL_FACTOR = 0x75007500, MINUS_EIGHT = 0xb600b600;       // 2^111, 2^107, -2^-19
-    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00, RATIO = 0x37803780;                           // 2^127, 2^123, 2^-16
+    static constexpr uint32_t BIG = 0x7f007f00, SMALL = 0x7d007d00;                                               // 2^127, 2^123
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rn(v));
@@ -268,10 +270,10 @@ template <> struct Num<true> {
     }
 };
 template <> struct Num<false> {
-    // a masked nibble is q 2^-24; UNIT 2^-25, STEP 2^-9
-    static constexpr float BACK = 33554432.f, STEP = 1.f / 512;
-    static constexpr uint32_t BIG_FACTOR = 0x38003800, SMALL_FACTOR = 0x28002800, MINUS_EIGHT = 0x80048004;       // 2^-1, 2^-5, -2^-22
-    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800, RATIO = 0x01000100;                           // 2^15, 2^11, 2^-16
+    // a masked nibble is q 2^-24
+    static constexpr float UNIT = 0.f, STEP = 1.f / 512;                                                          // always two steps
+    static constexpr uint32_t BIG_FACTOR = 0, SMALL_FACTOR = 0, MINUS_EIGHT = 0;
+    static constexpr uint32_t BIG = 0x78007800, SMALL = 0x68006800;                                               // 2^15, 2^11
     static __device__ __forceinline__ uint32_t both(float v)
     {
         const uint32_t b = __half_as_ushort(__float2half_rn(v));
@@ -312,6 +314,8 @@ enum { PLAIN = 0, SPLIT = 1, EXPERTS = 2 };
 template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
 {
     using N = Num<BF16>;
+    constexpr bool TWO_STEPS = ZEROS || !BF16;
+    constexpr float BACK = 1.f / (TWO_STEPS ? N::STEP : N::UNIT);             // what a sum is multiplied by beside 2^e
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t *const ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);      // the swizzle's groups start at multiples of 1024; the same place in every CTA
@@ -398,7 +402,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
         auto read_back = [&](int i) {
             const Tile t = tile_at(i);
             const int row = t.row0 + r;
-            const float back = N::BACK * p.exponents[t.nt * kW4Rows + r];
+            const float back = BACK * p.exponents[t.nt * kW4Rows + r];
             // where this group's rows of x (16 of every 64) go and their scales, two a lane, read before the wait
             int place[2] = {0, 0};
             float scale[2] = {1.f, 1.f};
@@ -519,9 +523,8 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                 if (!(b & ((1 << p.group_shift) - 1))) {
                     if (p.scale_bf16 == BF16) big = sc[b] | sc[b] << 16;
                     else big = N::both(scale_value(sc[b], p.scale_bf16));
-                    if (ZEROS) {
-                        minus = N::both(-N::STEP * float(z[b]));
-                        big = N::mul(big, N::RATIO);
+                    if (TWO_STEPS) {
+                        minus = N::both(-N::STEP * (ZEROS ? float(z[b]) : 8.f));
                     } else {
                         small = N::mul(big, N::SMALL_FACTOR);
                         minus = N::mul(big, N::MINUS_EIGHT);
@@ -532,7 +535,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                 for (int c = 0; c < 4; ++c) {
                     uint32_t *const to = v[b >> 1] + 16 * (b & 1) + 4 * c;
                     const uint32_t u = w[c][b], uu = u >> 8;
-                    if (ZEROS) {
+                    if (TWO_STEPS) {
                         to[0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), big);
                         to[1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), big);
                         to[2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), big);
@@ -655,7 +658,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                         y.z += part[b].z;
                         y.w += part[b].w;
                     }
-                const float factor = p.x_scale ? N::BACK * p.x_scale[t.t0 + i] : N::BACK;
+                const float factor = p.x_scale ? BACK * p.x_scale[t.t0 + i] : BACK;
                 const uint32_t lo = two_16_bits(y.x * back.x * factor, y.y * back.y * factor, bf16_out), hi = two_16_bits(y.z * back.z * factor, y.w * back.w * factor, bf16_out);
                 uint16_t *out = static_cast<uint16_t *>(p.out) + (t.t0 + i) * p.ldo + t.row0 + c;
                 if (wide) {

@@ -56,3 +56,37 @@ def test_up_to_16_rows_no_weight_is_rounded(dtype, scales, zeros):
         assert torch.equal(columns(lambda x: experts(x, ids, dtype=F16), dtype, 32), want)
         assert torch.equal(columns(lambda x: experts(x, ids, weights=one, dtype=F16), dtype, 32), want)
     binding.strassen_device_status()
+
+
+def check_beyond_16_rows(dtype, scales, zeros):
+    """Each weight is rounded once, to bf16 beside bf16 rows and to 11 bits beside f16 and e4m3 rows, whatever its group's scale; all
+    shapes of the tile kernel: split inner dimension, pairs of CTAs, rows in order of their experts."""
+    rounded = BF16 if dtype == BF16 else F16
+    for rows, m in ((N, 17), (N, 128), (6500, 512)):
+        q, s, z, w = wide_weights(zeros, scales, 2, rows)
+        matrix = sw().W4Matrix(q, s, z, group=GROUP)
+        x = torch.eye(K, device="cuda").to(dtype)
+        parts = [x[i:i + m] if K - i >= m else torch.cat([x[i:], x[:m - K + i]]) for i in range(0, K, m)]
+        got = torch.cat([matrix(p, dtype=F16) for p in parts])[:K].t()
+        assert torch.equal(got, w.float().to(rounded).to(F16))
+    q, s, z, w = wide_weights(zeros, scales, 3)
+    experts = sw().W4Experts(q.view(3, N // 3, -1), s.view(3, N // 3, -1), z.view(3, N // 3, -1) if zeros else None, group=GROUP)
+    for e in range(3):
+        ids = torch.full((128, 1), e, dtype=torch.int32, device="cuda")
+        one = torch.ones(128, 1, device="cuda")
+        want = w[e * N // 3:(e + 1) * N // 3].float().to(rounded).to(F16)
+        assert torch.equal(columns(lambda x: experts(x, ids, dtype=F16), dtype, 128), want)
+        assert torch.equal(columns(lambda x: experts(x, ids, weights=one, dtype=F16), dtype, 128), want)
+    binding.strassen_device_status()
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("scales", [BF16, F16])
+@pytest.mark.parametrize("dtype", [F16, E4M3])
+def test_beyond_16_rows_beside_f16_and_e4m3_rows(dtype, scales, zeros):
+    check_beyond_16_rows(dtype, scales, zeros)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_beyond_16_rows_beside_bf16_rows(zeros):
+    check_beyond_16_rows(BF16, BF16, zeros)
