@@ -76,7 +76,7 @@ struct Args {
     int x_stages, x_bytes;   // up to RING
     int a_buffers;           // GROUPS .. RING
     int out_type;
-    bool scale_bf16, out_pairs;
+    bool scale_bf16, has_zeros, out_pairs;
     const W4Tile *table;     // experts: the tiles of rows and their number; NULL: every `tokens` rows a tile
     const int *table_size;
     const int *order;        // experts: which pair a row of x is
@@ -244,6 +244,8 @@ __device__ __forceinline__ void ld_tmem16(uint32_t (&v)[16], uint32_t at)
 //   two steps  MUL(FMA(pair, BIG or SMALL, -z STEP), scale): (q - z) STEP first, exactly.  With zero points S z need not be exact; and in f16 the scale
 //              has to stay at the upper end of the range (one step leaves UNIT at 2^-10 of it, where scales below a sixteenth of the row's largest
 //              make subnormal weights): so it does down to 2^-20 of the row's largest
+//   and for f16 scales beside bf16 rows, whose 11 bits are two bf16 numbers of 8 and 3 (the product of the second is exact), d = (q - z) STEP:
+//              FMA(d, first, MUL(d, second)), so that the weight is rounded once
 // Nibbles in bits 4..7 take a sixteenth of the factor.
 template <bool BF16> struct Num;
 template <> struct Num<true> {
@@ -309,12 +311,14 @@ __device__ __forceinline__ uint32_t two_16_bits(float lo, float hi, bool bf16)
 }
 
 enum { PLAIN = 0, SPLIT = 1, EXPERTS = 2 };
+// How weights are made: without zero points; with them; of f16 scales for bf16 rows, with or without zero points.
+enum { EIGHT = 0, ZEROS = 1, FINE = 2 };
 
 // BF16: x and weights are bf16, else f16.
-template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
+template <bool BF16, int WEIGHTS, int CTAS, int MODE> __global__ void __launch_bounds__(THREADS, 1) w4_tile_kernel(const Args p, const __grid_constant__ CUtensorMap map)
 {
     using N = Num<BF16>;
-    constexpr bool TWO_STEPS = ZEROS || !BF16;
+    constexpr bool TWO_STEPS = WEIGHTS != EIGHT || !BF16;
     constexpr float BACK = 1.f / (TWO_STEPS ? N::STEP : N::UNIT);             // what a sum is multiplied by beside 2^e
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
@@ -511,7 +515,7 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                 } else {
                     const int at = (b >> p.group_shift) * kW4Rows + place;
                     sc[b] = *reinterpret_cast<const uint16_t *>(stage + kW4NibbleBytes + at * 2);
-                    z[b] = ZEROS ? stage[p.zero_off + at] : 0;
+                    z[b] = WEIGHTS == ZEROS || (WEIGHTS == FINE && p.has_zeros) ? stage[p.zero_off + at] : 8;
                 }
             }
             __syncwarp();
@@ -521,10 +525,17 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 if (!(b & ((1 << p.group_shift) - 1))) {
-                    if (p.scale_bf16 == BF16) big = sc[b] | sc[b] << 16;
-                    else big = N::both(scale_value(sc[b], p.scale_bf16));
+                    if (WEIGHTS == FINE) {
+                        const float scale = scale_value(sc[b], false);
+                        big = N::both(scale);
+                        small = N::both(scale - __uint_as_float(big & 0xffff0000u));
+                    } else if (p.scale_bf16 == BF16) {
+                        big = sc[b] | sc[b] << 16;
+                    } else {
+                        big = N::both(scale_value(sc[b], p.scale_bf16));
+                    }
                     if (TWO_STEPS) {
-                        minus = N::both(-N::STEP * (ZEROS ? float(z[b]) : 8.f));
+                        minus = N::both(-N::STEP * float(z[b]));
                     } else {
                         small = N::mul(big, N::SMALL_FACTOR);
                         minus = N::mul(big, N::MINUS_EIGHT);
@@ -536,10 +547,11 @@ template <bool BF16, bool ZEROS, int CTAS, int MODE> __global__ void __launch_bo
                     uint32_t *const to = v[b >> 1] + 16 * (b & 1) + 4 * c;
                     const uint32_t u = w[c][b], uu = u >> 8;
                     if (TWO_STEPS) {
-                        to[0] = N::mul(N::fma(u & 0x000f000f, N::BIG, minus), big);
-                        to[1] = N::mul(N::fma(u & 0x00f000f0, N::SMALL, minus), big);
-                        to[2] = N::mul(N::fma(uu & 0x000f000f, N::BIG, minus), big);
-                        to[3] = N::mul(N::fma(uu & 0x00f000f0, N::SMALL, minus), big);
+                        const auto weight = [&](uint32_t d) { return WEIGHTS == FINE ? N::fma(d, big, N::mul(d, small)) : N::mul(d, big); };
+                        to[0] = weight(N::fma(u & 0x000f000f, N::BIG, minus));
+                        to[1] = weight(N::fma(u & 0x00f000f0, N::SMALL, minus));
+                        to[2] = weight(N::fma(uu & 0x000f000f, N::BIG, minus));
+                        to[3] = weight(N::fma(uu & 0x00f000f0, N::SMALL, minus));
                     } else {
                         to[0] = N::fma(u & 0x000f000f, big, minus);
                         to[1] = N::fma(u & 0x00f000f0, small, minus);
@@ -858,25 +870,25 @@ struct Shape {
     int ctas, mode, columns, splits, bytes;
 };
 
-template <bool BF16, bool ZEROS, int CTAS, int MODE> cudaError_t launch_one(const Args &p, const CUtensorMap &map, const Shape &shape, cudaStream_t stream)
+template <bool BF16, int WEIGHTS, int CTAS, int MODE> cudaError_t launch_one(const Args &p, const CUtensorMap &map, const Shape &shape, cudaStream_t stream)
 {
     static std::atomic<uint64_t> opted_in{0};        // devices that this kernel has been given its shared memory on
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (!(opted_in.load(std::memory_order_relaxed) >> dev & 1)) {
-        e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
+        e = cudaFuncSetAttribute(w4_tile_kernel<BF16, WEIGHTS, CTAS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit);
         if (e != cudaSuccess) return e;
         opted_in.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
-    return launch_after(w4_tile_kernel<BF16, ZEROS, CTAS, MODE>, dim3(unsigned(shape.columns * CTAS), unsigned(shape.splits)), dim3(THREADS), size_t(shape.bytes), stream, dim3(CTAS, unsigned(shape.splits)), p, map);
+    return launch_after(w4_tile_kernel<BF16, WEIGHTS, CTAS, MODE>, dim3(unsigned(shape.columns * CTAS), unsigned(shape.splits)), dim3(THREADS), size_t(shape.bytes), stream, dim3(CTAS, unsigned(shape.splits)), p, map);
 }
 
-template <bool BF16, bool ZEROS> cudaError_t launch_shape(const Args &p, const CUtensorMap &map, const Shape &s, cudaStream_t stream)
+template <bool BF16, int WEIGHTS> cudaError_t launch_shape(const Args &p, const CUtensorMap &map, const Shape &s, cudaStream_t stream)
 {
-    if (s.mode == EXPERTS) return launch_one<BF16, ZEROS, 2, EXPERTS>(p, map, s, stream);
-    if (s.ctas == 2) return launch_one<BF16, ZEROS, 2, PLAIN>(p, map, s, stream);
-    return s.mode == SPLIT ? launch_one<BF16, ZEROS, 1, SPLIT>(p, map, s, stream) : launch_one<BF16, ZEROS, 1, PLAIN>(p, map, s, stream);
+    if (s.mode == EXPERTS) return launch_one<BF16, WEIGHTS, 2, EXPERTS>(p, map, s, stream);
+    if (s.ctas == 2) return launch_one<BF16, WEIGHTS, 2, PLAIN>(p, map, s, stream);
+    return s.mode == SPLIT ? launch_one<BF16, WEIGHTS, 1, SPLIT>(p, map, s, stream) : launch_one<BF16, WEIGHTS, 1, PLAIN>(p, map, s, stream);
 }
 
 // How many clusters of `size` of these CTAs, one to an SM, the device holds at a time: less than SMs / size, since a cluster lies within
@@ -886,7 +898,7 @@ int clusters_of(int size)
     static std::atomic<int> known[MAX_SPLITS + 1];
     int n = known[size].load(std::memory_order_relaxed);
     if (n > 0) return n;
-    const auto kernel = w4_tile_kernel<true, false, 1, SPLIT>;
+    const auto kernel = w4_tile_kernel<true, EIGHT, 1, SPLIT>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit) != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(64, unsigned(size));
@@ -965,6 +977,7 @@ Args common_args(const W4Args &a)
     p.tile_bytes = a.lay.tile_bytes;
     p.zero_off = a.lay.zero_off();
     p.scale_bf16 = a.lay.scale_type == STRASSEN_BF16;
+    p.has_zeros = a.lay.has_zeros;
     p.out_type = a.out_type;
     p.out_pairs = reinterpret_cast<uintptr_t>(p.out) % 4 == 0 && p.ldo % 2 == 0;
     p.scale_div = 1;
@@ -995,8 +1008,9 @@ cudaError_t launch_tiles(Args p, Shape shape, const W4Args &a, const void *x, in
     if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    if (a.type == STRASSEN_BF16) return a.lay.has_zeros ? launch_shape<true, true>(p, map, shape, stream) : launch_shape<true, false>(p, map, shape, stream);
-    return a.lay.has_zeros ? launch_shape<false, true>(p, map, shape, stream) : launch_shape<false, false>(p, map, shape, stream);
+    if (a.type == STRASSEN_BF16 && !p.scale_bf16) return launch_shape<true, FINE>(p, map, shape, stream);
+    if (a.type == STRASSEN_BF16) return a.lay.has_zeros ? launch_shape<true, ZEROS>(p, map, shape, stream) : launch_shape<true, EIGHT>(p, map, shape, stream);
+    return a.lay.has_zeros ? launch_shape<false, ZEROS>(p, map, shape, stream) : launch_shape<false, EIGHT>(p, map, shape, stream);
 }
 
 // Workspace of the products of experts: the order and its tables, the rows of x in order, and with weights the pairs' results in 32 bits.

@@ -90,3 +90,8 @@ def test_beyond_16_rows_beside_f16_and_e4m3_rows(dtype, scales, zeros):
 @pytest.mark.parametrize("zeros", [False, True])
 def test_beyond_16_rows_beside_bf16_rows(zeros):
     check_beyond_16_rows(BF16, BF16, zeros)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_beyond_16_rows_f16_scales_beside_bf16_rows(zeros):
+    check_beyond_16_rows(BF16, F16, zeros)
