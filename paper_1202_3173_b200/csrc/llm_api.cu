@@ -280,9 +280,10 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
     const int t = type_size(type);
     if (misaligned(x, t) || misaligned(x_scale, 4) || misaligned(out, 2)) return fail(STRASSEN_MISALIGNED, "x, x_scale and out must be aligned to their elements");
     const Range o = rows_of(out, m, l.n, ldo, 2);
-    if (overlap(o, rows_of(x, m, l.k, ldx, t)) || overlap(o, rows_of(x_scale, x_scale ? 1 : 0, m, m, 4)) ||
-        overlap(o, {reinterpret_cast<uintptr_t>(w->packed), reinterpret_cast<uintptr_t>(w->packed) + l.bytes}))
-        return fail(STRASSEN_ALIAS, "out overlaps an input");
+    const Range inputs[] = {rows_of(x, m, l.k, ldx, t), rows_of(x_scale, x_scale ? 1 : 0, m, m, 4),
+                            {reinterpret_cast<uintptr_t>(w->packed), reinterpret_cast<uintptr_t>(w->packed) + l.bytes}};
+    for (const Range &r : inputs)
+        if (overlap(o, r)) return fail(STRASSEN_ALIAS, "out overlaps an input");
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
     const W4Args a = {l, w->packed, m, type, x, ldx, x_scale, out_type, out, ldo, workspace, nullptr, 0, false, nullptr};
@@ -292,8 +293,9 @@ extern "C" int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, con
             return fail(STRASSEN_WORKSPACE_TOO_SMALL, "these rows need a workspace of " + std::to_string(need) + " bytes (strassen_w4_workspace_bytes)");
         if (misaligned(workspace, 256)) return fail(STRASSEN_MISALIGNED, "workspace must be 256-byte aligned");
         const Range ws = {reinterpret_cast<uintptr_t>(workspace), reinterpret_cast<uintptr_t>(workspace) + uintptr_t(need)};
-        if (overlap(ws, o) || overlap(ws, rows_of(x, m, l.k, ldx, t)) || overlap(ws, rows_of(x_scale, x_scale ? 1 : 0, m, m, 4)))
-            return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
+        if (overlap(ws, o)) return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
+        for (const Range &r : inputs)
+            if (overlap(ws, r)) return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
     }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = m <= kThinRows ? launch_w4_thin(a, sms, st) : launch_w4_tiles(a, sms, st);
