@@ -891,13 +891,16 @@ template <bool BF16, int WEIGHTS> cudaError_t launch_shape(const Args &p, const 
     return s.mode == SPLIT ? launch_one<BF16, WEIGHTS, 1, SPLIT>(p, map, s, stream) : launch_one<BF16, WEIGHTS, 1, PLAIN>(p, map, s, stream);
 }
 
-// How many clusters of `size` of these CTAs, one to an SM, the device holds at a time: less than SMs / size, since a cluster lies within
-// one group of SMs (33 of 4 and 15 of 8 on a B200 with 148 SMs).
+// How many clusters of `size` of these CTAs, one to an SM, the current device holds at a time: less than SMs / size, since a cluster lies within
+// one group of SMs (33 of 4 and 15 of 8 on a B200 with 148 SMs).  Devices differ in how their SMs are grouped, so each has its own answer, and with it
+// its own order of sums, whichever device was used first.
 int clusters_of(int size)
 {
-    static std::atomic<int> known[MAX_SPLITS + 1];
-    int n = known[size].load(std::memory_order_relaxed);
-    if (n > 0) return n;
+    constexpr int DEVICES = 64;              // as many as the entry points take
+    static std::atomic<int> known[DEVICES][MAX_SPLITS + 1];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return 0;
+    if ((n = known[dev][size].load(std::memory_order_relaxed)) > 0) return n;
     const auto kernel = w4_tile_kernel<true, EIGHT, 1, SPLIT>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamicLimit) != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg = {};
@@ -912,7 +915,7 @@ int clusters_of(int size)
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
-    known[size].store(n, std::memory_order_relaxed);
+    known[dev][size].store(n, std::memory_order_relaxed);
     return n;
 }
 
