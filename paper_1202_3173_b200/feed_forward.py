@@ -62,12 +62,14 @@ def _first(name, x, types):
 
 
 def _call(index, function, *args):
-    """function(*args, stream) on the device's current stream."""
+    """function(*args, stream) on the device's current stream, whose handle is returned."""
+    stream = _raw_stream(index)
     if index == torch.cuda.current_device():
-        function(*args, _raw_stream(index))
+        function(*args, stream)
     else:
         with torch.cuda.device(index):
-            function(*args, _raw_stream(index))
+            function(*args, stream)
+    return stream
 
 
 def quant_rows(m, k, device="cuda"):
@@ -156,8 +158,9 @@ class _W4:
         ldz = _rows("zeros", zeros.flatten(0, -2), groups, torch.uint8, self._index) if zeros is not None else 0
         q, scales, zeros = q.flatten(0, -2), scales.flatten(0, -2), zeros.flatten(0, -2) if zeros is not None else None
         self._packed = torch.empty(binding.strassen_w4_bytes(h), dtype=torch.uint8, device=self.device)
-        _call(self._index, binding.strassen_w4_pack, h, q.data_ptr(), ldq, scales.data_ptr(), lds, zeros.data_ptr() if zeros is not None else 0,
-              ldz, self._packed.data_ptr())
+        self._stream = _call(self._index, binding.strassen_w4_pack, h, q.data_ptr(), ldq, scales.data_ptr(), lds, zeros.data_ptr() if zeros is not None else 0,
+                             ldz, self._packed.data_ptr())
+        self._others = set()             # handles of the other streams that products were enqueued on
         torch.cuda.current_stream(self.device).synchronize()
 
     @property
@@ -182,17 +185,25 @@ class _W4:
             raise ValueError("the result is bfloat16 or float16, not %s" % out.dtype)
         return out, kind, _rows("out", out, (rows, self.n), out.dtype, self._index)
 
+    def _multiply(self, function, *args):
+        stream = _call(self._index, function, self._h, *args)
+        if stream != self._stream:
+            self._others.add(stream)
+
     def _workspace(self, need):
         # from the allocator of the current stream, which the call is enqueued on: free again when the call is done
         return torch.empty(need, dtype=torch.uint8, device=self.device)
 
     def close(self):
-        """Free the weights.  Products may still be in flight on any stream, so their device is synchronised first."""
+        """Free the weights.  Products may still be in flight: torch's allocator hands the memory out again when the streams that they
+        were enqueued on have passed this point.  Nothing is waited for, so a matrix may also be collected while a graph is being captured."""
         if self._h is not None:
+            h, self._h = self._h, None
+            binding.strassen_w4_destroy(h)
             if getattr(self, "_packed", None) is not None:
-                torch.cuda.synchronize(self.device)
-            binding.strassen_w4_destroy(self._h)
-            self._h = self._packed = None
+                for stream in getattr(self, "_others", ()):
+                    self._packed.record_stream(torch.cuda.ExternalStream(stream, self.device))
+            self._packed = None
 
     def __del__(self):
         try:
@@ -207,7 +218,8 @@ class W4Matrix(_W4):
 
     ``q``: uint8 (n, ceil(k / 2)), two positions a byte, the first in the low half; ``scales``: bfloat16 or float16 (n, ceil(k / group));
     ``zeros``: uint8 of the same shape, 0..15.  They are laid out once into memory of the matrix's own and not referred to afterwards;
-    the constructor waits for that, so the matrix can be used on any stream.
+    the constructor waits for that, so the matrix can be used on any stream that lives as long as it does.  A captured graph does not
+    keep it alive.
     """
 
     def __init__(self, q, scales, zeros=None, k=None, group=128):
@@ -233,7 +245,7 @@ class W4Matrix(_W4):
             if need:
                 workspace = self._workspace(need)
                 ws = workspace.data_ptr()
-        _call(index, binding.strassen_w4_matmul, self._h, m, kind, at, ldx, xs, out_kind, out.data_ptr(), ldo, ws, need)
+        self._multiply(binding.strassen_w4_matmul, m, kind, at, ldx, xs, out_kind, out.data_ptr(), ldo, ws, need)
         return out
 
 
@@ -276,7 +288,7 @@ class W4Experts(_W4):
             need = binding.strassen_w4_experts_workspace_bytes(self._h, tokens, top, weights is not None)
             workspace = self._workspace(need)
             ws = workspace.data_ptr()
-        _call(index, binding.strassen_w4_experts, self._h, tokens, top, i, kind, x.data_ptr(), ldx, rows != tokens, xs, w, out_kind, out.data_ptr(), ldo, ws, need)
+        self._multiply(binding.strassen_w4_experts, tokens, top, i, kind, x.data_ptr(), ldx, rows != tokens, xs, w, out_kind, out.data_ptr(), ldo, ws, need)
         return out
 
 

@@ -31,3 +31,38 @@ def test_a_workspace_in_the_weights_or_an_argument_is_refused():
         assert e.value.status == -4, str(e.value)
     torch.cuda.synchronize()
     assert torch.equal(matrix._packed, before)
+
+
+def test_a_matrix_collected_during_a_capture_leaves_it_whole():
+    q, s, z = weights(300, 512, 64, True, BF16, 3)
+    x, _ = rows(4, 512, BF16, 4)
+    kept, dropped = (sw().W4Matrix(q, s, z, group=64) for _ in range(2))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        want = dropped(x)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        del dropped
+        got = kept(x)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_the_memory_of_a_matrix_is_not_reused_under_products_on_other_streams():
+    n, k = 1024, 4096
+    q, s, z = weights(n, k, 128, False, BF16, 5)
+    x, _ = rows(4, k, BF16, 6)
+    want = sw().W4Matrix(q, s)(x)
+    torch.cuda.synchronize()
+    matrix = sw().W4Matrix(q, s)
+    nbytes, side = matrix.nbytes, torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100000000)             # some 50 ms
+        got = matrix(x)
+    del matrix
+    others = [torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    del others
