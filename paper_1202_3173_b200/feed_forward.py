@@ -6,10 +6,14 @@ current stream.  ``FeedForward`` runs them together as one block; ``python -m pa
 
 Rows are 2-D CUDA tensors whose last dimension is contiguous; rows may be any distance apart (views of wider tensors).  Calls are
 enqueued on the current stream, allocate nothing when ``out`` is given, and can be captured into a CUDA graph.
+
+The operators serve a model and have no backward pass: tensors that require grad are refused unless gradients are off
+(``torch.no_grad()``).  Tensors that are written count as modified in place.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding
 
@@ -23,14 +27,28 @@ _X_TYPES = {t: _TYPES[t] for t in (torch.bfloat16, torch.float16, E4M3)}
 _OUT_TYPES = {t: _TYPES[t] for t in (torch.bfloat16, torch.float16)}
 _SCORES = {"softmax": binding.STRASSEN_SOFTMAX, "sigmoid": binding.STRASSEN_SIGMOID}
 
+# Marks tensors as modified in place.  The public function looks at its argument's type first, which takes as long again.
+_written = getattr(torch._C, "_increment_version", None) or increment_version
+
+# The current device.  The public function looks first whether CUDA has been set up, which the tensors of a call show.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
 # The current stream's handle by device index.  The public way there makes a Stream object first, which costs as much as a launch.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _gradients_off(name):
+    """For a tensor that requires grad: its gradient is not dropped without a word."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires grad, and the operators have no backward pass: detach it, or call them under torch.no_grad()" % name)
 
 
 def _rows(name, t, shape, dtype, index):
     """Distance between the rows of ``t`` after checking it: the kernels index by the sizes alone, so a smaller tensor would be read or
     written out of bounds on the device."""
     if t.dtype is dtype and t.shape == shape and t.get_device() == index:
+        if t.requires_grad:
+            _gradients_off(name)
         ld, step = t.stride()
         if step == 1 or shape[1] == 1:
             return ld
@@ -47,6 +65,8 @@ def _packed(name, t, shape, dtype, index):
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, not %s %s on %s"
                          % (name, dtype, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
+    if t.requires_grad:
+        _gradients_off(name)
     return t.data_ptr()
 
 
@@ -64,7 +84,7 @@ def _first(name, x, types):
 def _call(index, function, *args):
     """function(*args, stream) on the device's current stream, whose handle is returned."""
     stream = _raw_stream(index)
-    if index == torch.cuda.current_device():
+    if index == _current_device():
         function(*args, stream)
     else:
         with torch.cuda.device(index):
@@ -86,7 +106,7 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, out=None):
     write to; its sum may be ``x`` or ``residual`` itself (the residual stream updated in place)."""
     shape, kind, index = _first("x", x, _ROW_TYPES)
     m, k = shape
-    dtype = x.dtype
+    dtype, given = x.dtype, out
     if out is None:
         out = quant_rows(m, k, x.device)
         if residual is not None:
@@ -101,6 +121,8 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, out=None):
         r, h = residual.data_ptr(), out[2].data_ptr()
     w, s = _packed("weight", weight, (k,), dtype, index), _packed("scale", out[1], (m,), torch.float32, index)
     _call(index, binding.strassen_rms_norm_quant, m, k, kind, x.data_ptr(), ldx, r, ldr, w, eps, h, ldh, q.data_ptr(), ldq, s)
+    if given is not None:
+        _written(out)
     return out
 
 
@@ -108,13 +130,15 @@ def silu_mul_quant(gate, up, out=None):
     """silu(gate) * up in 8 bits: (q, scale).  gate and up may be the halves of one tensor."""
     shape, kind, index = _first("gate", gate, _ROW_TYPES)
     m, k = shape
-    dtype = gate.dtype
+    dtype, given = gate.dtype, out
     if out is None:
         out = quant_rows(m, k, gate.device)
     q = out[0]
     ldg, ldu, ldq = _rows("gate", gate, shape, dtype, index), _rows("up", up, shape, dtype, index), _rows("q", q, shape, E4M3, index)
     s = _packed("scale", out[1], (m,), torch.float32, index)
     _call(index, binding.strassen_silu_mul_quant, m, k, kind, gate.data_ptr(), ldg, up.data_ptr(), ldu, q.data_ptr(), ldq, s)
+    if given is not None:
+        _written(out)
     return out
 
 
@@ -125,6 +149,7 @@ def route_experts(logits, top, score="softmax", bias=None, groups=1, top_groups=
     experts of the ``top_groups`` best groups can be chosen.  Logits of -inf leave an expert out; ids are -1, with weight 0, where too few are left."""
     shape, kind, index = _first("logits", logits, _ROW_TYPES)
     tokens, experts = shape
+    given = out
     if score not in _SCORES:
         raise ValueError("score must be one of %s, not %r" % (", ".join(sorted(_SCORES)), score))
     if out is None:
@@ -133,6 +158,8 @@ def route_experts(logits, top, score="softmax", bias=None, groups=1, top_groups=
     i, w = _packed("ids", out[0], (tokens, top), torch.int32, index), _packed("weights", out[1], (tokens, top), torch.float32, index)
     b = 0 if bias is None else _packed("bias", bias, (experts,), torch.float32, index)
     _call(index, binding.strassen_route_experts, tokens, experts, kind, logits.data_ptr(), ld, b, _SCORES[score], groups, top_groups, top, renormalize, factor, i, w)
+    if given is not None:
+        _written(out)
     return out
 
 
@@ -185,11 +212,6 @@ class _W4:
             raise ValueError("the result is bfloat16 or float16, not %s" % out.dtype)
         return out, kind, _rows("out", out, (rows, self.n), out.dtype, self._index)
 
-    def _multiply(self, function, *args):
-        stream = _call(self._index, function, self._h, *args)
-        if stream != self._stream:
-            self._others.add(stream)
-
     def _workspace(self, need):
         # from the allocator of the current stream, which the call is enqueued on: free again when the call is done
         return torch.empty(need, dtype=torch.uint8, device=self.device)
@@ -234,7 +256,7 @@ class W4Matrix(_W4):
         if self._h is None:
             raise ValueError("the matrix has been closed")
         shape, kind, index = _first("x", x, _X_TYPES)
-        m = shape[0]
+        m, given = shape[0], out
         ldx = _rows("x", x, (m, self.k), x.dtype, self._index)
         out, out_kind, ldo = self._output(x, m, out, dtype)
         xs = 0 if x_scale is None else _packed("x_scale", x_scale, (m,), torch.float32, index)
@@ -245,7 +267,11 @@ class W4Matrix(_W4):
             if need:
                 workspace = self._workspace(need)
                 ws = workspace.data_ptr()
-        self._multiply(binding.strassen_w4_matmul, m, kind, at, ldx, xs, out_kind, out.data_ptr(), ldo, ws, need)
+        stream = _call(index, binding.strassen_w4_matmul, self._h, m, kind, at, ldx, xs, out_kind, out.data_ptr(), ldo, ws, need)
+        if stream != self._stream:
+            self._others.add(stream)
+        if given is not None:
+            _written((out,))
         return out
 
 
@@ -276,7 +302,7 @@ class W4Experts(_W4):
         if len(ids.shape) != 2:
             raise ValueError("ids must be tokens x top, not %s" % (tuple(ids.shape),))
         tokens, top = ids.shape
-        rows = shape[0]
+        rows, given = shape[0], out
         if rows != tokens and rows != tokens * top:
             raise ValueError("x has %d rows; %d (one for each token) or %d (one for each id) are needed" % (rows, tokens, tokens * top))
         ldx, i = _rows("x", x, (rows, self.k), x.dtype, self._index), _packed("ids", ids, (tokens, top), torch.int32, index)
@@ -288,7 +314,11 @@ class W4Experts(_W4):
             need = binding.strassen_w4_experts_workspace_bytes(self._h, tokens, top, weights is not None)
             workspace = self._workspace(need)
             ws = workspace.data_ptr()
-        self._multiply(binding.strassen_w4_experts, tokens, top, i, kind, x.data_ptr(), ldx, rows != tokens, xs, w, out_kind, out.data_ptr(), ldo, ws, need)
+        stream = _call(index, binding.strassen_w4_experts, self._h, tokens, top, i, kind, x.data_ptr(), ldx, rows != tokens, xs, w, out_kind, out.data_ptr(), ldo, ws, need)
+        if stream != self._stream:
+            self._others.add(stream)
+        if given is not None:
+            _written((out,))
         return out
 
 

@@ -66,3 +66,46 @@ def test_the_memory_of_a_matrix_is_not_reused_under_products_on_other_streams():
     torch.cuda.synchronize()
     assert torch.equal(got, want)
     del others
+
+
+def test_gradients_are_refused_and_not_dropped():
+    x = torch.randn(4, 64, device="cuda")
+    w, leaf = torch.ones(64, device="cuda"), torch.randn(4, 64, device="cuda", requires_grad=True)
+    q, s, _ = weights(32, 64, 32, False, BF16, 1)
+    m = sw()
+    matrix, experts = m.W4Matrix(q, s, group=32), m.W4Experts(q.view(2, 16, -1), s.view(2, 16, -1), group=32)
+    ids, factor = m.route_experts(x[:, :2], 1)
+    half, leaf16, scale = x.to(BF16), leaf.detach().to(BF16).requires_grad_(), torch.ones(4, device="cuda", requires_grad=True)
+    calls = [lambda: m.rms_norm_quant(leaf, w), lambda: m.rms_norm_quant(x, w.clone().requires_grad_()), lambda: m.rms_norm_quant(x, w, residual=leaf),
+             lambda: m.rms_norm_quant(x, w, residual=x, out=m.quant_rows(4, 64) + (leaf,)), lambda: m.silu_mul_quant(x, leaf), lambda: m.silu_mul_quant(leaf, x),
+             lambda: m.route_experts(leaf, 2), lambda: m.route_experts(x, 2, bias=torch.zeros(64, device="cuda", requires_grad=True)),
+             lambda: matrix(leaf16), lambda: matrix(half, scale), lambda: experts(leaf16, ids), lambda: experts(half, ids, scale),
+             lambda: experts(half, ids, weights=factor.clone().requires_grad_())]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+            pytest.fail("call %d" % i)
+        with torch.no_grad():
+            call()
+        with torch.inference_mode():
+            call()
+
+
+def test_tensors_that_are_written_count_as_modified():
+    x, r, w = torch.randn(4, 64, device="cuda"), torch.randn(4, 64, device="cuda"), torch.ones(64, device="cuda", requires_grad=True)
+    m = sw()
+    loss = (r * w).sum()                         # saves r
+    m.rms_norm_quant(x, torch.ones(64, device="cuda"), residual=r, out=m.quant_rows(4, 64) + (r,))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    q, s, _ = weights(32, 64, 32, False, BF16, 1)
+    matrix, experts = m.W4Matrix(q, s, group=32), m.W4Experts(q.view(2, 16, -1), s.view(2, 16, -1), group=32)
+    ids, factor = m.route_experts(x[:, :2], 1)
+    eight, out, each = m.quant_rows(4, 64), torch.empty(4, 32, device="cuda", dtype=BF16), torch.empty(4, 16, device="cuda", dtype=BF16)
+    written = [*eight, out, each, ids, factor]
+    before = [t._version for t in written]
+    m.silu_mul_quant(x, r, out=eight)
+    m.route_experts(x[:, :2], 1, out=(ids, factor))
+    matrix(x.to(BF16), out=out)
+    experts(x.to(BF16), ids, out=each)
+    assert all(t._version > v for t, v in zip(written, before))
