@@ -332,12 +332,13 @@ class FeedForward:
         self.norm_weight, self.gate_up, self.down, self.eps = norm_weight, gate_up, down, eps
 
     def __call__(self, x, residual):
-        """(y, h): the block's output, to be added to the residual stream h by the next norm."""
+        """(y, h), both of x's type: the block's output, to be added to the residual stream h by the next norm.  Beside float32 rows the products
+        give bfloat16, and y holds its values."""
         q, s, h = rms_norm_quant(x, self.norm_weight, self.eps, residual=residual)
         gu = self.gate_up(q, s, dtype=x.dtype if x.dtype is not torch.float32 else None)
         f = self.down.k
         q, s = silu_mul_quant(gu[:, :f], gu[:, f:])
-        return self.down(q, s, dtype=gu.dtype), h
+        return self.down(q, s, dtype=gu.dtype).to(x.dtype), h
 
 
 class ExpertsFeedForward:
@@ -359,7 +360,7 @@ class ExpertsFeedForward:
         gu = self.gate_up(q, ids, s, dtype=x.dtype if x.dtype is not torch.float32 else None)
         f = self.down.k
         q, s = silu_mul_quant(gu[:, :f], gu[:, f:])
-        return self.down(q, ids, s, weights=weights, dtype=gu.dtype), h
+        return self.down(q, ids, s, weights=weights, dtype=gu.dtype).to(x.dtype), h
 
 
 def _check_block(norm_weight, gate_up, down):

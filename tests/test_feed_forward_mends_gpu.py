@@ -109,3 +109,24 @@ def test_tensors_that_are_written_count_as_modified():
     matrix(x.to(BF16), out=out)
     experts(x.to(BF16), ids, out=each)
     assert all(t._version > v for t, v in zip(written, before))
+
+
+@pytest.mark.parametrize("m", [1, 40])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_blocks_of_every_type_follow_one_another(m, dtype):
+    """A block's output goes into the next block beside its residual stream."""
+    width, inner, experts = 192, 256, 4
+    g = gen(m)
+    made = []
+    for n, k in ((2 * inner, width), (width, inner)):
+        q, s, _ = weights(experts * n, k, 64, False, BF16, n)
+        made.append((sw().W4Matrix(q[:n], s[:n], group=64), sw().W4Experts(q.view(experts, n, -1), s.view(experts, n, -1), group=64)))
+    norm = torch.ones(width, device="cuda", dtype=dtype)
+    router = torch.randn(experts, width, device="cuda", generator=g).to(dtype)
+    blocks = [sw().FeedForward(norm, made[0][0], made[1][0]), sw().ExpertsFeedForward(norm, router, made[0][1], made[1][1], 2), sw().FeedForward(norm, made[0][0], made[1][0])]
+    y, h = (torch.randn(m, width, device="cuda", generator=g).to(dtype) for _ in range(2))
+    for block in blocks:
+        total = y.float() + h.float()
+        y, h = block(y, h)
+        assert y.dtype == dtype and h.dtype == dtype and torch.isfinite(y).all()
+        assert torch.equal(h, total.to(dtype))
