@@ -1,6 +1,6 @@
 // Laying out 4-bit weights, once for a matrix: from rows of packed nibbles to the tiles that the products read (llm.h).
 //
-// Positions past the inner size hold the row's zero point (their value is 0), rows past the matrix the nibble 8 with a scale of 0.
+// Positions past the inner size hold their group's zero point (their value is 0), or past the last group 8 with a scale of 0, as rows past the matrix do.
 // Scales are held as S 2^-e with e such that 2^15 <= max_g |S_g| 2^-e < 2^16 in each row (the upper end of f16), and 2^e (32 bits) apart, in the exponent
 // section; the products multiply their 32-bit sums by 2^e.  Both steps are exact: f16 scales only ever move up.  (Of bf16 scales only those below 2^-141 of
 // their row's largest lose bits.)  A thread writes one 16-byte piece: once for a matrix, at the rate of scattered reads of nibbles; nothing that a
@@ -34,7 +34,8 @@ __global__ void __launch_bounds__(512) pack_weights_kernel(const W4PackArgs p)
     for (int w = 0; w < 4; ++w) {
         const int64_t k0 = kb * kW4Depth + 32 * w + 8 * c;
         uint32_t pad = 8;
-        if (p.lay.has_zeros && real && k0 < p.lay.k) pad = p.zeros[row * p.ldz + k0 / p.lay.group] & 15;
+        // a group that is cut short has its zero point to its end
+        if (p.lay.has_zeros && real && k0 / p.lay.group < (p.lay.k + p.lay.group - 1) / p.lay.group) pad = p.zeros[row * p.ldz + k0 / p.lay.group] & 15;
         uint32_t word = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

@@ -130,3 +130,34 @@ def test_blocks_of_every_type_follow_one_another(m, dtype):
         y, h = block(y, h)
         assert y.dtype == dtype and h.dtype == dtype and torch.isfinite(y).all()
         assert torch.equal(h, total.to(dtype))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("k", [1, 9, 70, 140, 255])
+def test_laid_out_positions_past_the_inner_size_are_worth_nothing(k, group):
+    """The laid-out tiles as their description has them: 128 x 128 nibbles in 16-byte chunks, then scales and zero points of each group."""
+    n = 130
+    q, s, z = weights(n, k, group, True, BF16, k)
+    z[:] = z % 8                                 # no zero point is 8
+    matrix = sw().W4Matrix(q, s, z, k=k, group=group)
+    per_tile, deep = 128 // group, -(-k // 128)
+    size = 8192 + per_tile * 128 * 3
+    data, hq, hz = matrix._packed.cpu(), q.cpu(), z.cpu()
+    for tile in range(2 * deep):
+        t = data[tile * size:(tile + 1) * size]
+        scale = t[8192:8192 + per_tile * 256].view(torch.int16)
+        zero = t[8192 + per_tile * 256:]
+        for r in range(0, 128, 5):
+            place = (r & ~15) | ((r & 7) << 1) | (r >> 3 & 1)
+            for c in range(4):
+                at = (r >> 3) * 512 + (r & 7) * 64 + (c ^ (r >> 1 & 3)) * 16
+                for w in range(4):
+                    word = int(t[at + 4 * w:at + 4 * w + 4].view(torch.int32)) & 0xffffffff
+                    for i in range(8):
+                        inner = 32 * w + 8 * c + i
+                        row, col, g = tile // deep * 128 + r, tile % deep * 128 + inner, inner // group * 128 + place
+                        nibble = word >> (4 * (i >> 1) + 16 * (i & 1)) & 15
+                        if row < n and col < k:
+                            assert nibble == int(hq[row, col // 2]) >> 4 * (col & 1) & 15 and int(zero[g]) == int(hz[row, col // group])
+                        else:
+                            assert nibble == int(zero[g]) or int(scale[g]) == 0
