@@ -466,9 +466,11 @@ void strassen_w4_destroy(strassen_w4 *w);
  *   x_scale   m floats (the scales of 8-bit rows), or NULL for ones
  *   out_type  STRASSEN_BF16 or STRASSEN_F16; out overlaps no input (STRASSEN_ALIAS)
  *   workspace as strassen_w4_workspace_bytes says, NULL if that is 0 (STRASSEN_WORKSPACE_TOO_SMALL)
- * Sums are held in 32 bits and rounded once.  For more than STRASSEN_W4_THIN_ROWS rows the weights are rounded to 16 bits on their way to the
- * tensor cores: to bf16 beside bf16 rows, to f16 beside f16 and e4m3 rows.  NaN and infinities in a row of x reach that row's outputs only.  Any number of calls
- * may use one matrix at a time, on any streams.
+ * Sums are held in 32 bits and rounded once.  Up to STRASSEN_W4_THIN_ROWS rows no weight is rounded, and a row's result has the same bits whatever rows are
+ * beside it.  For more rows each weight S (Q - Z) is rounded once, to 16 bits, on its way to the tensor cores: to bf16 beside bf16 rows; to f16 beside
+ * f16 and e4m3 rows, with all of its 11 bits down to weights of 2^-20 of their row's largest scale.  (A batch that grows beyond STRASSEN_W4_THIN_ROWS rows
+ * changes results by that much.)  NaN and infinities in a row of x reach that row's outputs only.  Any number of calls may use one matrix at a time, on any
+ * streams.
  */
 int strassen_w4_matmul(const strassen_w4 *w, int64_t m, int type, const void *x, int64_t ldx, const float *x_scale, int out_type,
                        void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);

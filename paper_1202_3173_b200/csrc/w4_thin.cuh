@@ -376,7 +376,10 @@ template <int XT, int GS, int RT, int TT, int U, bool ZEROS, int MODE> cudaError
         while (splits < 8 && tiles * WARPS * splits * 2 <= room && p.depth_tiles >= int64_t(splits) * 2 * WARPS) splits *= 2;
     const int staged_rows = MODE == ONE ? int(p.m < 8 * TT ? p.m : 8 * TT) : 1;
     const int64_t depth = MODE == SUM_OF_IDS ? p.depth_tiles : (p.depth_tiles + splits - 1) / splits, fit = (MOST / staged_rows - 64) / (kW4Depth * 2);
-    p.chunk = int(depth < fit ? depth : fit);
+    // as few and as even chunks as fit, each a multiple of WK: a warp's tiles, and with them the order of its sums, then do not depend on how many rows
+    // are staged, and a row's result has the same bits alone and among others
+    const int64_t whole = fit >> p.wk_shift << p.wk_shift, chunks = (depth + whole - 1) / whole, even = (depth + chunks - 1) / chunks, wk = int64_t(1) << p.wk_shift;
+    p.chunk = int(chunks == 1 ? depth : (even + wk - 1) / wk * wk);
     int bytes = staged_rows * (p.chunk * kW4Depth * 2 + 64);
     if (bytes < SUMS) bytes = SUMS;
     const int64_t groups = WARPS >> p.wk_shift;

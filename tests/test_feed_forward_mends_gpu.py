@@ -161,3 +161,15 @@ def test_laid_out_positions_past_the_inner_size_are_worth_nothing(k, group):
                             assert nibble == int(hq[row, col // 2]) >> 4 * (col & 1) & 15 and int(zero[g]) == int(hz[row, col // group])
                         else:
                             assert nibble == int(zero[g]) or int(scale[g]) == 0
+
+
+@pytest.mark.parametrize("n,k", [(64, 200), (4096, 16384), (900, 12345), (40, 40000)])
+def test_a_row_has_the_same_bits_alone_and_among_up_to_16(n, k):
+    q, s, z = weights(n, k, 64, True, BF16, 8)
+    matrix = sw().W4Matrix(q, s, z, k=k, group=64)
+    for dtype in (BF16, E4M3):
+        x, xs = rows(16, k, dtype, 1)
+        part = lambda a, b: matrix(x[a:b], None if xs is None else xs[a:b])  # noqa: E731
+        want = torch.cat([part(i, i + 1) for i in range(16)])
+        for m in (2, 5, 8, 9, 16):
+            assert torch.equal(torch.cat([part(i, min(16, i + m)) for i in range(0, 16, m)]), want)
