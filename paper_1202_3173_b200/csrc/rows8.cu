@@ -397,8 +397,9 @@ template <class T> __device__ __forceinline__ void cut(Words<T> &p, int count)
 
 template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) stream_kernel(const RowArgs p, int slots, int slot_bytes, int stage_at)
 {
+    static_assert(MODE != GATE, "norms only");
     extern __shared__ __align__(16) uint8_t memory[];            // the norm's weights, then the ring
-    constexpr bool TWO = MODE != NORM;                           // two inputs
+    constexpr bool TWO = MODE == NORM_RESIDUAL;                  // two inputs
     uint8_t *const ring = memory + int(blockDim.x) * ITEMS * 8 * int(sizeof(T));
     __shared__ float2 part[2][THREADS / 32];
     __shared__ uint64_t full[MOST_SLOTS];
