@@ -403,11 +403,11 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
     uint8_t *const ring = memory + int(blockDim.x) * ITEMS * 8 * int(sizeof(T));
     __shared__ float2 part[2][THREADS / 32];
     __shared__ uint64_t full[MOST_SLOTS];
-    __shared__ int dead;
+    __shared__ int dead[2];              // a wait gave up; of even and odd turns, so that none is set while it is still being read for the turn before
     if (threadIdx.x == 0) {
         for (int i = 0; i < slots; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&full[i])));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        dead = 0;
+        dead[0] = dead[1] = 0;
     }
     after_work_before();
     __syncthreads();
@@ -464,7 +464,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
     for (int r = blockIdx.x; r < rows; r += step) {
         Words<T> pa[ITEMS], pb[ITEMS];
         if (copied(r)) {
-            if (!wait_for(&full[slot], phases >> slot & 1)) dead = 1;
+            if (!wait_for(&full[slot], phases >> slot & 1)) dead[turn] = 1;
             phases ^= 1u << slot;
             const uint32_t off_a = uint32_t(base_a + r * ld_a) & 15, off_b = uint32_t(base_b + r * ld_b) & 15;
             const uint8_t *const at = ring + slot * slot_bytes;
@@ -520,7 +520,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
         if (lane == 0) part[turn][warp] = make_float2(sq, mx);
         __syncthreads();
         // every thread has its part of the row: its place is free
-        if (dead) break;
+        if (dead[turn]) break;
         if (threadIdx.x == 0) fetch(r + slots * step, slot);
         slot = slot + 1 == slots ? 0 : slot + 1;
         reduce_warps<MODE>(sq, mx, part[turn], warps);
@@ -554,7 +554,7 @@ template <class T, int MODE, int ITEMS, int THREADS> __global__ void __launch_bo
         }
     }
     // given up: the copies that are under way end before the CTA does
-    if (dead)
+    if (dead[0] | dead[1])
         for (int i = 0; i < 10000; ++i) __nanosleep(100);
 }
 
