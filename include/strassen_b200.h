@@ -410,7 +410,8 @@ int strassen_dgemm_static(int64_t n, const double *A, const double *B, double *C
  * strides select the wide accesses.  m = 0 rows is allowed and does nothing.
  *
  * 8-bit rows: v is held as q = e4m3(v / s), rounded to nearest even, with one scale per row, s = max(max|v| / 448, 2^-64): a row of zeros
- * is zeros with s = 2^-64.  A row that holds NaN gives NaN for its scale and throughout its q; so does an infinity in a norm's row.
+ * is zeros with s = 2^-64.  A row that holds NaN gives NaN for its scale and throughout its q; so does a norm's row with an infinity, with a sum
+ * of squares beyond the range of 32 bits (elements of about 2^63), or of zeros where eps is 0.
  */
 typedef enum strassen_type {
     STRASSEN_BF16 = 0,

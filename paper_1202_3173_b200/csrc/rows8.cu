@@ -8,7 +8,7 @@
 // inv > 0 is the same for the whole row, so max_k |v_k| = inv max_k |h_k w_k|: the sum of squares and the maximum come out of ONE
 // reduction, and a row that fits the registers of its CTA is read once.  Sums, the maximum and v are held in 32 bits; the
 // only roundings are h to its own type (the residual stream) and q.  A NaN, or an infinity in a norm's row, makes the
-// row's scale and outputs NaN (the maximum propagates NaN), as the formulas say.
+// row's scale and outputs NaN (the maximum propagates NaN), as the formulas say; so does a row whose squares do not fit 32 bits.
 //
 // A thread has pieces of 8 neighbouring elements.  Rows that do not start at a multiple of 16 bytes (odd lengths, halves of odd rows) are read and
 // written in the same 16-byte accesses: two aligned words around a piece are shifted into place, and on the way out neighbouring lanes pass
@@ -269,7 +269,8 @@ __device__ __forceinline__ float both(Pair v)
 // approximate instructions here too, within two units of the last place.
 template <int MODE> __device__ __forceinline__ float row_factor(float sq, float mx, float over_k, float eps, float &scale)
 {
-    const float inv = MODE == GATE ? 1.f : rsqrtf(sq * over_k + eps);
+    // squares that pass the range of 32 bits make NaN of their row; the root's reciprocal, 0, would make zeros
+    const float inv = MODE == GATE ? 1.f : sq < INFINITY ? rsqrtf(sq * over_k + eps) : NAN;
     const float s = mx * inv * (1.f / kE4M3Max);
     scale = s <= kMinRowScale ? kMinRowScale : s;        // NaN stays NaN
     return __fdividef(inv, scale);

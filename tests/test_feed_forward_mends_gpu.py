@@ -173,3 +173,15 @@ def test_a_row_has_the_same_bits_alone_and_among_up_to_16(n, k):
         want = torch.cat([part(i, i + 1) for i in range(16)])
         for m in (2, 5, 8, 9, 16):
             assert torch.equal(torch.cat([part(i, min(16, i + m)) for i in range(0, 16, m)]), want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,k", [(3, 300), (3, 20000), (700, 100), (5000, 8192)])
+def test_norm_whose_squares_pass_32_bits_is_nan_and_not_zeros(m, k, dtype):
+    x = torch.randn(m, k, device="cuda", generator=gen(k)).to(dtype)
+    x[1] *= 1e25
+    w, fine = torch.ones(k, device="cuda", dtype=dtype), torch.arange(m, device="cuda") != 1
+    for r in (None, torch.zeros_like(x)):
+        q, s = sw().rms_norm_quant(x, w, EPS, residual=r)[:2]
+        assert torch.isnan(s[1]) and torch.isnan(q[1].float()).all()
+        check_rows(q[fine], s[fine], norm64(x[fine], w))
