@@ -163,7 +163,7 @@ template <class T, int V> __global__ void __launch_bounds__(WARPS * 32) route_ke
     }
     if (lane < p.top) {
         p.ids[token * p.top + lane] = id;
-        p.weights[token * p.top + lane] = weight * p.factor;
+        p.weights[token * p.top + lane] = id >= 0 ? weight * p.factor : 0.f;         // 0 whatever the factor, an infinity too
     }
 }
 

@@ -185,3 +185,11 @@ def test_norm_whose_squares_pass_32_bits_is_nan_and_not_zeros(m, k, dtype):
         q, s = sw().rms_norm_quant(x, w, EPS, residual=r)[:2]
         assert torch.isnan(s[1]) and torch.isnan(q[1].float()).all()
         check_rows(q[fine], s[fine], norm64(x[fine], w))
+
+
+def test_experts_that_are_missing_weigh_nothing_whatever_the_factor():
+    logits = torch.randn(2, 16, device="cuda", generator=gen(1))
+    logits[:, 3:] = -float("inf")
+    for score in ("softmax", "sigmoid"):
+        ids, w = sw().route_experts(logits, 5, score=score, factor=float("inf"))
+        assert (ids[:, 3:] == -1).all() and (w[:, 3:] == 0).all() and torch.isinf(w[:, :3]).all()
