@@ -286,7 +286,7 @@ class W4Experts(_W4):
         for t in (q, scales) + (() if zeros is None else (zeros,)):
             if t.shape[0] != q.shape[0] or t.shape[1] != q.shape[1]:
                 raise ValueError("q, scales and zeros must agree in their first two dimensions")
-            if t.shape[0] > 1 and t.stride(0) != t.shape[1] * t.stride(1):
+            if t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * t.stride(1):
                 raise ValueError("the matrices of experts must lie one after another, their rows at one distance")
         self.experts = int(q.shape[0])
         super().__init__(q, scales, zeros, k, group, self.experts)

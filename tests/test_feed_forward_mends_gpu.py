@@ -193,3 +193,13 @@ def test_experts_that_are_missing_weigh_nothing_whatever_the_factor():
     for score in ("softmax", "sigmoid"):
         ids, w = sw().route_experts(logits, 5, score=score, factor=float("inf"))
         assert (ids[:, 3:] == -1).all() and (w[:, 3:] == 0).all() and torch.isinf(w[:, :3]).all()
+
+
+def test_experts_of_one_row_may_lie_at_any_distance():
+    q, s, z = weights(12, 64, 32, True, BF16, 1)
+    shape = lambda t: t.view(4, 3, -1)  # noqa: E731
+    wide = sw().W4Experts(*(shape(t) for t in (q, s, z)), group=32)
+    one = sw().W4Experts(*(shape(t)[:, :1] for t in (q, s, z)), group=32)
+    x, _ = rows(4, 64, BF16, 2)
+    ids = torch.arange(4, device="cuda", dtype=torch.int32)[:, None]
+    assert torch.equal(one(x, ids), wide(x, ids)[:, :1])
