@@ -342,20 +342,30 @@ class FeedForward:
 
 
 class ExpertsFeedForward:
-    """The same with experts: ``gate_up`` and ``down`` are W4Experts, ``router`` (experts x width, of x's type) gives the logits; further arguments are
-    those of ``route_experts``."""
+    """The same with experts: ``gate_up`` and ``down`` are W4Experts; further arguments are those of ``route_experts``.
+
+    ``router`` gives the logits.  As a matrix (experts x width, of x's type) it is multiplied, in 32 bits by torch, by the norm's 8-bit rows, which is
+    what the experts see; their three bits of fraction decide between experts that are close, so that some tokens go to other experts than the unrounded norm
+    would send them to.  A router that was trained on the norm in more bits is given as a function of the residual stream h, which returns the logits
+    (rows x experts): ``lambda h: torch.nn.functional.rms_norm(h, (width,), norm_weight, eps) @ matrix.t()``."""
 
     def __init__(self, norm_weight, router, gate_up, down, top, eps=1e-6, **routing):
         _check_block(norm_weight, gate_up, down)
-        if gate_up.experts != down.experts or tuple(router.shape) != (gate_up.experts, gate_up.k):
-            raise ValueError("%d and %d experts, and a router %s" % (gate_up.experts, down.experts, tuple(router.shape)))
+        if gate_up.experts != down.experts:
+            raise ValueError("%d and %d experts" % (gate_up.experts, down.experts))
+        if not callable(router) and tuple(router.shape) != (gate_up.experts, gate_up.k):
+            raise ValueError("%d experts of width %d, and a router %s" % (gate_up.experts, gate_up.k, tuple(router.shape)))
         self.norm_weight, self.router, self.gate_up, self.down, self.top, self.eps, self.routing = norm_weight, router, gate_up, down, top, eps, routing
 
     def __call__(self, x, residual):
         """(y, h), as FeedForward."""
         q, s, h = rms_norm_quant(x, self.norm_weight, self.eps, residual=residual)
-        # the logits of the norm: its factor for the row is not known here, and the 8-bit rows are what the experts see
-        logits = (q.to(torch.float32) * s[:, None]) @ self.router.float().t()
+        if callable(self.router):
+            logits = self.router(h)
+            if tuple(logits.shape) != (x.shape[0], self.gate_up.experts):
+                raise ValueError("the router gave logits of shape %s for %d rows and %d experts" % (tuple(logits.shape), x.shape[0], self.gate_up.experts))
+        else:
+            logits = (q.to(torch.float32) * s[:, None]) @ self.router.float().t()
         ids, weights = route_experts(logits, self.top, **self.routing)
         gu = self.gate_up(q, ids, s, dtype=x.dtype if x.dtype is not torch.float32 else None)
         f = self.down.k

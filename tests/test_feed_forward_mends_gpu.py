@@ -4,7 +4,7 @@ import torch
 
 from paper_1202_3173_b200 import StrassenError, binding
 
-from .test_feed_forward_gpu import BF16, E4M3, EPS, F16, F32, check_rows, gen, norm64, rows, strided, weights
+from .test_feed_forward_gpu import BF16, E4M3, EPS, F16, F32, check_rows, dense64, gen, norm64, rows, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -203,3 +203,41 @@ def test_experts_of_one_row_may_lie_at_any_distance():
     x, _ = rows(4, 64, BF16, 2)
     ids = torch.arange(4, device="cuda", dtype=torch.int32)[:, None]
     assert torch.equal(one(x, ids), wide(x, ids)[:, :1])
+
+
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_experts_block_whose_router_sees_the_unrounded_norm(tokens):
+    """The experts are those of the norm in 64 bits; the products' tolerance is that of their 8-bit rows, as for the block with a matrix."""
+    width, inner, experts, top = 128, 192, 6, 2
+    made, dense = [], []
+    for n, k in ((2 * inner, width), (width, inner)):
+        q, s, z = weights(experts * n, k, 64, True, BF16, n)
+        made.append(sw().W4Experts(*(t.view(experts, n, -1) for t in (q, s, z)), group=64))
+        dense.append(dense64(q, s, z, k, 64)[0].view(experts, n, k))
+    g = gen(3)
+    norm = (1 + 0.1 * torch.randn(width, device="cuda", generator=g)).to(BF16)
+    matrix = torch.randn(experts, width, device="cuda", generator=g)
+
+    def router(h):
+        v = h.float()
+        return v * (v.square().mean(-1, keepdim=True) + EPS).rsqrt() * norm.float() @ matrix.t()
+    block = sw().ExpertsFeedForward(norm, router, *made, top)
+    x, r = (torch.randn(tokens, width, device="cuda", generator=g).to(BF16) for _ in range(2))
+    y, h = block(x, r)
+    v = norm64(h, norm)
+    logits = v @ matrix.double().t()
+    score, ids = logits.topk(top, 1)
+    assert (logits.topk(top + 1, 1).values.diff(dim=1).abs() > 1e-3).all()       # no two experts are too close to tell in 32 bits
+    f, v = torch.softmax(score, 1), norm64(x, norm, r)
+    want = torch.zeros(tokens, width, dtype=torch.float64, device="cuda")
+    for t in range(tokens):
+        for j in range(top):
+            a, b = (dense[0][ids[t, j]] @ v[t]).split(inner)
+            want[t] += f[t, j] * (dense[1][ids[t, j]] @ (a * torch.special.expit(a) * b))
+    # the roundings of the norm's rows enter both factors of the gate, those of the inner rows come on top: each 2^-4 / sqrt(3) at most, root mean square
+    assert (y.double() - want).norm() <= 3 * 2.0 ** -4 * want.norm()
+    for bad in (lambda h: router(h)[:, :3], lambda h: router(h)[0]):
+        with pytest.raises(ValueError):
+            sw().ExpertsFeedForward(norm, bad, *made, top)(x, r)
+    with pytest.raises(ValueError):
+        sw().ExpertsFeedForward(norm, matrix[:3], *made, top)
