@@ -4,7 +4,7 @@ import torch
 
 from paper_1202_3173_b200 import StrassenError, binding
 
-from .test_feed_forward_gpu import BF16, E4M3, EPS, F16, F32, check_rows, dense64, gen, norm64, rows, weights
+from .test_feed_forward_gpu import BF16, E4M3, EPS, F16, F32, check_rows, dense64, gen, norm64, rows, strided, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -241,3 +241,43 @@ def test_experts_block_whose_router_sees_the_unrounded_norm(tokens):
             sw().ExpertsFeedForward(norm, bad, *made, top)(x, r)
     with pytest.raises(ValueError):
         sw().ExpertsFeedForward(norm, matrix[:3], *made, top)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (7, 0), (1, 3)])
+@pytest.mark.parametrize("k", [1025, 2048, 4099, 8192, 12345])
+def test_sums_in_place_of_x_over_many_megabytes(k, pad, shift, dtype):
+    """Norms with enough to do for CTAs that stay and copy ahead, the sum written over x while later rows of x are on their way."""
+    g = gen(k + pad)
+    m = 90000000 // (k * dtype.itemsize)
+    x = strided(torch.randn(m, k, device="cuda", generator=g).to(dtype), pad, shift)
+    r = torch.randn(m, k, device="cuda", generator=g).to(dtype)
+    w = (1 + 0.3 * torch.randn(k, device="cuda", generator=g)).to(dtype)
+    q, s = sw().quant_rows(m, k)
+    want, v = (x.float() + r.float()).to(dtype), norm64(x, w, r)
+    sw().rms_norm_quant(x, w, EPS, residual=r, out=(q, s, x))
+    check_rows(q, s, v)
+    assert torch.equal(x, want)
+    binding.strassen_device_status()
+
+
+@pytest.mark.parametrize("m", [40, 300])
+def test_block_of_many_rows_in_a_graph(m):
+    """Split inner dimension and pairs of CTAs, with the rows' conversion, captured and replayed on other inputs."""
+    width, inner = 256, 4096
+    made = []
+    for n, k in ((2 * inner, width), (width, inner)):
+        q, s, _ = weights(n, k, 128, False, BF16, n)
+        made.append(sw().W4Matrix(q, s))
+    block = sw().FeedForward(torch.ones(width, device="cuda", dtype=BF16), *made)
+    x, r = (torch.randn(m, width, device="cuda", generator=gen(1)).to(BF16) for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held, _ = block(x, r)
+    other = torch.randn(m, width, device="cuda", generator=gen(2)).to(BF16)
+    want, _ = block(other, r)
+    x.copy_(other)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(held, want)
+    binding.strassen_device_status()
