@@ -492,8 +492,8 @@ size_t strassen_w4_workspace_bytes(const strassen_w4 *w, int64_t m, int type, co
  *   top     1 .. 32: ids (tokens x top) receives the experts of the largest score + bias, in order, the lowest index first among equals;
  *           weights (tokens x top) their scores, divided by their sum if `renormalize`, times `factor`
  * experts 1 .. 1024; type of the logits (leading dimension ld): STRASSEN_BF16, STRASSEN_F16 or STRASSEN_F32; scores in 32 bits.  A logit of -inf
- * or NaN leaves the expert out: it takes no part in the softmax and is never chosen.  Where fewer than `top` are left the ids end in
- * -1 with weight 0.
+ * or NaN leaves the expert out: it takes no part in the softmax and is never chosen; infinite ones share the whole softmax.  A score + bias of -inf or NaN is not
+ * chosen either.  Where fewer than `top` are left the ids end in -1 with weight 0.
  */
 #define STRASSEN_SOFTMAX 0
 #define STRASSEN_SIGMOID 1
@@ -524,7 +524,7 @@ int strassen_w4_experts(const strassen_w4 *w, int64_t tokens, int64_t top, const
  * strassen_device_status -- wait for the current device and say whether one of the feed-forward operators' kernels has given up since
  * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
  * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else
- * STRASSEN_CUDA_ERROR, and the flag is cleared.
+ * STRASSEN_CUDA_ERROR, and the flag is cleared.  Nothing else reports it: a server asks from time to time, between steps.
  */
 int strassen_device_status(void);
 

@@ -12,8 +12,9 @@
 //
 // A thread has pieces of 8 neighbouring elements.  Rows that do not start at a multiple of 16 bytes (odd lengths, halves of odd rows) are read and
 // written in the same 16-byte accesses: two aligned words around a piece are shifted into place, and on the way out neighbouring lanes pass
-// each other the bytes that belong to the other's word.  Bound by HBM for many rows (norm with residual 9600 x 8192 bf16: 90 us, 6.1 TB/s; without 48 us,
-// 4.9 TB/s, gate 57 us, 6.9 TB/s), by shifting and staging where rows are misaligned (4099 x 12345 f16: 78 us, 4.5 TB/s), by launch and latency for few.
+// each other the bytes that belong to the other's word.  Many rows come near HBM: 9600 x 8192 bf16, inputs changing, norm with residual 89 us (6.2 TB/s), without 50 us
+// (4.7 TB/s), gate 58 us (6.7 TB/s, four bytes read for each one written; a copy, which writes as many as it reads, has 6.5).  Misaligned rows pay for shifting and
+// staging (4099 x 12345 f16: 80 us, 4.4 TB/s), few rows for launch and latency.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -224,8 +225,9 @@ __device__ __forceinline__ float max_abs(float m, Pair v)
 }
 
 // A piece's values before the row's factor, v = h w for the norm, silu(g) u for the gate; what they add to the row's sum of squares and maximum; and
-// for a norm with a residual h itself, in its type.  exp and the reciprocal are the approximate instructions: some 2^-21 of a value, against 2^-5 of its
-// rounding to e4m3.
+// for a norm with a residual h itself, in its type.  exp and the reciprocal are the approximate instructions: some 2^-21 of a value for gates of a few units,
+// and, since g log2(e) is rounded once, 2^-24 |g| for large negative ones (2^-17 at -80, where silu is below 2^-109); beyond -87 the reciprocal is flushed to 0.
+// All of it is far below the 2^-4 of the rounding to e4m3.
 template <class T, int MODE> __device__ __forceinline__ void values(const Words<T> &pa, const Words<T> &pb, const Words<T> &pw, Pair (&v)[4], Words<T> &sum, Pair &sq, float &mx)
 {
     float x[8], y[8], w[8];

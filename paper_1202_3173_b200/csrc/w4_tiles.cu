@@ -25,9 +25,11 @@
 // fixed order over distributed shared memory.  Rows of x that a tensor map cannot take as they are (e4m3, other alignments, the rows of an
 // expert's tokens) are first written to the workspace in order, in 16 bits (rows_kernel).
 //
-// Bound by the tensor cores for prompts (4096 x 16384 x 4096, e4m3 with zero points: 342 us with the rows' conversion in a run of calls on one input, 1.6 PFLOP/s,
-// 410 to 422 where the inputs change from call to call, 1.3 PFLOP/s); for tens of rows by what a step costs besides (turning the weights takes a
-// group some 1000 clocks of latency, four groups at a time: 48 x 4096 x 16384 in 16.2 us, 2.4 TB/s).
+// Bound by the tensor cores for prompts (4096 x 16384 x 4096, e4m3 with zero points, with the rows' conversion: 348 us in a run of calls on one input,
+// 1.6 PFLOP/s, and 409 to 413 where the inputs change from call to call, 1.3 PFLOP/s: the power cap).  For tens of rows by latency: 48 x 4096 x 16384 in 16.4 us, 2.4 TB/s.
+// Of the 26 900 clocks of a CTA there, 2 900 pass until its first weights are in shared memory, 18 100 in its 32 steps (a group of warps turns every fourth;
+// from one of its steps to the next it takes 2 260, waits included), 400 to read the results back, 2 000 for the cluster's barrier, 2 200 to
+// add and write the splits' sums, 1 300 for the barrier after that.
 //
 // Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
 #include <cuda.h>
@@ -1029,7 +1031,8 @@ ExpertsSpace experts_space(const W4Args &a)
     const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     ExpertsSpace s;
     s.pairs = a.m * a.top;
-    // Twice the average run (64 tokens, 8 of 64 experts: 80.1 us, 82.6 with tiles of 256, whose ring holds fewer steps), so that few runs take two tiles, and however uneven they are, there are at most half as many tiles again as experts.
+    // Twice the average run, so that few runs take two tiles, and however uneven they are, there are at most half as many tiles again as experts: 8 of 64
+    // experts of 2048 x 2048, 64 tokens 52.5 us, 53.4 with tiles of 256, whose ring holds fewer steps; 512 tokens 64.0 and 66.4; 16 tokens 51 and 50.
     const int64_t twice = (2 * s.pairs / a.lay.experts + 2 * STEP - 1) / (2 * STEP) * (2 * STEP);
     s.tokens = int(twice < LEAST ? LEAST : twice > TOKENS ? TOKENS : twice);
     s.most_tiles = s.pairs / s.tokens + (s.pairs < a.lay.experts ? s.pairs : a.lay.experts);

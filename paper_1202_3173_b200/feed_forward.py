@@ -9,6 +9,9 @@ enqueued on the current stream, allocate nothing when ``out`` is given, and can 
 
 The operators serve a model and have no backward pass: tensors that require grad are refused unless gradients are off
 (``torch.no_grad()``).  Tensors that are written count as modified in place.
+
+Every wait inside a kernel has a limit, after which the kernel returns with results that are not valid.  Calls do not wait for their kernels
+and so cannot say so: ``binding.strassen_device_status()`` waits for the device and raises ``StrassenError`` if it has happened.
 """
 from __future__ import annotations
 
@@ -252,7 +255,10 @@ class W4Matrix(_W4):
 
     def __call__(self, x, x_scale=None, out=None, dtype=None):
         """x @ W.T (m x n) for rows ``x`` (m x k) in bfloat16, float16 or float8_e4m3fn, times ``x_scale`` (m floats: the scales of 8-bit rows).
-        ``dtype``: of the result, bfloat16 or float16; x's own where it has 16 bits, else bfloat16."""
+        ``dtype``: of the result, bfloat16 or float16; x's own where it has 16 bits, else bfloat16.
+
+        Up to 16 rows no weight is rounded, and a row's result does not depend on the rows beside it.  For more rows each weight is rounded once, to
+        bfloat16 beside bfloat16 rows and to float16 beside the others."""
         if self._h is None:
             raise ValueError("the matrix has been closed")
         shape, kind, index = _first("x", x, _X_TYPES)
@@ -295,7 +301,8 @@ class W4Experts(_W4):
         """Products of rows with the matrices that ``ids`` (int32, tokens x top, as ``route_experts`` gives them) name.
 
         ``x`` has a row for each token, or one for each id (row token * top + j).  Without ``weights`` the result has a row for each id; with
-        ``weights`` (float32, tokens x top) one for each token: the weighted sum of its ids' rows.  Ids outside 0 .. experts - 1 are no expert."""
+        ``weights`` (float32, tokens x top) one for each token: the weighted sum of its ids' rows.  Ids outside 0 .. experts - 1 are no expert.
+        Weights of the matrices are rounded as ``W4Matrix`` does it, beyond 32 ids."""
         if self._h is None:
             raise ValueError("the matrices have been closed")
         shape, kind, index = _first("x", x, _X_TYPES)
