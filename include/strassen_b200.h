@@ -521,6 +521,74 @@ int strassen_w4_experts(const strassen_w4 *w, int64_t tokens, int64_t top, const
                         size_t workspace_bytes, void *stream);
 
 /*
+ * Attention of a served model over a paged cache of keys and values.
+ *
+ * Sequence b of a batch has lengths[b] rows (tokens) in the cache, the new ones included.  Row j lies in page table[b][j / page_size], slot j mod
+ * page_size; table is batch x width with a leading dimension.  Its new tokens are its last ones: rows offsets[b] .. offsets[b + 1] - 1 of q (offsets has
+ * batch + 1 entries), or row b alone where offsets is NULL.  The i-th of n new tokens has position lengths[b] - n + i.  lengths, offsets and table are 32-bit
+ * integers in device memory, so that a captured graph can be replayed for other lengths.
+ *
+ * Whatever they hold, memory outside the arguments is not touched: a page number outside 0 .. pages - 1 is no page (its rows read as zeros, and what is
+ * stored there is dropped), a sequence has at most width * page_size rows that are read, and offsets are cut to the rows of q.  Rows of q outside every
+ * sequence, and new tokens of negative position, have no result: what out holds for them stays as it was (strassen_rotate_append, rows outside), or
+ * is zeros (attention of a token that sees nothing).
+ *
+ * A key or a value row is head_size values, a multiple of 8 (e4m3: 16) up to 128.  page_size is a power of two, 8 .. 1024.  k and v have the same strides, in
+ * elements; they and the addresses are multiples of 16 bytes.  With type STRASSEN_E4M3 a row is held in 8 bits as above, its scale in
+ * k_scale or v_scale (packed: pages x kv_heads x page_size floats).
+ *
+ * q, k, v and out are rows of heads: element i of head h of row r is at r * row + h * head + i.  heads is a multiple of kv_heads; heads h * heads / kv_heads
+ * and on share key head h.  All calls are asynchronous on `stream`, allocate nothing, and give the same bits for the same inputs.
+ */
+typedef struct strassen_paged_cache {
+    int type;                    /* STRASSEN_BF16, STRASSEN_F16 or STRASSEN_E4M3 */
+    int kv_heads, head_size, page_size;
+    int64_t pages;
+    void *k, *v;
+    int64_t page_stride, head_stride, row_stride;
+    float *k_scale, *v_scale;    /* STRASSEN_E4M3 only, else NULL */
+} strassen_paged_cache;
+
+/*
+ * strassen_rotate_append -- rotary embedding of queries and keys, and the new tokens' keys and values stored into the cache.
+ *   type         of q, k, v and out: STRASSEN_BF16 or STRASSEN_F16, the cache's if that has 16 bits
+ *   frequencies  rotary / 2 floats; the pair f of a row at position p turns by p * frequencies[f]:
+ *                (x, y) -> (x cos - y sin, x sin + y cos).  Angles are taken in 64 bits.  NULL with rotary 0: nothing turns
+ *   rotary       even, 0 .. head_size: the first values of a row, which turn
+ *   interleaved  0: pair f is values f and f + rotary / 2; else 2 f and 2 f + 1
+ *   q, out       tokens x heads; out receives the turned queries, and may be q itself; heads 0 with both NULL: keys and values alone
+ *   k, v         tokens x kv_heads
+ * Turned keys are held in 32 bits until they are stored, rounded once.  out shares no element with k, v or the cache, nor with q unless it is q.  Two sequences
+ * with new tokens in one page are in order as long as they do not share a slot.
+ */
+int strassen_rotate_append(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
+                           const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, const void *k,
+                           int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head, void *out, int64_t out_row, int64_t out_head,
+                           const float *frequencies, int rotary, int interleaved, void *stream);
+
+/*
+ * strassen_decode_attention -- attention of one new token a sequence (row b of q and of out, at position lengths[b] - 1):
+ *   out_h = sum over j of softmax(scale q_h . k_j) v_j,  j = 0 .. lengths[b] - 1, with a window > 0 the last `window` of them.
+ *   type       of q and out: STRASSEN_BF16 or STRASSEN_F16, the cache's if that has 16 bits
+ *   workspace  as strassen_decode_attention_workspace_bytes says (256-byte aligned; free again once the call's kernels are done)
+ * Scores, the softmax's sums and the result are held in 32 bits; its weights, at most 1, are rounded to 16 bits for the product with the values.  The work is split evenly over
+ * the GPU along the sequences, whatever their lengths.  out does not overlap q.
+ */
+int strassen_decode_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
+                              int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out, int64_t out_row, int64_t out_head,
+                              float scale, int64_t window, void *workspace, size_t workspace_bytes, void *stream);
+size_t strassen_decode_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width);
+
+/*
+ * strassen_prompt_attention -- the same for many new tokens a sequence, each seeing the rows up to its own position (causal), with a window > 0 the
+ * last `window` of those.  offsets as above, not NULL.
+ */
+int strassen_prompt_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
+                              const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out,
+                              int64_t out_row, int64_t out_head, float scale, int64_t window, void *workspace, size_t workspace_bytes, void *stream);
+size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens);
+
+/*
  * strassen_device_status -- wait for the current device and say whether one of the feed-forward operators' kernels has given up since
  * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
  * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else

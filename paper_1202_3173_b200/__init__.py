@@ -11,15 +11,21 @@ from . import binding
 from .binding import StrassenError  # noqa: F401
 
 _FEED_FORWARD = ("W4Matrix", "W4Experts", "FeedForward", "ExpertsFeedForward", "rms_norm_quant", "silu_mul_quant", "route_experts", "quant_rows")
-__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError", *_FEED_FORWARD]
+_ATTENTION = ("PagedCache", "SelfAttention", "rotate_append", "decode_attention", "prompt_attention")
+__all__ = ["Plan", "matmul", "autotune", "binding", "StrassenError", *_FEED_FORWARD, *_ATTENTION]
 
 
 def __getattr__(name):
-    """The feed-forward operators, imported (with torch) on first use."""
+    """The feed-forward and attention operators, imported (with torch) on first use."""
     if name in _FEED_FORWARD:
         from . import feed_forward
         for n in _FEED_FORWARD:
             globals()[n] = getattr(feed_forward, n)
+        return globals()[name]
+    if name in _ATTENTION:
+        from . import attention
+        for n in _ATTENTION:
+            globals()[n] = getattr(attention, n)
         return globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))
 

@@ -45,6 +45,11 @@ class strassen_scheme(ctypes.Structure):
                 ("w", ctypes.POINTER(ctypes.c_int8))]
 
 
+class strassen_paged_cache(ctypes.Structure):
+    _fields_ = [("type", _int), ("kv_heads", _int), ("head_size", _int), ("page_size", _int), ("pages", _i64), ("k", _vp), ("v", _vp),
+                ("page_stride", _i64), ("head_stride", _i64), ("row_stride", _i64), ("k_scale", _vp), ("v_scale", _vp)]
+
+
 class strassen_tune_request(ctypes.Structure):
     _fields_ = [("n", _i64), ("batch", _i64), ("min_base", _i64), ("repetitions", _int), ("max_seconds", ctypes.c_double),
                 ("A", _vp), ("B", _vp), ("C", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("stream", _vp)]
@@ -100,6 +105,11 @@ SYMBOLS = [
     ("strassen_w4_create_experts", _vp, [_i64, _i64, _i64, _int, _int, _int]),
     ("strassen_w4_experts_workspace_bytes", _sz, [_vp, _i64, _i64, _int]),
     ("strassen_w4_experts", _int, [_vp, _i64, _i64, _vp, _int, _vp, _i64, _int, _vp, _vp, _int, _vp, _i64, _vp, _sz, _vp]),
+    ("strassen_rotate_append", _int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _int, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _int, _int, _vp]),
+    ("strassen_decode_attention", _int, [_vp, _i64, _vp, _i64, _i64, _vp, _int, _i64, _vp, _i64, _i64, _vp, _i64, _i64, ctypes.c_float, _i64, _vp, _sz, _vp]),
+    ("strassen_decode_attention_workspace_bytes", _sz, [_vp, _i64, _i64, _i64]),
+    ("strassen_prompt_attention", _int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _int, _i64, _vp, _i64, _i64, _vp, _i64, _i64, ctypes.c_float, _i64, _vp, _sz, _vp]),
+    ("strassen_prompt_attention_workspace_bytes", _sz, [_vp, _i64, _i64, _i64, _i64]),
     ("strassen_device_status", _int, []),
     ("strassen_last_error", _cp, []),
 ]
@@ -374,3 +384,33 @@ def strassen_w4_experts(matrices: int, tokens: int, top: int, ids: int, type: in
                         out_type: int, out: int, ldo: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
     _check(lib().strassen_w4_experts(matrices, tokens, top, ids, type, x, ldx, int(each), x_scale, weights, out_type, out, ldo, workspace,
                                      workspace_bytes, stream))
+
+
+def strassen_rotate_append(cache: int, batch: int, table: int, ld_table: int, width: int, lengths: int, offsets: int, tokens: int, type: int, heads: int,
+                           q: int, q_row: int, q_head: int, k: int, k_row: int, k_head: int, v: int, v_row: int, v_head: int, out: int, out_row: int,
+                           out_head: int, frequencies: int, rotary: int, interleaved: bool, stream: int = 0) -> None:
+    """cache: address of a strassen_paged_cache."""
+    _check(lib().strassen_rotate_append(cache, batch, table, ld_table, width, lengths, offsets, tokens, type, heads, q, q_row, q_head, k, k_row, k_head,
+                                        v, v_row, v_head, out, out_row, out_head, frequencies, rotary, interleaved, stream))
+
+
+def strassen_decode_attention(cache: int, batch: int, table: int, ld_table: int, width: int, lengths: int, type: int, heads: int, q: int, q_row: int,
+                              q_head: int, out: int, out_row: int, out_head: int, scale: float, window: int, workspace: int = 0,
+                              workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().strassen_decode_attention(cache, batch, table, ld_table, width, lengths, type, heads, q, q_row, q_head, out, out_row, out_head, scale,
+                                           window, workspace, workspace_bytes, stream))
+
+
+def strassen_decode_attention_workspace_bytes(cache: int, batch: int, heads: int, width: int) -> int:
+    return lib().strassen_decode_attention_workspace_bytes(cache, batch, heads, width)
+
+
+def strassen_prompt_attention(cache: int, batch: int, table: int, ld_table: int, width: int, lengths: int, offsets: int, tokens: int, type: int,
+                              heads: int, q: int, q_row: int, q_head: int, out: int, out_row: int, out_head: int, scale: float, window: int,
+                              workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().strassen_prompt_attention(cache, batch, table, ld_table, width, lengths, offsets, tokens, type, heads, q, q_row, q_head, out, out_row,
+                                           out_head, scale, window, workspace, workspace_bytes, stream))
+
+
+def strassen_prompt_attention_workspace_bytes(cache: int, batch: int, heads: int, width: int, tokens: int) -> int:
+    return lib().strassen_prompt_attention_workspace_bytes(cache, batch, heads, width, tokens)

@@ -1,0 +1,96 @@
+// Attention operators: what the host entry points (attention_api.cu) and the kernels share.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "strassen_b200.h"
+
+namespace strassen {
+
+constexpr int kMostHeadSize = 128, kMostHeads = 1024, kLeastPage = 8, kMostPage = 1024;
+
+// The cache as kernels see it; strides in bytes.
+struct CacheArgs {
+    int type, kv_heads, d, page_shift;       // rows of d values; 1 << page_shift rows of a head in a page
+    int64_t pages;
+    uint8_t *k, *v;
+    int64_t page_stride, head_stride, row_stride;
+    float *k_scale, *v_scale;                // e4m3: one for each row, (page * kv_heads + head) << page_shift | slot
+};
+
+// Where the sequences are.  offsets NULL: one new token each.
+struct SequenceArgs {
+    int batch, width;                        // entries of a row of the table
+    const int *table;
+    int64_t ld_table;
+    const int *lengths, *offsets;
+    int64_t tokens;                          // rows of q
+};
+
+struct Heads {
+    const void *p;
+    int64_t row, head;                       // elements between rows, between the heads of a row
+};
+
+struct AppendArgs {
+    CacheArgs cache;
+    SequenceArgs seq;
+    int type, heads;                         // heads 0: there is no q
+    Heads q, k, v;
+    void *out;
+    int64_t out_row, out_head;
+    const float *frequencies;
+    int rotary, interleaved;
+    bool wide;                               // all rows start at multiples of 16 bytes
+};
+
+struct AttentionArgs {
+    CacheArgs cache;
+    SequenceArgs seq;
+    int type, heads;
+    Heads q;
+    void *out;
+    int64_t out_row, out_head;
+    float scale;
+    int window;                              // 0: none
+    void *workspace;
+};
+
+cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t stream);
+int64_t decode_workspace(const AttentionArgs &a, int sm_count);
+cudaError_t launch_decode(const AttentionArgs &a, int sm_count, cudaStream_t stream);
+int64_t prompt_workspace(const AttentionArgs &a, int sm_count);
+cudaError_t launch_prompt(const AttentionArgs &a, int sm_count, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// The new tokens of sequence b: rows first .. end - 1 of q, whatever offsets hold; the last one is at position lengths[b] - 1.
+struct NewTokens {
+    int64_t first, end;
+    int length;
+};
+__device__ __forceinline__ NewTokens new_tokens(const SequenceArgs &s, int b)
+{
+    NewTokens n;
+    n.length = s.lengths[b];
+    n.first = b;
+    n.end = b + 1;
+    if (s.offsets) {
+        const int64_t first = s.offsets[b], end = s.offsets[b + 1];
+        n.first = first < 0 ? 0 : first < s.tokens ? first : s.tokens;
+        n.end = end < n.first ? n.first : end < s.tokens ? end : s.tokens;
+    }
+    return n;
+}
+// The page of row j of sequence b, -1 if there is none.
+__device__ __forceinline__ int page_of(const CacheArgs &c, const SequenceArgs &s, int b, int64_t j)
+{
+    const int64_t at = j >> c.page_shift;
+    if (at >= s.width) return -1;
+    const int page = s.table[b * s.ld_table + at];
+    return uint32_t(page) < uint64_t(c.pages) ? page : -1;
+}
+#endif
+
+}  // namespace strassen
