@@ -85,9 +85,7 @@ cudaError_t launch(const AttentionArgs &a, cudaStream_t stream)
 
 }  // namespace
 
-int64_t decode_workspace(const AttentionArgs &, int) { return 0; }
 int64_t prompt_workspace(const AttentionArgs &, int) { return 0; }
-cudaError_t launch_decode(const AttentionArgs &a, int, cudaStream_t stream) { return launch(a, stream); }
 cudaError_t launch_prompt(const AttentionArgs &a, int, cudaStream_t stream) { return launch(a, stream); }
 
 }  // namespace strassen
