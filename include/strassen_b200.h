@@ -581,7 +581,7 @@ size_t strassen_decode_attention_workspace_bytes(const strassen_paged_cache *cac
 
 /*
  * strassen_prompt_attention -- the same for many new tokens a sequence, each seeing the rows up to its own position (causal), with a window > 0 the
- * last `window` of those.  offsets as above, not NULL.
+ * last `window` of those.  offsets as above, not NULL.  q is 16-byte aligned, its strides multiples of 16 bytes (STRASSEN_MISALIGNED).
  */
 int strassen_prompt_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                               const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out,
@@ -589,7 +589,7 @@ int strassen_prompt_attention(const strassen_paged_cache *cache, int64_t batch, 
 size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens);
 
 /*
- * strassen_device_status -- wait for the current device and say whether one of the feed-forward operators' kernels has given up since
+ * strassen_device_status -- wait for the current device and say whether one of the feed-forward and attention operators' kernels has given up since
  * the last call: every wait inside it (for its copies, for its tensor instructions) has a limit, after which it
  * raises a flag, frees what it holds and returns with results that are not valid.  STRASSEN_OK if none has, else
  * STRASSEN_CUDA_ERROR, and the flag is cleared.  Nothing else reports it: a server asks from time to time, between steps.

@@ -179,6 +179,9 @@ def _attention(q, cache, table, lengths, offsets, scale, window, out):
     if scale is None:
         scale = size ** -0.5
     ws = need = 0
+    if offsets is not None and (q.data_ptr() | 2 * q_row | 2 * q_head) % 16:
+        q = torch.empty(shape, dtype=q.dtype, device=cache.device).copy_(q)         # prompts are read in boxes that start at multiples of 16 bytes
+        q_row, q_head, _ = q.stride()
     if offsets is None:
         need = binding.strassen_decode_attention_workspace_bytes(cache._at, batch, heads, width)
     else:

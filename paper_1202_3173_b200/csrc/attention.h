@@ -62,6 +62,8 @@ cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t stream
 int64_t decode_workspace(const AttentionArgs &a, int sm_count);
 cudaError_t launch_decode(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 int64_t prompt_workspace(const AttentionArgs &a, int sm_count);
+cudaError_t launch_simple(const AttentionArgs &a, cudaStream_t stream);
+cudaError_t prompt_gave_up(int *flag);        // reads and clears the flag of prompt_attention.cu
 cudaError_t launch_prompt(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 
 #ifdef __CUDACC__

@@ -227,6 +227,7 @@ extern "C" int strassen_prompt_attention(const strassen_paged_cache *cache, int6
     if (rc != STRASSEN_OK) return rc;
     if (batch > 0 && !offsets) return fail(STRASSEN_INVALID_ARG, "offsets must be non-NULL");
     if (batch == 0 || tokens == 0) return STRASSEN_OK;
+    if (!wide_strides(reinterpret_cast<uintptr_t>(q), a.q.row, a.q.head, 2)) return fail(STRASSEN_MISALIGNED, "q must be 16-byte aligned, with strides that are multiples of 16 bytes");
     int sms = 0;
     if ((rc = current_device(&sms)) != STRASSEN_OK) return rc;
     if ((rc = check_workspace(a, prompt_workspace(a, sms), workspace_bytes, "strassen_prompt_attention_workspace_bytes")) != STRASSEN_OK) return rc;

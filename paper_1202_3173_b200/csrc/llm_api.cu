@@ -5,6 +5,7 @@
 #include <new>
 #include <string>
 
+#include "attention.h"
 #include "entry.h"
 #include "llm.h"
 
@@ -311,10 +312,11 @@ extern "C" int strassen_device_status(void)
     int sms = 0, rc = current_device(&sms);
     if (rc != STRASSEN_OK) return rc;
     cudaError_t e = cudaDeviceSynchronize();
-    int tiles = 0, rows = 0;
+    int tiles = 0, rows = 0, prompts = 0;
     if (e == cudaSuccess) e = read_gave_up(&tiles);
     if (e == cudaSuccess) e = rows8_gave_up(&rows);
+    if (e == cudaSuccess) e = prompt_gave_up(&prompts);
     if (e != cudaSuccess) return cuda_fail(e, "reading the device's status");
-    if (tiles || rows) return fail(STRASSEN_CUDA_ERROR, "a kernel gave up waiting for its own copies or tensor instructions; its results are not valid");
+    if (tiles || rows || prompts) return fail(STRASSEN_CUDA_ERROR, "a kernel gave up waiting for its own copies or tensor instructions; its results are not valid");
     return STRASSEN_OK;
 }

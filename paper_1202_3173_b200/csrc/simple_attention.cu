@@ -78,14 +78,11 @@ __global__ void __launch_bounds__(128) attention_kernel(const AttentionArgs p)
         }
 }
 
-cudaError_t launch(const AttentionArgs &a, cudaStream_t stream)
+}  // namespace
+
+cudaError_t launch_simple(const AttentionArgs &a, cudaStream_t stream)
 {
     return launch_after(attention_kernel, dim3(unsigned(a.seq.tokens), unsigned((a.heads + 3) / 4)), dim3(128), 0, stream, dim3(1, 1), a);
 }
-
-}  // namespace
-
-int64_t prompt_workspace(const AttentionArgs &, int) { return 0; }
-cudaError_t launch_prompt(const AttentionArgs &a, int, cudaStream_t stream) { return launch(a, stream); }
 
 }  // namespace strassen
