@@ -581,12 +581,12 @@ size_t strassen_decode_attention_workspace_bytes(const strassen_paged_cache *cac
 
 /*
  * strassen_prompt_attention -- the same for many new tokens a sequence, each seeing the rows up to its own position (causal), with a window > 0 the
- * last `window` of those.  offsets as above, not NULL.  q is 16-byte aligned, its strides multiples of 16 bytes (STRASSEN_MISALIGNED).
+ * last `window` of those.  offsets as above, not NULL.  The workspace is 0 bytes but for few tokens behind many rows.  q is 16-byte aligned, its strides multiples of 16 bytes (STRASSEN_MISALIGNED).
  */
 int strassen_prompt_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                               const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out,
                               int64_t out_row, int64_t out_head, float scale, int64_t window, void *workspace, size_t workspace_bytes, void *stream);
-size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens);
+size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens, int64_t window);
 
 /*
  * strassen_device_status -- wait for the current device and say whether one of the feed-forward and attention operators' kernels has given up since

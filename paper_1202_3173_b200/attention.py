@@ -185,7 +185,7 @@ def _attention(q, cache, table, lengths, offsets, scale, window, out):
     if offsets is None:
         need = binding.strassen_decode_attention_workspace_bytes(cache._at, batch, heads, width)
     else:
-        need = binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, heads, width, tokens)
+        need = binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, heads, width, tokens, window)
     if need:
         # from the allocator of the current stream, which the call is enqueued on: free again when the call is done
         workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)

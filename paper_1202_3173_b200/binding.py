@@ -109,7 +109,7 @@ SYMBOLS = [
     ("strassen_decode_attention", _int, [_vp, _i64, _vp, _i64, _i64, _vp, _int, _i64, _vp, _i64, _i64, _vp, _i64, _i64, ctypes.c_float, _i64, _vp, _sz, _vp]),
     ("strassen_decode_attention_workspace_bytes", _sz, [_vp, _i64, _i64, _i64]),
     ("strassen_prompt_attention", _int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _int, _i64, _vp, _i64, _i64, _vp, _i64, _i64, ctypes.c_float, _i64, _vp, _sz, _vp]),
-    ("strassen_prompt_attention_workspace_bytes", _sz, [_vp, _i64, _i64, _i64, _i64]),
+    ("strassen_prompt_attention_workspace_bytes", _sz, [_vp, _i64, _i64, _i64, _i64, _i64]),
     ("strassen_device_status", _int, []),
     ("strassen_last_error", _cp, []),
 ]
@@ -412,5 +412,5 @@ def strassen_prompt_attention(cache: int, batch: int, table: int, ld_table: int,
                                            out_head, scale, window, workspace, workspace_bytes, stream))
 
 
-def strassen_prompt_attention_workspace_bytes(cache: int, batch: int, heads: int, width: int, tokens: int) -> int:
-    return lib().strassen_prompt_attention_workspace_bytes(cache, batch, heads, width, tokens)
+def strassen_prompt_attention_workspace_bytes(cache: int, batch: int, heads: int, width: int, tokens: int, window: int) -> int:
+    return lib().strassen_prompt_attention_workspace_bytes(cache, batch, heads, width, tokens, window)

@@ -61,6 +61,7 @@ struct AttentionArgs {
 cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t stream);
 int64_t decode_workspace(const AttentionArgs &a, int sm_count);
 cudaError_t launch_decode(const AttentionArgs &a, int sm_count, cudaStream_t stream);
+bool prompt_takes(const AttentionArgs &a, int sm_count);          // there are not too many tokens and heads
 int64_t prompt_workspace(const AttentionArgs &a, int sm_count);
 cudaError_t launch_simple(const AttentionArgs &a, cudaStream_t stream);
 cudaError_t prompt_gave_up(int *flag);        // reads and clears the flag of prompt_attention.cu

@@ -125,11 +125,11 @@ int check_workspace(const AttentionArgs &a, int64_t need, size_t given, const ch
 }
 
 // Sizes alone, for the workspace queries.
-bool sizes_only(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens, AttentionArgs *to)
+bool sizes_only(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens, int64_t window, AttentionArgs *to)
 {
     CacheArgs c = {};
-    if (check_cache(cache, &c) != STRASSEN_OK || batch < 0 || batch > kMaxExtent || width < 0 || width > kMaxExtent || tokens < 0 || tokens > kMaxExtent || heads < 1 ||
-        heads > kMostHeads || heads % c.kv_heads != 0)
+    if (check_cache(cache, &c) != STRASSEN_OK || batch < 0 || batch > kMaxExtent || width < 0 || width > kMaxExtent || tokens < 0 || tokens > kMaxExtent || window < 0 ||
+        heads < 1 || heads > kMostHeads || heads % c.kv_heads != 0)
         return false;
     *to = {};
     to->cache = c;
@@ -137,6 +137,7 @@ bool sizes_only(const strassen_paged_cache *cache, int64_t batch, int64_t heads,
     to->seq.width = int(width);
     to->seq.tokens = tokens;
     to->heads = int(heads);
+    to->window = window > 0x7fffffff ? 0x7fffffff : int(window);
     return true;
 }
 
@@ -213,7 +214,7 @@ extern "C" size_t strassen_decode_attention_workspace_bytes(const strassen_paged
 {
     AttentionArgs a;
     int sms = 0;
-    if (!sizes_only(cache, batch, heads, width, batch, &a) || current_device(&sms) != STRASSEN_OK) return 0;
+    if (!sizes_only(cache, batch, heads, width, batch, 0, &a) || current_device(&sms) != STRASSEN_OK) return 0;
     return size_t(decode_workspace(a, sms));
 }
 
@@ -230,15 +231,16 @@ extern "C" int strassen_prompt_attention(const strassen_paged_cache *cache, int6
     if (!wide_strides(reinterpret_cast<uintptr_t>(q), a.q.row, a.q.head, 2)) return fail(STRASSEN_MISALIGNED, "q must be 16-byte aligned, with strides that are multiples of 16 bytes");
     int sms = 0;
     if ((rc = current_device(&sms)) != STRASSEN_OK) return rc;
+    if (!prompt_takes(a, sms)) return fail(STRASSEN_INVALID_ARG, "too many tokens and heads for one call");
     if ((rc = check_workspace(a, prompt_workspace(a, sms), workspace_bytes, "strassen_prompt_attention_workspace_bytes")) != STRASSEN_OK) return rc;
     const cudaError_t e = launch_prompt(a, sms, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? STRASSEN_OK : cuda_fail(e, "kernel launch");
 }
 
-extern "C" size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens)
+extern "C" size_t strassen_prompt_attention_workspace_bytes(const strassen_paged_cache *cache, int64_t batch, int64_t heads, int64_t width, int64_t tokens, int64_t window)
 {
     AttentionArgs a;
     int sms = 0;
-    if (!sizes_only(cache, batch, heads, width, tokens, &a) || current_device(&sms) != STRASSEN_OK) return 0;
+    if (!sizes_only(cache, batch, heads, width, tokens, window, &a) || current_device(&sms) != STRASSEN_OK) return 0;
     return size_t(prompt_workspace(a, sms));
 }

@@ -2,23 +2,28 @@
 //
 // A row of a tile is a head of a token: the heads that share a key head and as many tokens as make up to 128 rows, so few tokens fill a tile as long as there
 // are many heads.  A CTA has two tiles (Q0, Q1) of neighbouring tokens and goes along the cache 128 rows (K, V) at a time:
-//     S (128 x 128, 32 bits, tensor memory) = Q K^T;   P = 2^(c S - M), rounded to 16 bits, over S;   O (128 x head_size, tensor memory) += P V
+//     S (128 x 128, 32 bits, tensor memory) = Q K^T;   P = 2^(c S - M), rounded to 16 bits, tensor memory;   O (128 x head_size, tensor memory) += P V
 // with a running maximum M and the rows' sums in registers.  12 warps:
 //   * warps 0-3 and 4-7: the softmax of tile 0 and 1, a thread a row.  O is scaled down only when a row's maximum has grown by more than 2^8: until
-//     then M stays as it is, which the division at the end makes good (weights are at most 2^8, in f16 2^14: RAISE).  No barrier is needed
-//     for that: S of the next rows is issued behind P V of these, so when S has arrived O is at rest;
+//     then M stays as it is, which the division at the end makes good (weights are at most 2^8, in f16 2^14: RAISE);
 //   * warp 8 brings Q, K and V by tensor-map copies, a page or a part of it a box, and a ring of tiles;
-//   * one lane of warp 9 issues the products.  While one tile's rows are in the softmax, the other's products run;
-//   * warp 10 clears the rows of V that no row of the CTA sees (a page's slots behind the sequence may hold NaN, and 0 * NaN is NaN);
-//   * warp 11 finds out what there is to do, ahead of the others.
+//   * one lane of warp 9 issues the products.  S has one place in tensor memory, which both tiles use in turn: its columns are read into registers at once, so
+//     that the next S is formed while the weights of this one are;
+//   * warp 11 clears the rows of V that no row of the CTA sees (a page's slots behind the sequence may hold NaN, and 0 * NaN is NaN);
+//   * warp 10 finds out what there is to do, ahead of the others.
 // The CTAs stay and take blocks of tokens, the last ones, which see most, first; in every other round in the opposite order, which evens out what they cost.
+// Where there are fewer blocks than SMs and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens behind
+// 8000: 28 us, 98 in one part).
 //
 // What a token does not see has no effect on it.  Scores are replaced, but a weight of 0 times a value that is no number is none either.  So where a tile holds rows that some of the
-// CTA's tokens see and some do not, warp 10 looks for such values of V, puts zeros in their place and raises a flag; then the tokens that do see them
+// CTA's tokens see and some do not, warp 11 looks for such values of V, puts zeros in their place and raises a flag; then the tokens that do see them
 // add them at the end, from memory.
 //
-// Bound by the tensor cores and the special-function units alike: a tile of 128 x 128 scores of head_size 128 takes 1024 clocks of each (8192
-// operations and 16 exponentials a clock).
+// Bound, for head_size 128, by power: 16384 tokens of 32 heads over 8 in 1.68 ms, 1.31 PFLOP/s, at 1.49 GHz (sampled in the kernel), where the tensor cores are busy for 2048 of
+// 2830 clocks of a pair of tiles; cuBLAS keeps up 1.38.  In short runs at 1.75 GHz 8192 tokens take 407 us, 1.35 PFLOP/s.  For smaller heads by the softmax: 128 exponentials
+// of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a scheduler and 2150 for two (timed alone), 2900 here.  What was tried: P over S, and S formed
+// behind P V (the first form): 462 us at 8192 tokens; a quarter of the exponentials by a polynomial of degree 4: 446 instead of 407; two threads a row: 570; warps
+// of exponentials in turns: 448 instead of 436; two places for S at head_size 64: the same.
 //
 // Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
 #include <cuda.h>
@@ -38,9 +43,13 @@ namespace {
 using namespace tc;
 
 constexpr int TILE = 128;                            // rows of Q and of K and V
-constexpr int LOAD_WARP = 8, MMA_WARP = 9, CLEAR_WARP = 10, PLAN_WARP = 11, THREADS = 32 * 12;
+constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, PLAN_WARP = 10, THREADS = 32 * 12;       // and one that clears
+constexpr int SOFTMAX_REGISTERS = 208, OTHER_REGISTERS = 88;
+// Columns of tensor memory: S, which both tiles of Q use in turn; P and O of each.
+constexpr int S_AT = 0, P_AT = TILE, P_WIDTH = TILE / 2, O_AT = 2 * TILE;
 constexpr int PLANS = 4, BLOCK = TILE * 128;         // bytes of a block of 64 values of 128 rows
-constexpr int64_t kWaitLimit = int64_t(1) << 31;     // clocks of a wait, about a second
+constexpr int64_t kWaitLimit = int64_t(1) << 36;     // clocks of a wait for others to be through with a block: 2^24 tiles of the longest sequence take as long
+constexpr int LEAST_TILES = 2;                       // tiles of K and V in a part (200 tokens of 8 heads over 2 behind 1000: 14.8 us; of 4: 18.7)
 
 // Set by a CTA that gave up on a wait; read and cleared by strassen_device_status.
 __device__ int g_gave_up;
@@ -50,9 +59,16 @@ struct Args {
     int heads, blocks;       // heads of a key head in a tile, and how many such blocks of heads a key head has
     int group;               // heads of a key head
     int tokens;              // of a tile
+    int block;               // of a block: of one tile or of two
     int box;                 // rows of K and V in a copy
     bool wide;               // out's rows start at multiples of 16 bytes
+    int parts;               // of a block's rows of the cache
+    float *sums;             // parts > 1: part_floats() for each part of each block
 };
+
+// A part: what it is of, M, the sum of weights, and O in fours of columns, of the rows of both tiles.
+constexpr int HEADER = 4;
+__host__ __device__ constexpr int64_t part_floats(int d) { return HEADER + 2 * TILE * int64_t(2 + d); }
 
 // What there is to do for one block of tokens and heads.
 struct Plan {
@@ -64,6 +80,7 @@ struct Plan {
     int from[2], to[2];      // tiles of K and V for each tile of Q; none: from == to
     int sees_from, sees_to;  // rows that some token sees ..
     int all_from, all_to;    // .. and that all see
+    int slot;                // where its sums go
     int bad;                 // a value of V was no number where not all see it
     __device__ __forceinline__ int first() const { return from[0] == to[0] ? from[1] : from[1] == to[1] || from[0] < from[1] ? from[0] : from[1]; }
     __device__ __forceinline__ int end() const { return to[0] > to[1] ? to[0] : to[1]; }
@@ -77,15 +94,29 @@ template <int DP> struct Shape {
 };
 
 struct Shared {
-    uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_ready[2], o_full[2], o_free[2], cleared[8], plan_full[PLANS], plan_empty[PLANS], plan_cleared[PLANS];
+    uint64_t full[8], empty[8], q_full, q_empty, s_full[2], s_free, p_ready[2], o_done[2], o_free[2], cleared[8], plan_full[PLANS], plan_empty[PLANS], plan_cleared[PLANS];
     Plan plan[PLANS];
     uint32_t tmem;
     int dead;
 };
 
-// Waits until phase `parity` of the barrier is over.  False: the limit was reached, here or elsewhere in the CTA; the caller leaves its loop, and the results of
-// the call are not valid.
+// Waits until phase `parity` of the barrier is over.  False: the limit was reached; the caller leaves its loop, and the results of the call are not valid.  A try
+// takes up to two microseconds, the wait two seconds.  One loop of three instructions: what a wait costs beyond the time waited comes between products (with the
+// clock read on the way, 8192 tokens took 432 us instead of 407).
 __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *sh)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, 0;\nAGAIN:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 2000;\n @p bra DONE;\n add.u32 n, n, 1;\n setp.lt.u32 q, n, 1048576;\n @q bra AGAIN;\nDONE:\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok)
+                 : "r"(smem_addr(b)), "r"(parity)
+                 : "memory");
+    if (ok) return true;
+    *reinterpret_cast<volatile int *>(&sh->dead) = 1;
+    g_gave_up = 1;
+    return false;
+}
+// The same where the others may have a whole block to do: until one of them gives up.
+__device__ __forceinline__ bool wait_for_block(uint64_t *b, uint32_t parity, Shared *sh)
 {
     if (bar_try(b, parity)) return true;
     for (const int64_t start = clock64(); clock64() - start < kWaitLimit;) {
@@ -128,67 +159,99 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     return d;
 }
 
-// The next block of tokens of this CTA that has any; `round` counts them.  The whole warp takes part.
-__device__ __forceinline__ bool next_plan(const Args &p, int &round, Plan &to)
+__device__ __forceinline__ float largest(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float largest(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+// offsets and lengths as the planning warp reads them: of up to 31 sequences once, one a lane, since each look at memory is half a microsecond that nothing
+// else is done in.
+struct Sequences {
+    const SequenceArgs &s;
+    int my_offset, my_length;
+    bool few;
+    __device__ __forceinline__ explicit Sequences(const SequenceArgs &of) : s(of), my_offset(0), my_length(0), few(of.batch < 32)
+    {
+        const int lane = threadIdx.x & 31;
+        if (few && lane <= s.batch) my_offset = s.offsets[lane];
+        if (few && lane < s.batch) my_length = s.lengths[lane];
+    }
+    // of a sequence that is the same in all lanes
+    __device__ __forceinline__ int offset(int b) const { return cut(few ? __shfl_sync(~0u, my_offset, b) : s.offsets[b]); }
+    __device__ __forceinline__ int length(int b) const { return few ? __shfl_sync(~0u, my_length, b) : s.lengths[b]; }
+    // of one of each lane's own; with few sequences the lane's number
+    __device__ __forceinline__ int lanes_offset(int b) const { return cut(few ? my_offset : s.offsets[b]); }
+    __device__ __forceinline__ int cut(int o) const { return o < 0 ? 0 : o < s.tokens ? o : int(s.tokens); }
+};
+
+// Blocks of tokens and heads are numbered so that sequence b's begin with offsets[b] / block + b: enough for its own, and found without adding up the ones before.
+__device__ __forceinline__ int all_blocks(const Args &p, int last_offset) { return (last_offset / p.block + p.a.seq.batch) * p.a.cache.kv_heads * p.blocks * p.parts; }
+
+// What number n of `all` is; false if it has no tokens.  The whole warp takes part.
+__device__ __forceinline__ bool plan_of(const Args &p, const Sequences &seq, int n, int all, Plan &to)
 {
     const AttentionArgs &a = p.a;
-    const int lane = threadIdx.x & 31, block = 2 * p.tokens, items = a.cache.kv_heads * p.blocks;
-    const auto offset = [&](int b) {
-        const int64_t o = a.seq.offsets[b];
-        return o < 0 ? 0 : o < a.seq.tokens ? o : a.seq.tokens;
-    };
-    // blocks are numbered so that sequence b's begin with offsets[b] / block + b: enough for its own, and found without adding up the ones before
-    const int64_t all = (offset(a.seq.batch) / block + a.seq.batch) * items;
-    for (;; ++round) {
-        const int64_t n = int64_t(round) * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-        if (int64_t(round) * gridDim.x >= all) return false;
-        if (n >= all) continue;
-        const int64_t id = all / items - 1 - n / items;
-        const int item = int(n % items);
-        int lo = 0;
-        for (int left = a.seq.batch; left > 1;) {
-            const int step = (left + 31) / 32;
-            const bool below = lane * step < left && offset(lo + lane * step) / block + lo + lane * step <= id;
-            const int k = __popc(__ballot_sync(~0u, below));
-            const int at = (k > 0 ? k - 1 : 0) * step;
-            lo += at;
-            left = left - at < step ? left - at : step;
-        }
-        const NewTokens s = new_tokens(a.seq, lo);
-        const int64_t at = (id - (offset(lo) / block + lo)) * block, n_tokens = s.end - s.first;
-        if (at < 0 || at >= n_tokens) continue;
-        to.done = 0;
-        to.b = lo;
-        to.kv = item / p.blocks;
-        to.head0 = to.kv * p.group + item % p.blocks * p.heads;
-        to.heads = min(p.heads, (to.kv + 1) * p.group - to.head0);
-        to.row0 = int(s.first + at);
-        to.count = int(n_tokens - at < block ? n_tokens - at : block);
-        const int64_t position = s.length - n_tokens + at, most = int64_t(a.seq.width) << a.cache.page_shift;
-        to.position = int(position > -(1 << 30) ? position : -(1 << 30));        // far below zero or just below is the same for up to 2^30 tokens' first ones
-        to.last = s.length <= 0 ? -1 : int((s.length < most ? s.length : most) - 1);
-        const auto low = [&](int64_t position) { return a.window && position >= a.window ? int(position - a.window + 1) : 0; };
-        to.sees_from = to.all_from = 0;
-        to.sees_to = to.all_to = -1;
-        for (int x = 0; x < 2; ++x) {
-            const int first = x * p.tokens, end = min((x + 1) * p.tokens, to.count);
-            to.from[x] = to.to[x] = 0;
-            if (first >= end) continue;
-            const int64_t p0 = int64_t(to.position) + first, p1 = int64_t(to.position) + end - 1;
-            const int from = low(p0), last = int(p1 < to.last ? p1 : to.last);
-            if (last < from) continue;
-            to.from[x] = from / TILE;
-            to.to[x] = last / TILE + 1;
-        }
-        // of the whole block
-        const int64_t p0 = to.position, p1 = p0 + to.count - 1;
-        to.sees_from = low(p0);
-        to.sees_to = int(p1 < to.last ? p1 : to.last);
-        to.all_from = low(p1);
-        to.all_to = int(p0 < to.last ? p0 : to.last);
-        to.bad = 0;
-        return true;
+    const int lane = threadIdx.x & 31, block = p.block, items = a.cache.kv_heads * p.blocks, whole = n / p.parts, part = n - whole * p.parts, id = all / (p.parts * items) - 1 - whole / items,
+              item = whole % items;
+    int lo = 0;
+    for (int left = a.seq.batch; left > 1;) {
+        const int step = (left + 31) / 32;
+        const bool below = lane * step < left && seq.lanes_offset(lo + lane * step) / block + lo + lane * step <= id;
+        const int k = __popc(__ballot_sync(~0u, below));
+        const int at = (k > 0 ? k - 1 : 0) * step;
+        lo += at;
+        left = left - at < step ? left - at : step;
     }
+    const int begin = seq.offset(lo), stop = seq.offset(lo + 1), length = seq.length(lo);
+    const int64_t at = int64_t(id - (begin / block + lo)) * block, n_tokens = stop - begin;
+    if (at < 0 || at >= n_tokens) return false;
+    to.slot = n;
+    to.done = 0;
+    to.b = lo;
+    to.kv = item / p.blocks;
+    to.head0 = to.kv * p.group + item % p.blocks * p.heads;
+    to.heads = min(p.heads, (to.kv + 1) * p.group - to.head0);
+    to.row0 = int(begin + at);
+    to.count = int(n_tokens - at < block ? n_tokens - at : block);
+    const int64_t position = length - n_tokens + at, most = int64_t(a.seq.width) << a.cache.page_shift;
+    to.position = int(position > -(1 << 30) ? position : -(1 << 30));        // far below zero or just below is the same for up to 2^30 tokens' first ones
+    to.last = length <= 0 ? -1 : int((length < most ? length : most) - 1);
+    const auto low = [&](int64_t position) { return a.window && position >= a.window ? int(position - a.window + 1) : 0; };
+    to.sees_from = to.all_from = 0;
+    to.sees_to = to.all_to = -1;
+    for (int x = 0; x < 2; ++x) {
+        const int first = x * p.tokens, end = min((x + 1) * p.tokens, to.count);
+        to.from[x] = to.to[x] = 0;
+        if (first >= end) continue;
+        const int64_t p0 = int64_t(to.position) + first, p1 = int64_t(to.position) + end - 1;
+        const int from = low(p0), last = int(p1 < to.last ? p1 : to.last);
+        if (last < from) continue;
+        to.from[x] = from / TILE;
+        to.to[x] = last / TILE + 1;
+    }
+    // of the whole block
+    const int64_t p0 = to.position, p1 = p0 + to.count - 1;
+    to.sees_from = low(p0);
+    to.sees_to = int(p1 < to.last ? p1 : to.last);
+    to.all_from = low(p1);
+    to.all_to = int(p0 < to.last ? p0 : to.last);
+    to.bad = 0;
+    if (p.parts > 1) {
+        const int first = to.first(), chunk = (to.end() - first + p.parts - 1) / p.parts, lowest = first + part * chunk;
+        for (int x = 0; x < 2; ++x) {
+            to.from[x] = max(to.from[x], lowest);
+            to.to[x] = min(to.to[x], lowest + chunk);
+            if (to.from[x] >= to.to[x]) to.from[x] = to.to[x] = 0;
+        }
+    }
+    return true;
 }
 
 template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
@@ -203,6 +266,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const AttentionArgs &a = p.a;
     const auto wait = [&](uint64_t *b, uint32_t parity) { return wait_for(b, parity, &sh); };
+    const auto warp_wait_block = [&](uint64_t *b, uint32_t parity) { return bool(__all_sync(~0u, wait_for_block(b, parity, &sh))); };
     const auto warp_wait = [&](uint64_t *b, uint32_t parity) { return bool(__all_sync(~0u, wait_for(b, parity, &sh))); };
 
     if (warp == LOAD_WARP && elected()) {
@@ -216,12 +280,13 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
         for (int x = 0; x < 2; ++x) {
             bar_init(&sh.s_full[x], 1);
             bar_init(&sh.p_ready[x], 4);
-            bar_init(&sh.o_full[x], 1);
+            bar_init(&sh.o_done[x], 1);
             bar_init(&sh.o_free[x], 4);
         }
+        bar_init(&sh.s_free, 4);
         for (int i = 0; i < PLANS; ++i) {
             bar_init(&sh.plan_full[i], 1);
-            bar_init(&sh.plan_empty[i], 11);         // 8 warps of softmax, the three others
+            bar_init(&sh.plan_empty[i], SOFTMAX_WARPS + 3);
             bar_init(&sh.plan_cleared[i], 1);
         }
         sh.dead = 0;
@@ -239,10 +304,10 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t tmem = sh.tmem;
     // the plan of this role's next block; false: it is over
     int seen = 0;
-    const auto take = [&](Plan &plan) {
-        if (!warp_wait(&sh.plan_full[seen % PLANS], (seen / PLANS) & 1)) return false;
-        plan = sh.plan[seen % PLANS];
-        return !plan.done;
+    const auto take = [&]() -> const Plan * {
+        if (!warp_wait_block(&sh.plan_full[seen % PLANS], (seen / PLANS) & 1)) return nullptr;
+        const Plan *const plan = &sh.plan[seen % PLANS];
+        return plan->done ? nullptr : plan;
     };
     const auto give_back = [&] {
         __syncwarp();
@@ -250,101 +315,118 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
         ++seen;
     };
 
-    if (warp < 8) {
-        // ---- softmax of tile x ------------------------------------------------------------------------------------------------
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    if (warp < SOFTMAX_WARPS) {
+        // ---- softmax of tile x, a thread a row ---------------------------------------------------------------------------------
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGISTERS));
         const int x = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = uint32_t((warp & 3) * 32) << 16, s_at = tmem + lanes + x * TILE, o_at = tmem + lanes + 2 * TILE + x * DP;
+        const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16), s_at = lanes + S_AT, p_at = lanes + P_AT + x * P_WIDTH, o_at = lanes + O_AT + x * DP;
         const bool negative = a.scale < 0.f;
         const float c = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1.17549435e-38f);        // not 0: -inf stays what it is
         const int token = r / p.heads, head = r - token * p.heads;
-        uint32_t tiles = 0, outputs = 0;             // of this tile so far: phases of s_full and o_full
+        uint32_t tiles = 0;                          // of this tile so far: phases of s_full and o_done
         bool alive = true;
-        Plan plan;
-        while (alive && take(plan)) {
+        while (alive) {
+            const Plan *const plan = take();
+            if (!plan) break;
             const int at = x * p.tokens + token;     // of the block's tokens
-            const bool mine = token < p.tokens && at < plan.count && head < plan.heads;
-            const int64_t position = int64_t(plan.position) + at;
+            const bool mine = token < p.tokens && at < plan->count && head < plan->heads;
+            const int64_t position = int64_t(plan->position) + at;
             // rows of the cache that this row sees
-            const int high = !mine ? -1 : int(position < plan.last ? position : plan.last), low = a.window && position >= a.window ? int(position - a.window + 1) : 0;
+            const int high = !mine ? -1 : int(position < plan->last ? position : plan->last), low = a.window && position >= a.window ? int(position - a.window + 1) : 0;
+            const int first = plan->from[x], end = plan->to[x];
             float m = -INFINITY, l = 0.f;
-            for (int j = plan.from[x]; j < plan.to[x]; ++j) {
+            for (int j = first; j < end; ++j) {
                 if (!(alive = warp_wait(&sh.s_full[x], tiles & 1))) break;
-                ++tiles;
                 after_sync();
                 float s[TILE];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) load32(s + 32 * i, s_at + 32 * i);
                 wait_loads();
+                before_sync();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.s_free);
                 if (negative) {
 #pragma unroll
                     for (int i = 0; i < TILE; ++i) s[i] = -s[i];
                 }
                 const int to = high - j * TILE, from = low - j * TILE;
-                if (__any_sync(~0u, to < TILE - 1 || from > 0)) {
+                const bool cut = __any_sync(~0u, to < TILE - 1 || from > 0);
+                if (cut) {
 #pragma unroll
                     for (int i = 0; i < TILE; ++i) s[i] = i <= to && i >= from ? s[i] : -INFINITY;
                 }
                 float most[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int i = 4; i < TILE; i += 4) {
+                for (int i = 4; i + 8 <= TILE; i += 8) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], s[i + e]);
+                    for (int e = 0; e < 4; ++e) most[e] = largest(most[e], s[i + 2 * e], s[i + 2 * e + 1]);
                 }
-                const float here = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c;
-                if (j == plan.from[x]) {
+                const float here = largest(largest(most[0], most[1], most[2]), most[3], largest(largest(s[TILE - 4], s[TILE - 3]), s[TILE - 2], s[TILE - 1])) * c;
+                float back = 1.f;
+                bool grows = false;
+                if (j == first) {
                     m = here;
-                } else if (__any_sync(~0u, here > m + SLACK)) {
-                    const float next = fmaxf(m, here), back = m == next ? 1.f : exp2_of(m - next);
+                } else if (__any_sync(~0u, !(here <= m + SLACK))) {
+                    // a score that is no number makes m, and with it the whole row, none
+                    const float next = largest(m, here);
+                    back = m == next ? 1.f : exp2_of(m - next);
                     m = next;
                     l *= back;
-#pragma unroll 1
-                    for (int i = 0; i < DP; i += 32) {
-                        float o[32];
-                        load32(o, o_at + i);
-                        wait_loads();
-                        uint32_t w[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * back);
-                        store16(o_at + i, w);
-                        store16(o_at + i + 16, w + 16);
-                    }
+                    grows = true;
                 }
-                // nothing but -inf so far: weights of 0
-                const float off = m == -INFINITY ? 0.f : RAISE - m;
+                // nothing but -inf so far: weights of 0; an infinite score: no numbers
+                const float off = m == -INFINITY ? 0.f : RAISE - m + (m - m);
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                uint32_t w[TILE / 2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float2 v = fma2(make_float2(s[32 * i + 2 * e], s[32 * i + 2 * e + 1]), make_float2(c, c), make_float2(off, off));
-                        v.x = exp2_of(v.x);
-                        v.y = exp2_of(v.y);
-                        sum[e & 1] = add2(sum[e & 1], v);
-                        w[e] = two_16_bits<BF>(v.x, v.y);
-                    }
-                    store16(s_at + 16 * i, w);
+                for (int e = 0; e < TILE / 2; ++e) {
+                    float2 v = fma2(make_float2(s[2 * e], s[2 * e + 1]), make_float2(c, c), make_float2(off, off));
+                    v.x = exp2_of(v.x);
+                    v.y = exp2_of(v.y);
+                    sum[e & 1] = add2(sum[e & 1], v);
+                    w[e] = two_16_bits<BF>(v.x, v.y);
                 }
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                // the product with the weights before is done: their place is free, and O at rest
+                if (j > first && !(alive = warp_wait(&sh.o_done[x], (tiles - 1) & 1))) break;
+                if (grows) {
+                    after_sync();
+#pragma unroll 1
+                    for (int i = 0; i < a.cache.d; i += 16) {
+                        float o[16];
+                        load16(o, o_at + i);
+                        wait_loads();
+                        uint32_t u[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(o[e] * back);
+                        store16(o_at + i, u);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store16(p_at + 16 * i, w + 16 * i);
+                ++tiles;
                 wait_stores();
                 before_sync();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sh.p_ready[x]);
             }
             if (!alive) break;
-            const bool any = plan.from[x] < plan.to[x];
             if (!(alive = warp_wait(&sh.plan_cleared[seen % PLANS], (seen / PLANS) & 1))) break;
-            const bool bad = sh.plan[seen % PLANS].bad != 0;
+            const bool bad = plan->bad != 0, any = first < end;
             if (any) {
-                if (!(alive = warp_wait(&sh.o_full[x], outputs & 1))) break;
-                ++outputs;
+                if (!(alive = warp_wait(&sh.o_done[x], (tiles - 1) & 1))) break;
                 after_sync();
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            uint16_t *const out = static_cast<uint16_t *>(a.out) + int64_t(plan.row0 + at) * a.out_row + (plan.head0 + head) * a.out_head;
+            // a part leaves its sums as they are
+            const float inv = p.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            float *const sums = p.sums + plan->slot * part_floats(a.cache.d) + HEADER + x * TILE + r;
+            if (p.parts > 1) {
+                sums[0] = m;
+                sums[2 * TILE] = l;
+            }
+            uint16_t *const out = static_cast<uint16_t *>(a.out) + int64_t(plan->row0 + at) * a.out_row + (plan->head0 + head) * a.out_head;
 #pragma unroll 1
-            for (int i = 0; i < DP; i += 32) {
+            for (int i = 0; i < a.cache.d; i += 32) {
                 float o[32];
                 if (any) {
                     load32(o, o_at + i);
@@ -355,11 +437,11 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 if (bad && mine) {
                     // values of V that are no numbers, in rows that not all tokens of the block see: this one's
                     for (int part = 0; part < 2; ++part) {
-                        const int first = part == 0 ? low : max(low, max(plan.all_to + 1, plan.all_from)), end = part == 0 ? min(high + 1, plan.all_from) : high + 1;
-                        for (int j = first; j < end; ++j) {
-                            const int page = page_of(a.cache, a.seq, plan.b, j);
+                        const int begin = part == 0 ? low : max(low, max(plan->all_to + 1, plan->all_from)), stop = part == 0 ? min(high + 1, plan->all_from) : high + 1;
+                        for (int j = begin; j < stop; ++j) {
+                            const int page = page_of(a.cache, a.seq, plan->b, j);
                             if (page < 0) continue;
-                            const uint16_t *const row = reinterpret_cast<const uint16_t *>(a.cache.v + page * a.cache.page_stride + plan.kv * a.cache.head_stride +
+                            const uint16_t *const row = reinterpret_cast<const uint16_t *>(a.cache.v + page * a.cache.page_stride + plan->kv * a.cache.head_stride +
                                                                                            (j & ((1 << a.cache.page_shift) - 1)) * a.cache.row_stride);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
@@ -370,7 +452,13 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                         }
                     }
                 }
-                if (mine) {
+                if (p.parts > 1) {
+                    if (any && mine) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (i + 4 * e < a.cache.d) *reinterpret_cast<float4 *>(sums - (x * TILE + r) + 4 * TILE + ((i / 4 + e) * 2 * TILE + x * TILE + r) * 4) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                } else if (mine) {
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) w[e] = two_16_bits<BF>(o[2 * e], o[2 * e + 1]);
@@ -394,15 +482,24 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             give_back();
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
         if (warp == PLAN_WARP) {
             // ---- what there is to do ---------------------------------------------------------------------------------------
-            int round = 0;
+            const Sequences seq(a.seq);
+            const int all = all_blocks(p, seq.offset(a.seq.batch));
+            int round = 0, from = 0;                 // from: this round's first
             for (int n = 0;; ++n) {
                 Plan plan;
-                const bool some = next_plan(p, round, plan);
-                ++round;
-                if (n >= PLANS && !warp_wait(&sh.plan_empty[n % PLANS], (n / PLANS - 1) & 1)) break;
+                bool some = false;
+                for (; !some && from < all; from += int(gridDim.x), ++round) {
+                    const int at = from + int(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+                    if (at >= all) continue;
+                    some = plan_of(p, seq, at, all, plan);
+                    // for the join kernel
+                    if (p.parts > 1 && lane == 0)
+                        *reinterpret_cast<int4 *>(p.sums + at * part_floats(a.cache.d)) = make_int4(some ? plan.count : 0, plan.row0, plan.head0, plan.heads);
+                }
+                if (n >= PLANS && !warp_wait_block(&sh.plan_empty[n % PLANS], (n / PLANS - 1) & 1)) break;
                 if (lane == 0) {
                     if (!some) plan.done = 1;
                     sh.plan[n % PLANS] = plan;
@@ -417,18 +514,20 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             const int boxes = TILE / p.box;
             int tiles = 0, blocks = 0;
             bool alive = true;
-            Plan plan;
             // the box that lane i brings of tile j: its page, or one past the last, which reads as zeros
-            const auto page_at = [&](int j) {
+            const auto page_at = [&](const Plan &plan, int j) {
                 const int64_t row = int64_t(j) * TILE + lane * p.box;
                 int page = -1;
                 if (lane < boxes && row <= plan.last) page = page_of(a.cache, a.seq, plan.b, row);
                 return page < 0 ? int(a.cache.pages) : page;
             };
-            while (alive && take(plan)) {
+            while (alive) {
+                const Plan *const taken = take();
+                if (!taken) break;
+                const Plan &plan = *taken;
                 const int first = plan.first(), end = plan.end();
                 if (first < end) {
-                    int page = page_at(first);
+                    int page = page_at(plan, first);
                     if (blocks > 0 && !(alive = warp_wait(&sh.q_empty, (blocks - 1) & 1))) break;
                     ++blocks;
                     if (elected()) {
@@ -438,16 +537,19 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                             for (int i = 0; i < S::BLOCKS; ++i) box3(q_to + x * S::BYTES + i * BLOCK, &q_map, 64 * i, plan.head0, plan.row0 + x * p.tokens, &sh.q_full);
                     }
                     __syncwarp();
-                    for (int j = first; j < end && alive; ++j) {
-                        const int pages = page;
-                        if (j + 1 < end) page = page_at(j + 1);
-                        for (int which = 0; which < 2; ++which, ++tiles) {
+                    // K of tile j + 1 before V of tile j
+                    int pages = page;
+                    for (int j = first - 1; j < end && alive; ++j) {
+                        const int before = pages;        // of tile j
+                        pages = page;
+                        if (j + 2 < end) page = page_at(plan, j + 2);
+                        for (int which = j + 1 < end ? 0 : 1; which < (j < first ? 1 : 2); ++which, ++tiles) {
                             const int stage = tiles % STAGES;
                             if (tiles >= STAGES && !(alive = warp_wait(&sh.empty[stage], (tiles / STAGES - 1) & 1))) break;
                             if (elected()) bar_expect(&sh.full[stage], S::BYTES);
                             __syncwarp();
                             for (int i = 0; i < boxes; ++i) {
-                                const int number = __shfl_sync(~0u, pages, i), slot = (j * TILE + i * p.box) & ((1 << a.cache.page_shift) - 1);
+                                const int number = __shfl_sync(~0u, which ? before : pages, i), slot = ((which ? j : j + 1) * TILE + i * p.box) & ((1 << a.cache.page_shift) - 1);
                                 if (elected()) {
 #pragma unroll
                                     for (int k = 0; k < S::BLOCKS; ++k)
@@ -466,120 +568,159 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             if (!alive)
                 for (int i = 0; i < 10000; ++i) __nanosleep(100);        // after giving up: the copies under way end before the CTA does
         } else if (warp == MMA_WARP) {
-            // ---- products ----------------------------------------------------------------------------------------------------
-            constexpr uint32_t format = BF ? 1 : 0;
-            constexpr uint32_t both = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(TILE >> 4) << 24);
-            constexpr uint32_t s_desc = both | (uint32_t(TILE >> 3) << 17), o_desc = both | (1u << 16) | (uint32_t(DP >> 3) << 17);
-            const uint32_t ring_from = smem_addr(ring), q_from = smem_addr(q_at);
-            int tiles = 0, blocks = 0;
-            uint32_t ready[2] = {0, 0}, outputs[2] = {0, 0};
-            bool alive = true;
-            Plan plan;
-            // S of tile x and K in `stage`
-            const auto scores = [&](int x, int stage) {
-                if (elected()) {
-                    const uint64_t qd = rows_operand(q_from + x * S::BYTES), kd = rows_operand(ring_from + stage * S::BYTES);
-#pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const int at = (k / 4) * (BLOCK / 16) + (k % 4) * 2;
-                        mma_ss(tmem + x * TILE, qd + at, kd + at, s_desc, k > 0);
+            // ---- products: one lane does it all, since what it does between them is time in which the tensor cores may run dry ---------
+            if (elected()) {
+                constexpr uint32_t format = BF ? 1 : 0;
+                constexpr uint32_t both = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(TILE >> 4) << 24);
+                constexpr uint32_t s_desc = both | (uint32_t(TILE >> 3) << 17);
+                const uint32_t o_desc = both | (1u << 16) | (uint32_t((a.cache.d + 15) / 16 * 2) << 17);
+                const uint64_t q_from = rows_operand(smem_addr(q_at)), k_from = rows_operand(smem_addr(ring)), v_from = columns_operand(smem_addr(ring), BLOCK);
+                const int steps = (a.cache.d + 15) / 16;
+                // A place in the ring: K of tile first, K of first + 1, V of first, K of first + 2, V of first + 1, .. V of end - 1
+                struct Place {
+                    int stage;
+                    uint32_t phase;
+                    __device__ __forceinline__ void skip(int n)
+                    {
+                        stage += n;
+                        if (stage >= STAGES) {
+                            stage -= STAGES;
+                            phase ^= 1;
+                        }
                     }
-                    commit(&sh.s_full[x]);
-                }
-                __syncwarp();
-            };
-            while (alive && take(plan)) {
-                const int first = plan.first(), end = plan.end();
-                if (first < end) {
-                    const auto active = [&](int x, int j) { return j >= plan.from[x] && j < plan.to[x]; };
-                    if (!(alive = warp_wait(&sh.q_full, blocks & 1))) break;
+                } k_place = {0, 0}, v_place;
+                uint32_t blocks = 0, scores = 0, ready[2] = {0, 0}, outputs[2] = {0, 0};
+                bool alive = true;
+                while (alive) {
+                    if (!(alive = wait_for_block(&sh.plan_full[seen % PLANS], (seen / PLANS) & 1, &sh))) break;
+                    const Plan &plan = sh.plan[seen % PLANS];
+                    if (plan.done) break;
+                    const int from0 = plan.from[0], to0 = plan.to[0], from1 = plan.from[1], to1 = plan.to[1], first = plan.first(), end = plan.end(), all_from = plan.all_from, all_to = plan.all_to;
+                    bar_arrive(&sh.plan_empty[seen % PLANS]);
+                    ++seen;
+                    if (first >= end) continue;
+                    const auto active = [&](int x, int j) { return x ? j >= from1 && j < to1 : j >= from0 && j < to0; };
+                    if (!(alive = wait(&sh.q_full, blocks & 1))) break;
                     ++blocks;
-                    if (!(alive = warp_wait(&sh.full[tiles % STAGES], (tiles / STAGES) & 1))) break;
-                    after_sync();
-                    for (int x = 0; x < 2; ++x)
-                        if (active(x, first)) scores(x, tiles % STAGES);
-                    if (elected()) {
-                        commit(&sh.empty[tiles % STAGES]);
-                        if (first + 1 == end) commit(&sh.q_empty);
-                    }
-                    __syncwarp();
-                    ++tiles;
-                    for (int j = first; j < end && alive; ++j) {
-                        const int v_stage = tiles % STAGES, k_stage = (tiles + 1) % STAGES;
-                        if (!(alive = warp_wait(&sh.full[v_stage], (tiles / STAGES) & 1))) break;
-                        if (plan.ragged(j) && !(alive = warp_wait(&sh.cleared[v_stage], (tiles / STAGES) & 1))) break;
-                        const bool more = j + 1 < end;
-                        bool k_here = false;
-                        for (int x = 0; x < 2 && alive; ++x) {
-                            if (active(x, j)) {
-                                if (j == plan.from[x] && outputs[x] > 0 && !(alive = warp_wait(&sh.o_free[x], (outputs[x] - 1) & 1))) break;
-                                if (!(alive = warp_wait(&sh.p_ready[x], ready[x] & 1))) break;
-                                ++ready[x];
-                                after_sync();
-                                if (elected()) {
-                                    const uint64_t vd = columns_operand(ring_from + v_stage * S::BYTES, BLOCK);
+                    v_place = k_place;
+                    v_place.skip(end - first > 1 ? 2 : 1);
+                    // S of tile kj for one tile of Q and then the other, as long as there are tiles
+                    int kj = first, kx = active(0, first) ? 0 : 1;
+                    bool k_here = false;
+                    const auto next_scores = [&] {
+                        if (kj >= end) return true;
+                        if (!k_here && !wait(&sh.full[k_place.stage], k_place.phase)) return false;
+                        if (scores > 0 && !wait(&sh.s_free, (scores - 1) & 1)) return false;
+                        ++scores;
+                        after_sync();
+                        const uint64_t kd = k_from + uint32_t(k_place.stage * (S::BYTES / 16)), qd = q_from + uint32_t(kx * (S::BYTES / 16));
 #pragma unroll
-                                    for (int k = 0; k < TILE / 16; ++k) mma_ts(tmem + 2 * TILE + x * DP, tmem + x * TILE + k * 8, vd + k * (16 * 128 / 16), o_desc, j > plan.from[x] || k > 0);
-                                    if (j + 1 == plan.to[x]) commit(&sh.o_full[x]);
-                                }
-                                __syncwarp();
-                                if (j + 1 == plan.to[x]) ++outputs[x];
+                        for (int k = 0; k < DP / 16; ++k) {
+                            if (k >= steps) break;
+                            const int at = (k / 4) * (BLOCK / 16) + (k % 4) * 2;
+                            mma_ss(tmem + S_AT, qd + at, kd + at, s_desc, k > 0);
+                        }
+                        commit(&sh.s_full[kx]);
+                        k_here = kx == 0 && active(1, kj);
+                        if (k_here) {
+                            kx = 1;
+                        } else {
+                            commit(&sh.empty[k_place.stage]);
+                            k_place.skip(kj == first ? 1 : 2);
+                            ++kj;
+                            kx = kj < end && active(0, kj) ? 0 : 1;
+                            if (kj == end) commit(&sh.q_empty);
+                        }
+                        return true;
+                    };
+                    // S is three ahead of P V: it can be formed when the one before has been read, which is when the weights of the one before that are done.
+                    // It comes in the middle of P V, whose first half fills the time until then, and whose second half nothing waits for.  Where there is one
+                    // tile of Q alone, two ahead: the weights of the next S but one would wait for this P V.
+                    const int ahead = from0 < to0 && from1 < to1 ? 3 : 2;
+                    for (int n = 0; n < ahead && alive; ++n) alive = next_scores();
+                    for (int j = first; j < end && alive; ++j) {
+                        const uint64_t vd = v_from + uint32_t(v_place.stage * (S::BYTES / 16));
+                        bool v_here = false;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            if (!active(x, j)) continue;
+                            if (!v_here) {
+                                if (!(alive = wait(&sh.full[v_place.stage], v_place.phase))) break;
+                                if ((j * TILE < all_from || j * TILE + TILE - 1 > all_to) && !(alive = wait(&sh.cleared[v_place.stage], v_place.phase))) break;
+                                v_here = true;
                             }
-                            if (more && active(x, j + 1)) {
-                                if (!k_here && !(alive = warp_wait(&sh.full[k_stage], ((tiles + 1) / STAGES) & 1))) break;
-                                k_here = true;
-                                after_sync();
-                                scores(x, k_stage);
-                            }
+                            const bool begins = j == (x ? from1 : from0);
+                            if (begins && outputs[x] > 0 && !(alive = wait(&sh.o_free[x], (outputs[x] - 1) & 1))) break;
+                            if (begins) ++outputs[x];
+                            if (!(alive = wait(&sh.p_ready[x], ready[x] & 1))) break;
+                            ++ready[x];
+                            after_sync();
+                            const auto values = [&](int k) { mma_ts(tmem + O_AT + x * DP, tmem + P_AT + x * P_WIDTH + k * 8, vd + k * (16 * 128 / 16), o_desc, !begins || k > 0); };
+#pragma unroll
+                            for (int k = 0; k < TILE / 32; ++k) values(k);
+                            if (!(alive = next_scores())) break;
+#pragma unroll
+                            for (int k = TILE / 32; k < TILE / 16; ++k) values(k);
+                            commit(&sh.o_done[x]);
                         }
                         if (!alive) break;
-                        if (elected()) {
-                            commit(&sh.empty[v_stage]);
-                            if (more) commit(&sh.empty[k_stage]);
-                            if (j + 2 == end) commit(&sh.q_empty);
-                        }
-                        __syncwarp();
-                        tiles += more ? 2 : 1;
+                        commit(&sh.empty[v_place.stage]);
+                        if (j + 1 < end) v_place.skip(j + 2 < end ? 2 : 1);
                     }
+                    k_place = v_place;
+                    k_place.skip(1);
                 }
-                if (alive) give_back();
             }
+            __syncwarp();
         } else {
             // ---- rows of V that not all tokens see -------------------------------------------------------------------------------
             int tiles = 0;
             bool alive = true;
-            Plan plan;
-            while (alive && take(plan)) {
+            while (alive) {
+                const Plan *const taken = take();
+                if (!taken) break;
+                const Plan &plan = *taken;
                 const int first = plan.first(), end = plan.end();
                 bool bad = false;
                 for (int n = 0; n < 2 * (end - first) && alive; ++n, ++tiles) {
-                    const int stage = tiles % STAGES, j = first + n / 2;
+                    const int stage = tiles % STAGES, last = 2 * (end - first) - 1, j = n == last ? end - 1 : first + n / 2 - 1;
                     if (!(alive = warp_wait(&sh.full[stage], (tiles / STAGES) & 1))) break;
-                    if ((n & 1) && plan.ragged(j)) {
-                        uint8_t *const v = ring + stage * S::BYTES;
+                    if ((n == last || (n > 0 && n % 2 == 0)) && plan.ragged(j)) {          // of V: the others are of K
+                        // a lane has one 16-byte chunk of every fourth row
+                        const int base = j * TILE;
+                        const int zeros_to = min(max(plan.sees_from - base, 0), TILE), zeros_from = min(max(plan.sees_to + 1 - base, 0), TILE);        // rows that none sees
+                        const int from = min(max(plan.all_from - base, 0), TILE), to = min(max(plan.all_to + 1 - base, from), TILE);            // rows that all see
 #pragma unroll 1
-                        for (int i = lane; i < S::BLOCKS * TILE * 8; i += 32) {
-                            const int row = (i >> 3) & (TILE - 1), number = j * TILE + row;
-                            uint4 *const at = reinterpret_cast<uint4 *>(v) + i;
-                            if (number >= plan.all_from && number <= plan.all_to) continue;
-                            if (number < plan.sees_from || number > plan.sees_to) {
-                                *at = make_uint4(0, 0, 0, 0);
-                                continue;
-                            }
-                            // exponents of all ones
-                            constexpr uint32_t ones = BF ? 0x7f807f80u : 0x7c007c00u;
-                            uint4 u = *at;
-                            uint32_t *const w = reinterpret_cast<uint32_t *>(&u);
-                            bool here = false;
+                        for (int k = 0; k < S::BLOCKS; ++k) {
+                            uint4 *const v = reinterpret_cast<uint4 *>(ring + stage * S::BYTES + k * BLOCK) + (lane & 7);
+                            const int first = lane >> 3;
+                            for (int r = first; r < zeros_to; r += 4) v[r * 8] = make_uint4(0, 0, 0, 0);
+                            for (int r = first + ((zeros_from - first + 3) & ~3); r < TILE; r += 4) v[r * 8] = make_uint4(0, 0, 0, 0);
+                            // before the rows that all see, and after
+                            for (int part = 0; part < 2; ++part) {
+                                const int begin = part ? max(to, zeros_to) : zeros_to, stop = part ? zeros_from : min(from, zeros_from);
+                                // exponents of all ones: one more in their last place carries into the sign's
+                                constexpr uint32_t ones = BF ? 0x7f807f80u : 0x7c007c00u, one = BF ? 0x00800080u : 0x04000400u, signs = 0x80008000u;
+                                constexpr int AT_ONCE = 8;
+                                for (int r0 = begin + first; r0 < stop; r0 += 4 * AT_ONCE) {
+                                    uint4 u[AT_ONCE];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const uint32_t e = __vcmpeq2(w[k] & ones, ones);
-                                here |= e != 0;
-                                w[k] &= ~e;
-                            }
-                            if (here) {
-                                *at = u;
-                                bad = true;
+                                    for (int n = 0; n < AT_ONCE; ++n) u[n] = r0 + 4 * n < stop ? v[(r0 + 4 * n) * 8] : make_uint4(0, 0, 0, 0);
+                                    uint32_t found = 0;
+#pragma unroll
+                                    for (int n = 0; n < AT_ONCE; ++n)
+                                        found |= ((u[n].x & ones) + one) | ((u[n].y & ones) + one) | ((u[n].z & ones) + one) | ((u[n].w & ones) + one);
+                                    if (found & signs) {
+                                        bad = true;
+#pragma unroll 1
+                                        for (int r = r0; r < min(stop, r0 + 4 * AT_ONCE); r += 4) {
+                                            uint32_t *const word = reinterpret_cast<uint32_t *>(v + r * 8);
+                                            for (int k = 0; k < 4; ++k)
+                                                for (int h = 0; h < 32; h += 16)
+                                                    if ((word[k] >> h & ones >> 16) == ones >> 16) word[k] &= ~(0xffffu << h);
+                                        }
+                                    }
+                                }
                             }
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -605,6 +746,98 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
     __syncthreads();
     after_sync();
     if (warp == MMA_WARP) dealloc(tmem);
+}
+
+// The parts of block blockIdx.x, added up in order: a CTA has 32 rows of 16 columns; lane r a row, and warp w the parts w, w + 8, ..
+constexpr int JOIN_WARPS = 8, JOIN_COLUMNS = 16;
+template <bool BF> __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const Args p)
+{
+    __shared__ float sh[JOIN_WARPS][2 + JOIN_COLUMNS][32];
+    after_work_before();
+    const AttentionArgs &a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = 32 * blockIdx.z + lane, x = row / TILE, r = row % TILE, token = r / p.heads, head = r - token * p.heads,
+              at = x * p.tokens + token, first = JOIN_COLUMNS * blockIdx.y;
+    if (int(blockIdx.x) * p.parts >= all_blocks(p, Sequences(a.seq).offset(a.seq.batch))) return;
+    const float *const header = p.sums + int64_t(blockIdx.x) * p.parts * part_floats(a.cache.d), *const first_part = header + HEADER;
+    const int4 of = *reinterpret_cast<const int4 *>(header);             // tokens, row, head, heads
+    const bool mine = token < p.tokens && at < of.x && head < of.w;
+    if (!__syncthreads_or(mine)) return;
+    float m = -INFINITY, l = 0.f, o[JOIN_COLUMNS];
+#pragma unroll
+    for (int e = 0; e < JOIN_COLUMNS; ++e) o[e] = 0.f;
+    if (mine) {
+#pragma unroll 4
+        for (int k = warp; k < p.parts; k += JOIN_WARPS) {
+            const float *const part = first_part + k * part_floats(a.cache.d);
+            const float here = part[row], sum = part[2 * TILE + row];
+            float4 v[JOIN_COLUMNS / 4];
+#pragma unroll
+            for (int e = 0; e < JOIN_COLUMNS / 4; ++e)
+                v[e] = first + 4 * e < a.cache.d ? reinterpret_cast<const float4 *>(part + 4 * TILE)[(first / 4 + e) * 2 * TILE + row] : make_float4(0.f, 0.f, 0.f, 0.f);
+            if (here == -INFINITY) continue;         // it has seen nothing, and may not have written its O
+            const float next = largest(m, here), back = m == next ? 1.f : exp2_of(m - next), w = here == next ? 1.f : exp2_of(here - next);
+            m = next;
+            l = l * back + w * sum;
+#pragma unroll
+            for (int e = 0; e < JOIN_COLUMNS / 4; ++e) {
+                o[4 * e] = o[4 * e] * back + w * v[e].x;
+                o[4 * e + 1] = o[4 * e + 1] * back + w * v[e].y;
+                o[4 * e + 2] = o[4 * e + 2] * back + w * v[e].z;
+                o[4 * e + 3] = o[4 * e + 3] * back + w * v[e].w;
+            }
+        }
+    }
+    sh[warp][0][lane] = m;
+    sh[warp][1][lane] = l;
+#pragma unroll
+    for (int e = 0; e < JOIN_COLUMNS; ++e) sh[warp][2 + e][lane] = o[e];
+    __syncthreads();
+    // warp w has columns 2 w and 2 w + 1 of every row
+    if (!mine || first + 2 * warp >= a.cache.d) return;
+    float most = -INFINITY, sum = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) most = largest(most, sh[w][0][lane]);
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) {
+        const float here = sh[w][0][lane], f = here == most ? 1.f : exp2_of(here - most);
+        if (here == -INFINITY) continue;
+        sum += f * sh[w][1][lane];
+        y0 += f * sh[w][2 + 2 * warp][lane];
+        y1 += f * sh[w][3 + 2 * warp][lane];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t *const out = static_cast<uint16_t *>(a.out) + int64_t(of.y + at) * a.out_row + (of.z + head) * a.out_head + first + 2 * warp;
+    const uint32_t both = two_16_bits<BF>(y0 * inv, y1 * inv);
+    if (p.wide) {
+        *reinterpret_cast<uint32_t *>(out) = both;
+    } else {
+        out[0] = uint16_t(both);
+        out[1] = uint16_t(both >> 16);
+    }
+}
+
+// How the work is cut up, from the sizes alone: lengths and offsets are the device's.
+struct Cut {
+    int blocks, heads, tokens, block, parts;
+    int64_t most;            // blocks of tokens and heads, at most
+};
+Cut cut_of(const AttentionArgs &a, int sm_count)
+{
+    Cut c;
+    const int group = a.heads / a.cache.kv_heads;
+    c.blocks = (group + TILE - 1) / TILE;
+    c.heads = (group + c.blocks - 1) / c.blocks;
+    c.tokens = TILE / c.heads;
+    const auto blocks = [&](int of) { return (a.seq.tokens / of + a.seq.batch) * a.cache.kv_heads * c.blocks; };
+    // one tile of Q a CTA as long as there are SMs enough: its softmax does not share the schedulers (512 tokens of 32 heads over 8: 15.1 us, 17.0 with two)
+    c.block = blocks(c.tokens) <= sm_count ? c.tokens : 2 * c.tokens;
+    c.most = blocks(c.block);
+    // tiles of the longest sequence that the table has room for
+    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window ? int64_t(a.window) + c.block + TILE : rows, tiles = ((seen < rows ? seen : rows) + TILE - 1) / TILE;
+    const int64_t parts = c.most > 0 ? sm_count / c.most : 0;
+    c.parts = int(parts < tiles / LEAST_TILES ? parts : tiles / LEAST_TILES);
+    if (c.parts < 2) c.parts = 1;
+    return c;
 }
 
 using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
@@ -636,15 +869,17 @@ bool encode(CUtensorMap *map, const void *at, int dims, const cuuint64_t *sizes,
 template <bool BF, int DP> cudaError_t launch(const Args &p, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int ctas, cudaStream_t stream)
 {
     const auto kernel = prompt_kernel<BF, DP>;
-    // The warps' shares of registers come out of what the block has from the start: 256 threads of 216 and 128 of 72.
+    // The warps' shares of registers come out of what the block has from the start.
     static const bool enough = [&] {
         cudaFuncAttributes attr;
-        return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs * THREADS >= 256 * 216 + 128 * 72;
+        return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs * THREADS >= 32 * SOFTMAX_WARPS * SOFTMAX_REGISTERS + (THREADS - 32 * SOFTMAX_WARPS) * OTHER_REGISTERS;
     }();
     if (!enough) return cudaErrorInvalidConfiguration;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    return launch_after(kernel, dim3(unsigned(ctas)), dim3(THREADS), Shape<DP>::SMEM, stream, dim3(1, 1), p, q, k, v);
+    const cudaError_t launched = launch_after(kernel, dim3(unsigned(ctas)), dim3(THREADS), Shape<DP>::SMEM, stream, dim3(1, 1), p, q, k, v);
+    if (launched != cudaSuccess || p.parts == 1) return launched;
+    return launch_after(join_kernel<BF>, dim3(unsigned(ctas / p.parts), unsigned((p.a.cache.d + JOIN_COLUMNS - 1) / JOIN_COLUMNS), unsigned((p.block > p.tokens ? 2 : 1) * TILE / 32)), dim3(32 * JOIN_WARPS), 0, stream, dim3(1, 1), p);
 }
 
 }  // namespace
@@ -657,7 +892,18 @@ cudaError_t prompt_gave_up(int *flag)
     return e != cudaSuccess || !*flag ? e : cudaMemcpyToSymbol(prompt::g_gave_up, &zero, sizeof(int));
 }
 
-int64_t prompt_workspace(const AttentionArgs &, int) { return 0; }
+bool prompt_takes(const AttentionArgs &a, int sm_count)
+{
+    const prompt::Cut c = prompt::cut_of(a, sm_count);
+    return c.most * c.parts <= 0x7fffffff - sm_count;
+}
+
+int64_t prompt_workspace(const AttentionArgs &a, int sm_count)
+{
+    if (a.cache.type == STRASSEN_E4M3) return 0;
+    const prompt::Cut c = prompt::cut_of(a, sm_count);
+    return c.parts > 1 ? c.most * c.parts * prompt::part_floats(a.cache.d) * 4 : 0;
+}
 
 cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t stream)
 {
@@ -665,10 +911,14 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
     prompt::Args p;
     p.a = given;
     AttentionArgs &a = p.a;
+    const prompt::Cut c = prompt::cut_of(a, sm_count);
     p.group = a.heads / a.cache.kv_heads;
-    p.blocks = (p.group + prompt::TILE - 1) / prompt::TILE;
-    p.heads = (p.group + p.blocks - 1) / p.blocks;
-    p.tokens = prompt::TILE / p.heads;
+    p.blocks = c.blocks;
+    p.heads = c.heads;
+    p.tokens = c.tokens;
+    p.block = c.block;
+    p.parts = c.parts;
+    p.sums = static_cast<float *>(a.workspace);
     const int page = 1 << a.cache.page_shift;
     p.box = page < prompt::TILE ? page : prompt::TILE;
     p.wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_row % 8 == 0 && a.out_head % 8 == 0;
@@ -689,8 +939,8 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
         a.seq.width = 0;
         k = v = q;
     }
-    const int64_t items = (a.seq.tokens / (2 * p.tokens) + a.seq.batch) * a.cache.kv_heads * p.blocks;
-    const int ctas = int(items < sm_count ? items : sm_count);
+    const int64_t all = c.most * c.parts;
+    const int ctas = int(all < sm_count ? all : sm_count);
     if (a.type == STRASSEN_BF16) return a.cache.d <= 64 ? prompt::launch<true, 64>(p, q, k, v, ctas, stream) : prompt::launch<true, 128>(p, q, k, v, ctas, stream);
     return a.cache.d <= 64 ? prompt::launch<false, 64>(p, q, k, v, ctas, stream) : prompt::launch<false, 128>(p, q, k, v, ctas, stream);
 }

@@ -70,7 +70,7 @@ def test_no_cache_and_nothing_to_do():
     prompt(cache(), batch=0, tokens=0)
     prompt(cache(), tokens=0, q=0, out=0)
     assert binding.strassen_decode_attention_workspace_bytes(0, 1, 4, 2) == 0
-    assert binding.strassen_prompt_attention_workspace_bytes(0, 1, 4, 2, 1) == 0
+    assert binding.strassen_prompt_attention_workspace_bytes(0, 1, 4, 2, 1, 0) == 0
 
 
 def test_the_package_offers_the_operators():
