@@ -11,7 +11,7 @@
 //     that the next S is formed while the weights of this one are;
 //   * warp 11 clears the rows of V that no row of the CTA sees (a page's slots behind the sequence may hold NaN, and 0 * NaN is NaN);
 //   * warp 10 finds out what there is to do, ahead of the others.
-// The CTAs stay and take blocks of tokens, the last ones, which see most, first; in every other round in the opposite order, which evens out what they cost.
+// The CTAs stay and take blocks of tokens, those that see most first, in every other round in the opposite order, which evens out what they cost.
 // Where there are fewer blocks than SMs and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens behind
 // 8000: 28 us, 98 in one part).
 //
@@ -47,6 +47,7 @@ constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, PLAN_WARP = 10, TH
 constexpr int SOFTMAX_REGISTERS = 208, OTHER_REGISTERS = 88;
 // Columns of tensor memory: S, which both tiles of Q use in turn; P and O of each.
 constexpr int S_AT = 0, P_AT = TILE, P_WIDTH = TILE / 2, O_AT = 2 * TILE;
+constexpr int MOST_BOXES = TILE / kLeastPage;
 constexpr int PLANS = 4, BLOCK = TILE * 128;         // bytes of a block of 64 values of 128 rows
 constexpr int64_t kWaitLimit = int64_t(1) << 36;     // clocks of a wait for others to be through with a block: 2^24 tiles of the longest sequence take as long
 constexpr int LEAST_TILES = 2;                       // tiles of K and V in a part (200 tokens of 8 heads over 2 behind 1000: 14.8 us; of 4: 18.7)
@@ -61,7 +62,7 @@ struct Args {
     int tokens;              // of a tile
     int block;               // of a block: of one tile or of two
     int box;                 // rows of K and V in a copy
-    bool wide;               // out's rows start at multiples of 16 bytes
+    int wide;                // bytes that out's rows start at multiples of, and are long: 32, 16 or 0 (less)
     int parts;               // of a block's rows of the cache
     float *sums;             // parts > 1: part_floats() for each part of each block
 };
@@ -171,56 +172,105 @@ __device__ __forceinline__ float largest(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-// offsets and lengths as the planning warp reads them: of up to 31 sequences once, one a lane, since each look at memory is half a microsecond that nothing
-// else is done in.
-struct Sequences {
+// The blocks of tokens in the order in which they are taken, as a whole warp sees them.
+//
+// Of up to 31 sequences, a lane one: offsets and lengths are read once, since each look at memory is half a microsecond that nothing else is done in, and
+// blocks are in order of what they cost, the dearest first, so that the CTAs, which take them in turn, end together (7 prompts of up to 2049
+// tokens, head_size 80: 245 us in pages of 16 rows, 274 in the sequences' order and with rows of no token masked).  How many blocks of a sequence cost c tiles or more needs no counting, so the n-th is found by halving.
+//
+// Of more sequences: the last first.  Sequence b's blocks begin with number offsets[b] / block + b, enough for its own, and found without adding up the ones before.
+struct Order {
+    const Args &p;
     const SequenceArgs &s;
-    int my_offset, my_length;
-    bool few;
-    __device__ __forceinline__ explicit Sequences(const SequenceArgs &of) : s(of), my_offset(0), my_length(0), few(of.batch < 32)
+    const bool few;
+    int my_begin, my_count, my_length, my_blocks, all;
+    __device__ __forceinline__ int cut(int o) const { return o < 0 ? 0 : o < s.tokens ? o : int(s.tokens); }
+    __device__ __forceinline__ explicit Order(const Args &of) : p(of), s(of.a.seq), few(of.a.seq.batch < 32), my_begin(0), my_count(0), my_length(0), my_blocks(0)
     {
         const int lane = threadIdx.x & 31;
-        if (few && lane <= s.batch) my_offset = s.offsets[lane];
-        if (few && lane < s.batch) my_length = s.lengths[lane];
+        if (!few) {
+            all = cut(s.offsets[s.batch]) / p.block + s.batch;
+            return;
+        }
+        if (lane <= s.batch) my_begin = cut(s.offsets[lane]);
+        if (lane < s.batch) my_length = s.lengths[lane];
+        const int stop = __shfl_down_sync(~0u, my_begin, 1);
+        if (lane < s.batch && stop > my_begin) my_count = stop - my_begin;
+        my_blocks = (my_count + p.block - 1) / p.block;
+        all = __reduce_add_sync(~0u, my_blocks);
     }
-    // of a sequence that is the same in all lanes
-    __device__ __forceinline__ int offset(int b) const { return cut(few ? __shfl_sync(~0u, my_offset, b) : s.offsets[b]); }
-    __device__ __forceinline__ int length(int b) const { return few ? __shfl_sync(~0u, my_length, b) : s.lengths[b]; }
-    // of one of each lane's own; with few sequences the lane's number
-    __device__ __forceinline__ int lanes_offset(int b) const { return cut(few ? my_offset : s.offsets[b]); }
-    __device__ __forceinline__ int cut(int o) const { return o < 0 ? 0 : o < s.tokens ? o : int(s.tokens); }
+    // Blocks of the lane's sequence whose last token sees c tiles or more before its own, with a window as many as it leaves.  They are the last ones.
+    __device__ __forceinline__ int dear(int c) const
+    {
+        const int64_t row = int64_t(c) * TILE, start = int64_t(my_length) - my_count;
+        if (my_count == 0 || start + my_count - 1 < row || (p.a.window && row > int64_t(p.a.window) + p.block)) return c <= 0 ? my_blocks : 0;
+        // here 0 <= row < length, so that 32 bits do: a division of 64 takes longer than the rest
+        const uint32_t before = row > start ? uint32_t(row - start) / uint32_t(p.block) : 0;
+        return my_blocks - (before < uint32_t(my_blocks) ? int(before) : my_blocks - 1);
+    }
+    // Number n: its sequence and first token there.  False: there is none (of many sequences some numbers are of no block).
+    __device__ __forceinline__ bool find(int n, int &b, int &first, int &begin, int &count, int &length) const
+    {
+        const int lane = threadIdx.x & 31;
+        if (few) {
+            // the largest c that more than n blocks cost
+            int lo = 0, hi = __reduce_max_sync(~0u, my_count > 0 && my_length > 0 ? my_length / TILE + 1 : 1);
+            while (hi - lo > 1) {
+                const int c = lo + (hi - lo) / 2;
+                if (__reduce_add_sync(~0u, dear(c)) > n) lo = c;
+                else hi = c;
+            }
+            const int upto = dear(lo), above = dear(lo + 1), mine = upto - above, left = n - __reduce_add_sync(~0u, above);
+            int before = mine;
+            for (int i = 1; i < 32; i <<= 1) {
+                const int other = __shfl_up_sync(~0u, before, i);
+                if (lane >= i) before += other;
+            }
+            before -= mine;
+            const unsigned found = __ballot_sync(~0u, left >= before && left < before + mine);
+            if (!found) return false;
+            b = __ffs(found) - 1;
+            first = __shfl_sync(~0u, my_blocks - upto + left - before, b) * p.block;
+            begin = __shfl_sync(~0u, my_begin, b);
+            count = __shfl_sync(~0u, my_count, b);
+            length = __shfl_sync(~0u, my_length, b);
+            return true;
+        }
+        const int id = all - 1 - n;
+        b = 0;
+        for (int left = s.batch; left > 1;) {
+            const int step = (left + 31) / 32;
+            const bool below = lane * step < left && cut(s.offsets[b + lane * step]) / p.block + b + lane * step <= id;
+            const int k = __popc(__ballot_sync(~0u, below));
+            const int at = (k > 0 ? k - 1 : 0) * step;
+            b += at;
+            left = left - at < step ? left - at : step;
+        }
+        begin = cut(s.offsets[b]);
+        count = cut(s.offsets[b + 1]) - begin;
+        length = s.lengths[b];
+        first = (id - (begin / p.block + b)) * p.block;
+        return first >= 0 && first < count;
+    }
 };
+__device__ __forceinline__ int all_plans(const Args &p, const Order &order) { return order.all * p.a.cache.kv_heads * p.blocks * p.parts; }
 
-// Blocks of tokens and heads are numbered so that sequence b's begin with offsets[b] / block + b: enough for its own, and found without adding up the ones before.
-__device__ __forceinline__ int all_blocks(const Args &p, int last_offset) { return (last_offset / p.block + p.a.seq.batch) * p.a.cache.kv_heads * p.blocks * p.parts; }
-
-// What number n of `all` is; false if it has no tokens.  The whole warp takes part.
-__device__ __forceinline__ bool plan_of(const Args &p, const Sequences &seq, int n, int all, Plan &to)
+// What number n is; false if it has no tokens.  The whole warp takes part.
+__device__ __forceinline__ bool plan_of(const Args &p, const Order &order, int n, Plan &to)
 {
     const AttentionArgs &a = p.a;
-    const int lane = threadIdx.x & 31, block = p.block, items = a.cache.kv_heads * p.blocks, whole = n / p.parts, part = n - whole * p.parts, id = all / (p.parts * items) - 1 - whole / items,
-              item = whole % items;
-    int lo = 0;
-    for (int left = a.seq.batch; left > 1;) {
-        const int step = (left + 31) / 32;
-        const bool below = lane * step < left && seq.lanes_offset(lo + lane * step) / block + lo + lane * step <= id;
-        const int k = __popc(__ballot_sync(~0u, below));
-        const int at = (k > 0 ? k - 1 : 0) * step;
-        lo += at;
-        left = left - at < step ? left - at : step;
-    }
-    const int begin = seq.offset(lo), stop = seq.offset(lo + 1), length = seq.length(lo);
-    const int64_t at = int64_t(id - (begin / block + lo)) * block, n_tokens = stop - begin;
-    if (at < 0 || at >= n_tokens) return false;
+    const int block = p.block, items = a.cache.kv_heads * p.blocks, whole = n / p.parts, part = n - whole * p.parts, item = whole % items;
+    int lo, at, begin, n_tokens, length;
+    if (!order.find(whole / items, lo, at, begin, n_tokens, length)) return false;
     to.slot = n;
     to.done = 0;
     to.b = lo;
     to.kv = item / p.blocks;
     to.head0 = to.kv * p.group + item % p.blocks * p.heads;
     to.heads = min(p.heads, (to.kv + 1) * p.group - to.head0);
-    to.row0 = int(begin + at);
-    to.count = int(n_tokens - at < block ? n_tokens - at : block);
-    const int64_t position = length - n_tokens + at, most = int64_t(a.seq.width) << a.cache.page_shift;
+    to.row0 = begin + at;
+    to.count = n_tokens - at < block ? n_tokens - at : block;
+    const int64_t position = int64_t(length) - n_tokens + at, most = int64_t(a.seq.width) << a.cache.page_shift;
     to.position = int(position > -(1 << 30) ? position : -(1 << 30));        // far below zero or just below is the same for up to 2^30 tokens' first ones
     to.last = length <= 0 ? -1 : int((length < most ? length : most) - 1);
     const auto low = [&](int64_t position) { return a.window && position >= a.window ? int(position - a.window + 1) : 0; };
@@ -331,8 +381,8 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             const int at = x * p.tokens + token;     // of the block's tokens
             const bool mine = token < p.tokens && at < plan->count && head < plan->heads;
             const int64_t position = int64_t(plan->position) + at;
-            // rows of the cache that this row sees
-            const int high = !mine ? -1 : int(position < plan->last ? position : plan->last), low = a.window && position >= a.window ? int(position - a.window + 1) : 0;
+            // rows of the cache that this row sees; one of no token: all, since its results go nowhere and where scores have to be replaced takes longer
+            const int high = !mine ? 0x7fffffff : int(position < plan->last ? position : plan->last), low = mine && a.window && position >= a.window ? int(position - a.window + 1) : 0;
             const int first = plan->from[x], end = plan->to[x];
             float m = -INFINITY, l = 0.f;
             for (int j = first; j < end; ++j) {
@@ -366,7 +416,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 bool grows = false;
                 if (j == first) {
                     m = here;
-                } else if (__any_sync(~0u, !(here <= m + SLACK))) {
+                } else if (__any_sync(~0u, mine && !(here <= m + SLACK))) {
                     // a score that is no number makes m, and with it the whole row, none
                     const float next = largest(m, here);
                     back = m == next ? 1.f : exp2_of(m - next);
@@ -465,7 +515,13 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (i + 8 * e >= a.cache.d) break;
-                        if (p.wide) {
+                        if (p.wide == 32) {
+                            // whole sectors: 16 values at a time
+                            if (e % 2 == 0)
+                                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i + 8 * e), "r"(w[4 * e]), "r"(w[4 * e + 1]), "r"(w[4 * e + 2]), "r"(w[4 * e + 3]),
+                                             "r"(w[4 * e + 4]), "r"(w[4 * e + 5]), "r"(w[4 * e + 6]), "r"(w[4 * e + 7])
+                                             : "memory");
+                        } else if (p.wide) {
                             *reinterpret_cast<uint4 *>(out + i + 8 * e) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
                         } else {
 #pragma unroll
@@ -485,8 +541,8 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
         if (warp == PLAN_WARP) {
             // ---- what there is to do ---------------------------------------------------------------------------------------
-            const Sequences seq(a.seq);
-            const int all = all_blocks(p, seq.offset(a.seq.batch));
+            const Order order(p);
+            const int all = all_plans(p, order);
             int round = 0, from = 0;                 // from: this round's first
             for (int n = 0;; ++n) {
                 Plan plan;
@@ -494,7 +550,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 for (; !some && from < all; from += int(gridDim.x), ++round) {
                     const int at = from + int(round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
                     if (at >= all) continue;
-                    some = plan_of(p, seq, at, all, plan);
+                    some = plan_of(p, order, at, plan);
                     // for the join kernel
                     if (p.parts > 1 && lane == 0)
                         *reinterpret_cast<int4 *>(p.sums + at * part_floats(a.cache.d)) = make_int4(some ? plan.count : 0, plan.row0, plan.head0, plan.heads);
@@ -546,17 +602,24 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                         for (int which = j + 1 < end ? 0 : 1; which < (j < first ? 1 : 2); ++which, ++tiles) {
                             const int stage = tiles % STAGES;
                             if (tiles >= STAGES && !(alive = warp_wait(&sh.empty[stage], (tiles / STAGES - 1) & 1))) break;
-                            if (elected()) bar_expect(&sh.full[stage], S::BYTES);
-                            __syncwarp();
-                            for (int i = 0; i < boxes; ++i) {
-                                const int number = __shfl_sync(~0u, which ? before : pages, i), slot = ((which ? j : j + 1) * TILE + i * p.box) & ((1 << a.cache.page_shift) - 1);
-                                if (elected()) {
+                            // the pages' numbers first, then all boxes in one go: one at a time, pages of 16 rows kept the tensor cores waiting
+                            int number[MOST_BOXES];
+                            const int mine = which ? before : pages, row = (which ? j : j + 1) * TILE;
 #pragma unroll
-                                    for (int k = 0; k < S::BLOCKS; ++k)
-                                        box4(ring_to + stage * S::BYTES + k * BLOCK + i * p.box * 128, which ? &v_map : &k_map, 64 * k, slot, plan.kv, number, &sh.full[stage]);
+                            for (int i = 0; i < MOST_BOXES; ++i) number[i] = __shfl_sync(~0u, mine, i);
+                            if (elected()) {
+                                const CUtensorMap *const map = which ? &v_map : &k_map;
+                                const uint32_t to = ring_to + stage * S::BYTES;
+                                bar_expect(&sh.full[stage], S::BYTES);
+#pragma unroll
+                                for (int i = 0; i < MOST_BOXES; ++i) {
+                                    if (i >= boxes) break;
+                                    const int slot = (row + i * p.box) & ((1 << a.cache.page_shift) - 1);
+#pragma unroll
+                                    for (int k = 0; k < S::BLOCKS; ++k) box4(to + k * BLOCK + i * p.box * 128, map, 64 * k, slot, plan.kv, number[i], &sh.full[stage]);
                                 }
-                                __syncwarp();
                             }
+                            __syncwarp();
                         }
                     }
                 }
@@ -757,7 +820,7 @@ template <bool BF> __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kerne
     const AttentionArgs &a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = 32 * blockIdx.z + lane, x = row / TILE, r = row % TILE, token = r / p.heads, head = r - token * p.heads,
               at = x * p.tokens + token, first = JOIN_COLUMNS * blockIdx.y;
-    if (int(blockIdx.x) * p.parts >= all_blocks(p, Sequences(a.seq).offset(a.seq.batch))) return;
+    if (int(blockIdx.x) * p.parts >= all_plans(p, Order(p))) return;
     const float *const header = p.sums + int64_t(blockIdx.x) * p.parts * part_floats(a.cache.d), *const first_part = header + HEADER;
     const int4 of = *reinterpret_cast<const int4 *>(header);             // tokens, row, head, heads
     const bool mine = token < p.tokens && at < of.x && head < of.w;
@@ -921,7 +984,8 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
     p.sums = static_cast<float *>(a.workspace);
     const int page = 1 << a.cache.page_shift;
     p.box = page < prompt::TILE ? page : prompt::TILE;
-    p.wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_row % 8 == 0 && a.out_head % 8 == 0;
+    const uintptr_t places = reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.out_row * 2) | uintptr_t(a.out_head * 2);
+    p.wide = (places | uintptr_t(a.cache.d * 2)) % 32 == 0 ? 32 : places % 16 == 0 ? 16 : 0;
     CUtensorMap q, k, v;
     {
         const cuuint64_t sizes[3] = {cuuint64_t(a.cache.d), cuuint64_t(a.heads), cuuint64_t(a.seq.tokens)};
