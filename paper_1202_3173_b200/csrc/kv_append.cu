@@ -1,12 +1,15 @@
 // Rotary embedding of queries and keys, and keys and values stored into a paged cache.
 //
-// A row of a head (up to 128 values) is 16 lanes' work, 8 values each: a row's pairs (x, y) turn by the angle p f,
-//     (x, y) -> (x cos - y sin, x sin + y cos),
-// and an 8-bit row's largest value is found among the 16.  Where pairs are a half of the turned values apart, a lane reads its partners' 8 values too
-// (they are in the first cache): it needs both to write its own.  A CTA takes a token; its angles, the same for all heads, are found once:
-// p f / 2 pi in 64 bits, of which the fraction is an angle in 32 bits with an error of 2^-24 of a turn's size wherever p is.
+//     (x, y) -> (x cos - y sin, x sin + y cos),   the angle of pair f at position p: p f,
+// for the pairs of a row of a head, and an 8-bit row's scale from its largest value.  A CTA has up to 8 tokens.  Their angles, the same for all heads, are found
+// first: p f / 2 pi in 64 bits, of which the fraction is an angle in 32 bits with an error of 2^-24 of a turn's size wherever p is.  Then it goes through
+// their rows; the first ones are on their way before offsets, lengths and angles are looked at, which take longer than a row.
 //
-// Bound by the bytes, read once and written once.
+// A lane has two chunks of 8 values of a row, both partners of its pairs, 8 lanes a row: a cosine and a sine for two values, and addresses for sixteen (Pairs).
+// Rows that do not come apart so, or are not aligned, are taken by 16 lanes with a chunk each, partners' values from theirs (Any).
+//
+// Bound by the bytes, read once and written once, and nearly as much by instructions: 16384 tokens of 32 + 2 x 8 heads of 128, 370 MB with an 8-bit cache, in
+// 69 us, 5.4 TB/s (400 MB, 69 us, with one in bf16); with a chunk a lane 99, with a token a CTA and its angles first 139.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -18,7 +21,7 @@ namespace strassen {
 
 namespace {
 
-constexpr int THREADS = 256, ROWS = THREADS / 16;
+constexpr int THREADS = 256, MOST_TOKENS = 8, MOST_PAIRS = kMostHeadSize / 2, CTAS_AN_SM = 3;
 
 template <bool BF16> __device__ __forceinline__ float2 two_floats(uint32_t w)
 {
@@ -30,6 +33,13 @@ template <bool BF16> __device__ __forceinline__ uint32_t two_16_bits(float lo, f
     uint32_t d;
     if (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+
+__device__ __forceinline__ float largest(float a, float b)       // NaN if one is
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
 
@@ -47,138 +57,254 @@ __device__ __forceinline__ int sequence_of(const SequenceArgs &s, int64_t t)
     return t >= n.first && t < n.end ? lo : -1;
 }
 
-template <bool BF16, bool WIDE> __device__ __forceinline__ void load8(float (&x)[8], const uint16_t *row, int at)
+// 8 values in 16 bits.
+template <bool WIDE> __device__ __forceinline__ uint4 load8(const uint16_t *at)
 {
-    if (WIDE) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(row + at);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if (WIDE) return *reinterpret_cast<const uint4 *>(at);
+    return make_uint4(at[0] | uint32_t(at[1]) << 16, at[2] | uint32_t(at[3]) << 16, at[4] | uint32_t(at[5]) << 16, at[6] | uint32_t(at[7]) << 16);
+}
+template <bool BF16> __device__ __forceinline__ void floats(float (&x)[8], uint4 u)
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = two_floats<BF16>(w[i]);
-            x[2 * i] = f.x;
-            x[2 * i + 1] = f.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = two_floats<BF16>(row[at + i]).x;
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = two_floats<BF16>(w[i]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
     }
 }
 
-template <bool BF16, bool E4M3, bool WIDE> __global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs p)
+// Where the CTA's tokens are, and their angles by pair.
+struct Tokens {
+    float cos[MOST_TOKENS][MOST_PAIRS], sin[MOST_TOKENS][MOST_PAIRS];
+    int page[MOST_TOKENS], position[MOST_TOKENS];            // position -1: of no sequence, or before its first row
+};
+__device__ __forceinline__ void look(const AppendArgs &p, int64_t t0, int tokens, Tokens &sh)
 {
-    __shared__ float angles[2][kMostHeadSize];       // cos and sin for each value of a row; 1 and 0 for those that do not turn
-    after_work_before();
-    const int64_t t = blockIdx.x;
-    const int d = p.cache.d, half = p.rotary / 2, lane = threadIdx.x & 15, first = 8 * lane;
-    const int b = sequence_of(p.seq, t);
-    if (b < 0) return;
-    const NewTokens n = new_tokens(p.seq, b);
-    const int64_t position = n.length - (n.end - t);
-    if (position < 0) return;
-    for (int i = threadIdx.x; i < kMostHeadSize; i += THREADS) {
-        float c = 1.f, s = 0.f;
-        if (i < p.rotary) {
-            // 1 / 2 pi
-            const double turns = double(position) * double(p.frequencies[p.interleaved ? i / 2 : i < half ? i : i - half]) * 0.15915494309189535;
-            sincospif(float(2 * (turns - rint(turns))), &s, &c);
-            if (p.interleaved ? !(i & 1) : i < half) s = -s;
+    if (threadIdx.x < tokens) {
+        const int64_t t = t0 + threadIdx.x;
+        const int b = sequence_of(p.seq, t);
+        int64_t position = -1;
+        if (b >= 0) {
+            const NewTokens n = new_tokens(p.seq, b);
+            position = n.length - (n.end - t);
         }
-        angles[0][i] = c;
-        angles[1][i] = s;
+        sh.position[threadIdx.x] = position < 0 ? -1 : int(position);
+        sh.page[threadIdx.x] = position < 0 ? -1 : page_of(p.cache, p.seq, b, position);
     }
     __syncthreads();
-    const int page = page_of(p.cache, p.seq, b, position);
-    const int64_t slot = position & ((1 << p.cache.page_shift) - 1);
-    const int rows = p.heads + 2 * p.cache.kv_heads;
-    for (int r = blockIdx.y * ROWS + (threadIdx.x >> 4); r < (rows + ROWS - 1) / ROWS * ROWS; r += gridDim.y * ROWS) {
-        const bool is_q = r < p.heads, is_v = r >= p.heads + p.cache.kv_heads;
-        const int h = is_q ? r : is_v ? r - p.heads - p.cache.kv_heads : r - p.heads;
-        const Heads &from = is_q ? p.q : is_v ? p.v : p.k;
-        const uint16_t *row = static_cast<const uint16_t *>(from.p) + t * from.row + h * from.head;
-        const bool mine = r < rows && first < d;
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        if (mine) {
-            load8<BF16, WIDE>(x, row, first);
-            if (!is_v && first < p.rotary) {
-                float y[8];
-                if (p.interleaved) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-                } else if (WIDE && half % 8 == 0) {
-                    load8<BF16, WIDE>(y, row, first < half ? first + half : first - half);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int at = first + i;
-                        y[i] = at < half ? two_floats<BF16>(row[at + half]).x : at < p.rotary ? two_floats<BF16>(row[at - half]).x : 0.f;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (first + i < p.rotary) x[i] = x[i] * angles[0][first + i] + y[i] * angles[1][first + i];
-            }
+    for (int i = threadIdx.x; i < tokens * MOST_PAIRS; i += THREADS) {
+        const int token = i / MOST_PAIRS, f = i % MOST_PAIRS;
+        if (f >= p.rotary / 2) continue;
+        // 1 / 2 pi
+        const double turn = double(sh.position[token]) * double(p.frequencies[f]) * 0.15915494309189535;
+        sincospif(float(2 * (turn - rint(turn))), &sh.sin[token][f], &sh.cos[token][f]);
+    }
+    __syncthreads();
+}
+
+// Row n of the CTA's: a token's queries, keys, values, then the next token's.
+struct Row {
+    int token, r;
+    __device__ __forceinline__ void next(int n, int rows)
+    {
+        r += n;
+        while (r >= rows) {
+            r -= rows;
+            ++token;
         }
-        __syncwarp();                    // in place: a row is read by all before it is written
-        if (is_q) {
-            if (!mine) continue;
-            uint16_t *to = static_cast<uint16_t *>(p.out) + t * p.out_row + h * p.out_head + first;
+    }
+};
+// Which of q, k and v the row is of, and its head there.
+struct Which {
+    bool is_q, is_v;
+    int head;
+    __device__ __forceinline__ Which(const AppendArgs &p, int r) : is_q(r < p.heads), is_v(r >= p.heads + p.cache.kv_heads), head(is_q ? r : is_v ? r - p.heads - p.cache.kv_heads : r - p.heads) {}
+};
+
+// LANES lanes have a row's values v, COUNT of them each, in chunks of 8 at places first[0], first[1]; chunks from head_size on are not there.
+template <bool BF16, bool E4M3, bool WIDE, int LANES, int CHUNKS> __device__ __forceinline__ void store(const AppendArgs &p, const Tokens &sh, int64_t t0, int token, Which of, float (&v)[CHUNKS][8], const int (&first)[CHUNKS])
+{
+    const int d = p.cache.d;
+    if (of.is_q) {
+        uint16_t *const row = static_cast<uint16_t *>(p.out) + (t0 + token) * p.out_row + of.head * p.out_head;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (first[k] >= d) continue;
             uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = two_16_bits<BF16>(x[2 * i], x[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) w[i] = two_16_bits<BF16>(v[k][2 * i], v[k][2 * i + 1]);
             if (WIDE) {
-                *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(row + first[k]) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) to[i] = uint16_t(w[i / 2] >> (16 * (i & 1)));
+                for (int i = 0; i < 8; ++i) row[first[k] + i] = uint16_t(w[i / 2] >> (16 * (i & 1)));
             }
-            continue;
         }
-        uint8_t *const to = (is_v ? p.cache.v : p.cache.k) + page * p.cache.page_stride + h * p.cache.head_stride + slot * p.cache.row_stride + first * (E4M3 ? 1 : 2);
-        if (E4M3) {
-            float most = 0.f;
+        return;
+    }
+    const int page = sh.page[token], slot = sh.position[token] & ((1 << p.cache.page_shift) - 1);
+    uint8_t *const row = (of.is_v ? p.cache.v : p.cache.k) + page * p.cache.page_stride + of.head * p.cache.head_stride + slot * p.cache.row_stride;
+    if (E4M3) {
+        float most = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+        for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most = x[i] == x[i] ? most : x[i];      // NaN stays
-            for (int i = 8; i > 0; i >>= 1) {
-                const float other = __shfl_xor_sync(0xffffu << (threadIdx.x & 16), most, i);       // the other half of the warp may have a row of q
-                most = most == most ? (other == other ? fmaxf(most, other) : other) : most;
-            }
-            const float scale = most == most ? fmaxf(most / kE4M3Max, kMinRowScale) : most;
-            if (!mine || page < 0) continue;
+            for (int i = 0; i < 8; ++i) most = largest(most, fabsf(v[k][i]));
+        const uint32_t mine = ((1u << LANES) - 1) << (threadIdx.x & 31 & ~(LANES - 1));
+#pragma unroll
+        for (int i = LANES / 2; i > 0; i >>= 1) most = largest(most, __shfl_xor_sync(mine, most, i));
+        // a row with NaN has NaN for its scale, and throughout
+        const float scale = largest(most / kE4M3Max, kMinRowScale), inv = 1.f / scale;
+        if (page < 0) return;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (first[k] >= d) continue;
             uint32_t w[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float *v = x + 4 * i;
-                const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0] / scale, v[1] / scale), __NV_SATFINITE, __NV_E4M3);
-                const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2] / scale, v[3] / scale), __NV_SATFINITE, __NV_E4M3);
+                const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[k][4 * i] * inv, v[k][4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+                const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[k][4 * i + 2] * inv, v[k][4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
                 w[i] = lo | hi << 16;
             }
-            *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-            if (lane == 0) (is_v ? p.cache.v_scale : p.cache.k_scale)[((int64_t(page) * p.cache.kv_heads + h) << p.cache.page_shift) + slot] = scale;
-        } else if (mine && page >= 0) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = two_16_bits<BF16>(x[2 * i], x[2 * i + 1]);
-            *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint2 *>(row + first[k]) = make_uint2(w[0], w[1]);
         }
+        if (threadIdx.x % LANES == 0) (of.is_v ? p.cache.v_scale : p.cache.k_scale)[((int64_t(page) * p.cache.kv_heads + of.head) << p.cache.page_shift) + slot] = scale;
+    } else if (page >= 0) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k)
+            if (first[k] < d)
+                *reinterpret_cast<uint4 *>(row + 2 * first[k]) = make_uint4(two_16_bits<BF16>(v[k][0], v[k][1]), two_16_bits<BF16>(v[k][2], v[k][3]), two_16_bits<BF16>(v[k][4], v[k][5]), two_16_bits<BF16>(v[k][6], v[k][7]));
     }
+}
+
+template <bool BF16, bool E4M3> __global__ void __launch_bounds__(THREADS, CTAS_AN_SM) pairs_kernel(const AppendArgs p, int per)
+{
+    constexpr int AT_ONCE = 2, SLOTS = THREADS / 8;         // rows of a lane under way at once
+    __shared__ Tokens sh;
+    after_work_before();
+    const int lane = threadIdx.x & 7, d = p.cache.d, half = p.rotary / 2, rows = p.heads + 2 * p.cache.kv_heads, stride = SLOTS * gridDim.y;
+    const int64_t t0 = int64_t(blockIdx.x) * per;
+    const int tokens = int(p.seq.tokens - t0 < per ? p.seq.tokens - t0 : per);
+    // the lane's chunks: partners where pairs are half of the turned values apart, else neighbours
+    const bool apart = !p.interleaved && 8 * lane < half;
+    const int first[2] = {16 * lane >= d ? d : apart ? 8 * lane : 16 * lane, 16 * lane >= d ? d : apart ? 8 * lane + half : 16 * lane + 8};
+    const bool there = 16 * lane < d;
+    Row at = {0, 0};
+    at.next(blockIdx.y * SLOTS + threadIdx.x / 8, rows);
+    uint4 x[AT_ONCE][2];
+    const auto load = [&] {
+        Row w = at;
+#pragma unroll
+        for (int n = 0; n < AT_ONCE; ++n) {
+            x[n][0] = x[n][1] = make_uint4(0, 0, 0, 0);
+            if (w.token < tokens && there) {
+                const Which of(p, w.r);
+                const Heads &from = of.is_q ? p.q : of.is_v ? p.v : p.k;
+                const uint16_t *const row = static_cast<const uint16_t *>(from.p) + (t0 + w.token) * from.row + of.head * from.head;
+                x[n][0] = *reinterpret_cast<const uint4 *>(row + first[0]);
+                x[n][1] = *reinterpret_cast<const uint4 *>(row + first[1]);
+            }
+            w.next(stride, rows);
+        }
+    };
+    load();
+    look(p, t0, tokens, sh);
+    while (at.token < tokens) {
+        Row w = at;
+#pragma unroll
+        for (int n = 0; n < AT_ONCE; ++n, w.next(stride, rows)) {
+            if (w.token >= tokens) break;
+            if (sh.position[w.token] < 0) continue;
+            const Which of(p, w.r);
+            float v[2][8];
+            floats<BF16>(v[0], x[n][0]);
+            floats<BF16>(v[1], x[n][1]);
+            if (!of.is_v && apart) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 c = *reinterpret_cast<const float4 *>(&sh.cos[w.token][8 * lane + i]), s = *reinterpret_cast<const float4 *>(&sh.sin[w.token][8 * lane + i]);
+                    const float cs[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = v[0][i + e], b = v[1][i + e];
+                        v[0][i + e] = a * cs[e] - b * ss[e];
+                        v[1][i + e] = a * ss[e] + b * cs[e];
+                    }
+                }
+            } else if (!of.is_v && p.interleaved) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (first[k] >= p.rotary) continue;
+                    const float4 c = *reinterpret_cast<const float4 *>(&sh.cos[w.token][first[k] / 2]), s = *reinterpret_cast<const float4 *>(&sh.sin[w.token][first[k] / 2]);
+                    const float cs[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = v[k][2 * e], b = v[k][2 * e + 1];
+                        v[k][2 * e] = a * cs[e] - b * ss[e];
+                        v[k][2 * e + 1] = a * ss[e] + b * cs[e];
+                    }
+                }
+            }
+            store<BF16, E4M3, true, 8, 2>(p, sh, t0, w.token, of, v, first);
+        }
+        at.next(AT_ONCE * stride, rows);
+        load();
+    }
+}
+
+template <bool BF16, bool E4M3, bool WIDE> __global__ void __launch_bounds__(THREADS) any_kernel(const AppendArgs p, int per)
+{
+    constexpr int SLOTS = THREADS / 16;
+    __shared__ Tokens sh;
+    after_work_before();
+    const int lane = threadIdx.x & 15, first[1] = {8 * lane}, d = p.cache.d, half = p.rotary / 2, rows = p.heads + 2 * p.cache.kv_heads, stride = SLOTS * gridDim.y;
+    const int64_t t0 = int64_t(blockIdx.x) * per;
+    const int tokens = int(p.seq.tokens - t0 < per ? p.seq.tokens - t0 : per);
+    look(p, t0, tokens, sh);
+    Row w = {0, 0};
+    for (w.next(blockIdx.y * SLOTS + threadIdx.x / 16, rows); w.token < tokens; w.next(stride, rows)) {
+        if (sh.position[w.token] < 0) continue;
+        const Which of(p, w.r);
+        const Heads &from = of.is_q ? p.q : of.is_v ? p.v : p.k;
+        const uint16_t *const row = static_cast<const uint16_t *>(from.p) + (t0 + w.token) * from.row + of.head * from.head;
+        float v[1][8];
+        floats<BF16>(v[0], first[0] < d ? load8<WIDE>(row + first[0]) : make_uint4(0, 0, 0, 0));
+        if (!of.is_v) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = first[0] + i;
+                if (e >= p.rotary) continue;             // those that do not turn stay what they are, whatever they are
+                const bool second = p.interleaved ? e & 1 : e >= half;
+                const int f = p.interleaved ? e / 2 : second ? e - half : e;
+                const float other = two_floats<BF16>(row[p.interleaved ? e ^ 1 : second ? e - half : e + half]).x, c = sh.cos[w.token][f], s = sh.sin[w.token][f];
+                v[0][i] = second ? other * s + v[0][i] * c : v[0][i] * c - other * s;
+            }
+        }
+        __syncwarp(0xffffu << (threadIdx.x & 16));           // in place: a row is read by all of its lanes before it is written
+        store<BF16, E4M3, WIDE, 16, 1>(p, sh, t0, w.token, of, v, first);
+    }
+}
+
+template <bool BF16, bool E4M3> cudaError_t launch(const AppendArgs &a, int sm_count, cudaStream_t stream)
+{
+    const bool pairs = a.wide && a.cache.d % 16 == 0 && a.rotary % (a.interleaved ? 8 : 16) == 0;
+    // as many tokens a CTA as leave each SM its CTAs; where there are few tokens, a token's rows in several
+    const int64_t tokens = a.seq.tokens / (CTAS_AN_SM * sm_count), per = tokens < 1 ? 1 : tokens < MOST_TOKENS ? tokens : MOST_TOKENS, ctas = (a.seq.tokens + per - 1) / per;
+    const int slots = THREADS / (pairs ? 8 : 16), steps = (a.heads + 2 * a.cache.kv_heads + slots - 1) / slots;
+    const dim3 grid(unsigned(ctas), unsigned(ctas >= sm_count ? 1 : steps < 16 ? steps : 16));
+    if (pairs) return launch_after(pairs_kernel<BF16, E4M3>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per));
+    return a.wide ? launch_after(any_kernel<BF16, E4M3, true>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per))
+                  : launch_after(any_kernel<BF16, E4M3, false>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per));
 }
 
 }  // namespace
 
 cudaError_t launch_append(const AppendArgs &a, int sm_count, cudaStream_t stream)
 {
-    const int rows = a.heads + 2 * a.cache.kv_heads, parts = (rows + ROWS - 1) / ROWS;
-    // one CTA a token and all of its rows, where there are tokens enough to fill the GPU
-    const dim3 grid(unsigned(a.seq.tokens), unsigned(a.seq.tokens >= sm_count ? 1 : parts), 1);
     const bool e = a.cache.type == STRASSEN_E4M3;
-    void (*kernel)(AppendArgs) = a.type == STRASSEN_BF16 ? (e ? (a.wide ? append_kernel<true, true, true> : append_kernel<true, true, false>) : (a.wide ? append_kernel<true, false, true> : append_kernel<true, false, false>))
-                                                         : (e ? (a.wide ? append_kernel<false, true, true> : append_kernel<false, true, false>) : (a.wide ? append_kernel<false, false, true> : append_kernel<false, false, false>));
-    void (*const k)(const AppendArgs) = kernel;
-    return launch_after(k, grid, dim3(THREADS), 0, stream, dim3(1, 1), a);
+    if (a.type == STRASSEN_BF16) return e ? launch<true, true>(a, sm_count, stream) : launch<true, false>(a, sm_count, stream);
+    return e ? launch<false, true>(a, sm_count, stream) : launch<false, false>(a, sm_count, stream);
 }
 
 }  // namespace strassen
