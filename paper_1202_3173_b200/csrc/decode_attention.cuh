@@ -143,13 +143,33 @@ template <int KIND, int DP> __device__ __forceinline__ int value_of(int i, int g
     return KIND == E4M3 ? 16 * g + 8 * half + i : 64 * half + 8 * g + i;
 }
 
+// a / b for numbers that are not negative.  Nearly always both have 32 bits, and the division that takes five times as long is not made: four of them were
+// 3000 clocks of the 4000 that pass before a CTA knows what to do.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
+{
+    if (((a | b) >> 32) == 0) return uint32_t(a) / uint32_t(b);
+    return a / b;
+}
+// `total` steps in `runs` runs: the first ones have one more.
+struct Runs {
+    int64_t size, longer;
+    __device__ __forceinline__ Runs(int64_t total, int runs) : size(quotient(total, runs)), longer(total - size * runs) {}
+    __device__ __forceinline__ int64_t begin(int run) const { return size * run + (run < longer ? run : longer); }
+    // the run that has step n
+    __device__ __forceinline__ int of(int64_t n) const
+    {
+        const int64_t in_longer = longer * (size + 1);
+        return int(n < in_longer ? quotient(n, size + 1) : longer + quotient(n - in_longer, size));
+    }
+};
+
 // Steps of all sequences, and which of them is step `at`.  All threads of the CTA take part; every thread gets the answer.
 template <int STEP> struct Plan {
-    int64_t total;
+    int64_t total, first;                    // first: of the thread's first sequence
     __device__ __forceinline__ static int64_t steps(const AttentionArgs &a, int b)
     {
         const Span s = span_of(a, b);
-        return (s.end - s.lo + STEP - 1) / STEP;
+        return int64_t(uint64_t(s.end - s.lo + STEP - 1) / STEP);
     }
     __device__ __forceinline__ static int64_t block_sum(int64_t v, int64_t *sh)
     {
@@ -164,7 +184,9 @@ template <int STEP> struct Plan {
     __device__ Plan(const AttentionArgs &a, int64_t *sh)
     {
         int64_t mine = 0;
-        for (int b = threadIdx.x; b < a.seq.batch; b += THREADS) mine += steps(a, b);
+        first = threadIdx.x < a.seq.batch ? steps(a, threadIdx.x) : 0;
+        mine = first;
+        for (int b = threadIdx.x + THREADS; b < a.seq.batch; b += THREADS) mine += steps(a, b);
         total = block_sum(mine, sh);
     }
     // The sequence that holds step `at` of total, and the steps before it.
@@ -173,7 +195,7 @@ template <int STEP> struct Plan {
         int64_t base = 0;
         for (int b0 = 0; b0 < a.seq.batch; b0 += THREADS) {
             const int mine = b0 + int(threadIdx.x);
-            const int64_t n = mine < a.seq.batch ? steps(a, mine) : 0;
+            const int64_t n = b0 == 0 ? first : mine < a.seq.batch ? steps(a, mine) : 0;
             int64_t upto = n;
             for (int i = 1; i < 32; i <<= 1) {
                 const int64_t other = __shfl_up_sync(~0u, upto, i);
@@ -226,10 +248,11 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
     }
     const Plan<S::STEP> plan(a, scratch);
     // no run is empty: an item's parts are in neighbouring ones
-    const int64_t total = plan.total * p.items, runs = total < gridDim.x ? total : gridDim.x;
+    const int64_t total = plan.total * p.items;
     if (threadIdx.x == 0) p.meta[blockIdx.x].last = -1;
-    if (blockIdx.x >= runs) return;
-    const int64_t from = total * blockIdx.x / runs, to = total * (blockIdx.x + 1) / runs;
+    if (blockIdx.x >= total) return;
+    const Runs runs(total, int(total < gridDim.x ? total : gridDim.x));
+    const int64_t from = runs.begin(blockIdx.x), to = runs.begin(blockIdx.x + 1);
 
     // A place in the order of all steps; one for the copies, which run ahead, one for the products.
     struct Place {
@@ -241,7 +264,7 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
             const Span s = span_of(a, b);
             lo = s.lo;
             end = s.end;
-            steps = (end - lo + S::STEP - 1) / S::STEP;
+            steps = int64_t(uint64_t(end - lo + S::STEP - 1) / S::STEP);
         }
         __device__ __forceinline__ void next(const Args &p)
         {
@@ -261,140 +284,170 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
     {
         int b;
         int64_t before;
-        plan.find(a, from / p.items, scratch, &b, &before);
+        plan.find(a, quotient(from, p.items), scratch, &b, &before);
         // steps of sequence b: item after item
         at.sequence(a, b);
         const int64_t inside = from - before * p.items;
-        at.item = int(inside / at.steps);
+        at.item = int(quotient(inside, at.steps));
         at.step = inside - at.item * at.steps;
         ahead = at;
     }
 
+    // ---- queries ----------------------------------------------------------------------------------------------------
+    uint32_t q[NT][KS][2];
+    float factor[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
+    int64_t first_step = 0;                              // of the item, in this run
+    // queries of the item that `at` is in, and nothing summed up yet
+    const auto begin_item = [&] {
+        first_step = at.step;
+        const int kv = p.blocks == 1 ? at.item : at.item / p.blocks, head0 = kv * p.group + (p.blocks == 1 ? 0 : (at.item % p.blocks) * 8 * NT);
+        const int heads = (kv + 1) * p.group - head0;          // of them, up to 8 * NT
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            // lane (g, t): head g's values beside the rows' chunks 4 c + t
+            const bool there = 8 * nt + g < heads;
+            const uint16_t *row = static_cast<const uint16_t *>(a.q.p) + at.b * a.q.row + (head0 + 8 * nt + g) * a.q.head;
+            uint32_t w[KS][2];
+            constexpr int LOADS = DP / 32;                      // of 8 values
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int first = KIND == E4M3 ? 16 * (4 * (i / 2) + t) + 8 * (i & 1) : 8 * (4 * i + t);
+                uint4 u = make_uint4(0, 0, 0, 0);
+                if (there && first < a.cache.d) {
+                    if (p.wide) {
+                        u = *reinterpret_cast<const uint4 *>(row + first);
+                    } else {
+                        u.x = row[first] | uint32_t(row[first + 1]) << 16;
+                        u.y = row[first + 2] | uint32_t(row[first + 3]) << 16;
+                        u.z = row[first + 4] | uint32_t(row[first + 5]) << 16;
+                        u.w = row[first + 6] | uint32_t(row[first + 7]) << 16;
+                    }
+                }
+                w[2 * i][0] = u.x;
+                w[2 * i][1] = u.y;
+                w[2 * i + 1][0] = u.z;
+                w[2 * i + 1][1] = u.w;
+            }
+            float back = 1.f;
+            if (KIND == E4M3 && a.type == STRASSEN_BF16) {
+                float most = 0.f;
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i][e] << 16)), fabsf(__uint_as_float(w[i][e] & 0xffff0000u))));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+                // the power of two that brings the largest to 1 .. 2; queries that are 0 or no numbers are left alone
+                const uint32_t e = __float_as_uint(most) >> 23;
+                const bool turn = e > 1 && e < 253;
+                const float down = turn ? __uint_as_float((254 - e) << 23) : 1.f;
+                back = turn ? __uint_as_float(e << 23) : 1.f;
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) w[i][e] = two_16_bits<false>(__uint_as_float(w[i][e] << 16) * down, __uint_as_float(w[i][e] & 0xffff0000u) * down);
+            }
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) q[nt][i][e] = w[i][e];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                factor[nt][e] = a.scale * 1.4426950408889634f * __shfl_sync(~0u, back, 4 * (2 * t + e));
+                m[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+        }
+    };
+
     // ---- copies ------------------------------------------------------------------------------------------------------
     const int64_t count = to - from;
     int64_t copied = 0;
-    int pages[(ROWS + 31) / 32];                         // of the rows lane, lane + 32 of the next stage
-    auto look_up = [&] {
+    constexpr int MINE = (ROWS + 31) / 32;
+    int pages[MINE];                                     // of the rows lane, lane + 32 of the next stage, as the table has them: not looked at before they are used,
+                                                         // so that nothing waits for the table (1300 clocks of a step's 2400 otherwise)
+    auto look_up = [&](int (&pages)[MINE], int64_t copied) {
 #pragma unroll
-        for (int i = 0; i < (ROWS + 31) / 32; ++i) {
+        for (int i = 0; i < MINE; ++i) {
             const int r = lane + 32 * i;
             const int64_t j = ahead.lo + (ahead.step * WARPS + warp) * ROWS + r;
-            pages[i] = copied < count && r < ROWS && j < ahead.end ? page_of(a.cache, a.seq, ahead.b, j) : -1;
+            pages[i] = -1;
+            if (copied < count && r < ROWS && j < ahead.end) pages[i] = a.seq.table[ahead.b * a.seq.ld_table + (j >> a.cache.page_shift)];
+        }
+    };
+    auto start = [&](int stage, const Place &ahead, const int (&pages)[MINE]) {
+        {
+            const int h = p.blocks == 1 ? ahead.item : ahead.item / p.blocks;
+            const int j0 = int(ahead.lo + (ahead.step * WARPS + warp) * ROWS), mask = (1 << a.cache.page_shift) - 1;
+            const uint32_t k_to = smem_addr(ring + stage * STAGE), v_to = k_to + HALF_STAGE;
+            // where the lane's rows begin; -1: nowhere
+            int64_t place[MINE];
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                const int slot = (j0 + lane + 32 * i) & mask;
+                const bool there = uint32_t(pages[i]) < uint64_t(a.cache.pages);
+                place[i] = there ? pages[i] * a.cache.page_stride + h * a.cache.head_stride + slot * a.cache.row_stride : -1;
+                if (KIND == E4M3 && lane + 32 * i < ROWS) {
+                    const int64_t from = there ? ((int64_t(pages[i]) * a.cache.kv_heads + h) << a.cache.page_shift) + slot : 0;
+                    const uint32_t to = smem_addr(scales + stage * S::SCALES) + 4 * (lane + 32 * i);
+                    copy4(to, a.cache.k_scale + from, there ? 4 : 0);
+                    copy4(to + 4 * ROWS, a.cache.v_scale + from, there ? 4 : 0);
+                }
+            }
+            const int chunk = lane % S::CHUNKS;
+            const bool inside = chunk * 16 < a.cache.d * S::SIZE;
+#pragma unroll
+            for (int i = 0; i < ROWS * S::CHUNKS / 32; ++i) {
+                const int r = i * (32 / S::CHUNKS) + lane / S::CHUNKS;
+                const int64_t at = __shfl_sync(~0u, place[ROWS > 32 ? (i * (32 / S::CHUNKS)) >> 5 : 0], r & 31);
+                const bool there = at >= 0 && inside;
+                const int64_t off = there ? at + chunk * 16 : 0;
+                const uint32_t to = S::place(r, chunk), bytes = there ? 16 : 0;
+                copy16(k_to + to, a.cache.k + off, bytes);
+                copy16(v_to + to, a.cache.v + off, bytes);
+            }
         }
     };
     auto copy = [&](int stage) {
         if (copied < count) {
-            const int h = p.blocks == 1 ? ahead.item : ahead.item / p.blocks;
-            const int64_t j0 = ahead.lo + (ahead.step * WARPS + warp) * ROWS;
-            const int mask = (1 << a.cache.page_shift) - 1;
-            const uint32_t k_to = smem_addr(ring + stage * STAGE), v_to = k_to + HALF_STAGE;
-            const int chunk = lane % S::CHUNKS;
-            const bool inside = chunk * 16 < a.cache.d * S::SIZE;
-            const int64_t base = h * a.cache.head_stride + chunk * 16;
-#pragma unroll
-            for (int i = 0; i < ROWS * S::CHUNKS / 32; ++i) {
-                const int r = i * (32 / S::CHUNKS) + lane / S::CHUNKS;
-                const int page = __shfl_sync(~0u, pages[ROWS > 32 ? r >> 5 : 0], r & 31);
-                const int64_t off = page < 0 ? 0 : page * a.cache.page_stride + (int(j0 + r) & mask) * a.cache.row_stride + base;
-                const uint32_t bytes = page >= 0 && inside ? 16 : 0, to = S::place(r, chunk);
-                copy16(k_to + to, a.cache.k + (bytes ? off : 0), bytes);
-                copy16(v_to + to, a.cache.v + (bytes ? off : 0), bytes);
-            }
-            if (KIND == E4M3) {
-#pragma unroll
-                for (int i = 0; i < (ROWS + 31) / 32; ++i) {
-                    const int r = lane + 32 * i;
-                    const int64_t from = pages[i] < 0 ? 0 : ((int64_t(pages[i]) * a.cache.kv_heads + h) << a.cache.page_shift) + (int(j0 + r) & mask);
-                    const uint32_t to = smem_addr(scales + stage * S::SCALES) + 4 * r;
-                    if (r < ROWS) {
-                        copy4(to, a.cache.k_scale + from, pages[i] < 0 ? 0 : 4);
-                        copy4(to + 4 * ROWS, a.cache.v_scale + from, pages[i] < 0 ? 0 : 4);
-                    }
-                }
-            }
+            start(stage, ahead, pages);
             ahead.next(p);
             ++copied;
-            look_up();
+            look_up(pages, copied);
+            if (warp == 0 && ahead.step == 0 && copied < count) {
+                // the next item's queries on their way to the second cache, in time before they are asked for
+                const int kv = p.blocks == 1 ? ahead.item : ahead.item / p.blocks, head = kv * p.group + (p.blocks == 1 ? 0 : (ahead.item % p.blocks) * 8 * NT) + lane / 2;
+                if (lane < 16 * NT && head < (kv + 1) * p.group && 64 * (lane & 1) < a.cache.d)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(a.q.p) + ahead.b * a.q.row + head * a.q.head + 64 * (lane & 1)));
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    look_up();
-#pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) copy(s);
+    // the pages of the first steps are looked up together
+    static_assert(STAGES == 3, "two steps ahead");
+    {
+        int first[MINE];
+        const Place before = ahead;
+        look_up(first, 0);
+        ahead.next(p);
+        look_up(pages, 1);
+        begin_item();                    // before the copies: behind them it would wait for 3 us
+        start(0, before, first);
+        copied = 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        copy(1);
+    }
 
     // ---- products ----------------------------------------------------------------------------------------------------
-    uint32_t q[NT][KS][2];
-    float factor[NT][2], m[NT][2], l[NT][2], o[NT][MT][4];
-    int64_t first_step = 0;                              // of the item, in this run
     int stage = 0;
 #pragma unroll 1
     for (int64_t n = 0; n < count; ++n) {
-        if (n == 0 || at.step == 0) {
-            first_step = at.step;
-            const int kv = p.blocks == 1 ? at.item : at.item / p.blocks, head0 = kv * p.group + (p.blocks == 1 ? 0 : (at.item % p.blocks) * 8 * NT);
-            const int heads = (kv + 1) * p.group - head0;          // of them, up to 8 * NT
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                // lane (g, t): head g's values beside the rows' chunks 4 c + t
-                const bool there = 8 * nt + g < heads;
-                const uint16_t *row = static_cast<const uint16_t *>(a.q.p) + at.b * a.q.row + (head0 + 8 * nt + g) * a.q.head;
-                uint32_t w[KS][2];
-                constexpr int LOADS = DP / 32;                      // of 8 values
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i) {
-                    const int first = KIND == E4M3 ? 16 * (4 * (i / 2) + t) + 8 * (i & 1) : 8 * (4 * i + t);
-                    uint4 u = make_uint4(0, 0, 0, 0);
-                    if (there && first < a.cache.d) {
-                        if (p.wide) {
-                            u = *reinterpret_cast<const uint4 *>(row + first);
-                        } else {
-                            u.x = row[first] | uint32_t(row[first + 1]) << 16;
-                            u.y = row[first + 2] | uint32_t(row[first + 3]) << 16;
-                            u.z = row[first + 4] | uint32_t(row[first + 5]) << 16;
-                            u.w = row[first + 6] | uint32_t(row[first + 7]) << 16;
-                        }
-                    }
-                    w[2 * i][0] = u.x;
-                    w[2 * i][1] = u.y;
-                    w[2 * i + 1][0] = u.z;
-                    w[2 * i + 1][1] = u.w;
-                }
-                float back = 1.f;
-                if (KIND == E4M3 && a.type == STRASSEN_BF16) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < KS; ++i)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i][e] << 16)), fabsf(__uint_as_float(w[i][e] & 0xffff0000u))));
-                    most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-                    most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-                    // the power of two that brings the largest to 1 .. 2; queries that are 0 or no numbers are left alone
-                    const uint32_t e = __float_as_uint(most) >> 23;
-                    const bool turn = e > 1 && e < 253;
-                    const float down = turn ? __uint_as_float((254 - e) << 23) : 1.f;
-                    back = turn ? __uint_as_float(e << 23) : 1.f;
-#pragma unroll
-                    for (int i = 0; i < KS; ++i)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) w[i][e] = two_16_bits<false>(__uint_as_float(w[i][e] << 16) * down, __uint_as_float(w[i][e] & 0xffff0000u) * down);
-                }
-#pragma unroll
-                for (int i = 0; i < KS; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) q[nt][i][e] = w[i][e];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    factor[nt][e] = a.scale * 1.4426950408889634f * __shfl_sync(~0u, back, 4 * (2 * t + e));
-                    m[nt][e] = -INFINITY;
-                    l[nt][e] = 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-            }
-        }
+        if (n > 0 && at.step == 0) begin_item();
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
         __syncwarp();                                    // the stage's copies of all lanes are here, and the one before has been read by all
         copy(stage == 0 ? STAGES - 1 : stage - 1);
@@ -661,9 +714,8 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
                             }
                     }
                     if (lane == 0 && first_step == 0) {
-                        // it ends with step `end` of all, in run ceil(end runs / total) - 1
-                        const int64_t end = from + n + (at.steps - at.step);
-                        p.meta[blockIdx.x] = {at.b, at.item, int((end * runs + total - 1) / total) - 1, 0};
+                        const int64_t last = from + n + (at.steps - at.step) - 1;            // the item's last step
+                        p.meta[blockIdx.x] = {at.b, at.item, runs.of(last), 0};
                     }
                 }
             }
@@ -674,49 +726,47 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
     }
 }
 
-// The parts of the item that begins in run blockIdx.x and ends in a later one, added up in order.  A CTA has one tile of 16 values of 8 heads.
-template <int KIND, int DP, int NT> __global__ void __launch_bounds__(128) join_kernel(const Args p)
+// The parts of the item that begins in run blockIdx.x and ends in a later one, added up in order.  A CTA has tiles of 16 values of 8 heads, a thread one number of
+// one; its GROUPS of four warps take every GROUPS-th part, and their sums are added in order.
+template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds__(128 * GROUPS) join_kernel(const Args p)
 {
-    constexpr int MT = DP / 16, MOST = 64;               // parts whose weights are found at a time
-    __shared__ float sh_w[MOST][8], sh_most[8];
+    constexpr int MT = DP / 16;
+    __shared__ float sh[GROUPS][3][128];
     after_work_before();
     const Meta meta = p.meta[blockIdx.x];
     if (meta.last < 0) return;
-    const int first = blockIdx.x, count = meta.last - first + 1, tile = blockIdx.y, nt = tile / MT, i = tile % MT;
-    const auto part = [&](int n) { return p.parts + (2 * int64_t(first + n) + (n == 0 ? 1 : 0)) * part_floats(DP, NT); };
-    const int lane = threadIdx.x & 31, e = threadIdx.x >> 5, head = 2 * (lane & 3) + (e & 1);
-    // largest M of each head: 16 threads a head
-    {
-        const int h = threadIdx.x & 7;
-        float most = -INFINITY;
-        for (int n = threadIdx.x >> 3; n < count; n += 16) most = fmaxf(most, part(n)[8 * NT * DP + 8 * nt + h]);
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
-        if (lane < 8) sh_w[e][lane] = most;
-        __syncthreads();
-        if (threadIdx.x < 8) sh_most[threadIdx.x] = fmaxf(fmaxf(sh_w[0][h], sh_w[1][h]), fmaxf(sh_w[2][h], sh_w[3][h]));
-        __syncthreads();
-    }
-    float sum = 0.f, weights = 0.f;
-    for (int n0 = 0; n0 < count; n0 += MOST) {
-        const int here = count - n0 < MOST ? count - n0 : MOST;
-        __syncthreads();
-        for (int n = threadIdx.x >> 3; n < here; n += 16) {
-            const int h = threadIdx.x & 7;
-            const float m = part(n0 + n)[8 * NT * DP + 8 * nt + h];
-            sh_w[n][h] = m == sh_most[h] ? 1.f : exp2_of(m - sh_most[h]);
+    const int count = meta.last - blockIdx.x + 1, group = threadIdx.x / 128, n = threadIdx.x % 128, lane = n & 31, e = n >> 5, head = 2 * (lane & 3) + (e & 1);
+    for (int tile = blockIdx.y; tile < NT * MT; tile += gridDim.y) {
+        const int nt = tile / MT, i = tile % MT;
+        float m = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll 4
+        for (int k = group; k < count; k += GROUPS) {
+            const float *const part = p.parts + (2 * int64_t(blockIdx.x + k) + (k == 0 ? 1 : 0)) * part_floats(DP, NT);
+            const float here = part[8 * NT * DP + 8 * nt + head], sum = part[8 * NT * DP + 8 * NT + 8 * nt + head], v = part[tile * 128 + n];
+            const float next = fmaxf(m, here), back = m == next ? 1.f : exp2_of(m - next), w = here == next ? 1.f : exp2_of(here - next);
+            m = next;
+            l = l * back + w * sum;
+            o = o * back + w * v;
         }
         __syncthreads();
-#pragma unroll 8
-        for (int n = 0; n < here; ++n) {
-            sum += sh_w[n][head] * part(n0 + n)[tile * 128 + threadIdx.x];
-            weights += sh_w[n][head] * part(n0 + n)[8 * NT * DP + 8 * NT + 8 * nt + head];
+        sh[group][0][n] = m;
+        sh[group][1][n] = l;
+        sh[group][2][n] = o;
+        __syncthreads();
+        const int kv = meta.item / p.blocks, h = kv * p.group + (meta.item % p.blocks) * 8 * NT + 8 * nt + head, at = value_of<KIND, DP>(i, lane >> 2, e >> 1);
+        if (group != 0 || h >= (kv + 1) * p.group || at >= p.a.cache.d) continue;
+        float most = m, sum = 0.f, y = 0.f;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) most = fmaxf(most, sh[k][0][n]);
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) {
+            const float f = sh[k][0][n] == most ? 1.f : exp2_of(sh[k][0][n] - most);
+            sum += f * sh[k][1][n];
+            y += f * sh[k][2][n];
         }
+        y = sum == 0.f ? 0.f : y / sum;
+        static_cast<uint16_t *>(p.a.out)[meta.b * p.a.out_row + h * p.a.out_head + at] = uint16_t(p.a.type == STRASSEN_BF16 ? two_16_bits<true>(y, 0.f) : two_16_bits<false>(y, 0.f));
     }
-    const int kv = meta.item / p.blocks, h = kv * p.group + (meta.item % p.blocks) * 8 * NT + 8 * nt + head, at = value_of<KIND, DP>(i, lane >> 2, e >> 1);
-    if (h >= (kv + 1) * p.group || at >= p.a.cache.d) return;
-    const float y = weights == 0.f ? 0.f : sum / weights;
-    static_cast<uint16_t *>(p.a.out)[meta.b * p.a.out_row + h * p.a.out_head + at] = uint16_t(p.a.type == STRASSEN_BF16 ? two_16_bits<true>(y, 0.f) : two_16_bits<false>(y, 0.f));
 }
 
 template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cudaStream_t stream)
@@ -729,8 +779,11 @@ template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cud
     const unsigned runs = unsigned(all < 2 * sm_count ? all : 2 * sm_count);
     e = launch_after(decode_kernel<KIND, DP, NT>, dim3(runs), dim3(THREADS), S::SMEM, stream, dim3(1, 1), p);
     // items of a single step are never cut
-    if (e == cudaSuccess && steps > 1) e = launch_after(join_kernel<KIND, DP, NT>, dim3(runs, NT * DP / 16), dim3(128), 0, stream, dim3(1, 1), p);
-    return e;
+    if (e != cudaSuccess || steps == 1) return e;
+    // many parts an item: a thread has a fourth of them, so that their latencies add up to less (one sequence of 131071 rows: 95.3 us, 93.1 so); few: as many CTAs
+    // as there are tiles (33 sequences of 4099: 77.3 us, 80.8 with the other)
+    if (runs >= 8 * p.items * int64_t(p.a.seq.batch)) return launch_after(join_kernel<KIND, DP, NT, 4>, dim3(runs, 4), dim3(512), 0, stream, dim3(1, 1), p);
+    return launch_after(join_kernel<KIND, DP, NT, 1>, dim3(runs, NT * DP / 16), dim3(128), 0, stream, dim3(1, 1), p);
 }
 
 cudaError_t launch_bf16(const Args &p, int dp, int nt, int sm_count, cudaStream_t stream);
