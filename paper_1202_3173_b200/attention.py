@@ -15,16 +15,18 @@ grad are refused unless gradients are off (``torch.no_grad()``).  Tensors that a
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
 
 from . import binding
-from .feed_forward import _OUT_TYPES, _TYPES, E4M3, W4Matrix, _call, _gradients_off, _packed, _written, quantize_w4, rms_norm_quant
+from .feed_forward import _OUT_TYPES, _TYPES, E4M3, W4Matrix, _call, _current_device, _gradients_off, _packed, _written, quantize_w4, rms_norm_quant
 
 __all__ = ["PagedCache", "SelfAttention", "rotate_append", "decode_attention", "prompt_attention"]
 
 _INT = torch.int32
+_HERE = contextlib.nullcontext()
 
 
 class PagedCache:
@@ -68,6 +70,7 @@ class PagedCache:
         self._c = binding.strassen_paged_cache(self._kind, self.kv_heads, self.head_size, self.page_size, self.pages, k.data_ptr(), v.data_ptr(),
                                                k.stride(0), k.stride(1), row, ks, vs)
         self._at = ctypes.addressof(self._c)
+        self._decode_workspace = {}      # by heads
 
     @classmethod
     def empty(cls, pages, kv_heads, head_size, page_size=64, dtype=torch.bfloat16, device="cuda"):
@@ -183,9 +186,14 @@ def _attention(q, cache, table, lengths, offsets, scale, window, out):
         q = torch.empty(shape, dtype=q.dtype, device=cache.device).copy_(q)         # prompts are read in boxes that start at multiples of 16 bytes
         q_row, q_head, _ = q.stride()
     if offsets is None:
-        need = binding.strassen_decode_attention_workspace_bytes(cache._at, batch, heads, width)
+        need = cache._decode_workspace.get(heads)
+        if need is None:                                        # the size goes by the heads alone
+            with torch.cuda.device(index):
+                need = binding.strassen_decode_attention_workspace_bytes(cache._at, batch, heads, width)
+            cache._decode_workspace[heads] = need
     else:
-        need = binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, heads, width, tokens, window)
+        with torch.cuda.device(index) if index != _current_device() else _HERE:
+            need = binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, heads, width, tokens, window)
     if need:
         # from the allocator of the current stream, which the call is enqueued on: free again when the call is done
         workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)

@@ -772,7 +772,7 @@ template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds_
 template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cudaStream_t stream)
 {
     using S = Shape<KIND, DP, NT>;
-    cudaError_t e = cudaFuncSetAttribute(decode_kernel<KIND, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    cudaError_t e = allow_shared<decode_kernel<KIND, DP, NT>>(S::SMEM);
     if (e != cudaSuccess) return e;
     const int64_t rows = int64_t(p.a.seq.width) << p.a.cache.page_shift, seen = p.a.window && p.a.window < rows ? p.a.window : rows;
     const int64_t steps = seen > 0 ? (seen + S::STEP - 1) / S::STEP : 1, all = steps * p.items * p.a.seq.batch;

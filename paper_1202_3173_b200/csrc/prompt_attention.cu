@@ -938,7 +938,7 @@ template <bool BF, int DP> cudaError_t launch(const Args &p, const CUtensorMap &
         return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs * THREADS >= 32 * SOFTMAX_WARPS * SOFTMAX_REGISTERS + (THREADS - 32 * SOFTMAX_WARPS) * OTHER_REGISTERS;
     }();
     if (!enough) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::SMEM);
+    const cudaError_t e = allow_shared<prompt_kernel<BF, DP>>(Shape<DP>::SMEM);
     if (e != cudaSuccess) return e;
     const cudaError_t launched = launch_after(kernel, dim3(unsigned(ctas)), dim3(THREADS), Shape<DP>::SMEM, stream, dim3(1, 1), p, q, k, v);
     if (launched != cudaSuccess || p.parts == 1) return launched;
