@@ -64,7 +64,6 @@ int64_t decode_workspace(const AttentionArgs &a, int sm_count);
 cudaError_t launch_decode(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 bool prompt_takes(const AttentionArgs &a, int sm_count);          // there are not too many tokens and heads
 int64_t prompt_workspace(const AttentionArgs &a, int sm_count);
-cudaError_t launch_simple(const AttentionArgs &a, cudaStream_t stream);
 cudaError_t prompt_gave_up(int *flag);        // reads and clears the flag of prompt_attention.cu
 cudaError_t launch_prompt(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 

@@ -19,6 +19,9 @@
 // CTA's tokens see and some do not, warp 11 looks for such values of V, puts zeros in their place and raises a flag; then the tokens that do see them
 // add them at the end, from memory.
 //
+// Over a cache in 8 bits the products are in f16, in which its values are exact.  Warps 12 to 15 then turn each tile of K and V, which a smaller ring brings, into 16 bits, and clear V, and queries in bf16 are brought into f16's range by a power of two a row.  Scores are multiplied by the key rows' scales, weights by the value rows', and
+// M is the largest of score + log2(value scale), so that scaled weights keep within f16's range.
+//
 // Bound, for head_size 128, by power: 16384 tokens of 32 heads over 8 in 1.68 ms, 1.31 PFLOP/s, at 1.49 GHz (sampled in the kernel), where the tensor cores are busy for 2048 of
 // 2830 clocks of a pair of tiles; cuBLAS keeps up 1.38.  In short runs at 1.75 GHz 8192 tokens take 407 us, 1.35 PFLOP/s.  For smaller heads by the softmax: 128 exponentials
 // of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a scheduler and 2150 for two (timed alone), 2900 here.  What was tried: P over S, and S formed
@@ -29,6 +32,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include <atomic>
 
@@ -43,11 +47,13 @@ namespace {
 using namespace tc;
 
 constexpr int TILE = 128;                            // rows of Q and of K and V
-constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, PLAN_WARP = 10, THREADS = 32 * 12;       // and one that clears
-constexpr int SOFTMAX_REGISTERS = 208, OTHER_REGISTERS = 88;
+constexpr int SOFTMAX_WARPS = 8, LOAD_WARP = 8, MMA_WARP = 9, PLAN_WARP = 10, CLEAR_WARP = 11;
 // Columns of tensor memory: S, which both tiles of Q use in turn; P and O of each.
 constexpr int S_AT = 0, P_AT = TILE, P_WIDTH = TILE / 2, O_AT = 2 * TILE;
 constexpr int MOST_BOXES = TILE / kLeastPage;
+// What the cache holds.
+enum { BF16 = 0, F16 = 1, EIGHT = 2 };
+constexpr int RAW = 3, SCALES = 3;                   // stages of tiles in 8 bits, and of their rows' scales
 constexpr int PLANS = 4, BLOCK = TILE * 128;         // bytes of a block of 64 values of 128 rows
 constexpr int64_t kWaitLimit = int64_t(1) << 36;     // clocks of a wait for others to be through with a block: 2^24 tiles of the longest sequence take as long
 constexpr int LEAST_TILES = 2;                       // tiles of K and V in a part (200 tokens of 8 heads over 2 behind 1000: 14.8 us; of 4: 18.7)
@@ -89,13 +95,20 @@ struct Plan {
     __device__ __forceinline__ bool ragged(int j) const { return j * TILE < all_from || j * TILE + TILE - 1 > all_to; }
 };
 
-template <int DP> struct Shape {
+template <int KIND, int DP> struct Shape {
+    // warps that clear V, in 8 bits four of a warpgroup of their own that turn tiles; all warps' registers
+    static constexpr int CLEARERS = KIND == EIGHT ? 4 : 1, THREADS = KIND == EIGHT ? 32 * 16 : 32 * 12, SOFTMAX_REGISTERS = KIND == EIGHT ? 184 : 208, OTHER_REGISTERS = KIND == EIGHT ? 72 : 88;
     static constexpr int BLOCKS = DP / 64, BYTES = BLOCKS * BLOCK;         // of a tile
-    static constexpr int STAGES = DP == 128 ? 5 : 8, SMEM = (2 + STAGES) * BYTES + 1024;
+    static constexpr int STAGES = DP == 128 ? (KIND == EIGHT ? 3 : 5) : (KIND == EIGHT ? 6 : 8);
+    // in 8 bits: tiles as they are in the cache; scales of a tile's rows of K and of V, as they are and as the softmax wants them
+    static constexpr int RAW_BYTES = DP * TILE, RAW_AT = (2 + STAGES) * BYTES, RAW_SCALES_AT = RAW_AT + RAW * RAW_BYTES, SCALES_AT = RAW_SCALES_AT + RAW * 2 * TILE * 4;
+    static constexpr int SMEM = (KIND == EIGHT ? SCALES_AT + SCALES * 3 * TILE * 4 : RAW_AT) + 1024;
+    static_assert(SMEM + 1024 <= 227 * 1024, "shared memory");
 };
 
 struct Shared {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[2], s_free, p_ready[2], o_done[2], o_free[2], cleared[8], plan_full[PLANS], plan_empty[PLANS], plan_cleared[PLANS];
+    uint64_t raw_full[RAW], raw_empty[RAW], scales_full[SCALES], scales_empty[SCALES], q_ready;
     Plan plan[PLANS];
     uint32_t tmem;
     int dead;
@@ -144,6 +157,19 @@ template <bool BF> __device__ __forceinline__ uint32_t two_16_bits(float lo, flo
     else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
+__device__ __forceinline__ float log2_of(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two e4m3 as two f16, exactly.
+__device__ __forceinline__ uint32_t two_of_e4m3(uint32_t v)
+{
+    uint32_t d;
+    asm("{\n .reg .b16 h;\n cvt.u16.u32 h, %1;\n cvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(d) : "r"(v));
+    return d;
+}
 // (a b + c) for two pairs at once
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
@@ -151,6 +177,12 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
     asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n fma.rn.f32x2 z, x, y, z;\n mov.b64 {%0, %1}, z;\n}"
         : "=f"(d.x), "=f"(d.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
 __device__ __forceinline__ float2 add2(float2 a, float2 b)
@@ -304,10 +336,11 @@ __device__ __forceinline__ bool plan_of(const Args &p, const Order &order, int n
     return true;
 }
 
-template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
+template <int KIND, int DP> __global__ void __launch_bounds__(Shape<KIND, DP>::THREADS, 1)
     prompt_kernel(const Args p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
-    using S = Shape<DP>;
+    using S = Shape<KIND, DP>;
+    constexpr bool BF = KIND == BF16;
     constexpr int STAGES = S::STAGES;
     constexpr float RAISE = BF ? 0.f : 6.f, SLACK = 8.f;
     extern __shared__ uint8_t raw[];
@@ -321,8 +354,8 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
 
     if (warp == LOAD_WARP && elected()) {
         for (int i = 0; i < STAGES; ++i) {
-            bar_init(&sh.full[i], 1);
-            bar_init(&sh.empty[i], 2);               // the products, and the warp that clears
+            bar_init(&sh.full[i], S::CLEARERS);              // in 16 bits of the copies
+            bar_init(&sh.empty[i], KIND == EIGHT ? 1 : 2);   // the products, and the warp that clears
             bar_init(&sh.cleared[i], 1);
         }
         bar_init(&sh.q_full, 1);
@@ -334,10 +367,21 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             bar_init(&sh.o_free[x], 4);
         }
         bar_init(&sh.s_free, 4);
+        if (KIND == EIGHT) {
+            for (int i = 0; i < RAW; ++i) {
+                bar_init(&sh.raw_full[i], 1 + 32);           // the tile, and each lane's scales
+                bar_init(&sh.raw_empty[i], S::CLEARERS);
+            }
+            for (int i = 0; i < SCALES; ++i) {
+                bar_init(&sh.scales_full[i], S::CLEARERS);
+                bar_init(&sh.scales_empty[i], SOFTMAX_WARPS);
+            }
+            bar_init(&sh.q_ready, SOFTMAX_WARPS);
+        }
         for (int i = 0; i < PLANS; ++i) {
             bar_init(&sh.plan_full[i], 1);
-            bar_init(&sh.plan_empty[i], SOFTMAX_WARPS + 3);
-            bar_init(&sh.plan_cleared[i], 1);
+            bar_init(&sh.plan_empty[i], SOFTMAX_WARPS + 2 + S::CLEARERS);
+            bar_init(&sh.plan_cleared[i], S::CLEARERS);
         }
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -352,6 +396,8 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
     after_sync();
     after_work_before();
     const uint32_t tmem = sh.tmem;
+    uint8_t *const raw_tiles = q_at + S::RAW_AT;
+    float *const raw_scales = reinterpret_cast<float *>(q_at + S::RAW_SCALES_AT), *const scales = reinterpret_cast<float *>(q_at + S::SCALES_AT);
     // the plan of this role's next block; false: it is over
     int seen = 0;
     const auto take = [&]() -> const Plan * {
@@ -367,13 +413,14 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
 
     if (warp < SOFTMAX_WARPS) {
         // ---- softmax of tile x, a thread a row ---------------------------------------------------------------------------------
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGISTERS));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SOFTMAX_REGISTERS));
         const int x = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16), s_at = lanes + S_AT, p_at = lanes + P_AT + x * P_WIDTH, o_at = lanes + O_AT + x * DP;
         const bool negative = a.scale < 0.f;
         const float c = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1.17549435e-38f);        // not 0: -inf stays what it is
         const int token = r / p.heads, head = r - token * p.heads;
         uint32_t tiles = 0;                          // of this tile so far: phases of s_full and o_done
+        uint32_t blocks = 0, scaled = 0;             // in 8 bits: blocks, and tiles of K and V, so far
         bool alive = true;
         while (alive) {
             const Plan *const plan = take();
@@ -384,8 +431,50 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             // rows of the cache that this row sees; one of no token: all, since its results go nowhere and where scores have to be replaced takes longer
             const int high = !mine ? 0x7fffffff : int(position < plan->last ? position : plan->last), low = mine && a.window && position >= a.window ? int(position - a.window + 1) : 0;
             const int first = plan->from[x], end = plan->to[x];
-            float m = -INFINITY, l = 0.f;
-            for (int j = first; j < end; ++j) {
+            float m = -INFINITY, l = 0.f, factor = c;        // factor: of scores
+            if (KIND == EIGHT && plan->first() < plan->end()) {
+                // this row of Q in f16
+                if (!(alive = warp_wait(&sh.q_full, blocks & 1))) break;
+                ++blocks;
+                if (a.type == STRASSEN_BF16 && plan->count > x * p.tokens) {
+                    uint8_t *const row = q_at + x * S::BYTES + r * 128;
+                    float most = 0.f;
+#pragma unroll 4
+                    for (int i = 0; i < S::BLOCKS * 8; ++i) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(row + (i >> 3) * BLOCK + (i & 7) * 16);
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
+                    }
+                    // the power of two that brings the largest to 1 .. 2; queries that are 0 or no numbers are left alone
+                    const uint32_t e = __float_as_uint(most) >> 23;
+                    const bool turn = e > 1 && e < 253;
+                    const float down = turn ? __uint_as_float((254 - e) << 23) : 1.f;
+                    factor = fmaxf(c * (turn ? __uint_as_float(e << 23) : 1.f), 1.17549435e-38f);
+#pragma unroll 4
+                    for (int i = 0; i < S::BLOCKS * 8; ++i) {
+                        uint4 *const at = reinterpret_cast<uint4 *>(row + (i >> 3) * BLOCK + (i & 7) * 16);
+                        uint32_t w[4] = {at->x, at->y, at->z, at->w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = two_16_bits<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
+                        *at = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.q_ready);
+            }
+            for (int j = KIND == EIGHT ? plan->first() : first; j < (KIND == EIGHT ? plan->end() : end); ++j) {
+                const float *const k_scale = scales + scaled % SCALES * 3 * TILE, *const v_scale = k_scale + TILE, *const v_log2 = v_scale + TILE;
+                if (KIND == EIGHT) {
+                    if (!(alive = warp_wait(&sh.scales_full[scaled % SCALES], (scaled / SCALES) & 1))) break;
+                    if (j < first || j >= end) {
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sh.scales_empty[scaled % SCALES]);
+                        ++scaled;
+                        continue;
+                    }
+                }
                 if (!(alive = warp_wait(&sh.s_full[x], tiles & 1))) break;
                 after_sync();
                 float s[TILE];
@@ -399,19 +488,41 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
                     for (int i = 0; i < TILE; ++i) s[i] = -s[i];
                 }
+                if (KIND == EIGHT) {
+#pragma unroll
+                    for (int i = 0; i < TILE; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(k_scale + i);
+                        const float2 lo = mul2(make_float2(s[i], s[i + 1]), make_float2(f.x, f.y)), hi = mul2(make_float2(s[i + 2], s[i + 3]), make_float2(f.z, f.w));
+                        s[i] = lo.x, s[i + 1] = lo.y, s[i + 2] = hi.x, s[i + 3] = hi.y;
+                    }
+                }
                 const int to = high - j * TILE, from = low - j * TILE;
                 const bool cut = __any_sync(~0u, to < TILE - 1 || from > 0);
                 if (cut) {
 #pragma unroll
                     for (int i = 0; i < TILE; ++i) s[i] = i <= to && i >= from ? s[i] : -INFINITY;
                 }
-                float most[4] = {s[0], s[1], s[2], s[3]};
+                float here;
+                if (KIND == EIGHT) {
+                    float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 4; i + 8 <= TILE; i += 8) {
+                    for (int i = 0; i < TILE; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4 *>(v_log2 + i);
+                        const float2 lo = fma2(make_float2(s[i], s[i + 1]), make_float2(factor, factor), make_float2(f.x, f.y)),
+                                     hi = fma2(make_float2(s[i + 2], s[i + 3]), make_float2(factor, factor), make_float2(f.z, f.w));
+                        most[0] = largest(most[0], lo.x, lo.y);
+                        most[1] = largest(most[1], hi.x, hi.y);
+                    }
+                    here = largest(most[0], most[1]);
+                } else {
+                    float most[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most[e] = largest(most[e], s[i + 2 * e], s[i + 2 * e + 1]);
+                    for (int i = 4; i + 8 <= TILE; i += 8) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most[e] = largest(most[e], s[i + 2 * e], s[i + 2 * e + 1]);
+                    }
+                    here = largest(largest(most[0], most[1], most[2]), most[3], largest(largest(s[TILE - 4], s[TILE - 3]), s[TILE - 2], s[TILE - 1])) * factor;
                 }
-                const float here = largest(largest(most[0], most[1], most[2]), most[3], largest(largest(s[TILE - 4], s[TILE - 3]), s[TILE - 2], s[TILE - 1])) * c;
                 float back = 1.f;
                 bool grows = false;
                 if (j == first) {
@@ -430,13 +541,19 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 uint32_t w[TILE / 2];
 #pragma unroll
                 for (int e = 0; e < TILE / 2; ++e) {
-                    float2 v = fma2(make_float2(s[2 * e], s[2 * e + 1]), make_float2(c, c), make_float2(off, off));
+                    float2 v = fma2(make_float2(s[2 * e], s[2 * e + 1]), make_float2(factor, factor), make_float2(off, off));
                     v.x = exp2_of(v.x);
                     v.y = exp2_of(v.y);
                     sum[e & 1] = add2(sum[e & 1], v);
+                    if (KIND == EIGHT) v = mul2(v, *reinterpret_cast<const float2 *>(v_scale + 2 * e));
                     w[e] = two_16_bits<BF>(v.x, v.y);
                 }
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                if (KIND == EIGHT) {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.scales_empty[scaled % SCALES]);
+                    ++scaled;
+                }
                 // the product with the weights before is done: their place is free, and O at rest
                 if (j > first && !(alive = warp_wait(&sh.o_done[x], (tiles - 1) & 1))) break;
                 if (grows) {
@@ -491,8 +608,19 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                         for (int j = begin; j < stop; ++j) {
                             const int page = page_of(a.cache, a.seq, plan->b, j);
                             if (page < 0) continue;
-                            const uint16_t *const row = reinterpret_cast<const uint16_t *>(a.cache.v + page * a.cache.page_stride + plan->kv * a.cache.head_stride +
-                                                                                           (j & ((1 << a.cache.page_shift) - 1)) * a.cache.row_stride);
+                            const int slot = j & ((1 << a.cache.page_shift) - 1);
+                            const uint8_t *const bytes = a.cache.v + page * a.cache.page_stride + plan->kv * a.cache.head_stride + slot * a.cache.row_stride;
+                            if (KIND == EIGHT) {
+                                const float f = a.cache.v_scale[((int64_t(page) * a.cache.kv_heads + plan->kv) << a.cache.page_shift) + slot];
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (i + e < a.cache.d) {
+                                        const float v = f * float(reinterpret_cast<const __nv_fp8_e4m3 *>(bytes)[i + e]);
+                                        if (!(v - v == 0.f)) o[e] += v;
+                                    }
+                                continue;
+                            }
+                            const uint16_t *const row = reinterpret_cast<const uint16_t *>(bytes);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (i + e < a.cache.d) {
@@ -511,7 +639,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 } else if (mine) {
                     uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) w[e] = two_16_bits<BF>(o[2 * e], o[2 * e + 1]);
+                    for (int e = 0; e < 16; ++e) w[e] = BF || (KIND == EIGHT && a.type == STRASSEN_BF16) ? two_16_bits<true>(o[2 * e], o[2 * e + 1]) : two_16_bits<false>(o[2 * e], o[2 * e + 1]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (i + 8 * e >= a.cache.d) break;
@@ -538,7 +666,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
             give_back();
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGISTERS));
         if (warp == PLAN_WARP) {
             // ---- what there is to do ---------------------------------------------------------------------------------------
             const Order order(p);
@@ -600,8 +728,11 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                         pages = page;
                         if (j + 2 < end) page = page_at(plan, j + 2);
                         for (int which = j + 1 < end ? 0 : 1; which < (j < first ? 1 : 2); ++which, ++tiles) {
-                            const int stage = tiles % STAGES;
-                            if (tiles >= STAGES && !(alive = warp_wait(&sh.empty[stage], (tiles / STAGES - 1) & 1))) break;
+                            // in 8 bits into the ring of those
+                            constexpr int RING = KIND == EIGHT ? RAW : STAGES;
+                            uint64_t *const full = KIND == EIGHT ? sh.raw_full : sh.full, *const empty = KIND == EIGHT ? sh.raw_empty : sh.empty;
+                            const int stage = tiles % RING;
+                            if (tiles >= RING && !(alive = warp_wait(&empty[stage], (tiles / RING - 1) & 1))) break;
                             // the pages' numbers first, then all boxes in one go: one at a time, pages of 16 rows kept the tensor cores waiting
                             int number[MOST_BOXES];
                             const int mine = which ? before : pages, row = (which ? j : j + 1) * TILE;
@@ -609,23 +740,45 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                             for (int i = 0; i < MOST_BOXES; ++i) number[i] = __shfl_sync(~0u, mine, i);
                             if (elected()) {
                                 const CUtensorMap *const map = which ? &v_map : &k_map;
-                                const uint32_t to = ring_to + stage * S::BYTES;
-                                bar_expect(&sh.full[stage], S::BYTES);
+                                const uint32_t to = KIND == EIGHT ? smem_addr(raw_tiles) + stage * S::RAW_BYTES : ring_to + stage * S::BYTES;
+                                bar_expect(&full[stage], KIND == EIGHT ? S::RAW_BYTES : S::BYTES);
 #pragma unroll
                                 for (int i = 0; i < MOST_BOXES; ++i) {
                                     if (i >= boxes) break;
                                     const int slot = (row + i * p.box) & ((1 << a.cache.page_shift) - 1);
+                                    if (KIND == EIGHT) {
+                                        box4(to + i * p.box * DP, map, 0, slot, plan.kv, number[i], &full[stage]);
+                                        continue;
+                                    }
 #pragma unroll
-                                    for (int k = 0; k < S::BLOCKS; ++k) box4(to + k * BLOCK + i * p.box * 128, map, 64 * k, slot, plan.kv, number[i], &sh.full[stage]);
+                                    for (int k = 0; k < S::BLOCKS; ++k) box4(to + k * BLOCK + i * p.box * 128, map, 64 * k, slot, plan.kv, number[i], &full[stage]);
                                 }
                             }
                             __syncwarp();
+                            if (KIND == EIGHT) {
+                                // with a tile of K the scales of its rows and of V's
+                                if (which == 0) {
+#pragma unroll
+                                    for (int i = 0; i < TILE / 32; ++i) {
+                                        const int r = lane + 32 * i, number = __shfl_sync(~0u, mine, r / p.box), slot = (row + r) & ((1 << a.cache.page_shift) - 1);
+                                        const bool there = number < a.cache.pages;
+                                        const int64_t at = there ? ((int64_t(number) * a.cache.kv_heads + plan.kv) << a.cache.page_shift) + slot : 0;
+                                        const uint32_t to = smem_addr(raw_scales) + (stage * 2 * TILE + r) * 4;
+                                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(a.cache.k_scale + at), "r"(there ? 4 : 0) : "memory");
+                                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + TILE * 4), "l"(a.cache.v_scale + at), "r"(there ? 4 : 0) : "memory");
+                                    }
+                                }
+                                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&full[stage])) : "memory");
+                            }
                         }
                     }
                 }
                 if (alive) give_back();
             }
             // what has been brought is used up, and the arrivals that say so are here, before the CTA is left
+            if (KIND == EIGHT) {
+                for (int n = tiles > RAW ? tiles - RAW : 0; n < tiles && alive; ++n) alive = warp_wait(&sh.raw_empty[n % RAW], (n / RAW) & 1);
+            }
             for (int n = tiles > STAGES ? tiles - STAGES : 0; n < tiles && alive; ++n) alive = warp_wait(&sh.empty[n % STAGES], (n / STAGES) & 1);
             if (alive && blocks > 0) alive = warp_wait(&sh.q_empty, (blocks - 1) & 1);
             if (!alive)
@@ -663,7 +816,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                     ++seen;
                     if (first >= end) continue;
                     const auto active = [&](int x, int j) { return x ? j >= from1 && j < to1 : j >= from0 && j < to0; };
-                    if (!(alive = wait(&sh.q_full, blocks & 1))) break;
+                    if (!(alive = wait(KIND == EIGHT ? &sh.q_ready : &sh.q_full, blocks & 1))) break;
                     ++blocks;
                     v_place = k_place;
                     v_place.skip(end - first > 1 ? 2 : 1);
@@ -709,7 +862,7 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                             if (!active(x, j)) continue;
                             if (!v_here) {
                                 if (!(alive = wait(&sh.full[v_place.stage], v_place.phase))) break;
-                                if ((j * TILE < all_from || j * TILE + TILE - 1 > all_to) && !(alive = wait(&sh.cleared[v_place.stage], v_place.phase))) break;
+                                if (KIND != EIGHT && (j * TILE < all_from || j * TILE + TILE - 1 > all_to) && !(alive = wait(&sh.cleared[v_place.stage], v_place.phase))) break;
                                 v_here = true;
                             }
                             const bool begins = j == (x ? from1 : from0);
@@ -735,9 +888,10 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 }
             }
             __syncwarp();
-        } else {
+        } else if (warp == (KIND == EIGHT ? 12 + (warp & 3) : CLEAR_WARP)) {
             // ---- rows of V that not all tokens see -------------------------------------------------------------------------------
             int tiles = 0;
+            uint32_t scaled = 0;                     // in 8 bits: tiles whose scales have been handed on
             bool alive = true;
             while (alive) {
                 const Plan *const taken = take();
@@ -747,6 +901,71 @@ template <bool BF, int DP> __global__ void __launch_bounds__(THREADS, 1)
                 bool bad = false;
                 for (int n = 0; n < 2 * (end - first) && alive; ++n, ++tiles) {
                     const int stage = tiles % STAGES, last = 2 * (end - first) - 1, j = n == last ? end - 1 : first + n / 2 - 1;
+                    if (KIND == EIGHT) {
+                        const bool is_v = n == last || (n > 0 && n % 2 == 0);
+                        const int raw_stage = tiles % RAW;
+                        if (!(alive = warp_wait(&sh.raw_full[raw_stage], (tiles / RAW) & 1))) break;
+                        if (!is_v) {
+                            // of K: its rows' scales, and those of V of the same tile; what no token sees weighs nothing, whatever its scale
+                            const int k_tile = n == 0 ? first : first + (n + 1) / 2;
+                            const uint32_t slot = scaled % SCALES;
+                            const int quarter = warp & 3;
+                            if (scaled >= SCALES && !(alive = warp_wait(&sh.scales_empty[slot], (scaled / SCALES - 1) & 1))) break;
+                            {
+                                const int r = lane + 32 * quarter, number = k_tile * TILE + r;
+                                const float *const from = raw_scales + raw_stage * 2 * TILE + r;
+                                float v = from[TILE];
+                                if (number < plan.sees_from || number > plan.sees_to) v = 0.f;
+                                if ((number < plan.all_from || number > plan.all_to) && !(v - v == 0.f)) {
+                                    v = 0.f;
+                                    bad = true;
+                                }
+                                float *const to = scales + slot * 3 * TILE + r;
+                                to[0] = from[0];
+                                to[TILE] = v;
+                                to[2 * TILE] = log2_of(fmaxf(fabsf(v), kMinRowScale));
+                            }
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(&sh.scales_full[slot]);
+                            ++scaled;
+                        }
+                        if (tiles >= STAGES && !(alive = warp_wait(&sh.empty[stage], (tiles / STAGES - 1) & 1))) break;
+                        // 16 values a lane: two chunks of a swizzled row, the second one first in the second block, so that lanes of both fall into different banks
+                        constexpr int PER_ROW = DP / 16;
+#pragma unroll 4
+                        for (int i = lane + (warp & 3) * (TILE / 4 * PER_ROW); i < ((warp & 3) + 1) * (TILE / 4 * PER_ROW); i += 32) {
+                            const int r = i / PER_ROW, c = i % PER_ROW, number = j * TILE + r;
+                            const uint4 u = *reinterpret_cast<const uint4 *>(raw_tiles + raw_stage * S::RAW_BYTES + i * 16);
+                            uint32_t w[4] = {u.x, u.y, u.z, u.w}, h[8];
+                            if (is_v && (number < plan.all_from || number > plan.all_to)) {
+                                const bool none = number < plan.sees_from || number > plan.sees_to;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    // NaN: all bits but the sign's
+                                    const uint32_t nan = __vcmpeq4(w[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                                    bad |= !none && nan != 0;
+                                    w[e] = none ? 0 : w[e] & ~nan;
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                h[2 * e] = two_of_e4m3(w[e]);
+                                h[2 * e + 1] = two_of_e4m3(w[e] >> 16);
+                            }
+                            uint8_t *const row = ring + stage * S::BYTES + c / 4 * BLOCK + r * 128;
+                            const int chunk = c % 4 * 2, swap = c / 4;
+                            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+                            *reinterpret_cast<uint4 *>(row + 16 * ((chunk + swap) ^ (r & 7))) = swap ? hi : lo;
+                            *reinterpret_cast<uint4 *>(row + 16 * ((chunk + 1 - swap) ^ (r & 7))) = swap ? lo : hi;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            bar_arrive(&sh.full[stage]);
+                            bar_arrive(&sh.raw_empty[raw_stage]);
+                        }
+                        continue;
+                    }
                     if (!(alive = warp_wait(&sh.full[stage], (tiles / STAGES) & 1))) break;
                     if ((n == last || (n > 0 && n % 2 == 0)) && plan.ragged(j)) {          // of V: the others are of K
                         // a lane has one 16-byte chunk of every fourth row
@@ -921,28 +1140,31 @@ EncodeTiled encode_tiled()
 }
 
 // strides in bytes, of all dimensions but the first
-bool encode(CUtensorMap *map, const void *at, int dims, const cuuint64_t *sizes, const cuuint64_t *strides, const cuuint32_t *box)
+bool encode(CUtensorMap *map, const void *at, int dims, const cuuint64_t *sizes, const cuuint64_t *strides, const cuuint32_t *box, bool bytes = false)
 {
     const EncodeTiled f = encode_tiled();
     const cuuint32_t steps[4] = {1, 1, 1, 1};
-    return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, cuuint32_t(dims), const_cast<void *>(at), sizes, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return f && f(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, cuuint32_t(dims), const_cast<void *>(at), sizes, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF, int DP> cudaError_t launch(const Args &p, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int ctas, cudaStream_t stream)
+template <int KIND, int DP> cudaError_t launch(const Args &p, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int ctas, cudaStream_t stream)
 {
-    const auto kernel = prompt_kernel<BF, DP>;
+    using S = Shape<KIND, DP>;
+    const auto kernel = prompt_kernel<KIND, DP>;
     // The warps' shares of registers come out of what the block has from the start.
     static const bool enough = [&] {
         cudaFuncAttributes attr;
-        return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs * THREADS >= 32 * SOFTMAX_WARPS * SOFTMAX_REGISTERS + (THREADS - 32 * SOFTMAX_WARPS) * OTHER_REGISTERS;
+        return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs * S::THREADS >= 32 * SOFTMAX_WARPS * S::SOFTMAX_REGISTERS + (S::THREADS - 32 * SOFTMAX_WARPS) * S::OTHER_REGISTERS;
     }();
     if (!enough) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = allow_shared<prompt_kernel<BF, DP>>(Shape<DP>::SMEM);
+    const cudaError_t e = allow_shared<prompt_kernel<KIND, DP>>(S::SMEM);
     if (e != cudaSuccess) return e;
-    const cudaError_t launched = launch_after(kernel, dim3(unsigned(ctas)), dim3(THREADS), Shape<DP>::SMEM, stream, dim3(1, 1), p, q, k, v);
+    const cudaError_t launched = launch_after(kernel, dim3(unsigned(ctas)), dim3(S::THREADS), S::SMEM, stream, dim3(1, 1), p, q, k, v);
     if (launched != cudaSuccess || p.parts == 1) return launched;
-    return launch_after(join_kernel<BF>, dim3(unsigned(ctas / p.parts), unsigned((p.a.cache.d + JOIN_COLUMNS - 1) / JOIN_COLUMNS), unsigned((p.block > p.tokens ? 2 : 1) * TILE / 32)), dim3(32 * JOIN_WARPS), 0, stream, dim3(1, 1), p);
+    const auto join = p.a.type == STRASSEN_BF16 ? join_kernel<true> : join_kernel<false>;
+    return launch_after(join, dim3(unsigned(ctas / p.parts), unsigned((p.a.cache.d + JOIN_COLUMNS - 1) / JOIN_COLUMNS), unsigned((p.block > p.tokens ? 2 : 1) * TILE / 32)), dim3(32 * JOIN_WARPS), 0, stream, dim3(1, 1), p);
 }
 
 }  // namespace
@@ -963,14 +1185,12 @@ bool prompt_takes(const AttentionArgs &a, int sm_count)
 
 int64_t prompt_workspace(const AttentionArgs &a, int sm_count)
 {
-    if (a.cache.type == STRASSEN_E4M3) return 0;
     const prompt::Cut c = prompt::cut_of(a, sm_count);
     return c.parts > 1 ? c.most * c.parts * prompt::part_floats(a.cache.d) * 4 : 0;
 }
 
 cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t stream)
 {
-    if (given.cache.type == STRASSEN_E4M3) return launch_simple(given, stream);
     prompt::Args p;
     p.a = given;
     AttentionArgs &a = p.a;
@@ -996,8 +1216,9 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
     if (a.cache.pages > 0) {
         const cuuint64_t sizes[4] = {cuuint64_t(a.cache.d), cuuint64_t(page), cuuint64_t(a.cache.kv_heads), cuuint64_t(a.cache.pages)};
         const cuuint64_t strides[3] = {cuuint64_t(a.cache.row_stride), cuuint64_t(a.cache.head_stride), cuuint64_t(a.cache.page_stride)};
-        const cuuint32_t box[4] = {64, cuuint32_t(p.box), 1, 1};
-        if (!prompt::encode(&k, a.cache.k, 4, sizes, strides, box) || !prompt::encode(&v, a.cache.v, 4, sizes, strides, box)) return cudaErrorInvalidValue;
+        const bool eight = a.cache.type == STRASSEN_E4M3;             // whole rows, not swizzled
+        const cuuint32_t box[4] = {cuuint32_t(eight && a.cache.d > 64 ? 128 : 64), cuuint32_t(p.box), 1, 1};
+        if (!prompt::encode(&k, a.cache.k, 4, sizes, strides, box, eight) || !prompt::encode(&v, a.cache.v, 4, sizes, strides, box, eight)) return cudaErrorInvalidValue;
     } else {
         // rows that are not there read as zeros, whose mean is what a token that sees nothing gets
         a.seq.width = 0;
@@ -1005,8 +1226,10 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
     }
     const int64_t all = c.most * c.parts;
     const int ctas = int(all < sm_count ? all : sm_count);
-    if (a.type == STRASSEN_BF16) return a.cache.d <= 64 ? prompt::launch<true, 64>(p, q, k, v, ctas, stream) : prompt::launch<true, 128>(p, q, k, v, ctas, stream);
-    return a.cache.d <= 64 ? prompt::launch<false, 64>(p, q, k, v, ctas, stream) : prompt::launch<false, 128>(p, q, k, v, ctas, stream);
+    const bool narrow = a.cache.d <= 64;
+    if (a.cache.type == STRASSEN_BF16) return narrow ? prompt::launch<prompt::BF16, 64>(p, q, k, v, ctas, stream) : prompt::launch<prompt::BF16, 128>(p, q, k, v, ctas, stream);
+    if (a.cache.type == STRASSEN_F16) return narrow ? prompt::launch<prompt::F16, 64>(p, q, k, v, ctas, stream) : prompt::launch<prompt::F16, 128>(p, q, k, v, ctas, stream);
+    return narrow ? prompt::launch<prompt::EIGHT, 64>(p, q, k, v, ctas, stream) : prompt::launch<prompt::EIGHT, 128>(p, q, k, v, ctas, stream);
 }
 
 }  // namespace strassen

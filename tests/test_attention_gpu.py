@@ -258,11 +258,12 @@ def test_nothing_to_do():
 
 # ---- prompts --------------------------------------------------------------------------------------------------------
 
+@pytest.mark.parametrize("cache", [None, E4M3])
 @pytest.mark.parametrize("page", [8, 16, 64, 128, 512])
 @pytest.mark.parametrize("lengths,counts", [([1], [1]), ([7, 130, 1], [7, 130, 1]), ([128, 256, 127, 129], [128, 256, 127, 129]), ([700], [700]),
                                             ([500, 40, 1000, 0, 300], [3, 40, 129, 0, 17]), ([2000], [64])])
-def test_prompt_lengths(lengths, counts, page):
-    c = Case(lengths, counts, page=page, seed=page)
+def test_prompt_lengths(lengths, counts, page, cache):
+    c = Case(lengths, counts, page=page, seed=page, cache=cache)
     close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
 
 
@@ -279,26 +280,30 @@ def test_prompt_head_sizes_of_16_bits():
         close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
 
 
+@pytest.mark.parametrize("cache", [None, E4M3])
 @pytest.mark.parametrize("window", [1, 2, 16, 100, 129, 300, 5000, 2 ** 40])
-def test_prompt_window(window):
-    c = Case([1, 99, 100, 901, 1500], [1, 99, 7, 901, 300], page=16, heads=4, kv=2, seed=window % 1000)
+def test_prompt_window(window, cache):
+    c = Case([1, 99, 100, 901, 1500], [1, 99, 7, 901, 300], page=16, heads=4, kv=2, seed=window % 1000, cache=cache)
     close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, window=window), *c.reference(window=window))
 
 
 @pytest.mark.parametrize("layout", ["rows", "heads"])
-def test_prompt_other_orders_of_the_cache(layout):
-    c = Case([333, 65], [333, 60], layout=layout, heads=6, kv=3)
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_prompt_other_orders_of_the_cache(layout, cache):
+    c = Case([333, 65], [333, 60], layout=layout, heads=6, kv=3, cache=cache)
     close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
 
 
-def test_prompt_long_and_many():
-    for lengths, counts, kv in (([3500], [3500], 1), ([1 + 37 * i % 200 for i in range(150)], None, 1), ([20000, 33], [100, 33], 2)):
-        c = Case(lengths, counts or lengths, heads=4 * kv, kv=kv, page=64, seed=len(lengths))
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_prompt_long_and_many(cache):
+    for lengths, counts, kv in (([3500], [3500], 1), ([1 + 37 * i % 200 for i in range(150)], None, 1), ([20000, 33], [100, 33], 2), ([300 + i for i in range(33)], [1 + 5 * i for i in range(33)], 1)):
+        c = Case(lengths, counts or lengths, heads=4 * kv, kv=kv, page=64, seed=len(lengths), cache=cache)
         close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
 
 
-def test_prompt_scores_far_apart():
-    c = Case([1000, 513], [1000, 200], spread=6.0, dtype=torch.float16, seed=3, heads=4, kv=1)
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_prompt_scores_far_apart(cache):
+    c = Case([1000, 513], [1000, 200], spread=6.0, dtype=torch.float16, seed=3, heads=4, kv=1, cache=cache)
     for scale in (0.02, -0.03, 0.0):
         close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, scale=scale), *c.reference(scale=scale))
     # scores that rise by hundreds, so that what was added up before is scaled down again and again
@@ -308,6 +313,32 @@ def test_prompt_scores_far_apart():
     fill(c, 0, k, torch.randn(n, 1, 128, device="cuda", generator=gen(4)))
     c.q[:, :, 0] = 1.0
     close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, scale=1.0), *c.reference(scale=1.0))
+
+
+def test_prompt_values_of_very_different_rows_in_8_bits():
+    """Value rows of 2^-60 and of 2^20 side by side, zeros among them; queries of 2^-30 and of 2^30."""
+    n = 300
+    c = Case([n], [200], heads=4, kv=1, d=64, cache=E4M3)
+    g = gen(5)
+    v = torch.randn(n, 1, 64, device="cuda", generator=g) * torch.exp2(torch.randint(-60, 20, (n, 1, 1), device="cuda", generator=g).float())
+    v[7] = 0
+    fill(c, 0, torch.randn(n, 1, 64, device="cuda", generator=g), v)
+    close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
+    fill(c, 0, torch.randn(n, 1, 64, device="cuda", generator=g) * 2.0 ** -30, v)
+    c.q = (c.q.float() * 2.0 ** 30).bfloat16()
+    close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
+    fill(c, 0, torch.randn(n, 1, 64, device="cuda", generator=g) * 2.0 ** 30, v)
+    c.q = (c.q.float() * 2.0 ** -60).bfloat16()
+    close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets), *c.reference())
+    close(sw.decode_attention(c.q[-1:], c.cache, c.table, c.lengths), *(x[-1:] for x in c.reference()))
+
+
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_few_tokens_behind_many_rows_in_parts(cache):
+    """Where the cache is cut into parts: tokens that see a part only, windows that leave parts empty, several sequences of very different lengths."""
+    for lengths, counts, heads, kv, window in (([5000], [3], 4, 1, 0), ([5000], [70], 8, 2, 0), ([5000, 60, 0, 1300], [2, 60, 0, 5], 2, 1, 0), ([5000], [40], 4, 1, 300), ([4000], [1], 1, 1, 0), ([900], [20], 130, 1, 0)):
+        c = Case(lengths, counts, heads=heads, kv=kv, d=80, page=64, dtype=torch.float16, cache=cache, seed=counts[0])
+        close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, window=window), *c.reference(window=window))
 
 
 def test_prompt_strided_and_misaligned_queries_and_results():
@@ -360,16 +391,21 @@ def test_offsets_of_any_kind_touch_nothing_else(offsets):
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("at", [0, 1, 150, 255, 399])
-def test_what_a_token_does_not_see_has_no_effect(bad, which, at):
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_what_a_token_does_not_see_has_no_effect(bad, which, at, cache):
     """One bad row at a position of a prompt: the tokens before it, and those a window later, are as if it were finite; the others are not."""
     window = 70
-    c = Case([400], [400], heads=4, kv=2, d=64, page=16)
+    c = Case([400], [400], heads=4, kv=2, d=64, page=16, cache=cache)
     for w in (0, window):
         want, tol = c.reference(window=w)
         store = c.cache.k if which == "k" else c.cache.v
         page, slot = int(c.table[0, at // 16]), at % 16
+        if cache == E4M3:                                        # there an infinity can be a row's scale
+            store, column = c.cache.k_scale if which == "k" else c.cache.v_scale, ()
+        else:
+            column = (5,)
         keep = store[page, 1, slot].clone()
-        store[page, 1, slot, 5] = bad
+        store[(page, 1, slot) + column] = bad
         got = sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, window=w)
         one = sw.decode_attention(c.q[-1:], c.cache, c.table, c.lengths, window=w)
         store[page, 1, slot] = keep
@@ -377,7 +413,9 @@ def test_what_a_token_does_not_see_has_no_effect(bad, which, at):
         sees[at:at + w if w else None] = True
         close(got[~sees], want[~sees], tol[~sees])
         close(got[:, :2], want[:, :2], tol[:, :2])
-        if which == "v":                                         # the column is what the definition gives, the others are as ever
+        if cache == E4M3:
+            assert not bool(torch.isfinite(got[sees][:, 2:]).any()) if which == "v" else (bad == bad or bool(torch.isnan(got[sees][:, 2:]).all()))
+        elif which == "v":                                       # the column is what the definition gives, the others are as ever
             assert bool((got[sees][:, 2:, 5].float().nan_to_num(1.5, 2.5, -2.5) == torch.tensor(bad).nan_to_num(1.5, 2.5, -2.5).item()).all())
             others = [i for i in range(64) if i != 5]
             close(got[..., others], want[..., others], tol[..., others])
