@@ -8,7 +8,7 @@ devices, the memory and the current stream.  ``SelfAttention`` runs them togethe
 Row j of sequence b lies in page ``table[b, j // page_size]``, slot ``j % page_size``.  ``lengths[b]`` counts the sequence's rows with its new ones, which are the
 last ``offsets[b + 1] - offsets[b]``: rows ``offsets[b]`` to ``offsets[b + 1] - 1`` of q.  Without offsets each sequence has one new token.  ``table``,
 ``lengths`` and ``offsets`` are int32 CUDA tensors that the kernels read, so that a captured graph can be replayed for other lengths; which pages are
-handed to which sequence is the caller's to decide.
+handed to which sequence is the caller's to decide.  Rows that belong to no sequence are not written (what a new result holds for them is not defined).
 
 Calls are enqueued on the current stream and can be captured into a CUDA graph.  The operators serve a model and have no backward pass: tensors that require
 grad are refused unless gradients are off (``torch.no_grad()``).  Tensors that are written count as modified in place.
@@ -245,11 +245,11 @@ class SelfAttention:
             raise ValueError("the block has %d key heads of %d, the cache %d of %d" % (self.kv_heads, self.head_size, cache.kv_heads, cache.head_size))
         n, s, h = rms_norm_quant(x, self.norm_weight, self.eps, residual=residual)
         dtype = x.dtype if x.dtype is not torch.float32 else cache.dtype if cache.dtype is not E4M3 else torch.bfloat16
-        rows = self.qkv(n, s, dtype=dtype).view(x.shape[0], -1, self.head_size)
+        rows = self.qkv(n, s, dtype=dtype).view(x.shape[0], self.heads + 2 * self.kv_heads, self.head_size)
         q, k, v = rows[:, :self.heads], rows[:, self.heads:self.heads + self.kv_heads], rows[:, self.heads + self.kv_heads:]
         rotate_append(q, k, v, cache, table, lengths, self.frequencies, offsets, self.interleaved, out=q)
         a = _attention(q, cache, table, lengths, offsets, self.scale, self.window, None)
-        return self.o(a.view(x.shape[0], -1)).to(x.dtype), h
+        return self.o(a.view(x.shape[0], self.o.k)).to(x.dtype), h
 
 
 def main():

@@ -33,6 +33,7 @@ cudaError_t launch_decode(const AttentionArgs &a, int sm_count, cudaStream_t str
     const Shape s = shape_of(a);
     decode::Args p;
     p.a = a;
+    if (a.cache.pages == 0) p.a.seq.width = 0;       // rows that are not there read as zeros, whose mean is what a token that sees nothing gets
     p.items = a.cache.kv_heads * s.blocks;
     p.blocks = s.blocks;
     p.group = a.heads / a.cache.kv_heads;

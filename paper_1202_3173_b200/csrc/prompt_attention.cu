@@ -229,13 +229,15 @@ struct Order {
         const int stop = __shfl_down_sync(~0u, my_begin, 1);
         if (lane < s.batch && stop > my_begin) my_count = stop - my_begin;
         my_blocks = (my_count + p.block - 1) / p.block;
-        all = __reduce_add_sync(~0u, my_blocks);
+        // no more than there are places for, whatever offsets hold
+        all = min(__reduce_add_sync(~0u, my_blocks), int(s.tokens / p.block) + s.batch);
     }
     // Blocks of the lane's sequence whose last token sees c tiles or more before its own, with a window as many as it leaves.  They are the last ones.
     __device__ __forceinline__ int dear(int c) const
     {
+        if (c <= 0) return my_blocks;                // those of tokens that see nothing among them
         const int64_t row = int64_t(c) * TILE, start = int64_t(my_length) - my_count;
-        if (my_count == 0 || start + my_count - 1 < row || (p.a.window && row > int64_t(p.a.window) + p.block)) return c <= 0 ? my_blocks : 0;
+        if (my_count == 0 || start + my_count - 1 < row || (p.a.window && row > int64_t(p.a.window) + p.block)) return 0;
         // here 0 <= row < length, so that 32 bits do: a division of 64 takes longer than the rest
         const uint32_t before = row > start ? uint32_t(row - start) / uint32_t(p.block) : 0;
         return my_blocks - (before < uint32_t(my_blocks) ? int(before) : my_blocks - 1);
@@ -389,12 +391,13 @@ template <int KIND, int DP> __global__ void __launch_bounds__(Shape<KIND, DP>::T
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     }
+    // tensor memory is taken when the work before is done: none is held while waiting for a kernel that may want it
+    after_work_before();
     if (warp == MMA_WARP) alloc(&sh.tmem);
     __syncwarp();
     before_sync();
     __syncthreads();
     after_sync();
-    after_work_before();
     const uint32_t tmem = sh.tmem;
     uint8_t *const raw_tiles = q_at + S::RAW_AT;
     float *const raw_scales = reinterpret_cast<float *>(q_at + S::RAW_SCALES_AT), *const scales = reinterpret_cast<float *>(q_at + S::SCALES_AT);

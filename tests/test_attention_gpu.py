@@ -378,6 +378,32 @@ def test_rows_outside_every_sequence_stay_and_more_new_tokens_than_rows_give_zer
     close(out[8:20], *(x[:12] for x in d.reference()))
 
 
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_many_more_new_tokens_than_rows_give_zeros(cache):
+    """300 new tokens of a sequence that has 12 rows: whole blocks of tokens see nothing."""
+    c = Case([300, 40], [300, 40], heads=4, kv=1, cache=cache)
+    out = torch.full_like(c.q, 9.0)
+    sw.prompt_attention(c.q, c.cache, c.table, torch.tensor([12, 40], dtype=torch.int32, device="cuda"), c.offsets, out=out)
+    assert not bool(out[:288].any())
+    want, tol = c.reference()
+    close(out[300:], want[300:], tol[300:])
+    c.q, c.counts, c.lengths_host, c.offsets_host = c.q[288:300], [12], [12], [0, 12]
+    c.k64[0], c.v64[0] = c.k64[0][:12], c.v64[0][:12]
+    close(out[288:300], *c.reference())
+
+
+@pytest.mark.parametrize("offsets", [[0, 40, 0, 40, 0, 40, 0, 40, 0], [0, 1, 40, 3, 40, 2, 40, 0, 40], [40] * 9, [0] * 8 + [10 ** 9]])
+def test_sequences_that_overlap_touch_nothing_else(offsets):
+    """Offsets that go to and fro, where the cache is cut into parts: more blocks of tokens than there are places for."""
+    c = Case([3000], [40], heads=1, kv=1, d=64, page=64)
+    table, lengths = c.table.expand(8, -1).contiguous(), c.lengths.expand(8).contiguous()
+    out = torch.full((40 + 64, 1, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    sw.prompt_attention(c.q, c.cache, table, lengths, torch.tensor(offsets, dtype=torch.int32, device="cuda"), out=out[:40])
+    torch.cuda.synchronize()
+    binding.strassen_device_status()
+    assert bool((out[40:] == 9).all())
+
+
 @pytest.mark.parametrize("offsets", [[0, 90, 30], [-5, 10, 10 ** 9], [2 ** 31 - 1, 0, 5], [-2 ** 31, -7, -1]])
 def test_offsets_of_any_kind_touch_nothing_else(offsets):
     c = Case([20, 30], [20, 30], heads=4, kv=1)
@@ -423,6 +449,49 @@ def test_what_a_token_does_not_see_has_no_effect(bad, which, at, cache):
             assert bool(torch.isnan(got[sees][:, 2:]).all())
         if not bool(sees[-1]):
             close(one, want[-1:], tol[-1:])
+
+
+@pytest.mark.parametrize("cache", [None, E4M3])
+def test_bad_queries_of_one_token_stay_with_their_heads(cache):
+    c = Case([300, 41, 700], heads=8, kv=2, cache=cache)
+    want, tol = c.reference()
+    c.q[1, 3, 3] = math.nan
+    c.q[2, 6, 3] = math.inf
+    got = sw.decode_attention(c.q, c.cache, c.table, c.lengths)
+    good = torch.ones(3, 8, dtype=torch.bool, device="cuda")
+    good[1, 3] = good[2, 6] = False
+    close(got[good], want[good], tol[good])
+    assert bool(torch.isnan(got[1, 3]).all())
+
+
+@pytest.mark.parametrize("cache_type", [torch.bfloat16, E4M3])
+def test_pages_beyond_four_gigabytes(cache_type):
+    """The last pages of a cache whose offsets in elements, and in bytes, take more than 32 bits."""
+    kv, d, page = 4, 128, 128
+    pages = (2 ** 32 + 2 ** 29) // (kv * d * page)
+    cache = sw.PagedCache.empty(pages, kv, d, page, cache_type)
+    f = frequencies(d)
+    g = gen(21)
+    n = 200
+    k, v, q = (torch.randn(n, h, d, device="cuda", generator=g).bfloat16() for h in (kv, kv, 8))
+    lengths, offsets = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([n], [0, n]))
+    small = sw.PagedCache.empty(2, kv, d, page, cache_type)
+    got = []
+    for c, table in ((cache, [[pages - 1, pages - 2]]), (small, [[0, 1]])):
+        table = torch.tensor(table, dtype=torch.int32, device="cuda")
+        turned = sw.rotate_append(q, k, v, c, table, lengths, f, offsets)
+        got.append((turned, sw.prompt_attention(turned, c, table, lengths, offsets), sw.decode_attention(turned[-1:], c, table, lengths)))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_a_cache_without_pages():
+    c = Case([30], [5], heads=4, kv=1, d=64)
+    for dtype in (torch.bfloat16, E4M3):
+        cache = sw.PagedCache.empty(0, 1, 64, 16, dtype)
+        sw.rotate_append(c.q, c.q[:, :1], c.q[:, :1], cache, c.table, c.lengths, None, c.offsets)
+        assert not bool(sw.prompt_attention(c.q, cache, c.table, c.lengths, c.offsets).any())
+        assert not bool(sw.decode_attention(c.q[:1], cache, c.table, c.lengths).any())
 
 
 def test_bad_queries_stay_in_their_rows():
@@ -653,6 +722,14 @@ def test_the_block(dtype, cache_type):
         q = sw.rotate_append(qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:], caches[1], table, lengths, f, offsets)
         a = sw.prompt_attention(q, caches[1], table, lengths, offsets, window=40) if offsets is not None else sw.decode_attention(q, caches[1], table, lengths, window=40)
         assert torch.equal(h, want_h) and torch.equal(y, blk.o(a.flatten(1)).to(dtype))
+
+
+def test_the_block_without_rows():
+    blk, _ = block(256, 6, 2, 64, gen(2))
+    cache = sw.PagedCache.empty(8, 2, 64, 16)
+    x = torch.empty(0, 256, dtype=torch.bfloat16, device="cuda")
+    y, h = blk(x, x, cache, torch.empty(0, 4, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert y.shape == h.shape == (0, 256)
 
 
 def test_the_example_runs():
