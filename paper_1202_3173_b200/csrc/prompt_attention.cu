@@ -1045,7 +1045,8 @@ template <bool BF> __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kerne
     if (int(blockIdx.x) * p.parts >= all_plans(p, Order(p))) return;
     const float *const header = p.sums + int64_t(blockIdx.x) * p.parts * part_floats(a.cache.d), *const first_part = header + HEADER;
     const int4 of = *reinterpret_cast<const int4 *>(header);             // tokens, row, head, heads
-    const bool mine = token < p.tokens && at < of.x && head < of.w;
+    // (of a CTA that gave up there may be no header)
+    const bool mine = token < p.tokens && at < of.x && head < of.w && of.y >= 0 && int64_t(of.y) + at < a.seq.tokens && of.z >= 0 && of.z < a.heads - head;
     if (!__syncthreads_or(mine)) return;
     float m = -INFINITY, l = 0.f, o[JOIN_COLUMNS];
 #pragma unroll
