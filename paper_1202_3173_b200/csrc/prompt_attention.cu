@@ -97,7 +97,7 @@ struct Plan {
 
 template <int KIND, int DP> struct Shape {
     // warps that clear V, in 8 bits four of a warpgroup of their own that turn tiles; all warps' registers
-    static constexpr int CLEARERS = KIND == EIGHT ? 4 : 1, THREADS = KIND == EIGHT ? 32 * 16 : 32 * 12, SOFTMAX_REGISTERS = KIND == EIGHT ? 184 : 208, OTHER_REGISTERS = KIND == EIGHT ? 72 : 88;
+    static constexpr int CLEARERS = KIND == EIGHT ? 4 : 1, THREADS = KIND == EIGHT ? 32 * 16 : 32 * 12, SOFTMAX_REGISTERS = KIND == EIGHT ? 184 : 216, OTHER_REGISTERS = 72;
     static constexpr int BLOCKS = DP / 64, BYTES = BLOCKS * BLOCK;         // of a tile
     static constexpr int STAGES = DP == 128 ? (KIND == EIGHT ? 3 : 5) : (KIND == EIGHT ? 6 : 8);
     // in 8 bits: tiles as they are in the cache; scales of a tile's rows of K and of V, as they are and as the softmax wants them
