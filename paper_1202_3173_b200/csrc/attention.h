@@ -68,14 +68,15 @@ cudaError_t prompt_gave_up(int *flag);        // reads and clears the flag of pr
 cudaError_t launch_prompt(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 
 #ifdef __CUDACC__
-// Allows Kernel its dynamic shared memory on the current device, the first time it is launched there: asked each time, a launch takes a microsecond longer.
-template <auto Kernel> cudaError_t allow_shared(int bytes)
+// Allows Kernel its dynamic shared memory, and clusters of up to 16 CTAs where it has such, on the current device, the first time it is launched there: asked each time, a launch takes a microsecond longer.
+template <auto Kernel> cudaError_t allow_shared(int bytes, bool large_clusters = false)
 {
     static std::atomic<uint64_t> done{0};            // a bit for each device; entry points refuse more than 64
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (done.load(std::memory_order_acquire) >> dev & 1)) return e;
     e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) done.fetch_or(uint64_t(1) << dev, std::memory_order_release);
     return e;
 }

@@ -34,6 +34,7 @@ namespace strassen {
 namespace decode {
 
 constexpr int WARPS = 4, STAGES = 3, THREADS = 32 * WARPS;
+constexpr int MOST_RANKS = 16;                        // CTAs of a cluster
 constexpr int HALF_STAGE = 4096, STAGE = 2 * HALF_STAGE;       // a warp's rows of K, then of V
 enum { BF16 = 0, F16 = 1, E4M3 = 2 };                          // what the cache holds
 
@@ -50,6 +51,7 @@ struct Args {
     AttentionArgs a;
     int items;            // key heads * blocks of heads
     int blocks, group;    // blocks of heads of a key head; heads of a key head
+    int ranks;            // CTAs of a cluster, where one has an item
     bool wide;            // q's rows start at multiples of 16 bytes
     Meta *meta;
     float *parts;
@@ -228,7 +230,22 @@ template <int STEP> struct Plan {
     }
 };
 
-template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2) decode_kernel(const Args p)
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The number at `at` in the shared memory of a CTA of the cluster.
+__device__ __forceinline__ float of_rank(const float *at, uint32_t rank)
+{
+    uint32_t there;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_addr(at)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
+
+// TOGETHER: a cluster has one item, whose parts its CTAs add up at the end, out of one another's shared memory.
+template <int KIND, int DP, int NT, bool TOGETHER> __global__ void __launch_bounds__(THREADS, 2) decode_kernel(const Args p)
 {
     using S = Shape<KIND, DP, NT>;
     constexpr bool BF = KIND == BF16;
@@ -236,27 +253,13 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
     constexpr float RAISE = BF ? 0.f : 12.f;             // weights are 2^(s - M + RAISE)
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ int64_t scratch[WARPS + 2];
-    __shared__ float sh_m[WARPS][8 * NT], sh_l[WARPS][8 * NT];
+    __shared__ float sh_m[WARPS][8 * NT], sh_l[WARPS][8 * NT], all_sums[2 * 8 * NT];
     const AttentionArgs &a = p.a;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     uint8_t *const ring = smem + warp * S::RING;
     uint8_t *const scales = smem + WARPS * S::RING + warp * STAGES * S::SCALES;
 
     after_work_before();
-    // sequences that see nothing
-    for (int b = blockIdx.x; b < a.seq.batch; b += gridDim.x) {
-        if (Plan<S::STEP>::steps(a, b) > 0) continue;
-        for (int i = threadIdx.x; i < a.heads * a.cache.d; i += THREADS)
-            static_cast<uint16_t *>(a.out)[b * a.out_row + i / a.cache.d * a.out_head + i % a.cache.d] = 0;
-    }
-    const Plan<S::STEP> plan(a, scratch);
-    // no run is empty: an item's parts are in neighbouring ones
-    const int64_t total = plan.total * p.items;
-    if (threadIdx.x == 0) p.meta[blockIdx.x].last = -1;
-    if (blockIdx.x >= total) return;
-    const Runs runs(total, int(total < gridDim.x ? total : gridDim.x));
-    const int64_t from = runs.begin(blockIdx.x), to = runs.begin(blockIdx.x + 1);
-
     // A place in the order of all steps; one for the copies, which run ahead, one for the products.
     struct Place {
         int b, item;
@@ -284,7 +287,30 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
             } while (steps == 0);
         }
     } ahead, at;
-    {
+    int64_t from, to;
+    Runs runs(0, 1);
+    if (TOGETHER) {
+        const int which = blockIdx.x / p.ranks, rank = blockIdx.x % p.ranks;
+        at.sequence(a, p.items == 1 ? which : which / p.items);
+        at.item = which - at.b * p.items;
+        runs = Runs(at.steps, p.ranks);
+        from = runs.begin(rank), to = runs.begin(rank + 1);
+        at.step = from;
+        ahead = at;
+    } else {
+        // sequences that see nothing
+        for (int b = blockIdx.x; b < a.seq.batch; b += gridDim.x) {
+            if (Plan<S::STEP>::steps(a, b) > 0) continue;
+            for (int i = threadIdx.x; i < a.heads * a.cache.d; i += THREADS)
+                static_cast<uint16_t *>(a.out)[b * a.out_row + i / a.cache.d * a.out_head + i % a.cache.d] = 0;
+        }
+        const Plan<S::STEP> plan(a, scratch);
+        // no run is empty: an item's parts are in neighbouring ones
+        const int64_t total = plan.total * p.items;
+        if (threadIdx.x == 0) p.meta[blockIdx.x].last = -1;
+        if (blockIdx.x >= total) return;
+        runs = Runs(total, int(total < gridDim.x ? total : gridDim.x));
+        from = runs.begin(blockIdx.x), to = runs.begin(blockIdx.x + 1);
         int b;
         int64_t before;
         plan.find(a, quotient(from, p.items), scratch, &b, &before);
@@ -683,7 +709,7 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
             __syncthreads();
             if (warp == 0) {
                 add(part(1));
-                if (ends && first_step == 0) {
+                if (!TOGETHER && ends && first_step == 0) {
                     const int kv = p.blocks == 1 ? at.item : at.item / p.blocks, head0 = kv * p.group + (p.blocks == 1 ? 0 : (at.item % p.blocks) * 8 * NT);
                     uint16_t *const out = static_cast<uint16_t *>(a.out) + at.b * a.out_row;
 #pragma unroll
@@ -705,18 +731,19 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
                         }
                 } else {
                     // the run's first item, begun in another run, or its last
-                    float *const to = p.parts + (2 * int64_t(blockIdx.x) + (first_step == 0 ? 1 : 0)) * part_floats(DP, NT);
+                    float *const to = TOGETHER ? reinterpret_cast<float *>(smem) : p.parts + (2 * int64_t(blockIdx.x) + (first_step == 0 ? 1 : 0)) * part_floats(DP, NT);
+                    float *const sums = TOGETHER ? all_sums : to + 8 * NT * DP;
                     put(to);
                     if (g == 0) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                to[8 * NT * DP + 8 * nt + 2 * t + e] = all_m[nt][e];
-                                to[8 * NT * DP + 8 * NT + 8 * nt + 2 * t + e] = all_l[nt][e];
+                                sums[8 * nt + 2 * t + e] = all_m[nt][e];
+                                sums[8 * NT + 8 * nt + 2 * t + e] = all_l[nt][e];
                             }
                     }
-                    if (lane == 0 && first_step == 0) {
+                    if (!TOGETHER && lane == 0 && first_step == 0) {
                         const int64_t last = from + n + (at.steps - at.step) - 1;            // the item's last step
                         p.meta[blockIdx.x] = {at.b, at.item, runs.of(last), 0};
                     }
@@ -726,6 +753,36 @@ template <int KIND, int DP, int NT> __global__ void __launch_bounds__(THREADS, 2
         }
         at.next(p);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    if (TOGETHER) {
+        // each CTA adds up some of the tiles of 16 values of 8 heads, a thread a number of one; ranks beyond the steps have none
+        cluster_barrier();
+        const int which = blockIdx.x / p.ranks, item = p.items == 1 ? 0 : which % p.items, b = p.items == 1 ? which : which / p.items, parts = int(runs.size > 0 ? p.ranks : runs.longer), n = threadIdx.x, head = 2 * t + (warp & 1);
+        for (int tile = blockIdx.x % p.ranks; tile < NT * MT; tile += p.ranks) {
+            const int nt = tile / MT, i = tile % MT;
+            float m[MOST_RANKS], l[MOST_RANKS], v[MOST_RANKS], most = -INFINITY, sum = 0.f, y = 0.f;
+#pragma unroll
+            for (int k = 0; k < MOST_RANKS; ++k) {
+                m[k] = -INFINITY, l[k] = v[k] = 0.f;
+                if (k >= parts) continue;
+                m[k] = of_rank(all_sums + 8 * nt + head, k);
+                l[k] = of_rank(all_sums + 8 * NT + 8 * nt + head, k);
+                v[k] = of_rank(reinterpret_cast<const float *>(smem) + tile * 128 + n, k);
+            }
+#pragma unroll
+            for (int k = 0; k < MOST_RANKS; ++k) most = fmaxf(most, m[k]);
+#pragma unroll
+            for (int k = 0; k < MOST_RANKS; ++k) {
+                const float f = m[k] == most ? 1.f : exp2_of(m[k] - most);
+                sum += f * l[k];
+                y += f * v[k];
+            }
+            const int kv = p.blocks == 1 ? item : item / p.blocks, h = kv * p.group + (p.blocks == 1 ? 0 : item % p.blocks * 8 * NT) + 8 * nt + head, at_value = value_of<KIND, DP>(i, g, warp >> 1);
+            y = sum == 0.f ? 0.f : y / sum;
+            if (h < (kv + 1) * p.group && at_value < a.cache.d)
+                static_cast<uint16_t *>(a.out)[b * a.out_row + h * a.out_head + at_value] = uint16_t(a.type == STRASSEN_BF16 ? two_16_bits<true>(y, 0.f) : two_16_bits<false>(y, 0.f));
+        }
+        cluster_barrier();                               // no CTA leaves while another reads its sums
     }
 }
 
@@ -775,12 +832,25 @@ template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds_
 template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cudaStream_t stream)
 {
     using S = Shape<KIND, DP, NT>;
-    cudaError_t e = allow_shared<decode_kernel<KIND, DP, NT>>(S::SMEM);
-    if (e != cudaSuccess) return e;
+    cudaError_t e;
     const int64_t rows = int64_t(p.a.seq.width) << p.a.cache.page_shift, seen = p.a.window && p.a.window < rows ? p.a.window : rows;
     const int64_t steps = seen > 0 ? (seen + S::STEP - 1) / S::STEP : 1, all = steps * p.items * p.a.seq.batch;
     const unsigned runs = unsigned(all < 2 * sm_count ? all : 2 * sm_count);
-    e = launch_after(decode_kernel<KIND, DP, NT>, dim3(runs), dim3(THREADS), S::SMEM, stream, dim3(1, 1), p);
+    // Few short items, as the table's width has it: each has a cluster, of as many CTAs as there is room for and steps to do, and there is no second kernel and no plan
+    // to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
+    // where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
+    // steps of a CTA, 16 where the clusters fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000: 40.9 for 38.2).
+    const int64_t items = p.items * int64_t(p.a.seq.batch);
+    p.ranks = 16 * items <= sm_count ? 16 : 8;
+    while (p.ranks > 1 && (p.ranks >= 2 * steps || p.ranks * items > 2 * sm_count)) p.ranks /= 2;
+    if (p.ranks * items <= 2 * sm_count && steps <= (p.ranks == 8 && p.ranks * items >= sm_count ? 16 : 8) * p.ranks) {
+        e = allow_shared<decode_kernel<KIND, DP, NT, true>>(S::SMEM, true);
+        if (e != cudaSuccess) return e;
+        return launch_after(decode_kernel<KIND, DP, NT, true>, dim3(unsigned(p.ranks * p.items * p.a.seq.batch)), dim3(THREADS), S::SMEM, stream, dim3(unsigned(p.ranks), 1), p);
+    }
+    e = allow_shared<decode_kernel<KIND, DP, NT, false>>(S::SMEM);
+    if (e != cudaSuccess) return e;
+    e = launch_after(decode_kernel<KIND, DP, NT, false>, dim3(runs), dim3(THREADS), S::SMEM, stream, dim3(1, 1), p);
     // items of a single step are never cut
     if (e != cudaSuccess || steps == 1) return e;
     // many parts an item: a thread has a fourth of them, so that their latencies add up to less (one sequence of 131071 rows: 95.3 us, 93.1 so); few: as many CTAs

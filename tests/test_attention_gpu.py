@@ -452,6 +452,21 @@ def test_what_a_token_does_not_see_has_no_effect(bad, which, at, cache):
 
 
 @pytest.mark.parametrize("cache", [None, E4M3])
+@pytest.mark.parametrize("heads,kv,d", [(8, 8, 64), (8, 2, 128), (32, 2, 80), (12, 1, 128)])
+@pytest.mark.parametrize("lengths", [[65, 0, 300, 1], [2000], [1000, 640, 641, 37, 999], [5000], [500 - 11 * i for i in range(40)]], ids=lambda x: "%dx%d" % (len(x), max(x)))
+def test_few_short_sequences_in_narrow_and_wide_tables(lengths, heads, kv, d, cache):
+    """A table's width says what there may be to do, the lengths what there is: work is cut by the first, results go by the second."""
+    c = Case(lengths, heads=heads, kv=kv, d=d, page=16, dtype=torch.float16 if d == 80 else torch.bfloat16, cache=cache, seed=5)
+    for window in (0, 130):
+        want, tol = c.reference(window=window)
+        for rows in (0, 1500, 7000, 40000, 200000):
+            table = torch.nn.functional.pad(c.table, (0, rows // c.page), value=-1)
+            out = torch.full_like(c.q, 9.0)
+            close(sw.decode_attention(c.q, c.cache, table, c.lengths, window=window, out=out), want, tol)
+            assert torch.equal(out, sw.decode_attention(c.q, c.cache, table, c.lengths, window=window))
+
+
+@pytest.mark.parametrize("cache", [None, E4M3])
 def test_bad_queries_of_one_token_stay_with_their_heads(cache):
     c = Case([300, 41, 700], heads=8, kv=2, cache=cache)
     want, tol = c.reference()
