@@ -570,9 +570,9 @@ int strassen_rotate_append(const strassen_paged_cache *cache, int64_t batch, con
  * strassen_decode_attention -- attention of one new token a sequence (row b of q and of out, at position lengths[b] - 1):
  *   out_h = sum over j of softmax(scale q_h . k_j) v_j,  j = 0 .. lengths[b] - 1, with a window > 0 the last `window` of them.
  *   type       of q and out: STRASSEN_BF16 or STRASSEN_F16, the cache's if that has 16 bits
- *   workspace  as strassen_decode_attention_workspace_bytes says (256-byte aligned; free again once the call's kernels are done)
+ *   workspace  as strassen_decode_attention_workspace_bytes says for the current device (0 bytes for few short sequences; 256-byte aligned; free again once the call's kernels are done)
  * Scores, the softmax's sums and the result are held in 32 bits; its weights, at most 1, are rounded to 16 bits for the product with the values.  The work is split evenly over
- * the GPU along the sequences, whatever their lengths.  out does not overlap q.
+ * the GPU along the sequences, whatever their lengths, but for few short sequences (by width), of which each is split over as many CTAs.  out does not overlap q.
  */
 int strassen_decode_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                               int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out, int64_t out_row, int64_t out_head,

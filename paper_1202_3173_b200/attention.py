@@ -70,7 +70,7 @@ class PagedCache:
         self._c = binding.strassen_paged_cache(self._kind, self.kv_heads, self.head_size, self.page_size, self.pages, k.data_ptr(), v.data_ptr(),
                                                k.stride(0), k.stride(1), row, ks, vs)
         self._at = ctypes.addressof(self._c)
-        self._decode_workspace = {}      # by heads
+        self._decode_workspace = {}      # by heads, sequences and the table's width
 
     @classmethod
     def empty(cls, pages, kv_heads, head_size, page_size=64, dtype=torch.bfloat16, device="cuda"):
@@ -186,11 +186,14 @@ def _attention(q, cache, table, lengths, offsets, scale, window, out):
         q = torch.empty(shape, dtype=q.dtype, device=cache.device).copy_(q)         # prompts are read in boxes that start at multiples of 16 bytes
         q_row, q_head, _ = q.stride()
     if offsets is None:
-        need = cache._decode_workspace.get(heads)
-        if need is None:                                        # the size goes by the heads alone
+        sizes = heads, batch, width
+        need = cache._decode_workspace.get(sizes)
+        if need is None:                                        # the size goes by these alone
+            if len(cache._decode_workspace) >= 4096:
+                cache._decode_workspace.clear()
             with torch.cuda.device(index):
                 need = binding.strassen_decode_attention_workspace_bytes(cache._at, batch, heads, width)
-            cache._decode_workspace[heads] = need
+            cache._decode_workspace[sizes] = need
     else:
         with torch.cuda.device(index) if index != _current_device() else _HERE:
             need = binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, heads, width, tokens, window)

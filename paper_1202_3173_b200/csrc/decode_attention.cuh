@@ -125,11 +125,13 @@ __device__ __forceinline__ void copy4(uint32_t to, const void *from, uint32_t by
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
+constexpr int step_of(int row) { return WARPS * (HALF_STAGE / row); }
+
 // KIND: of the cache; DP: head_size, padded with zeros; NT: blocks of 8 heads.
 template <int KIND, int DP, int NT> struct Shape {
     static constexpr int SIZE = KIND == E4M3 ? 1 : 2, ROW = DP * SIZE, CHUNKS = ROW / 16;
     static constexpr int ROWS = HALF_STAGE / ROW;              // of a warp's stage: 16, 32 or 64
-    static constexpr int STEP = WARPS * ROWS;
+    static constexpr int STEP = step_of(ROW);                  // rows of a step
     static constexpr int SCALES = KIND == E4M3 ? 8 * ROWS : 0; // bytes of the rows' scales in a stage, of K, then of V
     static constexpr int RING = STAGES * STAGE, SMEM = WARPS * STAGES * (STAGE + SCALES);
     static constexpr int MT = DP / 16;                         // tiles of 16 values in O^T
@@ -829,21 +831,36 @@ template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds_
     }
 }
 
+// Steps of a sequence at most, by the table's width.
+inline int64_t steps_of(const AttentionArgs &a, int step)
+{
+    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window && a.window < rows ? a.window : rows;
+    return seen > 0 ? (seen + step - 1) / step : 1;
+}
+
+// CTAs of an item's cluster; 0: even runs and the join kernel.
+//
+// Few short items, as the table's width has it: each has a cluster, of as many CTAs as there is room for and steps to do, and there is no second kernel and no plan
+// to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
+// where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
+// steps of a CTA, 16 where eights fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000, not taken: 40.9 for 38.2).
+// What has clusters without a window has them with one: no more steps, and no fewer CTAs than those.
+inline int ranks_of(const AttentionArgs &a, int step, int64_t heads, int sm_count)
+{
+    const int64_t steps = steps_of(a, step), items = heads * a.seq.batch;
+    int64_t ranks = 16 * items <= sm_count ? 16 : 8;
+    while (ranks > 1 && (ranks >= 2 * steps || ranks * items > 2 * sm_count)) ranks /= 2;
+    return ranks * items <= 2 * sm_count && steps <= (ranks == 8 && ranks * items >= sm_count ? 16 : 8) * ranks ? int(ranks) : 0;
+}
+
 template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cudaStream_t stream)
 {
     using S = Shape<KIND, DP, NT>;
     cudaError_t e;
-    const int64_t rows = int64_t(p.a.seq.width) << p.a.cache.page_shift, seen = p.a.window && p.a.window < rows ? p.a.window : rows;
-    const int64_t steps = seen > 0 ? (seen + S::STEP - 1) / S::STEP : 1, all = steps * p.items * p.a.seq.batch;
+    const int64_t steps = steps_of(p.a, S::STEP), all = steps * p.items * p.a.seq.batch;
     const unsigned runs = unsigned(all < 2 * sm_count ? all : 2 * sm_count);
-    // Few short items, as the table's width has it: each has a cluster, of as many CTAs as there is room for and steps to do, and there is no second kernel and no plan
-    // to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
-    // where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
-    // steps of a CTA, 16 where the clusters fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000: 40.9 for 38.2).
-    const int64_t items = p.items * int64_t(p.a.seq.batch);
-    p.ranks = 16 * items <= sm_count ? 16 : 8;
-    while (p.ranks > 1 && (p.ranks >= 2 * steps || p.ranks * items > 2 * sm_count)) p.ranks /= 2;
-    if (p.ranks * items <= 2 * sm_count && steps <= (p.ranks == 8 && p.ranks * items >= sm_count ? 16 : 8) * p.ranks) {
+    p.ranks = ranks_of(p.a, S::STEP, p.items, sm_count);
+    if (p.ranks > 0) {
         e = allow_shared<decode_kernel<KIND, DP, NT, true>>(S::SMEM, true);
         if (e != cudaSuccess) return e;
         return launch_after(decode_kernel<KIND, DP, NT, true>, dim3(unsigned(p.ranks * p.items * p.a.seq.batch)), dim3(THREADS), S::SMEM, stream, dim3(unsigned(p.ranks), 1), p);
