@@ -1,15 +1,18 @@
 // Rotary embedding of queries and keys, and keys and values stored into a paged cache.
 //
 //     (x, y) -> (x cos - y sin, x sin + y cos),   the angle of pair f at position p: p f,
-// for the pairs of a row of a head, and an 8-bit row's scale from its largest value.  A CTA has up to 8 tokens.  Their angles, the same for all heads, are found
-// first: p f / 2 pi in 64 bits, of which the fraction is an angle in 32 bits with an error of 2^-24 of a turn's size wherever p is.  Then it goes through
+// for the pairs of a row of a head, and an 8-bit row's scale from its largest value.  A CTA has up to 8 tokens, of few heads up to 64.  Their angles, the same for all heads,
+// are found first: p f / 2 pi in 64 bits, of which the fraction is an angle in 32 bits with an error of 2^-24 of a turn's size wherever p is.  Then it goes through
 // their rows; the first ones are on their way before offsets, lengths and angles are looked at, which take longer than a row.
 //
-// A lane has two chunks of 8 values of a row, both partners of its pairs, 8 lanes a row: a cosine and a sine for two values, and addresses for sixteen (Pairs).
-// Rows that do not come apart so, or are not aligned, are taken by 16 lanes with a chunk each, partners' values from theirs (Any).
+// A lane has two chunks of 8 values of a row, both partners of its pairs, as many lanes a row as it has such pairs of chunks and as many rows a warp as that leaves
+// room for: a cosine and a sine for two values, and addresses for sixteen (pairs_kernel).  Rows that do not come apart so, or are not aligned, are taken by 16
+// lanes with a chunk each, partners' values from theirs (any_kernel).
 //
 // Bound by the bytes, read once and written once, and nearly as much by instructions: 16384 tokens of 32 + 2 x 8 heads of 128, 370 MB with an 8-bit cache, in
-// 69 us, 5.4 TB/s (400 MB, 69 us, with one in bf16); with a chunk a lane 99, with a token a CTA and its angles first 139.
+// 70 us, 5.3 TB/s (400 MB, 69 us, with one in bf16); with a chunk a lane 99, with a token a CTA and its angles first 139.  Heads of 64, 49152 tokens of 16 + 2 x 8: 53 us
+// (80 with 8 lanes a row, half of them idle); of 80, 39320 tokens: 81 (90).  One head over one, 262144 tokens: 66 us (108 with 8 tokens a CTA), of 64 values, 524288 tokens:
+// 107 (269); there the angles and where a token goes are most of the work.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -21,7 +24,7 @@ namespace strassen {
 
 namespace {
 
-constexpr int THREADS = 256, MOST_TOKENS = 8, MOST_PAIRS = kMostHeadSize / 2, CTAS_AN_SM = 3;
+constexpr int THREADS = 256, MOST_TOKENS = 64, ROWS = 384, MOST_PAIRS = kMostHeadSize / 2, CTAS_AN_SM = 3;
 
 template <bool BF16> __device__ __forceinline__ float2 two_floats(uint32_t w)
 {
@@ -93,8 +96,9 @@ __device__ __forceinline__ void look(const AppendArgs &p, int64_t t0, int tokens
         sh.page[threadIdx.x] = position < 0 ? -1 : page_of(p.cache, p.seq, b, position);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < tokens * MOST_PAIRS; i += THREADS) {
-        const int token = i / MOST_PAIRS, f = i % MOST_PAIRS;
+    const int shift = 32 - __clz(max(p.rotary / 2 - 1, 0));             // pairs, rounded up to a power of two
+    for (int i = threadIdx.x; i < tokens << shift; i += THREADS) {
+        const int token = i >> shift, f = i & ((1 << shift) - 1);
         if (f >= p.rotary / 2) continue;
         // 1 / 2 pi
         const double turn = double(sh.position[token]) * double(p.frequencies[f]) * 0.15915494309189535;
@@ -122,8 +126,8 @@ struct Which {
     __device__ __forceinline__ Which(const AppendArgs &p, int r) : is_q(r < p.heads), is_v(r >= p.heads + p.cache.kv_heads), head(is_q ? r : is_v ? r - p.heads - p.cache.kv_heads : r - p.heads) {}
 };
 
-// LANES lanes have a row's values v, COUNT of them each, in chunks of 8 at places first[0], first[1]; chunks from head_size on are not there.
-template <bool BF16, bool E4M3, bool WIDE, int LANES, int CHUNKS> __device__ __forceinline__ void store(const AppendArgs &p, const Tokens &sh, int64_t t0, int token, Which of, float (&v)[CHUNKS][8], const int (&first)[CHUNKS])
+// `lanes` neighbouring lanes, up to 16, have a row's values v, lane `lane` of them chunks of 8 at places first[0], first[1]; chunks from head_size on are not there.
+template <bool BF16, bool E4M3, bool WIDE, int CHUNKS> __device__ __forceinline__ void store(int lane, int lanes, const AppendArgs &p, const Tokens &sh, int64_t t0, int token, Which of, float (&v)[CHUNKS][8], const int (&first)[CHUNKS])
 {
     const int d = p.cache.d;
     if (of.is_q) {
@@ -151,9 +155,10 @@ template <bool BF16, bool E4M3, bool WIDE, int LANES, int CHUNKS> __device__ __f
         for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) most = largest(most, fabsf(v[k][i]));
-        const uint32_t mine = ((1u << LANES) - 1) << (threadIdx.x & 31 & ~(LANES - 1));
-#pragma unroll
-        for (int i = LANES / 2; i > 0; i >>= 1) most = largest(most, __shfl_xor_sync(mine, most, i));
+        const int begin = (threadIdx.x & 31) - lane;
+        const uint32_t mine = ((1u << lanes) - 1) << begin;
+        // each lane's with that of the next, of the next but one, ..: all of them, however many there are, since some twice do no harm
+        for (int i = 1; i < lanes; i <<= 1) most = largest(most, __shfl_sync(mine, most, begin + (lane + i < lanes ? lane + i : lane + i - lanes)));
         // a row with NaN has NaN for its scale, and throughout
         const float scale = largest(most / kE4M3Max, kMinRowScale), inv = 1.f / scale;
         if (page < 0) return;
@@ -169,7 +174,7 @@ template <bool BF16, bool E4M3, bool WIDE, int LANES, int CHUNKS> __device__ __f
             }
             *reinterpret_cast<uint2 *>(row + first[k]) = make_uint2(w[0], w[1]);
         }
-        if (threadIdx.x % LANES == 0) (of.is_v ? p.cache.v_scale : p.cache.k_scale)[((int64_t(page) * p.cache.kv_heads + of.head) << p.cache.page_shift) + slot] = scale;
+        if (lane == 0) (of.is_v ? p.cache.v_scale : p.cache.k_scale)[((int64_t(page) * p.cache.kv_heads + of.head) << p.cache.page_shift) + slot] = scale;
     } else if (page >= 0) {
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k)
@@ -178,20 +183,25 @@ template <bool BF16, bool E4M3, bool WIDE, int LANES, int CHUNKS> __device__ __f
     }
 }
 
-template <bool BF16, bool E4M3> __global__ void __launch_bounds__(THREADS, CTAS_AN_SM) pairs_kernel(const AppendArgs p, int per)
+// LANES: of a row, 0 for `given`.
+template <bool BF16, bool E4M3, int LANES> __global__ void __launch_bounds__(THREADS, CTAS_AN_SM) pairs_kernel(const AppendArgs p, int per, int given)
 {
-    constexpr int AT_ONCE = 2, SLOTS = THREADS / 8;         // rows of a lane under way at once
+    const int lanes = LANES ? LANES : given;
+    constexpr int AT_ONCE = 2;                              // rows of a lane under way at once
     __shared__ Tokens sh;
     after_work_before();
-    const int lane = threadIdx.x & 7, d = p.cache.d, half = p.rotary / 2, rows = p.heads + 2 * p.cache.kv_heads, stride = SLOTS * gridDim.y;
+    // a warp has as many rows as fit; lanes left over have none
+    const int in_warp = 32 / lanes, group = (threadIdx.x & 31) / lanes, lane = (threadIdx.x & 31) - group * lanes, slots = THREADS / 32 * in_warp;
+    const int d = p.cache.d, half = p.rotary / 2, rows = p.heads + 2 * p.cache.kv_heads, stride = slots * gridDim.y;
     const int64_t t0 = int64_t(blockIdx.x) * per;
     const int tokens = int(p.seq.tokens - t0 < per ? p.seq.tokens - t0 : per);
     // the lane's chunks: partners where pairs are half of the turned values apart, else neighbours
     const bool apart = !p.interleaved && 8 * lane < half;
     const int first[2] = {16 * lane >= d ? d : apart ? 8 * lane : 16 * lane, 16 * lane >= d ? d : apart ? 8 * lane + half : 16 * lane + 8};
-    const bool there = 16 * lane < d;
+    const bool there = 16 * lane < d && group < in_warp;
     Row at = {0, 0};
-    at.next(blockIdx.y * SLOTS + threadIdx.x / 8, rows);
+    if (group < in_warp) at.next(blockIdx.y * slots + threadIdx.x / 32 * in_warp + group, rows);
+    else at.token = tokens;
     uint4 x[AT_ONCE][2];
     const auto load = [&] {
         Row w = at;
@@ -246,7 +256,7 @@ template <bool BF16, bool E4M3> __global__ void __launch_bounds__(THREADS, CTAS_
                     }
                 }
             }
-            store<BF16, E4M3, true, 8, 2>(p, sh, t0, w.token, of, v, first);
+            store<BF16, E4M3, true, 2>(lane, lanes, p, sh, t0, w.token, of, v, first);
         }
         at.next(AT_ONCE * stride, rows);
         load();
@@ -282,18 +292,32 @@ template <bool BF16, bool E4M3, bool WIDE> __global__ void __launch_bounds__(THR
             }
         }
         __syncwarp(0xffffu << (threadIdx.x & 16));           // in place: a row is read by all of its lanes before it is written
-        store<BF16, E4M3, WIDE, 16, 1>(p, sh, t0, w.token, of, v, first);
+        store<BF16, E4M3, WIDE, 1>(lane, 16, p, sh, t0, w.token, of, v, first);
     }
 }
 
 template <bool BF16, bool E4M3> cudaError_t launch(const AppendArgs &a, int sm_count, cudaStream_t stream)
 {
     const bool pairs = a.wide && a.cache.d % 16 == 0 && a.rotary % (a.interleaved ? 8 : 16) == 0;
-    // as many tokens a CTA as leave each SM its CTAs; where there are few tokens, a token's rows in several
-    const int64_t tokens = a.seq.tokens / (CTAS_AN_SM * sm_count), per = tokens < 1 ? 1 : tokens < MOST_TOKENS ? tokens : MOST_TOKENS, ctas = (a.seq.tokens + per - 1) / per;
-    const int slots = THREADS / (pairs ? 8 : 16), steps = (a.heads + 2 * a.cache.kv_heads + slots - 1) / slots;
+    const int rows = a.heads + 2 * a.cache.kv_heads, lanes = pairs ? (a.cache.d + 15) / 16 : 16;
+    // as many tokens a CTA as leave each SM its CTAs, up to 8, or of few heads 64, about ROWS rows: then a CTA has more to do than to look up where its
+    // tokens are; where there are few tokens, a token's rows in several
+    const int64_t tokens = a.seq.tokens / (CTAS_AN_SM * sm_count), most = rows * 8 >= ROWS ? 8 : ROWS / rows < MOST_TOKENS ? ROWS / rows : MOST_TOKENS,
+                  per = tokens < 1 ? 1 : tokens < most ? tokens : most, ctas = (a.seq.tokens + per - 1) / per;
+    const int slots = THREADS / 32 * (32 / lanes), steps = (rows + slots - 1) / slots;
     const dim3 grid(unsigned(ctas), unsigned(ctas >= sm_count ? 1 : steps < 16 ? steps : 16));
-    if (pairs) return launch_after(pairs_kernel<BF16, E4M3>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per));
+    // with the number of lanes known to the compiler 66 us where it is 71 (24576 tokens of 16 + 2 x 8 heads of 128, 8-bit cache), so the larger heads have it
+    const auto with = [&](auto kernel) { return launch_after(kernel, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per), lanes); };
+    if (pairs) {
+        switch (lanes) {
+        case 8: return with(pairs_kernel<BF16, E4M3, 8>);
+        case 7: return with(pairs_kernel<BF16, E4M3, 7>);
+        case 6: return with(pairs_kernel<BF16, E4M3, 6>);
+        case 5: return with(pairs_kernel<BF16, E4M3, 5>);
+        case 4: return with(pairs_kernel<BF16, E4M3, 4>);
+        default: return with(pairs_kernel<BF16, E4M3, 0>);
+        }
+    }
     return a.wide ? launch_after(any_kernel<BF16, E4M3, true>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per))
                   : launch_after(any_kernel<BF16, E4M3, false>, grid, dim3(THREADS), 0, stream, dim3(1, 1), a, int(per));
 }

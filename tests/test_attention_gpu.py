@@ -600,6 +600,13 @@ def test_append(heads, kv, d, rotary, interleaved, dtype, cache):
     check_append(heads, kv, d, dtype, cache, rotary, interleaved, [37, 100, 0, 1], [37, 9, 0, 1])
 
 
+@pytest.mark.parametrize("cache", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("d", [16, 32, 48, 64, 80, 96, 112, 128])
+def test_append_many_tokens_of_few_heads(d, cache):
+    """Blocks of up to 64 tokens, of several sequences, and rows of 1 to 8 lanes."""
+    check_append(1, 1, d, torch.bfloat16, cache, d if d % 32 else 32, d % 32 == 0, [12000, 700, 0, 65, 9001, 3000, 64], [12000, 3, 0, 65, 9001, 2999, 64], page=32)
+
+
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("cache", [torch.bfloat16, E4M3])
 def test_append_one_token_each(cache, in_place):
