@@ -42,9 +42,9 @@ enum { BF16 = 0, F16 = 1, E4M3 = 2 };                          // what the cache
 __host__ __device__ constexpr int part_floats(int dp, int nt) { return 8 * nt * (dp + 2); }
 
 struct Meta {
-    int b, item;          // the item that begins in this run and does not end in it
-    int last;             // the run it ends in; -1: there is no such item
-    int unused;
+    int b, item;          // the item that begins in this run and does not end in it, or (by_item) this item
+    int last;             // the run it ends in; -1: there is no such item, or it is in one run
+    int first;            // the run it begins in
 };
 
 struct Args {
@@ -53,6 +53,7 @@ struct Args {
     int blocks, group;    // blocks of heads of a key head; heads of a key head
     int ranks;            // CTAs of a cluster, where one has an item
     bool wide;            // q's rows start at multiples of 16 bytes
+    bool by_item;         // a Meta for each item; else for each run
     Meta *meta;
     float *parts;
 };
@@ -303,13 +304,14 @@ template <int KIND, int DP, int NT, bool TOGETHER> __global__ void __launch_boun
         // sequences that see nothing
         for (int b = blockIdx.x; b < a.seq.batch; b += gridDim.x) {
             if (Plan<S::STEP>::steps(a, b) > 0) continue;
+            for (int i = threadIdx.x; p.by_item && i < p.items; i += THREADS) p.meta[b * p.items + i].last = -1;
             for (int i = threadIdx.x; i < a.heads * a.cache.d; i += THREADS)
                 static_cast<uint16_t *>(a.out)[b * a.out_row + i / a.cache.d * a.out_head + i % a.cache.d] = 0;
         }
         const Plan<S::STEP> plan(a, scratch);
         // no run is empty: an item's parts are in neighbouring ones
         const int64_t total = plan.total * p.items;
-        if (threadIdx.x == 0) p.meta[blockIdx.x].last = -1;
+        if (!p.by_item && threadIdx.x == 0) p.meta[blockIdx.x].last = -1;
         if (blockIdx.x >= total) return;
         runs = Runs(total, int(total < gridDim.x ? total : gridDim.x));
         from = runs.begin(blockIdx.x), to = runs.begin(blockIdx.x + 1);
@@ -714,6 +716,7 @@ template <int KIND, int DP, int NT, bool TOGETHER> __global__ void __launch_boun
                 if (!TOGETHER && ends && first_step == 0) {
                     const int kv = p.blocks == 1 ? at.item : at.item / p.blocks, head0 = kv * p.group + (p.blocks == 1 ? 0 : (at.item % p.blocks) * 8 * NT);
                     uint16_t *const out = static_cast<uint16_t *>(a.out) + at.b * a.out_row;
+                    if (p.by_item && lane == 0) p.meta[at.b * p.items + at.item].last = -1;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -747,7 +750,7 @@ template <int KIND, int DP, int NT, bool TOGETHER> __global__ void __launch_boun
                     }
                     if (!TOGETHER && lane == 0 && first_step == 0) {
                         const int64_t last = from + n + (at.steps - at.step) - 1;            // the item's last step
-                        p.meta[blockIdx.x] = {at.b, at.item, runs.of(last), 0};
+                        p.meta[p.by_item ? at.b * p.items + at.item : int(blockIdx.x)] = {at.b, at.item, runs.of(last), int(blockIdx.x)};
                     }
                 }
             }
@@ -788,7 +791,7 @@ template <int KIND, int DP, int NT, bool TOGETHER> __global__ void __launch_boun
     }
 }
 
-// The parts of the item that begins in run blockIdx.x and ends in a later one, added up in order.  A CTA has tiles of 16 values of 8 heads, a thread one number of
+// The parts of an item that begins in one run and ends in a later one, added up in order.  A CTA has tiles of 16 values of 8 heads, a thread one number of
 // one; its GROUPS of four warps take every GROUPS-th part, and their sums are added in order.
 template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds__(128 * GROUPS) join_kernel(const Args p)
 {
@@ -797,13 +800,13 @@ template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds_
     after_work_before();
     const Meta meta = p.meta[blockIdx.x];
     if (meta.last < 0) return;
-    const int count = meta.last - blockIdx.x + 1, group = threadIdx.x / 128, n = threadIdx.x % 128, lane = n & 31, e = n >> 5, head = 2 * (lane & 3) + (e & 1);
+    const int count = meta.last - meta.first + 1, group = threadIdx.x / 128, n = threadIdx.x % 128, lane = n & 31, e = n >> 5, head = 2 * (lane & 3) + (e & 1);
     for (int tile = blockIdx.y; tile < NT * MT; tile += gridDim.y) {
         const int nt = tile / MT, i = tile % MT;
         float m = -INFINITY, l = 0.f, o = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int k = group; k < count; k += GROUPS) {
-            const float *const part = p.parts + (2 * int64_t(blockIdx.x + k) + (k == 0 ? 1 : 0)) * part_floats(DP, NT);
+            const float *const part = p.parts + (2 * int64_t(meta.first + k) + (k == 0 ? 1 : 0)) * part_floats(DP, NT);
             const float here = part[8 * NT * DP + 8 * nt + head], sum = part[8 * NT * DP + 8 * NT + 8 * nt + head], v = part[tile * 128 + n];
             const float next = fmaxf(m, here), back = m == next ? 1.f : exp2_of(m - next), w = here == next ? 1.f : exp2_of(here - next);
             m = next;
@@ -844,6 +847,7 @@ inline int64_t steps_of(const AttentionArgs &a, int step)
 // to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
 // where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
 // steps of a CTA, 16 where eights fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000, not taken: 40.9 for 38.2).
+// Many short items are better off in runs (64 sequences of 240: 21 us, 25 with a CTA each; of 57: 9.6, 19).
 // What has clusters without a window has them with one: no more steps, and no fewer CTAs than those.
 inline int ranks_of(const AttentionArgs &a, int step, int64_t heads, int sm_count)
 {
@@ -867,12 +871,15 @@ template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cud
     }
     e = allow_shared<decode_kernel<KIND, DP, NT, false>>(S::SMEM);
     if (e != cudaSuccess) return e;
+    const int64_t items = p.items * int64_t(p.a.seq.batch);
+    p.by_item = runs >= 8 * items;
     e = launch_after(decode_kernel<KIND, DP, NT, false>, dim3(runs), dim3(THREADS), S::SMEM, stream, dim3(1, 1), p);
     // items of a single step are never cut
     if (e != cudaSuccess || steps == 1) return e;
-    // many parts an item: a thread has a fourth of them, so that their latencies add up to less (one sequence of 131071 rows: 95.3 us, 93.1 so); few: as many CTAs
-    // as there are tiles (33 sequences of 4099: 77.3 us, 80.8 with the other)
-    if (runs >= 8 * p.items * int64_t(p.a.seq.batch)) return launch_after(join_kernel<KIND, DP, NT, 4>, dim3(runs, 4), dim3(512), 0, stream, dim3(1, 1), p);
+    // many parts an item: a thread has an eighth of them, so that their latencies add up to less, and there is a CTA for each item's tile (one sequence of 131071
+    // rows, 32 heads over 8: 89.9 us, 94.0 with quarters and four CTAs for each run; of 20000 rows, 16 heads over one: 19.8, 93.7); few: a CTA for each run and tile (33 sequences of 4099: 77.3 us, 80.8 with
+    // eighths)
+    if (p.by_item) return launch_after(join_kernel<KIND, DP, NT, 8>, dim3(unsigned(items), NT * DP / 16), dim3(1024), 0, stream, dim3(1, 1), p);
     return launch_after(join_kernel<KIND, DP, NT, 1>, dim3(runs, NT * DP / 16), dim3(128), 0, stream, dim3(1, 1), p);
 }
 
