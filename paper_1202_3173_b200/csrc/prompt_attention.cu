@@ -56,6 +56,7 @@ enum { BF16 = 0, F16 = 1, EIGHT = 2 };
 constexpr int RAW = 3, SCALES = 3;                   // stages of tiles in 8 bits, and of their rows' scales
 constexpr int PLANS = 4, BLOCK = TILE * 128;         // bytes of a block of 64 values of 128 rows
 constexpr int64_t kWaitLimit = int64_t(1) << 36;     // clocks of a wait for others to be through with a block: 2^24 tiles of the longest sequence take as long
+constexpr int ONE_TILE = 48;                         // tiles of K and V up to which a CTA may have one tile of Q
 constexpr int LEAST_TILES = 2;                       // tiles of K and V in a part (200 tokens of 8 heads over 2 behind 1000: 14.8 us; of 4: 18.7)
 
 // Set by a CTA that gave up on a wait; read and cleared by strassen_device_status.
@@ -1117,11 +1118,13 @@ Cut cut_of(const AttentionArgs &a, int sm_count)
     c.heads = (group + c.blocks - 1) / c.blocks;
     c.tokens = TILE / c.heads;
     const auto blocks = [&](int of) { return (a.seq.tokens / of + a.seq.batch) * a.cache.kv_heads * c.blocks; };
-    // one tile of Q a CTA as long as there are SMs enough: its softmax does not share the schedulers (512 tokens of 32 heads over 8: 15.1 us, 17.0 with two)
-    c.block = blocks(c.tokens) <= sm_count ? c.tokens : 2 * c.tokens;
-    c.most = blocks(c.block);
     // tiles of the longest sequence that the table has room for
-    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window ? int64_t(a.window) + c.block + TILE : rows, tiles = ((seen < rows ? seen : rows) + TILE - 1) / TILE;
+    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window ? int64_t(a.window) + 2 * c.tokens + TILE : rows, tiles = ((seen < rows ? seen : rows) + TILE - 1) / TILE;
+    // One tile of Q a CTA as long as there are SMs enough: its softmax does not share the schedulers (512 tokens of 32 heads over 8: 15.1 us, 17.0 with two; behind 1000: 25.4, 44.2).
+    // Behind many rows two, and more parts: half as many bytes out of the second cache, which bounds that (200 tokens behind 16000: 72.6 us, 96.4 with one; 8 x 37 of
+    // 32 heads over 2 behind up to 15724: 69.8, 92.5; the other way round 512 behind 4000: 62.1, 54.3).
+    c.block = blocks(c.tokens) <= sm_count && tiles <= ONE_TILE ? c.tokens : 2 * c.tokens;
+    c.most = blocks(c.block);
     const int64_t parts = c.most > 0 ? sm_count / c.most : 0;
     c.parts = int(parts < tiles / LEAST_TILES ? parts : tiles / LEAST_TILES);
     if (c.parts < 2) c.parts = 1;
