@@ -12,7 +12,7 @@
 //   * warp 11 clears the rows of V that no row of the CTA sees (a page's slots behind the sequence may hold NaN, and 0 * NaN is NaN);
 //   * warp 10 finds out what there is to do, ahead of the others.
 // The CTAs stay and take blocks of tokens, those that see most first, in every other round in the opposite order, which evens out what they cost.
-// Where there are fewer blocks than SMs and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens behind
+// Where there are few blocks and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens behind
 // 8000: 28 us, 98 in one part).
 //
 // What a token does not see has no effect on it.  Scores are replaced, but a weight of 0 times a value that is no number is none either.  So where a tile holds rows that some of the
@@ -71,6 +71,7 @@ struct Args {
     int box;                 // rows of K and V in a copy
     int wide;                // bytes that out's rows start at multiples of, and are long: 32, 16 or 0 (less)
     int parts;               // of a block's rows of the cache
+    int most;                // blocks at most
     float *sums;             // parts > 1: part_floats() for each part of each block
 };
 
@@ -1125,9 +1126,14 @@ Cut cut_of(const AttentionArgs &a, int sm_count)
     // 32 heads over 2 behind up to 15724: 69.8, 92.5; the other way round 512 behind 4000: 62.1, 54.3).
     c.block = blocks(c.tokens) <= sm_count && tiles <= ONE_TILE ? c.tokens : 2 * c.tokens;
     c.most = blocks(c.block);
-    const int64_t parts = c.most > 0 ? sm_count / c.most : 0;
-    c.parts = int(parts < tiles / LEAST_TILES ? parts : tiles / LEAST_TILES);
-    if (c.parts < 2) c.parts = 1;
+    // Parts: the fewest rounds of the shortest pieces, where a piece takes some 4 tiles' time more and the join as long once.  Rounds that are not full cost most where
+    // blocks are few and long: 24 sequences of up to 406 tokens behind 6763, 2 heads of 64: 53.9 us, 102.0 in one part; 32 of 21 behind 7569, 32 over 4: 95.6, 146.4.
+    c.parts = 1;
+    if (c.most > 0 && c.most < 2 * sm_count) {
+        const auto cost = [&](int64_t parts) { return (c.most * parts + sm_count - 1) / sm_count * ((tiles + parts - 1) / parts + 4) + (parts > 1 ? 4 : 0); };
+        for (int64_t parts = 2; parts <= tiles / LEAST_TILES && parts <= sm_count; ++parts)
+            if (cost(parts) < cost(c.parts)) c.parts = int(parts);
+    }
     return c;
 }
 
@@ -1173,7 +1179,7 @@ template <int KIND, int DP, bool LINEAR> cudaError_t launch_as(const Args &p, co
     const cudaError_t launched = launch_after(kernel, dim3(unsigned(ctas)), dim3(S::THREADS), S::SMEM, stream, dim3(1, 1), p, q, k, v);
     if (launched != cudaSuccess || p.parts == 1) return launched;
     const auto join = p.a.type == STRASSEN_BF16 ? join_kernel<true> : join_kernel<false>;
-    return launch_after(join, dim3(unsigned(ctas / p.parts), unsigned((p.a.cache.d + JOIN_COLUMNS - 1) / JOIN_COLUMNS), unsigned((p.block > p.tokens ? 2 : 1) * TILE / 32)), dim3(32 * JOIN_WARPS), 0, stream, dim3(1, 1), p);
+    return launch_after(join, dim3(unsigned(p.most), unsigned((p.a.cache.d + JOIN_COLUMNS - 1) / JOIN_COLUMNS), unsigned((p.block > p.tokens ? 2 : 1) * TILE / 32)), dim3(32 * JOIN_WARPS), 0, stream, dim3(1, 1), p);
 }
 template <int KIND, int DP> cudaError_t launch(const Args &p, bool linear, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int ctas, cudaStream_t stream)
 {
@@ -1214,6 +1220,7 @@ cudaError_t launch_prompt(const AttentionArgs &given, int sm_count, cudaStream_t
     p.tokens = c.tokens;
     p.block = c.block;
     p.parts = c.parts;
+    p.most = int(c.most);
     p.sums = static_cast<float *>(a.workspace);
     const int page = 1 << a.cache.page_shift;
     p.box = page < prompt::TILE ? page : prompt::TILE;

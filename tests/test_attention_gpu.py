@@ -379,6 +379,15 @@ def test_rows_outside_every_sequence_stay_and_more_new_tokens_than_rows_give_zer
 
 
 @pytest.mark.parametrize("cache", [None, E4M3])
+@pytest.mark.parametrize("window", [0, 5000])
+def test_more_parts_than_fit_the_gpu_at_once(cache, window):
+    """Few tokens behind many rows, of so many sequences that their parts are taken in turns."""
+    counts = [200 - 7 * i for i in range(24)]
+    c = Case([7000 - 211 * i for i in range(23)] + [39], counts, heads=2, kv=2, d=64, page=16, cache=cache)
+    close(sw.prompt_attention(c.q, c.cache, c.table, c.lengths, c.offsets, window=window), *c.reference(window=window))
+
+
+@pytest.mark.parametrize("cache", [None, E4M3])
 def test_many_more_new_tokens_than_rows_give_zeros(cache):
     """300 new tokens of a sequence that has 12 rows: whole blocks of tokens see nothing."""
     c = Case([300, 40], [300, 40], heads=4, kv=1, cache=cache)
