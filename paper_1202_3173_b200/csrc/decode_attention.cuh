@@ -8,12 +8,13 @@
 //
 // Bound by the cache's bytes.  Each warp has rows of its own and a ring of its own in shared memory that it fills by asynchronous copies of 16 bytes, rows outside the
 // sequence and values beyond head_size as zeros: nothing in the loop waits for another warp.  About 128 KB are under way on an SM: 32 sequences of up to 32768 tokens of
-// 8 key heads of 128 values, 2.75 GB, in 422 us, 6.5 TB/s; one of 131071, 537 MB, in 94 us, 5.7 TB/s; 64 of up to 8192 of 4 key heads in 8 bits, 331 MB, in 70 us, 4.7 TB/s;
+// 8 key heads of 128 values, 2.75 GB, in 422 us, 6.5 TB/s; one of 131071, 537 MB, in 90 us, 6.0 TB/s; 64 of up to 8192 of 4 key heads in 8 bits, 331 MB, in 70 us, 4.7 TB/s;
 // 33 of up to 4099 of 12 heads of 80 values, 328 MB, in 74 us, 4.4 TB/s.  The last two wait for dependent instructions (47 and 41 % of issue slots; two warps a
 // scheduler): queries of one or seven heads fill an eighth of the products or nearly all, at the same cost in instructions.  16-byte
 // chunks of a row are permuted by the row's number, so that reads by 8 lanes, of two rows or of four, fall into different banks.
 //
-// The work is cut evenly, whatever the lengths: steps of WARPS * ROWS rows, of all sequences and key heads one after another, in as many equal runs as there are CTAs. A
+// Few short items have a cluster each (ranks_of), whose CTAs add their parts up out of one another's shared memory.  Else the
+// work is cut evenly, whatever the lengths: steps of WARPS * ROWS rows, of all sequences and key heads one after another, in as many equal runs as there are CTAs. A
 // run's first and last item may be a part of one: its sums go to the workspace, and the join kernel adds an item's parts in order.  No atomics: the
 // same bits every time.
 //

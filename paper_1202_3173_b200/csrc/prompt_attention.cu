@@ -12,8 +12,8 @@
 //   * warp 11 clears the rows of V that no row of the CTA sees (a page's slots behind the sequence may hold NaN, and 0 * NaN is NaN);
 //   * warp 10 finds out what there is to do, ahead of the others.
 // The CTAs stay and take blocks of tokens, those that see most first, in every other round in the opposite order, which evens out what they cost.
-// Where there are few blocks and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens behind
-// 8000: 28 us, 98 in one part).
+// Where there are few blocks and many rows in the cache, the rows are cut into parts, whose sums the join kernel adds in order (64 tokens of 32
+// heads over 8 behind 16000: 40 us).
 //
 // What a token does not see has no effect on it.  Scores are replaced, but a weight of 0 times a value that is no number is none either.  So where a tile holds rows that some of the
 // CTA's tokens see and some do not, warp 11 looks for such values of V, puts zeros in their place and raises a flag; then the tokens that do see them
@@ -23,10 +23,13 @@
 // M is the largest of score + log2(value scale), so that scaled weights keep within f16's range.
 //
 // Bound, for head_size 128, by power: 16384 tokens of 32 heads over 8 in 1.68 ms, 1.31 PFLOP/s, at 1.49 GHz (sampled in the kernel), where the tensor cores are busy for 2048 of
-// 2830 clocks of a pair of tiles; cuBLAS keeps up 1.38.  In short runs at 1.75 GHz 8192 tokens take 407 us, 1.35 PFLOP/s.  For smaller heads by the softmax: 128 exponentials
-// of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a scheduler and 2150 for two (timed alone), 2900 here.  What was tried: P over S, and S formed
-// behind P V (the first form): 462 us at 8192 tokens; a quarter of the exponentials by a polynomial of degree 4: 446 instead of 407; two threads a row: 570; warps
-// of exponentials in turns: 448 instead of 436; two places for S at head_size 64: the same.
+// 2830 clocks of a pair of tiles; cuBLAS keeps up 1.38.  In short runs at 1.75 GHz 8192 tokens take 407 us, 1.35 PFLOP/s.  For smaller heads by the softmax (8192 tokens of 64 heads
+// over 8 of 64 values: 685 us, 0.8 PFLOP/s): 128 exponentials of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a
+// scheduler and 2150 for two (timed alone), 2820 here, where a warp also waits for S (260), reads it (130), finds its largest (410), waits for the product before (200) and writes P
+// (190 clocks a tile) while the other's exponentials take the issue slots.  What was tried: P over S, and S formed behind P V (the first form): 462 us at 8192 tokens of 32 heads
+// over 8 of 128, then 407; a quarter of the exponentials by a polynomial of degree 4 446, for heads of 64 of degree 3 744 instead of 685, an eighth 687; two threads a row: 570; warps
+// of exponentials in turns: 448 instead of 436; two places for S at head_size 64: the same; S in halves, the second one's largest found between the first one's exponentials: 436 instead of
+// 406, for heads of 64 759 instead of 690; one vote a tile on the waits' outcome in place of three: 705 instead of 679.
 //
 // Every wait has a limit, after which the CTA gives up, frees its tensor memory and raises a flag (wait_for).
 #include <cuda.h>
@@ -210,7 +213,7 @@ __device__ __forceinline__ float largest(float a, float b)
 //
 // Of up to 31 sequences, a lane one: offsets and lengths are read once, since each look at memory is half a microsecond that nothing else is done in, and
 // blocks are in order of what they cost, the dearest first, so that the CTAs, which take them in turn, end together (7 prompts of up to 2049
-// tokens, head_size 80: 245 us in pages of 16 rows, 274 in the sequences' order and with rows of no token masked).  How many blocks of a sequence cost c tiles or more needs no counting, so the n-th is found by halving.
+// tokens, head_size 80: 245 us at the time, 274 in the sequences' order and with rows of no token masked).  How many blocks of a sequence cost c tiles or more needs no counting, so the n-th is found by halving.
 //
 // Of more sequences: the last first.  Sequence b's blocks begin with number offsets[b] / block + b, enough for its own, and found without adding up the ones before.
 struct Order {
