@@ -1132,10 +1132,21 @@ Cut cut_of(const AttentionArgs &a, int sm_count)
     // Parts: the fewest rounds of the shortest pieces, where a piece takes some 4 tiles' time more and the join as long once.  Rounds that are not full cost most where
     // blocks are few and long: 24 sequences of up to 406 tokens behind 6763, 2 heads of 64: 53.9 us, 102.0 in one part; 32 of 21 behind 7569, 32 over 4: 95.6, 146.4.
     c.parts = 1;
+    // Of the numbers of parts with as many rounds the largest is looked at, made smaller as far as pieces stay as they are.
+    const auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     if (c.most > 0 && c.most < 2 * sm_count) {
-        const auto cost = [&](int64_t parts) { return (c.most * parts + sm_count - 1) / sm_count * ((tiles + parts - 1) / parts + 4) + (parts > 1 ? 4 : 0); };
-        for (int64_t parts = 2; parts <= tiles / LEAST_TILES && parts <= sm_count; ++parts)
-            if (cost(parts) < cost(c.parts)) c.parts = int(parts);
+        int64_t best = over(c.most, sm_count) * (tiles + 4);
+        const int64_t limit = tiles / LEAST_TILES < sm_count ? tiles / LEAST_TILES : sm_count;
+        for (int64_t rounds = 1; rounds <= 16; ++rounds) {
+            const int64_t most = rounds * sm_count / c.most;
+            if ((most < limit ? most : limit) < 2) continue;
+            const int64_t piece = over(tiles, most < limit ? most : limit), parts = over(tiles, piece), cost = over(c.most * parts, sm_count) * (piece + 4) + 4;
+            if (cost < best) {
+                best = cost;
+                c.parts = int(parts);
+            }
+            if (most >= limit) break;
+        }
     }
     return c;
 }
