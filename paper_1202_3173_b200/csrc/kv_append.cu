@@ -39,6 +39,25 @@ template <bool BF16> __device__ __forceinline__ uint32_t two_16_bits(float lo, f
     return d;
 }
 
+// (a b + c) for two numbers at once
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n fma.rn.f32x2 z, x, y, z;\n mov.b64 {%0, %1}, z;\n}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// v / scale in 8 bits, of two values; inv: 1 / scale, back: -scale, or 0 if that is infinite (finite values are 0 then).  v inv is not always the quotient's nearest number in
+// 32 bits, and next to a border between two e4m3 values that is the wrong one of them (one of 2000 of rows in bf16).  So what is left of v is found, exactly, and its own
+// quotient added (Markstein, IBM J. Res. Dev. 34 (1990): the result is the rounded quotient).  Two numbers an instruction: 79.0 us where v inv alone takes 77.4 (49152 tokens of
+// 16 + 2 x 8 heads of 64, 8-bit cache), a division 96.8; 16384 of 32 + 2 x 8 of 128: 70.3, 70.1 and 76.6.
+__device__ __forceinline__ uint32_t two_of_8_bits(float2 v, float inv, float back)
+{
+    const float2 by = make_float2(inv, inv), y = make_float2(v.x * inv, v.y * inv), quotient = fma2(fma2(make_float2(back, back), y, v), by, y);
+    return __nv_cvt_float2_to_fp8x2(quotient, __NV_SATFINITE, __NV_E4M3);
+}
+
 __device__ __forceinline__ float largest(float a, float b)       // NaN if one is
 {
     float d;
@@ -160,18 +179,15 @@ template <bool BF16, bool E4M3, bool WIDE, int CHUNKS> __device__ __forceinline_
         // each lane's with that of the next, of the next but one, ..: all of them, however many there are, since some twice do no harm
         for (int i = 1; i < lanes; i <<= 1) most = largest(most, __shfl_sync(mine, most, begin + (lane + i < lanes ? lane + i : lane + i - lanes)));
         // a row with NaN has NaN for its scale, and throughout
-        const float scale = largest(most / kE4M3Max, kMinRowScale), inv = 1.f / scale;
+        const float scale = largest(most / kE4M3Max, kMinRowScale), inv = 1.f / scale, back = scale < INFINITY ? -scale : 0.f;
         if (page < 0) return;
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             if (first[k] >= d) continue;
             uint32_t w[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[k][4 * i] * inv, v[k][4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-                const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[k][4 * i + 2] * inv, v[k][4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-                w[i] = lo | hi << 16;
-            }
+            for (int i = 0; i < 2; ++i)
+                w[i] = two_of_8_bits(make_float2(v[k][4 * i], v[k][4 * i + 1]), inv, back) | two_of_8_bits(make_float2(v[k][4 * i + 2], v[k][4 * i + 3]), inv, back) << 16;
             *reinterpret_cast<uint2 *>(row + first[k]) = make_uint2(w[0], w[1]);
         }
         if (lane == 0) (of.is_v ? p.cache.v_scale : p.cache.k_scale)[((int64_t(page) * p.cache.kv_heads + of.head) << p.cache.page_shift) + slot] = scale;
