@@ -558,8 +558,9 @@ typedef struct strassen_paged_cache {
  *   interleaved  0: pair f is values f and f + rotary / 2; else 2 f and 2 f + 1
  *   q, out       tokens x heads; out receives the turned queries, and may be q itself; heads 0 with both NULL: keys and values alone
  *   k, v         tokens x kv_heads
- * Turned keys are held in 32 bits until they are stored, rounded once.  out shares no element with k, v or the cache, nor with q unless it is q.  Two sequences
- * with new tokens in one page are in order as long as they do not share a slot.
+ * Turned keys are held in 32 bits until they are stored, rounded once.  out shares no element with k or v, nor with q unless it is q (looked for element by element where rows
+ * are the same distance apart, as those of one wider tensor are, else by ranges of memory); neither out nor the cache overlaps anything else, and the cache's
+ * keys and values are apart (STRASSEN_ALIAS).  Two sequences with new tokens in one page are in order as long as they do not share a slot.
  */
 int strassen_rotate_append(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                            const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, const void *k,
@@ -572,7 +573,8 @@ int strassen_rotate_append(const strassen_paged_cache *cache, int64_t batch, con
  *   type       of q and out: STRASSEN_BF16 or STRASSEN_F16, the cache's if that has 16 bits
  *   workspace  as strassen_decode_attention_workspace_bytes says for the current device (0 bytes for few short sequences; 256-byte aligned; free again once the call's kernels are done)
  * Scores, the softmax's sums and the result are held in 32 bits; its weights, at most 1, are rounded to 16 bits for the product with the values.  The work is split evenly over
- * the GPU along the sequences, whatever their lengths, but for few short sequences (by width), of which each is split over as many CTAs.  out does not overlap q.
+ * the GPU along the sequences, whatever their lengths, but for few short sequences (by width), of which each is split over as many CTAs.  out and the workspace
+ * overlap no other argument, the cache's scales, the table and the lengths included (STRASSEN_ALIAS).
  */
 int strassen_decode_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                               int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out, int64_t out_row, int64_t out_head,

@@ -65,6 +65,59 @@ Range cache_range(const CacheArgs &c, const uint8_t *p)
     return {lo, lo + uintptr_t((c.pages - 1) * c.page_stride + (c.kv_heads - 1) * c.head_stride + ((int64_t(1) << c.page_shift) - 1) * c.row_stride + c.d * type_size(c.type))};
 }
 
+Range scale_range(const CacheArgs &c, const float *p)
+{
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    return {lo, lo + (p ? uintptr_t((c.pages * c.kv_heads) << c.page_shift) * 4 : 0)};
+}
+Range ints_of(const int *p, int64_t n)
+{
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    return {lo, lo + (p && n > 0 ? uintptr_t(n) * 4 : 0)};
+}
+
+// Whether `r` lies over the scales, the table, the lengths or the offsets, all of which are read while results are written.
+bool over_what_is_read(const Range &r, const CacheArgs &c, const SequenceArgs &s)
+{
+    return overlap(r, scale_range(c, c.k_scale)) || overlap(r, scale_range(c, c.v_scale)) || overlap(r, ints_of(s.table, s.batch > 0 && s.width > 0 ? (s.batch - 1) * s.ld_table + s.width : 0)) ||
+           overlap(r, ints_of(s.lengths, s.batch)) || overlap(r, ints_of(s.offsets, s.batch + int64_t(1)));
+}
+
+// Rows of heads as the kernels see them.
+struct RowsOfHeads {
+    const void *p;
+    int64_t rows, row, heads, head;
+    Range range(int d) const { return heads_of(p, rows, row, heads, head, d, 2); }
+};
+bool same(const RowsOfHeads &a, const RowsOfHeads &b) { return a.p == b.p && a.row == b.row && a.head == b.head; }
+// Whether an element is in both.  Rows of views of one wider tensor are the same distance apart and lie between one another: there it is found out exactly; else ranges of memory are compared.
+bool share(const RowsOfHeads &a, const RowsOfHeads &b, int d)
+{
+    if (!a.p || !b.p || !overlap(a.range(d), b.range(d))) return false;
+    if (a.row != b.row) return true;
+    const int64_t apart = (int64_t(reinterpret_cast<uintptr_t>(b.p)) - int64_t(reinterpret_cast<uintptr_t>(a.p))) / 2, row = a.row, as_long = (a.heads - 1) * a.head + d, bs_long = (b.heads - 1) * b.head + d;
+    if (row > 0 && as_long <= row && bs_long <= row) {
+        const int64_t behind = (apart % row + row) % row;        // from the begin of a row of a to the next one of b
+        if (behind >= as_long && behind + bs_long <= row) return false;
+    }
+    // A head of a row of b begins `off` behind one of the same row of a: whether they, or those of rows n apart, have an element in common.
+    const auto meet = [&](int64_t off) {
+        off = off < 0 ? -off : off;
+        if (off < d) return true;
+        const int64_t n = off < row || row == 0 ? 0 : off / row, left = off - n * row;
+        return (left < d && n < a.rows) || (row > 0 && row - left < d && n + 1 < a.rows);
+    };
+    if (a.head == b.head) {
+        for (int64_t i = 1 - a.heads; i < b.heads; ++i)
+            if (meet(apart + i * a.head)) return true;
+        return false;
+    }
+    for (int64_t i = 0; i < a.heads; ++i)
+        for (int64_t j = 0; j < b.heads; ++j)
+            if (meet(apart + j * b.head - i * a.head)) return true;
+    return false;
+}
+
 int check_sequences(int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths, const int *offsets, int64_t tokens, SequenceArgs *to)
 {
     if (batch < 0 || batch > kMaxExtent || width < 0 || width > kMaxExtent || tokens < 0 || tokens > kMaxExtent)
@@ -103,8 +156,8 @@ int check_attention(const strassen_paged_cache *cache, int64_t batch, const int 
         if (rc == STRASSEN_OK) rc = check_heads("out", out, tokens, out_row, heads, out_head, c.d);
         if (rc != STRASSEN_OK) return rc;
         const Range o = heads_of(out, tokens, out_row, heads, out_head, c.d, 2);
-        if (overlap(o, heads_of(q, tokens, q_row, heads, q_head, c.d, 2)) || overlap(o, cache_range(c, c.k)) || overlap(o, cache_range(c, c.v)))
-            return fail(STRASSEN_ALIAS, "out overlaps q or the cache");
+        if (overlap(o, heads_of(q, tokens, q_row, heads, q_head, c.d, 2)) || overlap(o, cache_range(c, c.k)) || overlap(o, cache_range(c, c.v)) || over_what_is_read(o, c, s))
+            return fail(STRASSEN_ALIAS, "out overlaps another argument");
     }
     *to = {c, s, type, int(heads), {q, tokens > 1 ? q_row : 0, heads > 1 ? q_head : 0}, out, tokens > 1 ? out_row : 0, heads > 1 ? out_head : 0, scale,
            window > 0x7fffffff ? 0x7fffffff : int(window), workspace};
@@ -119,7 +172,8 @@ int check_workspace(const AttentionArgs &a, int64_t need, size_t given, const ch
     const uintptr_t lo = reinterpret_cast<uintptr_t>(a.workspace);
     const Range ws = {lo, lo + uintptr_t(need)};
     if (overlap(ws, heads_of(a.out, a.seq.tokens, a.out_row, a.heads, a.out_head, a.cache.d, 2)) ||
-        overlap(ws, heads_of(a.q.p, a.seq.tokens, a.q.row, a.heads, a.q.head, a.cache.d, 2)) || overlap(ws, cache_range(a.cache, a.cache.k)) || overlap(ws, cache_range(a.cache, a.cache.v)))
+        overlap(ws, heads_of(a.q.p, a.seq.tokens, a.q.row, a.heads, a.q.head, a.cache.d, 2)) || overlap(ws, cache_range(a.cache, a.cache.k)) || overlap(ws, cache_range(a.cache, a.cache.v)) ||
+        over_what_is_read(ws, a.cache, a.seq))
         return fail(STRASSEN_ALIAS, "workspace overlaps another argument");
     return STRASSEN_OK;
 }
@@ -182,13 +236,16 @@ extern "C" int strassen_rotate_append(const strassen_paged_cache *cache, int64_t
     a.interleaved = interleaved != 0;
     a.wide = wide_strides(reinterpret_cast<uintptr_t>(k), a.k.row, a.k.head, 2) && wide_strides(reinterpret_cast<uintptr_t>(v), a.v.row, a.v.head, 2) &&
              wide_strides(reinterpret_cast<uintptr_t>(q), a.q.row, a.q.head, 2) && wide_strides(reinterpret_cast<uintptr_t>(out), a.out_row, a.out_head, 2);
-    const Range o = heads_of(out, tokens, a.out_row, heads, a.out_head, d, 2);
-    const Range fixed[] = {cache_range(a.cache, a.cache.k), cache_range(a.cache, a.cache.v)};
-    const Range inputs[] = {heads_of(q, tokens, a.q.row, heads, a.q.head, d, 2), heads_of(k, tokens, a.k.row, kv, a.k.head, d, 2), heads_of(v, tokens, a.v.row, kv, a.v.head, d, 2), o};
-    for (const Range &f : fixed)
-        for (const Range &r : inputs)
+    const CacheArgs &c = a.cache;
+    const RowsOfHeads o = {out, tokens, a.out_row, heads, a.out_head}, qs = {q, tokens, a.q.row, heads, a.q.head}, ks = {k, tokens, a.k.row, kv, a.k.head}, vs = {v, tokens, a.v.row, kv, a.v.head};
+    const Range turns = ints_of(reinterpret_cast<const int *>(frequencies), rotary / 2);
+    for (const Range &f : {cache_range(c, c.k), cache_range(c, c.v), scale_range(c, c.k_scale), scale_range(c, c.v_scale)})
+        for (const Range &r : {qs.range(d), ks.range(d), vs.range(d), o.range(d), turns, ints_of(a.seq.table, width > 0 ? (batch - 1) * ld_table + width : 0), ints_of(lengths, batch), ints_of(offsets, batch + 1)})
             if (overlap(f, r)) return fail(STRASSEN_ALIAS, "the cache overlaps another argument");
-    if (q && q == out && (a.q.row != a.out_row || a.q.head != a.out_head)) return fail(STRASSEN_ALIAS, "out may be q itself, with its strides");
+    if (c.pages > 0 && (c.k == c.v || overlap(scale_range(c, c.k_scale), scale_range(c, c.v_scale)))) return fail(STRASSEN_ALIAS, "keys and values of the cache are in the same place");
+    if (overlap(o.range(d), turns) || over_what_is_read(o.range(d), c, a.seq)) return fail(STRASSEN_ALIAS, "out overlaps another argument");
+    if (!same(o, qs) && share(o, qs, d)) return fail(STRASSEN_ALIAS, "out overlaps q; it may be q itself, with its strides");
+    if (share(o, ks, d) || share(o, vs, d)) return fail(STRASSEN_ALIAS, "out overlaps k or v");
     int sms = 0;
     if ((rc = current_device(&sms)) != STRASSEN_OK) return rc;
     const cudaError_t e = launch_append(a, sms, static_cast<cudaStream_t>(stream));

@@ -56,3 +56,53 @@ def test_rows_in_8_bits_are_the_rounded_quotients(kv, d, dtype):
         assert torch.equal(scales, scale)
         nan = torch.isnan(want.float())
         assert torch.equal(codes[~nan], want.view(torch.uint8)[~nan]) and bool(((codes[nan] & 127) == 127).all())
+
+
+@pytest.mark.parametrize("which", ["decode", "prompt"])
+def test_a_workspace_over_what_is_read_is_refused(which):
+    """Before anything is launched: over the table, the lengths and the cache's scales."""
+    kv, d, page, width = 2, 64, 64, 4000
+    cache = sw.PagedCache.empty(16, kv, d, page, E4M3)
+    lengths, offsets = ints([100], [0, 4])
+    q = torch.zeros(4 if which == "prompt" else 1, 4, d, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 9.0)
+    table = torch.zeros(1, width, dtype=torch.int32, device="cuda")
+    at = cache._at
+    if which == "decode":
+        need = binding.strassen_decode_attention_workspace_bytes(at, 1, 4, width)
+    else:
+        need = binding.strassen_prompt_attention_workspace_bytes(at, 1, 4, width, 4, 0)
+    assert need > 0
+    for over, inside in ((table, 0), (lengths, 0), (cache.k_scale, 0), (cache.v_scale, 0)) + (((offsets, 0),) if which == "prompt" else ()):
+        ws = (over.data_ptr() + inside) // 256 * 256
+        assert ws + need > over.data_ptr()
+        with pytest.raises(StrassenError) as e:
+            if which == "decode":
+                binding.strassen_decode_attention(at, 1, table.data_ptr(), width, width, lengths.data_ptr(), 0, 4, q.data_ptr(), 4 * d, d, out.data_ptr(), 4 * d, d, 0.125, 0, ws, need)
+            else:
+                binding.strassen_prompt_attention(at, 1, table.data_ptr(), width, width, lengths.data_ptr(), offsets.data_ptr(), 4, 0, 4, q.data_ptr(), 4 * d, d, out.data_ptr(), 4 * d, d,
+                                                  0.125, 0, ws, need)
+        assert e.value.status == -4 and "workspace" in str(e.value)
+    torch.cuda.synchronize()
+    assert bool((out == 9).all())
+
+
+def test_results_over_keys_or_values_of_one_product_are_refused():
+    """Queries, keys and values as views of one product's rows: turned in place, but not over the keys or values beside them."""
+    rows = torch.randn(20, 4 + 2 + 2, 64, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    q, k, v = rows[:, :4], rows[:, 4:6], rows[:, 6:]
+    cache = sw.PagedCache.empty(2, 2, 64, 16)
+    table, lengths, offsets = ints([[0, 1]], [20], [0, 20])
+    keep = rows.clone()
+    for out in (rows[:, 2:6], rows[:, 4:], rows[:, 1:5]):
+        with pytest.raises(StrassenError):
+            sw.rotate_append(q, k, v, cache, table, lengths, None, offsets, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(rows, keep)
+    assert sw.rotate_append(q, k, v, cache, table, lengths, None, offsets, out=q) is q and torch.equal(rows, keep)
+    # every head's query, key and value side by side
+    each = keep[:, :6].reshape(20, 2, 3, 64).clone()
+    want = sw.rotate_append(each[:, :, 0].contiguous(), each[:, :, 1], each[:, :, 2], cache, table, lengths, None, offsets)
+    assert torch.equal(sw.rotate_append(each[:, :, 0], each[:, :, 1], each[:, :, 2], cache, table, lengths, None, offsets, out=each[:, :, 0]), want)
+    with pytest.raises(StrassenError):
+        sw.rotate_append(each[:, :, 0], each[:, :, 1], each[:, :, 2], cache, table, lengths, None, offsets, out=each[:, :, 2])
