@@ -21,6 +21,13 @@ struct CacheArgs {
     float *k_scale, *v_scale;                // e4m3: one for each row, (page * kv_heads + head) << page_shift | slot
 };
 
+// Whether the cache's rows are one after another, head after head and page after page.  The stride of a dimension of one is nobody's.
+inline bool rows_in_a_row(const CacheArgs &c)
+{
+    const int64_t of_head = c.row_stride << c.page_shift;
+    return (c.kv_heads == 1 || c.head_stride == of_head) && (c.pages == 1 || c.page_stride == of_head * c.kv_heads);
+}
+
 // Where the sequences are.  offsets NULL: one new token each.
 struct SequenceArgs {
     int batch, width;                        // entries of a row of the table

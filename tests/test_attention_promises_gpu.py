@@ -106,3 +106,36 @@ def test_results_over_keys_or_values_of_one_product_are_refused():
     assert torch.equal(sw.rotate_append(each[:, :, 0], each[:, :, 1], each[:, :, 2], cache, table, lengths, None, offsets, out=each[:, :, 0]), want)
     with pytest.raises(StrassenError):
         sw.rotate_append(each[:, :, 0], each[:, :, 1], each[:, :, 2], cache, table, lengths, None, offsets, out=each[:, :, 2])
+
+
+@pytest.mark.parametrize("cache_type", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("kv,pages,page", [(1, 70, 16), (1, 1, 1024), (2, 1, 1024), (1, 9, 128), (3, 70, 16)])
+def test_one_key_head_or_one_page_wherever_pages_lie(kv, pages, page, cache_type):
+    """Rows one after another and pages with room between them are brought by different copies: the same bits.  (A stride of a dimension of one says nothing.)"""
+    d, n = 64, 1000
+    g = torch.Generator("cuda").manual_seed(pages)
+    table = torch.full((1, max(pages, -(-n // page)) + 1), -1, dtype=torch.int32, device="cuda")
+    used = -(-n // page)
+    table[0, :used] = torch.randperm(pages, device="cuda", generator=g)[:used]
+    table[0, used // 2] = pages if pages > 1 else table[0, used // 2]                # a page that is not there
+    lengths, offsets = ints([n], [0, 300])
+    q = torch.randn(300, 4 * kv, d, device="cuda", generator=g).bfloat16()
+    k, v = (torch.randn(pages, kv, page, d, device="cuda", generator=g).to(cache_type) for _ in range(2))
+    scales = [torch.rand(pages, kv, page, device="cuda", generator=g) + 0.5 if cache_type == E4M3 else None for _ in range(2)]
+
+    def wide(x, shape, strides, total):
+        t = torch.full((total,), math.nan, device="cuda").to(cache_type)
+        t = torch.as_strided(t, shape, strides)
+        (t.view(torch.uint8) if cache_type == E4M3 else t).copy_(x.view(torch.uint8) if cache_type == E4M3 else x)
+        return t
+
+    got = []
+    shape = (pages, kv, page, d)
+    for strides in ((kv * page * d, page * d, d, 1), (kv * page * d + 64, page * d, d, 1), (kv * page * (d + 32), page * (d + 32), d + 32, 1), (7 * kv * page * d, 7 * page * d, d, 1)):
+        total = sum((n - 1) * s for n, s in zip(shape, strides)) + 1
+        cache = sw.PagedCache(wide(k, shape, strides, total), wide(v, shape, strides, total), *scales)
+        got.append((sw.prompt_attention(q, cache, table, lengths, offsets), sw.prompt_attention(q, cache, table, lengths, offsets, window=77), sw.decode_attention(q[-1:], cache, table, lengths)))
+    assert bool(torch.isfinite(got[0][0]).all())
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a, b)
