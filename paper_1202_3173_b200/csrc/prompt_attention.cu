@@ -119,8 +119,8 @@ struct Shared {
     int dead;
 };
 
-// Waits until phase `parity` of the barrier is over.  False: the limit was reached; the caller leaves its loop, and the results of the call are not valid.  A try
-// takes up to two microseconds, the wait two seconds.  One loop of three instructions: what a wait costs beyond the time waited comes between products (with the
+// Waits until phase `parity` of the barrier is over.  False: the limit was reached; the caller leaves its loop, and the results of the call are not valid.  It is a
+// number of tries, 2^20 of up to two microseconds each, which the hardware may end sooner: two seconds at most, and for what is a few tiles away.  One loop of three instructions: what a wait costs beyond the time waited comes between products (with the
 // clock read on the way, 8192 tokens took 432 us instead of 407).
 __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *sh)
 {
@@ -134,7 +134,8 @@ __device__ __forceinline__ bool wait_for(uint64_t *b, uint32_t parity, Shared *s
     g_gave_up = 1;
     return false;
 }
-// The same where the others may have a whole block to do: until one of them gives up.
+// The same where the others may have a whole block to do, until one of them gives up: for plans (plan_full, plan_empty), and for the clearing of a block's last tile of V
+// (plan_cleared), which a tile of Q without rows of the cache waits for from the block's start.  All other waits are for a few tiles: the rings' stages.
 __device__ __forceinline__ bool wait_for_block(uint64_t *b, uint32_t parity, Shared *sh)
 {
     if (bar_try(b, parity)) return true;
@@ -587,7 +588,8 @@ template <int KIND, int DP, bool LINEAR> __global__ void __launch_bounds__(Shape
                 if (lane == 0) bar_arrive(&sh.p_ready[x]);
             }
             if (!alive) break;
-            if (!(alive = warp_wait(&sh.plan_cleared[seen % PLANS], (seen / PLANS) & 1))) break;
+            // the whole block for the warps of a tile that has no rows of the cache
+            if (!(alive = warp_wait_block(&sh.plan_cleared[seen % PLANS], (seen / PLANS) & 1))) break;
             const bool bad = plan->bad != 0, any = first < end;
             if (any) {
                 if (!(alive = warp_wait(&sh.o_done[x], (tiles - 1) & 1))) break;

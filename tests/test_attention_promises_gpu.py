@@ -139,3 +139,28 @@ def test_one_key_head_or_one_page_wherever_pages_lie(kv, pages, page, cache_type
     for other in got[1:]:
         for a, b in zip(got[0], other):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("cache_type", [torch.bfloat16, E4M3])
+def test_tiles_without_rows_wait_for_the_whole_block(cache_type):
+    """300 sequences of one token behind 120000 rows (the same pages): every block of two tiles of queries has one without rows, which waits for all of the other's."""
+    d, page, n, batch = 64, 1024, 120000, 300
+    pages = -(-n // page)
+    k = torch.zeros(pages, 1, page, d, device="cuda").to(cache_type)
+    v = torch.zeros(pages, 1, page, d, device="cuda")
+    v[:, :, ::2, 0] = 1.0                                    # every second row: its mean is 1/2
+    v[0, 0, 0, 1] = 256.0                                    # the first and the last row
+    v[-1, 0, (n - 1) % page, 2] = 256.0
+    scales = [torch.ones(pages, 1, page, device="cuda") if cache_type == E4M3 else None for _ in range(2)]
+    cache = sw.PagedCache(k, v.to(cache_type), *scales)
+    table = torch.arange(pages, device="cuda", dtype=torch.int32)[None].expand(batch, -1).contiguous()
+    lengths = torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    offsets = torch.arange(batch + 1, device="cuda", dtype=torch.int32)
+    q = torch.randn(batch, 2, d, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    assert binding.strassen_prompt_attention_workspace_bytes(cache._at, batch, 2, pages, batch, 0) == 0
+    out = sw.prompt_attention(q, cache, table, lengths, offsets)
+    binding.strassen_device_status()
+    want = torch.zeros(d, dtype=torch.float64, device="cuda")
+    want[0], want[1], want[2] = 0.5, 256 / n, 256 / n
+    # equal weights, exact in 16 bits; sums in 32 bits of 2^17 terms and one rounding to bf16
+    assert bool(((out.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -18)).all())
