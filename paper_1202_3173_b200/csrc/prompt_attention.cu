@@ -615,7 +615,8 @@ template <int KIND, int DP, bool LINEAR> __global__ void __launch_bounds__(Shape
                 if (bad && mine) {
                     // values of V that are no numbers, in rows that not all tokens of the block see: this one's
                     for (int part = 0; part < 2; ++part) {
-                        const int begin = part == 0 ? low : max(low, max(plan->all_to + 1, plan->all_from)), stop = part == 0 ? min(high + 1, plan->all_from) : high + 1;
+                        // of the tiles that this part of the block has: an infinity of another part's, added to sums that weigh 0 in the end, would be NaN
+                        const int begin = max(part == 0 ? low : max(low, max(plan->all_to + 1, plan->all_from)), first * TILE), stop = min(part == 0 ? min(high + 1, plan->all_from) : high + 1, end * TILE);
                         for (int j = begin; j < stop; ++j) {
                             const int page = page_of(a.cache, a.seq, plan->b, j);
                             if (page < 0) continue;

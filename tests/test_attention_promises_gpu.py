@@ -164,3 +164,41 @@ def test_tiles_without_rows_wait_for_the_whole_block(cache_type):
     want[0], want[1], want[2] = 0.5, 256 / n, 256 / n
     # equal weights, exact in 16 bits; sums in 32 bits of 2^17 terms and one rounding to bf16
     assert bool(((out.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -18)).all())
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("cache_type", [torch.bfloat16, torch.float16, E4M3])
+@pytest.mark.parametrize("window", [0, 2000])
+def test_infinite_values_behind_many_rows_in_parts(bad, cache_type, window):
+    """The last row's value is infinite, and its score so far above all others that these weigh 0 in 32 bits; with a window so is the value of a row that the first two tokens see
+    alone, in another part of the cut.  A token that sees such a value has it, as the formula has, whatever its parts weigh; one that does not is as ever."""
+    d, page, n, count = 64, 64, 20000, 4
+    pages = -(-n // page)
+    k, v = (torch.zeros(pages, 1, page, d, device="cuda") for _ in range(2))
+    rows = [n - 1] + ([n - count - window + 2] if window else [])
+    k[(n - 1) // page, 0, (n - 1) % page, 0] = 256.0
+    v[..., 1] = 1.0
+    scales = [torch.ones(pages, 1, page, device="cuda") if cache_type == E4M3 else None for _ in range(2)]
+    v = v.to(cache_type)
+    for r in rows:
+        if cache_type == E4M3:
+            scales[1][r // page, 0, r % page] = bad           # column 1 infinite; 0 times that, in the others, is NaN
+        else:
+            v[r // page, 0, r % page, 1] = bad
+    cache = sw.PagedCache(k.to(cache_type), v, *scales)
+    q = torch.zeros(count, 2, d, dtype=torch.float16 if cache_type == torch.float16 else torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    table = torch.arange(pages, device="cuda", dtype=torch.int32)[None]
+    lengths, offsets = ints([n], [0, count])
+    assert binding.strassen_prompt_attention_workspace_bytes(cache._at, 1, 2, pages, count, window) > 0
+    out = sw.prompt_attention(q, cache, table, lengths, offsets, scale=1.0, window=window).double()
+    for i in range(count):
+        p = n - count + i
+        sees = [r for r in rows if r <= p and (not window or r > p - window)]
+        assert len(sees) == ((i == 3) if not window else (1, 1, 0, 1)[i])
+        if sees:
+            assert torch.equal(out[i, :, 1].nan_to_num(1.5, 2.5, -2.5), torch.full((2,), bad, dtype=torch.float64, device="cuda").nan_to_num(1.5, 2.5, -2.5)), i
+        else:
+            assert bool(((out[i, :, 1] - 1.0).abs() <= 2.0 ** -8 + 2.0 ** -18).all())
+        if cache_type != E4M3 or not sees:
+            assert not bool(out[i, :, 0].any()) and not bool(out[i, :, 2:].any())
