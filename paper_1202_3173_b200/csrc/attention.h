@@ -74,6 +74,34 @@ int64_t prompt_workspace(const AttentionArgs &a, int sm_count);
 cudaError_t prompt_gave_up(int *flag);        // reads and clears the flag of prompt_attention.cu
 cudaError_t launch_prompt(const AttentionArgs &a, int sm_count, cudaStream_t stream);
 
+// How the attention of one token is cut up, from the sizes alone.
+namespace decode {
+constexpr int MOST_RANKS = 16;                        // CTAs of a cluster
+
+// Steps of a sequence at most, by the table's width.
+inline int64_t steps_of(const AttentionArgs &a, int step)
+{
+    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window && a.window < rows ? a.window : rows;
+    return seen > 0 ? (seen + step - 1) / step : 1;
+}
+
+// CTAs of an item's cluster; 0: even runs and the join kernel.  most: 16, or 8 where the device holds no larger cluster.
+//
+// Few short items, as the table's width has it: each has a cluster, of as many CTAs as there is room for and steps to do, and there is no second kernel and no plan
+// to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
+// where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
+// steps of a CTA, 16 where eights fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000, not taken: 40.9 for 38.2).
+// Many short items are better off in runs (64 sequences of 240: 21 us, 25 with a CTA each; of 57: 9.6, 19).
+// What has clusters without a window has them with one: no more steps, and no fewer CTAs than those.
+inline int ranks_of(const AttentionArgs &a, int step, int64_t heads, int sm_count, int most)
+{
+    const int64_t steps = steps_of(a, step), items = heads * a.seq.batch;
+    int64_t ranks = most >= 16 && 16 * items <= sm_count ? 16 : 8;
+    while (ranks > 1 && (ranks >= 2 * steps || ranks * items > 2 * sm_count)) ranks /= 2;
+    return ranks * items <= 2 * sm_count && steps <= (ranks == 8 && ranks * items >= sm_count ? 16 : 8) * ranks ? int(ranks) : 0;
+}
+}  // namespace decode
+
 #ifdef __CUDACC__
 // Allows Kernel its dynamic shared memory, and clusters of up to 16 CTAs where it has such, on the current device, the first time it is launched there: asked each time, a launch takes a microsecond longer.
 template <auto Kernel> cudaError_t allow_shared(int bytes, bool large_clusters = false)

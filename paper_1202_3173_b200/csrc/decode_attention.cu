@@ -24,7 +24,8 @@ Shape shape_of(const AttentionArgs &a)
 int64_t decode_workspace(const AttentionArgs &a, int sm_count)
 {
     const Shape s = shape_of(a);
-    if (decode::ranks_of(a, decode::step_of(s.dp * (a.cache.type == STRASSEN_E4M3 ? 1 : 2)), a.cache.kv_heads * int64_t(s.blocks), sm_count) > 0) return 0;
+    const auto ranks = a.cache.type == STRASSEN_BF16 ? decode::ranks_bf16 : a.cache.type == STRASSEN_F16 ? decode::ranks_f16 : decode::ranks_e4m3;
+    if (ranks(a, s.dp, s.nt, a.cache.kv_heads * int64_t(s.blocks), sm_count) > 0) return 0;
     // two parts and a note for each run
     return 2 * sm_count * (2 * int64_t(decode::part_floats(s.dp, s.nt)) * 4 + int64_t(sizeof(decode::Meta)));
 }

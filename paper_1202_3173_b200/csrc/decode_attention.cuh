@@ -35,7 +35,6 @@ namespace strassen {
 namespace decode {
 
 constexpr int WARPS = 4, STAGES = 3, THREADS = 32 * WARPS;
-constexpr int MOST_RANKS = 16;                        // CTAs of a cluster
 constexpr int HALF_STAGE = 4096, STAGE = 2 * HALF_STAGE;       // a warp's rows of K, then of V
 enum { BF16 = 0, F16 = 1, E4M3 = 2 };                          // what the cache holds
 
@@ -127,13 +126,11 @@ __device__ __forceinline__ void copy4(uint32_t to, const void *from, uint32_t by
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
-constexpr int step_of(int row) { return WARPS * (HALF_STAGE / row); }
-
 // KIND: of the cache; DP: head_size, padded with zeros; NT: blocks of 8 heads.
 template <int KIND, int DP, int NT> struct Shape {
     static constexpr int SIZE = KIND == E4M3 ? 1 : 2, ROW = DP * SIZE, CHUNKS = ROW / 16;
     static constexpr int ROWS = HALF_STAGE / ROW;              // of a warp's stage: 16, 32 or 64
-    static constexpr int STEP = step_of(ROW);                  // rows of a step
+    static constexpr int STEP = WARPS * ROWS;                  // rows of a step
     static constexpr int SCALES = KIND == E4M3 ? 8 * ROWS : 0; // bytes of the rows' scales in a stage, of K, then of V
     static constexpr int RING = STAGES * STAGE, SMEM = WARPS * STAGES * (STAGE + SCALES);
     static constexpr int MT = DP / 16;                         // tiles of 16 values in O^T
@@ -835,27 +832,40 @@ template <int KIND, int DP, int NT, int GROUPS> __global__ void __launch_bounds_
     }
 }
 
-// Steps of a sequence at most, by the table's width.
-inline int64_t steps_of(const AttentionArgs &a, int step)
+// CTAs of the largest cluster of Kernel that the current device holds: 16, which has to fit one of its GPU processing clusters, as every device allows 8.  Asked once a device.
+template <auto Kernel> int most_ranks(int bytes)
 {
-    const int64_t rows = int64_t(a.seq.width) << a.cache.page_shift, seen = a.window && a.window < rows ? a.window : rows;
-    return seen > 0 ? (seen + step - 1) / step : 1;
+    static std::atomic<uint64_t> asked{0}, sixteen{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 8;
+    const uint64_t bit = uint64_t(1) << dev;
+    if (!(asked.load(std::memory_order_acquire) & bit)) {
+        if (allow_shared<Kernel>(bytes, true) != cudaSuccess) return 8;
+        cudaLaunchAttribute size = {};
+        size.id = cudaLaunchAttributeClusterDimension;
+        size.val.clusterDim.x = MOST_RANKS;
+        size.val.clusterDim.y = size.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(MOST_RANKS);
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = size_t(bytes);
+        cfg.attrs = &size;
+        cfg.numAttrs = 1;
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, Kernel, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            clusters = 0;
+        }
+        if (clusters > 0) sixteen.fetch_or(bit, std::memory_order_release);
+        asked.fetch_or(bit, std::memory_order_release);
+    }
+    return sixteen.load(std::memory_order_acquire) & bit ? MOST_RANKS : 8;
 }
-
-// CTAs of an item's cluster; 0: even runs and the join kernel.
-//
-// Few short items, as the table's width has it: each has a cluster, of as many CTAs as there is room for and steps to do, and there is no second kernel and no plan
-// to make (32 heads over 8 of 128, bf16: 1000 rows 6.8 us instead of 10.2, 4000 10.1 instead of 17.5, 8000 14.1 for 18.4; 8 sequences of 1000 10.3 for 13.1).  Clusters of 16 only
-// where they all have SMs to themselves (two sequences of 1000: 7.5 in eights, 12.0 in sixteens).  Longer ones take turns that are uneven where lengths are, and up to 8
-// steps of a CTA, 16 where eights fill the GPU, that costs less than the rest spares (4 sequences of 8000: 24.9 for 30.6; 16 of 4000, not taken: 40.9 for 38.2).
-// Many short items are better off in runs (64 sequences of 240: 21 us, 25 with a CTA each; of 57: 9.6, 19).
-// What has clusters without a window has them with one: no more steps, and no fewer CTAs than those.
-inline int ranks_of(const AttentionArgs &a, int step, int64_t heads, int sm_count)
+template <int KIND, int DP, int NT> int ranks_for(const AttentionArgs &a, int64_t heads, int sm_count)
 {
-    const int64_t steps = steps_of(a, step), items = heads * a.seq.batch;
-    int64_t ranks = 16 * items <= sm_count ? 16 : 8;
-    while (ranks > 1 && (ranks >= 2 * steps || ranks * items > 2 * sm_count)) ranks /= 2;
-    return ranks * items <= 2 * sm_count && steps <= (ranks == 8 && ranks * items >= sm_count ? 16 : 8) * ranks ? int(ranks) : 0;
+    using S = Shape<KIND, DP, NT>;
+    const int ranks = ranks_of(a, S::STEP, heads, sm_count, MOST_RANKS);
+    return ranks < MOST_RANKS ? ranks : ranks_of(a, S::STEP, heads, sm_count, most_ranks<decode_kernel<KIND, DP, NT, true>>(S::SMEM));
 }
 
 template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cudaStream_t stream)
@@ -864,7 +874,7 @@ template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cud
     cudaError_t e;
     const int64_t steps = steps_of(p.a, S::STEP), all = steps * p.items * p.a.seq.batch;
     const unsigned runs = unsigned(all < 2 * sm_count ? all : 2 * sm_count);
-    p.ranks = ranks_of(p.a, S::STEP, p.items, sm_count);
+    p.ranks = ranks_for<KIND, DP, NT>(p.a, p.items, sm_count);
     if (p.ranks > 0) {
         e = allow_shared<decode_kernel<KIND, DP, NT, true>>(S::SMEM, true);
         if (e != cudaSuccess) return e;
@@ -887,6 +897,9 @@ template <int KIND, int DP, int NT> cudaError_t launch(Args p, int sm_count, cud
 cudaError_t launch_bf16(const Args &p, int dp, int nt, int sm_count, cudaStream_t stream);
 cudaError_t launch_f16(const Args &p, int dp, int nt, int sm_count, cudaStream_t stream);
 cudaError_t launch_e4m3(const Args &p, int dp, int nt, int sm_count, cudaStream_t stream);
+int ranks_bf16(const AttentionArgs &a, int dp, int nt, int64_t heads, int sm_count);
+int ranks_f16(const AttentionArgs &a, int dp, int nt, int64_t heads, int sm_count);
+int ranks_e4m3(const AttentionArgs &a, int dp, int nt, int64_t heads, int sm_count);
 
 }  // namespace decode
 }  // namespace strassen

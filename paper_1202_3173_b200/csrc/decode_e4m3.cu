@@ -9,5 +9,11 @@ cudaError_t launch_e4m3(const Args &p, int dp, int nt, int sm_count, cudaStream_
     return nt == 1 ? launch<E4M3, 128, 1>(p, sm_count, stream) : launch<E4M3, 128, 2>(p, sm_count, stream);
 }
 
+int ranks_e4m3(const AttentionArgs &a, int dp, int nt, int64_t heads, int sm_count)
+{
+    if (dp == 64) return nt == 1 ? ranks_for<E4M3, 64, 1>(a, heads, sm_count) : ranks_for<E4M3, 64, 2>(a, heads, sm_count);
+    return nt == 1 ? ranks_for<E4M3, 128, 1>(a, heads, sm_count) : ranks_for<E4M3, 128, 2>(a, heads, sm_count);
+}
+
 }  // namespace decode
 }  // namespace strassen

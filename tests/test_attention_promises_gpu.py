@@ -1,5 +1,8 @@
 """What the attention operators' documentation promises beyond their formulas: the codes of 8-bit rows, every row counted once, what is refused."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -202,3 +205,28 @@ def test_infinite_values_behind_many_rows_in_parts(bad, cache_type, window):
             assert bool(((out[i, :, 1] - 1.0).abs() <= 2.0 ** -8 + 2.0 ** -18).all())
         if cache_type != E4M3 or not sees:
             assert not bool(out[i, :, 0].any()) and not bool(out[i, :, 2:].any())
+
+
+FIRST = """
+import torch, paper_1202_3173_b200 as sw
+cache = sw.PagedCache.empty(16, 8, 128, 64)
+cache.k.normal_(), cache.v.normal_()
+q = torch.randn(1, 32, 128, device="cuda").bfloat16()
+table = torch.arange(16, dtype=torch.int32, device="cuda")[None]
+lengths = torch.tensor([1000], dtype=torch.int32, device="cuda")
+out, graph, stream = torch.zeros_like(q), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph, stream=stream):
+    sw.decode_attention(q, cache, table, lengths, out=out)
+graph.replay()
+torch.cuda.synchronize()
+want = sw.decode_attention(q, cache, table, lengths)
+assert torch.equal(out, want) and bool(out.any())
+print("ok")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """What a call asks the device once (the largest cluster, the shared memory) it may ask while a graph is being captured."""
+    done = subprocess.run([sys.executable, "-c", FIRST], capture_output=True, text=True, timeout=120, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0 and done.stdout.strip() == "ok", done.stderr[-2000:]
