@@ -11,7 +11,7 @@ last ``offsets[b + 1] - offsets[b]``: rows ``offsets[b]`` to ``offsets[b + 1] - 
 handed to which sequence is the caller's to decide.  Rows that belong to no sequence are not written (what a new result holds for them is not defined).
 
 Calls are enqueued on the current stream and can be captured into a CUDA graph.  The operators serve a model and have no backward pass: tensors that require
-grad are refused unless gradients are off (``torch.no_grad()``).  Tensors that are written count as modified in place.
+grad are refused unless gradients are off (``torch.no_grad()``), tensors with forward-mode tangents always.  Tensors that are written count as modified in place.
 """
 from __future__ import annotations
 
@@ -21,7 +21,7 @@ import ctypes
 import torch
 
 from . import binding
-from .feed_forward import _OUT_TYPES, _TYPES, E4M3, W4Matrix, _call, _current_device, _gradients_off, _packed, _written, quantize_w4, rms_norm_quant
+from .feed_forward import _OUT_TYPES, _TYPES, E4M3, W4Matrix, _call, _current_device, _forward_mode, _gradients_off, _packed, _tangents_off, _written, quantize_w4, rms_norm_quant
 
 __all__ = ["PagedCache", "SelfAttention", "rotate_append", "decode_attention", "prompt_attention"]
 
@@ -37,6 +37,8 @@ class PagedCache:
     rows, as long as rows are contiguous, strides and addresses are multiples of 16 bytes, and both have the same strides."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
+        if _forward_mode():
+            _tangents_off(k=k, v=v, k_scale=k_scale, v_scale=v_scale)
         if k.dim() != 4 or k.dtype not in _CACHE_TYPES or not k.is_cuda:
             raise ValueError("k must be a CUDA tensor (pages, kv_heads, page_size, head_size) of one of %s, not %s %s on %s"
                              % (", ".join(str(t) for t in _CACHE_TYPES), k.dtype, tuple(k.shape), k.device))
@@ -137,6 +139,8 @@ def rotate_append(q, k, v, cache, table, lengths, frequencies=None, offsets=None
     ``q``: (tokens, heads, head_size) or None; ``k``, ``v``: (tokens, kv_heads, head_size); any of them may be views of one wider tensor.  ``frequencies``: float32,
     one for each pair that turns (up to head_size / 2); pair f of a token at position p turns by p * frequencies[f].  Pairs are the values f and f + n of the first
     2 n of a row, or, ``interleaved``, 2 f and 2 f + 1.  Without frequencies nothing turns.  ``out``: to write the turned queries to; may be ``q`` itself."""
+    if _forward_mode():
+        _tangents_off(q=q, k=k, v=v, frequencies=frequencies, out=out)
     kind = _type_of(k, cache, "k")
     index, tokens, size = cache._index, k.shape[0], cache.head_size
     seq = _sequences(k, cache, table, lengths, offsets)
@@ -169,6 +173,8 @@ def rotate_append(q, k, v, cache, table, lengths, frequencies=None, offsets=None
 
 
 def _attention(q, cache, table, lengths, offsets, scale, window, out):
+    if _forward_mode():
+        _tangents_off(q=q, out=out)
     kind = _type_of(q, cache)
     index = cache._index
     batch, table_at, ld, width, lengths_at, offsets_at = _sequences(q, cache, table, lengths, offsets)

@@ -8,7 +8,7 @@ Rows are 2-D CUDA tensors whose last dimension is contiguous; rows may be any di
 enqueued on the current stream, allocate nothing when ``out`` is given, and can be captured into a CUDA graph.
 
 The operators serve a model and have no backward pass: tensors that require grad are refused unless gradients are off
-(``torch.no_grad()``).  Tensors that are written count as modified in place.
+(``torch.no_grad()``), tensors with forward-mode tangents always.  Tensors that are written count as modified in place.
 
 Every wait inside a kernel has a limit, after which the kernel returns with results that are not valid.  Calls do not wait for their kernels
 and so cannot say so: ``binding.strassen_device_status()`` waits for the device and raises ``StrassenError`` if it has happened.
@@ -16,6 +16,7 @@ and so cannot say so: ``binding.strassen_device_status()`` waits for the device 
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.graph import increment_version
 
 from . import binding
@@ -44,6 +45,19 @@ def _gradients_off(name):
     """For a tensor that requires grad: its gradient is not dropped without a word."""
     if torch.is_grad_enabled():
         raise ValueError("%s requires grad, and the operators have no backward pass: detach it, or call them under torch.no_grad()" % name)
+
+
+def _forward_mode():
+    """Whether tensors may have tangents: within ``forward_ad.dual_level()``."""
+    return getattr(forward_ad, "_current_level", 0) >= 0
+
+
+def _tangents_off(**tensors):
+    """Of the tensors of a call in forward mode: no tangent is dropped without a word."""
+    for name, t in tensors.items():
+        for part in t if isinstance(t, (tuple, list)) else (t,):
+            if part is not None and forward_ad.unpack_dual(part).tangent is not None:
+                raise ValueError("%s has a tangent, and the operators have no forward-mode derivative: use forward_ad.unpack_dual(t).primal" % name)
 
 
 def _rows(name, t, shape, dtype, index):
@@ -107,6 +121,8 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, out=None):
 
     Returns (q, scale), or (q, scale, sum) with a residual: v ~ q * scale[:, None], sum = x + residual in x's type.  ``out`` is such a tuple to
     write to; its sum may be ``x`` or ``residual`` itself (the residual stream updated in place)."""
+    if _forward_mode():
+        _tangents_off(x=x, weight=weight, residual=residual, out=out)
     shape, kind, index = _first("x", x, _ROW_TYPES)
     m, k = shape
     dtype, given = x.dtype, out
@@ -131,6 +147,8 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, out=None):
 
 def silu_mul_quant(gate, up, out=None):
     """silu(gate) * up in 8 bits: (q, scale).  gate and up may be the halves of one tensor."""
+    if _forward_mode():
+        _tangents_off(gate=gate, up=up, out=out)
     shape, kind, index = _first("gate", gate, _ROW_TYPES)
     m, k = shape
     dtype, given = gate.dtype, out
@@ -150,6 +168,8 @@ def route_experts(logits, top, score="softmax", bias=None, groups=1, top_groups=
 
     ``score``: "softmax" or "sigmoid"; ``bias`` (float32, one per expert) is added to the scores for the choice alone; with ``groups`` only the
     experts of the ``top_groups`` best groups can be chosen.  Logits of -inf leave an expert out; ids are -1, with weight 0, where too few are left."""
+    if _forward_mode():
+        _tangents_off(logits=logits, bias=bias, out=out)
     shape, kind, index = _first("logits", logits, _ROW_TYPES)
     tokens, experts = shape
     given = out
@@ -171,6 +191,8 @@ class _W4:
 
     def __init__(self, q, scales, zeros, k, group, experts):
         self._h = None
+        if _forward_mode():
+            _tangents_off(scales=scales)
         if q.dtype != torch.uint8 or not q.is_cuda:
             raise ValueError("q must be a CUDA uint8 tensor, not %s on %s" % (q.dtype, q.device))
         if scales.dtype not in _OUT_TYPES:
@@ -261,6 +283,8 @@ class W4Matrix(_W4):
         bfloat16 beside bfloat16 rows and to float16 beside the others."""
         if self._h is None:
             raise ValueError("the matrix has been closed")
+        if _forward_mode():
+            _tangents_off(x=x, x_scale=x_scale, out=out)
         shape, kind, index = _first("x", x, _X_TYPES)
         m, given = shape[0], out
         ldx = _rows("x", x, (m, self.k), x.dtype, self._index)
@@ -305,6 +329,8 @@ class W4Experts(_W4):
         Weights of the matrices are rounded as ``W4Matrix`` does it, beyond 32 ids."""
         if self._h is None:
             raise ValueError("the matrices have been closed")
+        if _forward_mode():
+            _tangents_off(x=x, x_scale=x_scale, weights=weights, out=out)
         shape, kind, index = _first("x", x, _X_TYPES)
         if len(ids.shape) != 2:
             raise ValueError("ids must be tokens x top, not %s" % (tuple(ids.shape),))
