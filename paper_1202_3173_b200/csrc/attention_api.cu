@@ -65,22 +65,19 @@ Range cache_range(const CacheArgs &c, const uint8_t *p)
     return {lo, lo + uintptr_t((c.pages - 1) * c.page_stride + (c.kv_heads - 1) * c.head_stride + ((int64_t(1) << c.page_shift) - 1) * c.row_stride + c.d * type_size(c.type))};
 }
 
-Range scale_range(const CacheArgs &c, const float *p)
+// n numbers of 32 bits one after another.
+Range packed(const void *p, int64_t n)
 {
     const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    return {lo, lo + (p ? uintptr_t((c.pages * c.kv_heads) << c.page_shift) * 4 : 0)};
+    return p && n > 0 ? Range{lo, lo + uintptr_t(n) * 4} : Range{0, 0};
 }
-Range ints_of(const int *p, int64_t n)
-{
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    return {lo, lo + (p && n > 0 ? uintptr_t(n) * 4 : 0)};
-}
+Range scale_range(const CacheArgs &c, const float *p) { return packed(p, (c.pages * c.kv_heads) << c.page_shift); }
 
 // Whether `r` lies over the scales, the table, the lengths or the offsets, all of which are read while results are written.
 bool over_what_is_read(const Range &r, const CacheArgs &c, const SequenceArgs &s)
 {
-    return overlap(r, scale_range(c, c.k_scale)) || overlap(r, scale_range(c, c.v_scale)) || overlap(r, ints_of(s.table, s.batch > 0 && s.width > 0 ? (s.batch - 1) * s.ld_table + s.width : 0)) ||
-           overlap(r, ints_of(s.lengths, s.batch)) || overlap(r, ints_of(s.offsets, s.batch + int64_t(1)));
+    return overlap(r, scale_range(c, c.k_scale)) || overlap(r, scale_range(c, c.v_scale)) || overlap(r, packed(s.table, s.batch > 0 && s.width > 0 ? (s.batch - 1) * s.ld_table + s.width : 0)) ||
+           overlap(r, packed(s.lengths, s.batch)) || overlap(r, packed(s.offsets, s.batch + int64_t(1)));
 }
 
 // Rows of heads as the kernels see them.
@@ -238,9 +235,9 @@ extern "C" int strassen_rotate_append(const strassen_paged_cache *cache, int64_t
              wide_strides(reinterpret_cast<uintptr_t>(q), a.q.row, a.q.head, 2) && wide_strides(reinterpret_cast<uintptr_t>(out), a.out_row, a.out_head, 2);
     const CacheArgs &c = a.cache;
     const RowsOfHeads o = {out, tokens, a.out_row, heads, a.out_head}, qs = {q, tokens, a.q.row, heads, a.q.head}, ks = {k, tokens, a.k.row, kv, a.k.head}, vs = {v, tokens, a.v.row, kv, a.v.head};
-    const Range turns = ints_of(reinterpret_cast<const int *>(frequencies), rotary / 2);
+    const Range turns = packed(frequencies, rotary / 2);
     for (const Range &f : {cache_range(c, c.k), cache_range(c, c.v), scale_range(c, c.k_scale), scale_range(c, c.v_scale)})
-        for (const Range &r : {qs.range(d), ks.range(d), vs.range(d), o.range(d), turns, ints_of(a.seq.table, width > 0 ? (batch - 1) * ld_table + width : 0), ints_of(lengths, batch), ints_of(offsets, batch + 1)})
+        for (const Range &r : {qs.range(d), ks.range(d), vs.range(d), o.range(d), turns, packed(a.seq.table, width > 0 ? (batch - 1) * ld_table + width : 0), packed(lengths, batch), packed(offsets, batch + 1)})
             if (overlap(f, r)) return fail(STRASSEN_ALIAS, "the cache overlaps another argument");
     if (c.pages > 0 && (c.k == c.v || overlap(scale_range(c, c.k_scale), scale_range(c, c.v_scale)))) return fail(STRASSEN_ALIAS, "keys and values of the cache are in the same place");
     if (overlap(o.range(d), turns) || over_what_is_read(o.range(d), c, a.seq)) return fail(STRASSEN_ALIAS, "out overlaps another argument");

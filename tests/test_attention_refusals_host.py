@@ -87,3 +87,12 @@ def test_views_of_one_tensor_are_looked_at_element_by_element():
         assert got == (ALIAS if want else None), (views, tokens, d)
         seen[want] += 1
     assert min(seen.values()) > 500
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are no memory: without a device no kernel is launched")
+def test_what_is_empty_shares_nothing():
+    """A table without columns, wherever it points to; a cache without pages."""
+    assert answer(decode, cache(), width=0, table=131072 + 64) is None
+    assert answer(append, cache(), width=0, table=131072 + 64) is None
+    assert answer(append, cache(), width=0, table=(1 << 20) + 64) is None
+    assert answer(decode, cache(pages=0, type=binding.STRASSEN_E4M3, k_scale=131072 + 4, v_scale=131072 + 4)) is None
