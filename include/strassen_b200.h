@@ -572,7 +572,9 @@ int strassen_rotate_append(const strassen_paged_cache *cache, int64_t batch, con
  *   out_h = sum over j of softmax(scale q_h . k_j) v_j,  j = 0 .. lengths[b] - 1, with a window > 0 the last `window` of them.
  *   type       of q and out: STRASSEN_BF16 or STRASSEN_F16, the cache's if that has 16 bits
  *   workspace  as strassen_decode_attention_workspace_bytes says for the current device (0 bytes for few short sequences; 256-byte aligned; free again once the call's kernels are done)
- * Scores, the softmax's sums and the result are held in 32 bits; its weights, at most 1, are rounded to 16 bits for the product with the values.  The work is split evenly over
+ * Scores, the softmax's sums and the result are held in 32 bits; its weights, at most 1, are rounded once for the product with the values, to the cache's type or, over one in 8
+ * bits, to f16.  Queries in bf16 are brought into f16's range beside a cache in 8 bits: exactly down to 2^-17 of their head's largest value, smaller ones with an error
+ * of at most 2^-25 of that.  The work is split evenly over
  * the GPU along the sequences, whatever their lengths, but for few short sequences (by width), of which each is split over as many CTAs.  out and the workspace
  * overlap no other argument, the cache's scales, the table and the lengths included (STRASSEN_ALIAS).
  */
@@ -583,7 +585,10 @@ size_t strassen_decode_attention_workspace_bytes(const strassen_paged_cache *cac
 
 /*
  * strassen_prompt_attention -- the same for many new tokens a sequence, each seeing the rows up to its own position (causal), with a window > 0 the
- * last `window` of those.  offsets as above, not NULL.  The workspace is 0 bytes but for few tokens behind many rows.  q is 16-byte aligned, its strides multiples of 16 bytes (STRASSEN_MISALIGNED).
+ * last `window` of those.  offsets as above, not NULL.  q is 16-byte aligned, its strides multiples of 16 bytes (STRASSEN_MISALIGNED).
+ * Where blocks of tokens would leave the GPU idle in turns, the rows of the cache that the table (and the window) has room for are cut into parts, whose sums go to the workspace, up
+ * to some 300 MB of it.  So a table much wider than its sequences costs a workspace and time (2048 tokens behind none, 32 heads over 8 of 128: none and 41 us with a table for 2048
+ * rows, 176 MB and 170 us with one for 32768): pass a narrower one where the sequences are known to be short.  Without parts it is 0 bytes.
  */
 int strassen_prompt_attention(const strassen_paged_cache *cache, int64_t batch, const int *table, int64_t ld_table, int64_t width, const int *lengths,
                               const int *offsets, int64_t tokens, int type, int64_t heads, const void *q, int64_t q_row, int64_t q_head, void *out,

@@ -8,7 +8,8 @@ devices, the memory and the current stream.  ``SelfAttention`` runs them togethe
 Row j of sequence b lies in page ``table[b, j // page_size]``, slot ``j % page_size``.  ``lengths[b]`` counts the sequence's rows with its new ones, which are the
 last ``offsets[b + 1] - offsets[b]``: rows ``offsets[b]`` to ``offsets[b + 1] - 1`` of q.  Without offsets each sequence has one new token.  ``table``,
 ``lengths`` and ``offsets`` are int32 CUDA tensors that the kernels read, so that a captured graph can be replayed for other lengths; which pages are
-handed to which sequence is the caller's to decide.  Rows that belong to no sequence are not written (what a new result holds for them is not defined).
+handed to which sequence is the caller's to decide.  How work is cut goes by the table's width, which the host sees: a table no wider than the longest sequence needs is the
+fastest (prompts in one for many times their rows take several times as long and up to some 300 MB of workspace).  Rows that belong to no sequence are not written (what a new result holds for them is not defined).
 
 Calls are enqueued on the current stream and can be captured into a CUDA graph.  The operators serve a model and have no backward pass: tensors that require
 grad are refused unless gradients are off (``torch.no_grad()``), tensors with forward-mode tangents always.  Tensors that are written count as modified in place.

@@ -8,9 +8,10 @@
 //
 // Bound by the cache's bytes.  Each warp has rows of its own and a ring of its own in shared memory that it fills by asynchronous copies of 16 bytes, rows outside the
 // sequence and values beyond head_size as zeros: nothing in the loop waits for another warp.  About 128 KB are under way on an SM: 32 sequences of up to 32768 tokens of
-// 8 key heads of 128 values, 2.75 GB, in 422 us, 6.5 TB/s; one of 131071, 537 MB, in 90 us, 6.0 TB/s; 64 of up to 8192 of 4 key heads in 8 bits, 331 MB, in 70 us, 4.7 TB/s;
-// 33 of up to 4099 of 12 heads of 80 values, 328 MB, in 74 us, 4.4 TB/s.  The last two wait for dependent instructions (47 and 41 % of issue slots; two warps a
-// scheduler): queries of one or seven heads fill an eighth of the products or nearly all, at the same cost in instructions.  16-byte
+// 8 key heads of 128 values, 2.84 GB, in 422 us, 6.7 TB/s (a kernel that does nothing but read as much: 387 us, 7.3); one of 131071, 537 MB, in 90 us, 6.0 TB/s; 64 of up to 8192 of
+// 4 key heads in 8 bits, 331 MB, in 71 us, 4.7 TB/s; 33 of up to 4099 of 12 heads of 80 values, 328 MB, in 74 us, 4.4 TB/s.  The last two wait for dependent instructions (47 and 41 %
+// of issue slots; two warps a scheduler): queries of one or seven heads fill an eighth of the products or nearly all, at the same cost in instructions, and 80 values cost what 128 do,
+// three eighths of both products, of the copies and of the ring being zeros.  16-byte
 // chunks of a row are permuted by the row's number, so that reads by 8 lanes, of two rows or of four, fall into different banks.
 //
 // Few short items have a cluster each (ranks_of), whose CTAs add their parts up out of one another's shared memory.  Else the
@@ -18,10 +19,12 @@
 // run's first and last item may be a part of one: its sums go to the workspace, and the join kernel adds an item's parts in order.  No atomics: the
 // same bits every time.
 //
-// Weights are rounded to 16 bits for the second product.  They are at most 2^12, not 1, in f16: what lies below f16's smallest number is then 2^-37 of the
+// Weights are rounded to 16 bits for the second product, whose operands have one type: that of the cache's values.  A weight is off by half a step of it at most, so a result by as much
+// of the sum of weight times |value|, which is what rounding the result to that type costs where values have one sign.  As two numbers in 16 bits each it would take a second product and as
+// many instructions more, of which shapes in 8 bits and of one head have too many as it is.  They are at most 2^12, not 1, in f16: what lies below f16's smallest number is then 2^-37 of the
 // largest, too little to matter in 2^17 rows.  Rows in 8 bits are exact in f16: s is scaled by the key row's scale, a weight by the value row's, and M is the
 // largest of s + log2(value scale), so that scaled weights keep within f16's range whatever the scales are.  Queries in bf16 are brought into f16's by a
-// power of two a head.
+// power of two a head: exactly down to 2^-17 of the head's largest value; what is smaller is off by 2^-25 of that at most, as a sum in 32 bits is by 2^-24 of its largest term.
 #pragma once
 
 #include <cuda_bf16.h>

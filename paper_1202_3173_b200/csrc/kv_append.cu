@@ -10,9 +10,10 @@
 // lanes with a chunk each, partners' values from theirs (any_kernel).
 //
 // Bound by the bytes, read once and written once, and nearly as much by instructions: 16384 tokens of 32 + 2 x 8 heads of 128, 370 MB with an 8-bit cache, in
-// 70 us, 5.3 TB/s (400 MB, 69 us, with one in bf16); with a chunk a lane 99, with a token a CTA and its angles first 139.  Heads of 64, 49152 tokens of 16 + 2 x 8: 53 us
-// (80 with 8 lanes a row, half of them idle); of 80, 39320 tokens: 81 (90).  One head over one, 262144 tokens: 66 us (108 with 8 tokens a CTA), of 64 values, 524288 tokens:
-// 107 (269); there the angles and where a token goes are most of the work.
+// 70 us, 5.3 TB/s (400 MB, 71 us, with one in bf16); with a chunk a lane 99, with a token a CTA and its angles first 139.  One sequence of 402 MB each, whose bytes take 62 us: 49152
+// tokens of 16 + 2 x 8 heads of 64 70 us (106 with 8 lanes a row, half of them idle); 39320 of 80 values 79 (93); 262144 of one head over one of 128 117 (200 with 8 tokens a CTA),
+// 524288 of 64 values 155 (395): there the angles and where a token goes are most of the work.  With an 8-bit cache heads of 64 and of 80 take 79 and 90 where the bytes take 54: a
+// row's largest value, scale and address are as many instructions for half the bytes.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

@@ -20,11 +20,16 @@
 // add them at the end, from memory.
 //
 // Over a cache in 8 bits the products are in f16, in which its values are exact.  Warps 12 to 15 then turn each tile of K and V, which a smaller ring brings, into 16 bits, and clear V, and queries in bf16 are brought into f16's range by a power of two a row.  Scores are multiplied by the key rows' scales, weights by the value rows', and
-// M is the largest of score + log2(value scale), so that scaled weights keep within f16's range.
+// M is the largest of score + log2(value scale), so that scaled weights keep within f16's range.  That is a multiplication by the key row's scale, an fma for the maximum and a
+// multiplication by the value row's scale a score more than in 16 bits, and warps that turn tiles beside them: 2.3 times the instructions, 868 us for 8192 tokens of 32 heads over 8 of 128
+// where 16 bits take 407 (0.63 PFLOP/s; tensor cores busy for 25 % of the time).
 //
-// Bound, for head_size 128, by power: 16384 tokens of 32 heads over 8 in 1.68 ms, 1.31 PFLOP/s, at 1.49 GHz (sampled in the kernel), where the tensor cores are busy for 2048 of
-// 2830 clocks of a pair of tiles; cuBLAS keeps up 1.38.  In short runs at 1.75 GHz 8192 tokens take 407 us, 1.35 PFLOP/s.  For smaller heads by the softmax (8192 tokens of 64 heads
-// over 8 of 64 values: 685 us, 0.8 PFLOP/s): 128 exponentials of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a
+// A weight is rounded to 16 bits for its product, whose operands have one type: off by half a step of it, so a result by as much of the sum of weight times |value|, which is
+// what rounding the result to that type costs where values have one sign.
+//
+// Bound, for head_size 128, by power: 16384 tokens of 32 heads over 8 run on and on in 1.78 ms, 1.24 PFLOP/s, at 1.46 GHz, where cuBLAS keeps up 1.38; the tensor cores are busy for 2048
+// of 2830 clocks of a pair of tiles.  In short runs, at up to 1.9 GHz, they take 1.55 ms, 1.42 PFLOP/s, and 8192 tokens 407 us, 1.35.  For smaller heads by the softmax (8192 tokens of 64
+// heads over 8 of 64 values: 673 us, 0.82 PFLOP/s; on and on 718): 128 exponentials of a thread take the special-function units 1050 clocks, with all around it 1250 for one warp of a
 // scheduler and 2150 for two (timed alone), 2820 here, where a warp also waits for S (260), reads it (130), finds its largest (410), waits for the product before (200) and writes P
 // (190 clocks a tile) while the other's exponentials take the issue slots.  What was tried: P over S, and S formed behind P V (the first form): 462 us at 8192 tokens of 32 heads
 // over 8 of 128, then 407; a quarter of the exponentials by a polynomial of degree 4 446, for heads of 64 of degree 3 744 instead of 685, an eighth 687; two threads a row: 570; warps
