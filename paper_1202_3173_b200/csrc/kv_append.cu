@@ -50,7 +50,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
     return d;
 }
 // v / scale in 8 bits, of two values; inv: 1 / scale, back: -scale, or 0 if that is infinite (finite values are 0 then).  v inv is not always the quotient's nearest number in
-// 32 bits, and next to a border between two e4m3 values that is the wrong one of them (one of 2000 of rows in bf16).  So what is left of v is found, exactly, and its own
+// 32 bits, and next to a border between two e4m3 values that gives the wrong one of them (for one value in 2000 of rows in bf16).  So what is left of v is found, exactly, and its own
 // quotient added (Markstein, IBM J. Res. Dev. 34 (1990): the result is the rounded quotient).  Two numbers an instruction: 79.0 us where v inv alone takes 77.4 (49152 tokens of
 // 16 + 2 x 8 heads of 64, 8-bit cache), a division 96.8; 16384 of 32 + 2 x 8 of 128: 70.3, 70.1 and 76.6.
 __device__ __forceinline__ uint32_t two_of_8_bits(float2 v, float inv, float back)
